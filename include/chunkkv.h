@@ -305,6 +305,69 @@ CHUNKKV_API int chunkkv_compress_layer_alg1(const void* q_obs, const void* K, co
                                 void* stream);
 
 /*
+ * The decode side of the compacted cache: what a program does with a cache [num_pages, page_size, Hkv, d] that
+ * chunkkv_compress_*_paged or chunkkv_gather_paged has filled. (Nothing of this is in the paper, which ends where decoding begins.)
+ * Shared by these calls:
+ *   block_tables [B, max_pages] int32   page of each page_size rows of a sequence; entries outside [0, num_pages) stand for no
+ *                              page: rows there are not seen, and what would be written there is dropped
+ *   lengths [B, Hkv] int32     rows of every head, of its own: a head that kept the clipped last chunk has fewer than its
+ *                              neighbours (the entries of its idx that are not -1). Below 0 counts as 0, above
+ *                              max_pages * page_size as that.
+ *   weights [B, Hkv, max_pages * page_size] f32   sums of the attention that every row received; a program starts with
+ *                              zeros, and rows at and behind `lengths` are to be zero (chunkkv_evict_paged leaves them so)
+ * Pages that a call writes must belong to one sequence, and lengths and tables must not change while a call runs. Limits: d in
+ * {64, 128}, max_pages * page_size < 2^30, num_pages * page_size < 2^31, Hq <= 65535 and a multiple of Hkv, B * Hq < 2^30 (T * Hq
+ * likewise); any number of query heads a KV head; B = 0 (T = 0) does nothing. No call keeps anything or uses
+ * chunkkv_set_workspace's buffer, so calls on different streams, captured or not, have nothing in common but the tensors given.
+ *
+ * chunkkv_rotate_qk: queries and keys of T tokens out of a fused QKV activation qkv [T, row_elems] bf16 (query heads first,
+ *   then key heads; row_elems >= (Hq + Hkv) d, a multiple of 8), before the rotary embedding. With q_gain / k_gain [d] bf16 (or
+ *   NULL: no norm) every head is first divided by its root mean square and multiplied by the gain, x / sqrt(mean(x^2) + eps) *
+ *   gain; then it is rotated as in chunkkv_window_queries, by row positions[t] of cos_t / sin_t [n_pos, d / 2] f32. Computed in
+ *   32 bits, rounded once. A token whose position is outside [0, n_pos) gets zeros. Row (t, h) of out_q starts at element
+ *   t * q_token_stride + h * q_head_stride (likewise out_k; strides multiples of 8, at least d): token-major [T, Hq, d],
+ *   head-major (chunkkv_compress_layer's [Hkv, L, d] and q_obs), or the place in qkv that it was read from; otherwise the outputs
+ *   must not overlap qkv or each other.
+ *
+ * chunkkv_append_paged: the same for one token of each of B sequences: queries to out_q [B, Hq, d], and the keys and values
+ *   (qkv [B, row_elems], row_elems >= (Hq + 2 Hkv) d) into the cache, as row lengths[b, h] - 1 of head h: `lengths` counts the
+ *   token already, one addition a step for all layers. A head whose length is 0 (a padded batch) or beyond the table gets no row.
+ *
+ * chunkkv_attend_paged: attention of one new token a sequence, q [B, Hq, d] bf16 (rotated), over the rows j < lengths[b, h] of
+ *   its KV head: out [B, Hq, d] bf16 = softmax(q K^T / sqrt(d)) V, in 32 bits, rounded once. A head with no row to see, or none
+ *   with a logit above -inf, gets zeros; other infinite or not-a-number products go the way of the formula. weights != NULL:
+ *   weights[b, h, j] += the row's attention, summed over the query heads of KV head h. scratch: device memory of the call's own
+ *   until it has finished, 256-byte aligned, chunkkv_attend_scratch_bytes(...) bytes (0: invalid sizes; its contents do not
+ *   matter); CHUNKKV_ENOWORKSPACE when smaller. Same result every time: sums are taken in a fixed order.
+ *
+ * chunkkv_evict_paged: heads with n = lengths[b, h] > budget rows go back to at most budget: C = floor((n - w) / c) chunks of c
+ *   rows from row 0, r = n - C c rows behind them (w <= r < w + c), k = floor((budget - r) / c) of the chunks stay, those with
+ *   the largest sums of weights (summed in 64 bits, compared in 32; not-a-number above all; ties to the lower chunk), and all r
+ *   rows. Kept chunks below place k stay where they are, the j-th kept chunk at or above it goes to the j-th free place below it,
+ *   the r rows follow at row k c in their order. weights move with their rows, those behind become 0, lengths[b, h] = k c + r.
+ *   out_idx [B, Hkv, budget] int32: the former row of every row, -1 behind. Heads with at most budget rows stay as they are. Cache
+ *   rows behind the new length are left as they were. (A row in no page moves as zeros.)
+ *   w >= 0, c >= 1, budget >= max(1, w + c - 1); CHUNKKV_ETOOLARGE with more than 65535 chunks in max_pages * page_size rows.
+ */
+CHUNKKV_API int chunkkv_rotate_qk(const void* qkv, long long row_elems, int T, int Hq, int Hkv, int d, const void* q_gain,
+                                  const void* k_gain, float eps, const float* cos_t, const float* sin_t, int n_pos,
+                                  const int32_t* positions, long long q_token_stride, long long q_head_stride,
+                                  long long k_token_stride, long long k_head_stride, void* out_q, void* out_k, void* stream);
+CHUNKKV_API int chunkkv_append_paged(const void* qkv, long long row_elems, int B, int Hq, int Hkv, int d, const void* q_gain,
+                                     const void* k_gain, float eps, const float* cos_t, const float* sin_t, int n_pos,
+                                     const int32_t* positions, const int32_t* block_tables, int max_pages,
+                                     const int32_t* lengths, int page_size, int num_pages, void* cache_K, void* cache_V,
+                                     void* out_q, void* stream);
+CHUNKKV_API size_t chunkkv_attend_scratch_bytes(int B, int Hq, int Hkv, int d, int max_pages, int page_size, int with_weights);
+CHUNKKV_API int chunkkv_attend_paged(const void* q, const int32_t* block_tables, int max_pages, const int32_t* lengths,
+                                     int page_size, int num_pages, const void* cache_K, const void* cache_V, int B, int Hq,
+                                     int Hkv, int d, float* weights_or_null, void* out, void* scratch, size_t scratch_bytes,
+                                     void* stream);
+CHUNKKV_API int chunkkv_evict_paged(float* weights, const int32_t* block_tables, int max_pages, int32_t* lengths, int page_size,
+                                    int num_pages, void* cache_K, void* cache_V, int B, int Hkv, int d, int w, int c, int budget,
+                                    int32_t* out_idx, void* stream);
+
+/*
  * Index similarity between two layers (the paper's section on layer-wise index reuse reports the
  * Jaccard similarity of the preserved indices of adjacent layers; Algorithm 2 shares indices
  * because it is high). Per KV head h: out_ratio[h] = |A n B| / |A u B| (1 when both are empty),

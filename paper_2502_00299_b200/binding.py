@@ -5,6 +5,7 @@ other than plain tensors and ints and for whatever fails a check; those, and all
 module (built for another torch or Python) every call does."""
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import importlib.util
 import os
@@ -92,6 +93,16 @@ def _load() -> ctypes.CDLL:
     L.chunkkv_pipe_status.argtypes = [vp, vp]
     L.chunkkv_pipe_close.restype = i32
     L.chunkkv_pipe_close.argtypes = [vp]
+    L.chunkkv_rotate_qk.restype = i32
+    L.chunkkv_rotate_qk.argtypes = [vp, ctypes.c_longlong] + [i32] * 4 + [vp, vp, ctypes.c_float, vp, vp, i32, vp] + [ctypes.c_longlong] * 4 + [vp, vp, vp]
+    L.chunkkv_append_paged.restype = i32
+    L.chunkkv_append_paged.argtypes = [vp, ctypes.c_longlong] + [i32] * 4 + [vp, vp, ctypes.c_float, vp, vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp]
+    L.chunkkv_attend_scratch_bytes.restype = sz
+    L.chunkkv_attend_scratch_bytes.argtypes = [i32] * 7
+    L.chunkkv_attend_paged.restype = i32
+    L.chunkkv_attend_paged.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp] + [i32] * 4 + [vp, vp, vp, sz, vp]
+    L.chunkkv_evict_paged.restype = i32
+    L.chunkkv_evict_paged.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp] + [i32] * 6 + [vp, vp]
     L.chunkkv_jaccard.restype = i32
     L.chunkkv_jaccard.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp]
     L.chunkkv_score_noalloc.restype = i32
@@ -485,6 +496,164 @@ def compress_layer_paged(q_obs: Optional[torch.Tensor], K: torch.Tensor, V: torc
                                             _ptr(reuse_idx), block_table.data_ptr(), cache_K.shape[1], cache_K.shape[0],
                                             cache_K.data_ptr(), cache_V.data_ptr(), out_idx.data_ptr(), _stream(stream)),
            "chunkkv_compress_layer_paged")
+    return out_idx
+
+
+@contextlib.contextmanager
+def _on(dev: torch.device, stream: Optional[torch.cuda.Stream]):
+    """The device of a call's tensors and its stream as the current ones: what is allocated inside belongs to that stream."""
+    with torch.cuda.device(dev), torch.cuda.stream(stream):
+        yield
+
+
+def _together(first: torch.Tensor, **others: Optional[torch.Tensor]) -> None:
+    for name, t in others.items():
+        if t is not None and t.device != first.device:
+            raise ValueError(f"{name} must be on {first.device}")
+
+
+def _angles(cos: torch.Tensor, sin: torch.Tensor, d: int) -> int:
+    """Rows of the angle tables [n_pos, d / 2] f32."""
+    for t, name in ((cos, "cos"), (sin, "sin")):
+        if _dev(t, torch.float32, name).dim() != 2 or t.shape[1] != d // 2 or t.shape[0] != cos.shape[0]:
+            raise ValueError(f"{name} must be [positions, {d // 2}]")
+    return cos.shape[0]
+
+
+def _fused(qkv: torch.Tensor, heads: int, d: int, positions: torch.Tensor, q_gain: Optional[torch.Tensor], k_gain: Optional[torch.Tensor]) -> Tuple[int, int]:
+    """Tokens and row length of a fused activation of so many heads, with its tokens' positions and the heads' gains."""
+    if _dev(qkv, torch.bfloat16, "qkv").dim() != 2 or qkv.shape[1] < heads * d:
+        raise ValueError(f"qkv must be [tokens, at least {heads * d}]")
+    _sized(positions, torch.int32, qkv.shape[0], "positions")
+    for t, name in ((q_gain, "q_gain"), (k_gain, "k_gain")):
+        if t is not None:
+            _sized(t, torch.bfloat16, d, name)
+    return qkv.shape[0], qkv.shape[1]
+
+
+def _cache(block_tables: torch.Tensor, lengths: torch.Tensor, cache_K: torch.Tensor, cache_V: torch.Tensor, B: int) -> Tuple[int, int, int, int, int]:
+    """(pages, page_size, Hkv, d, max_pages) of a paged cache [pages, page_size, Hkv, d] with tables [B, max_pages] and lengths [B, Hkv]."""
+    if _dev(cache_K, torch.bfloat16, "cache_K").dim() != 4:
+        raise ValueError("cache_K must be [pages, page_size, Hkv, d]")
+    if tuple(_dev(cache_V, torch.bfloat16, "cache_V").shape) != tuple(cache_K.shape):
+        raise ValueError("cache_V must be as large as cache_K")
+    if _dev(block_tables, torch.int32, "block_tables").dim() != 2 or block_tables.shape[0] != B:
+        raise ValueError(f"block_tables must be [{B}, pages of a sequence]")
+    if tuple(_dev(lengths, torch.int32, "lengths").shape) != (B, cache_K.shape[2]):
+        raise ValueError(f"lengths must be [{B}, {cache_K.shape[2]}]")
+    return (*cache_K.shape, block_tables.shape[1])
+
+
+def _sums(weights: torch.Tensor, B: int, Hkv: int, rows: int) -> None:
+    if tuple(_dev(weights, torch.float32, "weights").shape) != (B, Hkv, rows):
+        raise ValueError(f"weights must be [{B}, {Hkv}, {rows}]")
+
+
+def rotate_qk(qkv: torch.Tensor, Hq: int, Hkv: int, d: int, cos: torch.Tensor, sin: torch.Tensor, positions: torch.Tensor,
+              q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
+              out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None,
+              stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Queries [T, Hq, d] and keys [T, Hkv, d] bf16 of a fused QKV activation [T, row_elems] bf16, with each head's norm
+    (where gains [d] are given) and the rotary embedding of rows positions [T] int32 of cos / sin [n_pos, d / 2] f32. out_q / out_k
+    may be views of any token and head stride with a contiguous last dimension, such as ``K.permute(1, 0, 2)`` of keys [Hkv, T, d]
+    or the place in qkv."""
+    r = _native.rotate_qk(qkv, Hq, Hkv, d, cos, sin, positions, q_gain, k_gain, eps, out_q, out_k, stream)
+    if r is not None:
+        return _done(r, "chunkkv_rotate_qk")
+    T, row_elems = _fused(qkv, Hq + Hkv, d, positions, q_gain, k_gain)
+    n_pos = _angles(cos, sin, d)
+    for t, H, name in ((out_q, Hq, "out_q"), (out_k, Hkv, "out_k")):
+        if t is not None and not (t.is_cuda and t.dtype == torch.bfloat16 and tuple(t.shape) == (T, H, d) and t.stride(2) == 1):
+            raise ValueError(f"{name}: a CUDA bf16 [{T}, {H}, {d}] view with a contiguous last dimension is required")
+    _together(qkv, cos=cos, sin=sin, positions=positions, q_gain=q_gain, k_gain=k_gain, out_q=out_q, out_k=out_k)
+    with _on(qkv.device, stream):
+        if out_q is None:
+            out_q = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=qkv.device)
+        if out_k is None:
+            out_k = torch.empty((T, Hkv, d), dtype=torch.bfloat16, device=qkv.device)
+        # (the strides of a single token or head are free)
+        st = [d if n <= 1 else s for t in (out_q, out_k) for s, n in zip(t.stride()[:2], t.shape)]
+        _check(lib.chunkkv_rotate_qk(qkv.data_ptr(), row_elems, T, Hq, Hkv, d, _ptr(q_gain), _ptr(k_gain), eps, cos.data_ptr(), sin.data_ptr(),
+                                     n_pos, positions.data_ptr(), *st, out_q.data_ptr(), out_k.data_ptr(), _stream(stream)), "chunkkv_rotate_qk")
+    return out_q, out_k
+
+
+def append_paged(qkv: torch.Tensor, Hq: int, cos: torch.Tensor, sin: torch.Tensor, positions: torch.Tensor, block_tables: torch.Tensor,
+                 lengths: torch.Tensor, cache_K: torch.Tensor, cache_V: torch.Tensor, q_gain: Optional[torch.Tensor] = None,
+                 k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6, out_q: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """One token of each of B sequences: its queries [B, Hq, d], normalised and rotated as by rotate_qk, and its keys and values as
+    the last of the lengths [B, Hkv] int32 rows (the token counted) of every head of a paged cache with tables [B, max_pages] int32."""
+    r = _native.append_paged(qkv, Hq, cos, sin, positions, block_tables, lengths, cache_K, cache_V, q_gain, k_gain, eps, out_q, stream)
+    if r is not None:
+        return _done(r, "chunkkv_append_paged")
+    B = _dev(qkv, torch.bfloat16, "qkv").shape[0]
+    pages, page_size, Hkv, d, max_pages = _cache(block_tables, lengths, cache_K, cache_V, B)
+    _, row_elems = _fused(qkv, Hq + 2 * Hkv, d, positions, q_gain, k_gain)
+    n_pos = _angles(cos, sin, d)
+    if out_q is not None:
+        _sized(out_q, torch.bfloat16, B * Hq * d, "out_q")
+    _together(qkv, cos=cos, sin=sin, positions=positions, block_tables=block_tables, lengths=lengths, cache_K=cache_K, cache_V=cache_V,
+              q_gain=q_gain, k_gain=k_gain, out_q=out_q)
+    with _on(qkv.device, stream):
+        if out_q is None:
+            out_q = torch.empty((B, Hq, d), dtype=torch.bfloat16, device=qkv.device)
+        _check(lib.chunkkv_append_paged(qkv.data_ptr(), row_elems, B, Hq, Hkv, d, _ptr(q_gain), _ptr(k_gain), eps, cos.data_ptr(), sin.data_ptr(),
+                                        n_pos, positions.data_ptr(), block_tables.data_ptr(), max_pages, lengths.data_ptr(), page_size, pages,
+                                        cache_K.data_ptr(), cache_V.data_ptr(), out_q.data_ptr(), _stream(stream)), "chunkkv_append_paged")
+    return out_q
+
+
+def attend_paged(q: torch.Tensor, block_tables: torch.Tensor, lengths: torch.Tensor, cache_K: torch.Tensor, cache_V: torch.Tensor,
+                 weights: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Attention [B, Hq, d] of one token a sequence (q [B, Hq, d] bf16) over the first lengths [B, Hkv] rows of every head of a paged
+    cache. With weights [B, Hkv, max_pages * page_size] f32, the attention that every row received is added to them."""
+    r = _native.attend_paged(q, block_tables, lengths, cache_K, cache_V, weights, out, stream)
+    if r is not None:
+        return _done(r, "chunkkv_attend_paged")
+    if _dev(q, torch.bfloat16, "q").dim() != 3:
+        raise ValueError("q must be [B, Hq, d]")
+    B, Hq = q.shape[0], q.shape[1]
+    pages, page_size, Hkv, d, max_pages = _cache(block_tables, lengths, cache_K, cache_V, B)
+    if q.shape[2] != d:
+        raise ValueError(f"q must be [B, Hq, {d}]")
+    if weights is not None:
+        _sums(weights, B, Hkv, max_pages * page_size)
+    if out is not None:
+        _sized(out, torch.bfloat16, B * Hq * d, "out")
+    _together(q, block_tables=block_tables, lengths=lengths, cache_K=cache_K, cache_V=cache_V, weights=weights, out=out)
+    with _on(q.device, stream):
+        if out is None:
+            out = torch.empty((B, Hq, d), dtype=torch.bfloat16, device=q.device)
+        # scratch of this call: the allocator hands it out again only behind it on its stream
+        need = int(lib.chunkkv_attend_scratch_bytes(B, Hq, Hkv, d, max_pages, page_size, int(weights is not None)))
+        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+        _check(lib.chunkkv_attend_paged(q.data_ptr(), block_tables.data_ptr(), max_pages, lengths.data_ptr(), page_size, pages, cache_K.data_ptr(),
+                                        cache_V.data_ptr(), B, Hq, Hkv, d, _ptr(weights), out.data_ptr(), scratch.data_ptr(), need, _stream(stream)),
+               "chunkkv_attend_paged")
+    return out
+
+
+def evict_paged(weights: torch.Tensor, block_tables: torch.Tensor, lengths: torch.Tensor, cache_K: torch.Tensor, cache_V: torch.Tensor, w: int,
+                c: int, budget: int, out_idx: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Every head of more than `budget` rows back to at most that many, in place: whole chunks of c rows with the largest weights, and
+    the last w rows. weights [B, Hkv, max_pages * page_size] f32, lengths and the cache change; returns idx [B, Hkv, budget] int32, the
+    former row of every row (-1 behind the last)."""
+    r = _native.evict_paged(weights, block_tables, lengths, cache_K, cache_V, w, c, budget, out_idx, stream)
+    if r is not None:
+        return _done(r, "chunkkv_evict_paged")
+    B = _dev(lengths, torch.int32, "lengths").shape[0]
+    pages, page_size, Hkv, d, max_pages = _cache(block_tables, lengths, cache_K, cache_V, B)
+    _sums(weights, B, Hkv, max_pages * page_size)
+    if out_idx is not None:
+        _sized(out_idx, torch.int32, B * Hkv * budget, "out_idx")
+    _together(weights, block_tables=block_tables, lengths=lengths, cache_K=cache_K, cache_V=cache_V, out_idx=out_idx)
+    with _on(weights.device, stream):
+        if out_idx is None:
+            out_idx = torch.empty((B, Hkv, max(budget, 0)), dtype=torch.int32, device=weights.device)
+        _check(lib.chunkkv_evict_paged(weights.data_ptr(), block_tables.data_ptr(), max_pages, lengths.data_ptr(), page_size, pages, cache_K.data_ptr(),
+                                       cache_V.data_ptr(), B, Hkv, d, w, c, budget, out_idx.data_ptr(), _stream(stream)), "chunkkv_evict_paged")
     return out_idx
 
 

@@ -2,6 +2,7 @@
 // launch sequence of each entry point. Every step of the method runs in the kernels of
 // score.cu / select.cu / gather.cu; this file only validates and dispatches.
 #include "../../include/chunkkv.h"
+#include "decode.h"
 #include "internal.h"
 
 #include <math.h>
@@ -737,6 +738,157 @@ int chunkkv_jaccard(const int32_t* idx_a, const int32_t* idx_b, int Hkv, int n_a
     cudaError_t e = launch_jaccard(idx_a, idx_b, Hkv, n_a, n_b, out_ratio, out_counts, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e);
     return CHUNKKV_OK;
+}
+
+// ---- The decode side of the compacted cache: queries and keys of a token normalised, rotated and appended, attention over the
+//      paged cache, and eviction from it.
+static int check_decode_heads(int n, int Hq, int Hkv, int d) {
+    if (n < 0 || Hkv < 1 || Hq < Hkv || Hq % Hkv != 0 || Hq > 65535 || (d != 64 && d != 128)) return CHUNKKV_EINVAL_SHAPE;
+    return static_cast<long long>(n) * Hq >= (1LL << 30) ? CHUNKKV_EINVAL_SHAPE : CHUNKKV_OK;
+}
+static int check_decode_cache(int max_pages, int page_size, int num_pages) {
+    if (max_pages < 1 || page_size < 1 || num_pages < 1) return CHUNKKV_EINVAL_SHAPE;
+    if (static_cast<long long>(max_pages) * page_size >= (1LL << 30) || static_cast<long long>(num_pages) * page_size >= (1LL << 31))
+        return CHUNKKV_EINVAL_SHAPE;
+    return CHUNKKV_OK;
+}
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+static PagedCache paged_cache(const int32_t* tables, int max_pages, int page_size, int num_pages) {
+    return {tables, max_pages, page_size, num_pages, max_pages * page_size};
+}
+
+int chunkkv_rotate_qk(const void* qkv, long long row_elems, int T, int Hq, int Hkv, int d, const void* q_gain, const void* k_gain, float eps,
+                      const float* cos_t, const float* sin_t, int n_pos, const int32_t* positions, long long q_token_stride,
+                      long long q_head_stride, long long k_token_stride, long long k_head_stride, void* out_q, void* out_k, void* stream) {
+    int st = check_decode_heads(T, Hq, Hkv, d);
+    if (st != CHUNKKV_OK) return st;
+    if (row_elems < static_cast<long long>(Hq + Hkv) * d || n_pos < 1 || !(eps >= 0.f) || isinf(eps)) return CHUNKKV_EINVAL_SHAPE;
+    for (long long s : {q_token_stride, q_head_stride, k_token_stride, k_head_stride})
+        if (s < d || (s & 7) != 0) return CHUNKKV_EINVAL_SHAPE;
+    if (T == 0) return CHUNKKV_OK;
+    if (qkv == nullptr || cos_t == nullptr || sin_t == nullptr || positions == nullptr || out_q == nullptr || out_k == nullptr) return CHUNKKV_EINVAL_NULL;
+    if ((row_elems & 7) != 0 || !aligned16(qkv) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned16(cos_t) || !aligned16(sin_t) ||
+        !aligned4(positions) || !aligned16(out_q) || !aligned16(out_k))
+        return CHUNKKV_EINVAL_ALIGN;
+    std::lock_guard<std::mutex> lk(g_mu);
+    DeviceCtx* ctx;
+    st = get_ctx(&ctx);
+    if (st != CHUNKKV_OK) return st;
+    RotateArgs a = {};
+    a.qkv = static_cast<const __nv_bfloat16*>(qkv);
+    a.row_elems = row_elems; a.T = T; a.Hq = Hq; a.Hkv = Hkv;
+    a.gain_q = static_cast<const __nv_bfloat16*>(q_gain);
+    a.gain_k = static_cast<const __nv_bfloat16*>(k_gain);
+    a.eps = eps; a.cos_t = cos_t; a.sin_t = sin_t; a.n_pos = n_pos; a.positions = positions;
+    a.out_q = static_cast<__nv_bfloat16*>(out_q);
+    a.out_k = static_cast<__nv_bfloat16*>(out_k);
+    a.q_token = q_token_stride; a.q_head = q_head_stride; a.k_token = k_token_stride; a.k_head = k_head_stride;
+    const cudaError_t e = launch_rotate(a, d, ctx->num_sms, static_cast<cudaStream_t>(stream));
+    return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
+}
+
+int chunkkv_append_paged(const void* qkv, long long row_elems, int B, int Hq, int Hkv, int d, const void* q_gain, const void* k_gain, float eps,
+                         const float* cos_t, const float* sin_t, int n_pos, const int32_t* positions, const int32_t* block_tables,
+                         int max_pages, const int32_t* lengths, int page_size, int num_pages, void* cache_K, void* cache_V, void* out_q,
+                         void* stream) {
+    int st = check_decode_heads(B, Hq, Hkv, d);
+    if (st == CHUNKKV_OK) st = check_decode_cache(max_pages, page_size, num_pages);
+    if (st != CHUNKKV_OK) return st;
+    if (row_elems < static_cast<long long>(Hq + 2 * Hkv) * d || n_pos < 1 || !(eps >= 0.f) || isinf(eps)) return CHUNKKV_EINVAL_SHAPE;
+    if (B == 0) return CHUNKKV_OK;
+    if (qkv == nullptr || cos_t == nullptr || sin_t == nullptr || positions == nullptr || block_tables == nullptr || lengths == nullptr ||
+        cache_K == nullptr || cache_V == nullptr || out_q == nullptr)
+        return CHUNKKV_EINVAL_NULL;
+    if ((row_elems & 7) != 0 || !aligned16(qkv) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned16(cos_t) || !aligned16(sin_t) ||
+        !aligned4(positions) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) || !aligned16(out_q))
+        return CHUNKKV_EINVAL_ALIGN;
+    std::lock_guard<std::mutex> lk(g_mu);
+    DeviceCtx* ctx;
+    st = get_ctx(&ctx);
+    if (st != CHUNKKV_OK) return st;
+    RotateArgs a = {};
+    a.qkv = static_cast<const __nv_bfloat16*>(qkv);
+    a.row_elems = row_elems; a.T = B; a.Hq = Hq; a.Hkv = Hkv;
+    a.gain_q = static_cast<const __nv_bfloat16*>(q_gain);
+    a.gain_k = static_cast<const __nv_bfloat16*>(k_gain);
+    a.eps = eps; a.cos_t = cos_t; a.sin_t = sin_t; a.n_pos = n_pos; a.positions = positions;
+    a.out_q = static_cast<__nv_bfloat16*>(out_q);
+    a.q_token = static_cast<long long>(Hq) * d; a.q_head = d;
+    a.cache_K = static_cast<__nv_bfloat16*>(cache_K);
+    a.cache_V = static_cast<__nv_bfloat16*>(cache_V);
+    a.lengths = lengths;
+    a.cache = paged_cache(block_tables, max_pages, page_size, num_pages);
+    const cudaError_t e = launch_rotate(a, d, ctx->num_sms, static_cast<cudaStream_t>(stream));
+    return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
+}
+
+size_t chunkkv_attend_scratch_bytes(int B, int Hq, int Hkv, int d, int max_pages, int page_size, int with_weights) {
+    if (B < 1 || check_decode_heads(B, Hq, Hkv, d) != CHUNKKV_OK || check_decode_cache(max_pages, page_size, 1) != CHUNKKV_OK) return 0;
+    return attend_plan(B, Hq, Hkv, d, max_pages * page_size, with_weights != 0).bytes;
+}
+
+int chunkkv_attend_paged(const void* q, const int32_t* block_tables, int max_pages, const int32_t* lengths, int page_size, int num_pages,
+                         const void* cache_K, const void* cache_V, int B, int Hq, int Hkv, int d, float* weights, void* out, void* scratch,
+                         size_t scratch_bytes, void* stream) {
+    int st = check_decode_heads(B, Hq, Hkv, d);
+    if (st == CHUNKKV_OK) st = check_decode_cache(max_pages, page_size, num_pages);
+    if (st != CHUNKKV_OK) return st;
+    const int cap = max_pages * page_size;
+    if (weights != nullptr && static_cast<long long>(B) * Hkv * (cap / 512 + 1) >= (1LL << 30)) return CHUNKKV_EINVAL_SHAPE;   // CTAs of a launch
+    if (B == 0) return CHUNKKV_OK;
+    if (q == nullptr || block_tables == nullptr || lengths == nullptr || cache_K == nullptr || cache_V == nullptr || out == nullptr) return CHUNKKV_EINVAL_NULL;
+    if (!aligned16(q) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) || !aligned4(weights) || !aligned16(out))
+        return CHUNKKV_EINVAL_ALIGN;
+    const AttendPlan plan = attend_plan(B, Hq, Hkv, d, cap, weights != nullptr);
+    if (scratch == nullptr || scratch_bytes < plan.bytes) return CHUNKKV_ENOWORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return CHUNKKV_EINVAL_ALIGN;
+    std::lock_guard<std::mutex> lk(g_mu);
+    DeviceCtx* ctx;
+    st = get_ctx(&ctx);
+    if (st != CHUNKKV_OK) return st;
+    AttendArgs a = {};
+    a.q = static_cast<const __nv_bfloat16*>(q);
+    a.K = static_cast<const __nv_bfloat16*>(cache_K);
+    a.V = static_cast<const __nv_bfloat16*>(cache_V);
+    a.lengths = lengths;
+    a.cache = paged_cache(block_tables, max_pages, page_size, num_pages);
+    a.B = B; a.Hq = Hq; a.Hkv = Hkv;
+    a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(d)));
+    a.weights = weights;
+    a.out = static_cast<__nv_bfloat16*>(out);
+    const cudaError_t e = launch_attend(a, plan, d, static_cast<char*>(scratch), ctx->num_sms, static_cast<cudaStream_t>(stream));
+    return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
+}
+
+int chunkkv_evict_paged(float* weights, const int32_t* block_tables, int max_pages, int32_t* lengths, int page_size, int num_pages,
+                        void* cache_K, void* cache_V, int B, int Hkv, int d, int w, int c, int budget, int32_t* out_idx, void* stream) {
+    int st = check_decode_heads(B, Hkv, Hkv, d);
+    if (st == CHUNKKV_OK) st = check_decode_cache(max_pages, page_size, num_pages);
+    if (st != CHUNKKV_OK) return st;
+    if (w < 0 || c < 1 || budget < 1 || static_cast<long long>(budget) < static_cast<long long>(w) + c - 1) return CHUNKKV_EINVAL_SHAPE;
+    const int cap = max_pages * page_size;
+    if (cap / c > 65535) return CHUNKKV_ETOOLARGE;
+    if (B == 0) return CHUNKKV_OK;
+    if (weights == nullptr || block_tables == nullptr || lengths == nullptr || cache_K == nullptr || cache_V == nullptr || out_idx == nullptr)
+        return CHUNKKV_EINVAL_NULL;
+    if (!aligned4(weights) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) || !aligned4(out_idx))
+        return CHUNKKV_EINVAL_ALIGN;
+    std::lock_guard<std::mutex> lk(g_mu);
+    DeviceCtx* ctx;
+    st = get_ctx(&ctx);
+    if (st != CHUNKKV_OK) return st;
+    EvictArgs a = {};
+    a.weights = weights;
+    a.lengths = lengths;
+    a.K = static_cast<uint4*>(cache_K);
+    a.V = static_cast<uint4*>(cache_V);
+    a.cache = paged_cache(block_tables, max_pages, page_size, num_pages);
+    a.Hkv = Hkv; a.w = w; a.c = c; a.budget = budget;
+    a.out_idx = out_idx;
+    const EvictPlan plan = evict_plan(cap, c, smem_budget(*ctx));
+    if (!plan.fits) return CHUNKKV_ETOOLARGE;
+    const cudaError_t e = launch_evict(a, plan, B, d, ctx->num_sms, static_cast<cudaStream_t>(stream));
+    return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
 }
 
 int chunkkv_compress_layer(const void* q_obs, const void* K, const void* V, int L, int Hq, int Hkv,

@@ -1,0 +1,483 @@
+// Attention of one new token over a paged cache: out = softmax(q K^T / sqrt(d)) V for every query head, over the rows that its KV head
+// has (a length of its own), and, on request, the attention that every row received added to a running sum.
+//
+// What bounds it is the cache: every row is read once, 4 d bytes for 4 G d operations (G query heads of a KV head), so the product must not be what
+// the memory waits for. The products run on the tensor cores with the heads of a group as eight columns: a warp takes 16 rows at
+// a time, S = Q K^T as m16n8k16 (heads x rows; half of the 16 heads are zero up to G = 8) and O^T += V^T P^T (dims x heads). Keys and values go
+// from global memory to registers in 16-byte loads with no stop in shared memory: which 8 of a row's dims a lane holds is free as long
+// as queries (for the product over dims) or outputs (for the dims of O^T) are dealt the same way, and V^T comes out of two rows' registers by
+// byte permutes. P is split into two bf16 terms, so that its rounding (2^-16) is not seen beside that of the output.
+//
+// The rows of all (sequence, KV head) units are cut into tiles of 64 and dealt evenly to the CTAs in one line, so that lengths need not be
+// alike; a CTA walks the units in its share and leaves (max, sum, O) records for those that it shares with others, which a second launch joins in
+// the order of the CTAs (same result every time). The records live in scratch of the call's own: calls at the same time, and
+// captured ones, have nothing in common.
+#include "decode.cuh"
+
+namespace chunkkv {
+
+namespace {
+
+constexpr int kAttWarps = 4;
+constexpr int kAttThreads = 32 * kAttWarps;
+constexpr int kAttStep = 16;                          // rows of a warp's step
+constexpr int kAttTile = kAttWarps * kAttStep;        // rows that are dealt together
+constexpr int kJoinRows = 512;                        // rows of the sums that a CTA of the join takes
+constexpr int kJoinThreads = 128;
+static_assert(kJoinThreads == kAttThreads, "both kernels deal with as many threads");
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// A maximum as the reference of exponents: 0 where nothing was seen.
+__device__ __forceinline__ float reference_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+__device__ __forceinline__ int rows_of(const AttendArgs& a, int bh) { return min(max(__ldg(a.lengths + bh), 0), a.cache.cap); }
+__device__ __forceinline__ int tiles_of(int rows) { return (rows + kAttTile - 1) / kAttTile; }
+
+// The line of tiles: the units (sequence, KV head) in order, each `groups` times its tiles (one for each group of query heads).
+struct Deal {
+    long long total;      // tiles in all
+    int bh;               // the unit asked for, or the one that holds the tile asked for
+    long long first;      // its first tile
+};
+struct DealSmem {
+    long long warp[kAttWarps];
+    long long first;
+    int bh;
+};
+// CTAs that the line is dealt to: no more than it has tiles, so that each has one at least.
+__device__ __forceinline__ int dealt_to(long long total, int n_cta) { return static_cast<int>(min(total, static_cast<long long>(n_cta))); }
+
+// All threads. want >= 0: that unit; else the one that holds the first tile of CTA `cta` of a launch of n_cta.
+__device__ __forceinline__ Deal deal(const AttendArgs& a, int want, int cta, int n_cta, DealSmem& sm) {
+    const int units = a.B * a.Hkv, per = (units + kAttThreads - 1) / kAttThreads;
+    const int u0 = min(static_cast<int>(threadIdx.x) * per, units), u1 = min(u0 + per, units);
+    long long mine = 0;
+    for (int u = u0; u < u1; ++u) mine += tiles_of(rows_of(a, u));
+    mine *= a.groups;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long inc = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const long long v = __shfl_up_sync(0xffffffffu, inc, off);
+        if (lane >= off) inc += v;
+    }
+    if (lane == 31) sm.warp[warp] = inc;
+    if (threadIdx.x == 0) sm.bh = units;
+    __syncthreads();
+    long long total = 0;
+#pragma unroll
+    for (int w = 0; w < kAttWarps; ++w) {
+        if (w < warp) inc += sm.warp[w];
+        total += sm.warp[w];
+    }
+    const int n = dealt_to(total, n_cta);
+    const long long tile = want < 0 ? (cta < n ? total * cta / n : total) : 0;
+    long long at = inc - mine;
+    if (want < 0 ? (at <= tile && tile < inc) : (u0 <= want && want < u1)) {       // one thread, if any
+        for (int u = u0; u < u1; ++u) {
+            const long long t = static_cast<long long>(tiles_of(rows_of(a, u))) * a.groups;
+            if (want < 0 ? tile < at + t : u == want) { sm.bh = u; sm.first = at; break; }
+            at += t;
+        }
+    }
+    __syncthreads();
+    return {total, sm.bh, sm.first};
+}
+// The CTA of n that tile x falls to, where CTA i has the tiles [i total / n, (i + 1) total / n).
+__device__ __forceinline__ int owner_of(long long x, long long total, int n) { return static_cast<int>(((x + 1) * n - 1) / total); }
+
+// Where records of CTA `cta` are: one for a unit that an earlier CTA has begun, one for a unit that it begins itself.
+__device__ __forceinline__ size_t record(int cta, bool begins) { return static_cast<size_t>(cta) * 2 + (begins ? 1 : 0); }
+
+template <int D, int NH>
+struct AttSmem {
+    static constexpr int kPad = D + 4;
+    float o[kAttWarps][8 * NH][kPad];
+    float m[kAttWarps][8 * NH], l[kAttWarps][8 * NH];
+    DealSmem deal;
+};
+
+// D: head dim; NH: query heads of a group in eights.
+template <int D, int NH, bool SUMS>
+__global__ void __launch_bounds__(kAttThreads, NH == 1 ? 3 : 2) attend_kernel(const AttendArgs a) {
+    constexpr unsigned kFull = 0xffffffffu;
+    constexpr int kCh = D / 32;                   // 16-byte pieces of a key row that a lane holds
+    constexpr int kVh = D / 64;                   // and of a value row
+    __shared__ __align__(16) AttSmem<D, NH> sm;
+    begin_dependent();
+    const int cta = blockIdx.x, units = a.B * a.Hkv;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const Deal dl = deal(a, -1, cta, gridDim.x, sm.deal);
+    const int n_cta = dealt_to(dl.total, gridDim.x);
+    if (cta >= n_cta) return;
+    long long x = dl.total * cta / n_cta;
+    const long long x1 = dl.total * (cta + 1) / n_cta;
+    int bh = dl.bh;
+    long long first = dl.first;
+    while (x < x1 && bh < units) {
+        const int rows = rows_of(a, bh), tiles = tiles_of(rows);
+        const int grp = static_cast<int>((x - first) / tiles);
+        const long long unit0 = first + static_cast<long long>(grp) * tiles;              // the unit's first tile
+        const int tile0 = static_cast<int>(x - unit0), tile1 = static_cast<int>(min(x1 - unit0, static_cast<long long>(tiles)));
+        const int b = bh / a.Hkv, h = bh - b * a.Hkv;
+        const int G = a.Hq / a.Hkv, g0 = grp * 8 * NH, heads = min(8 * NH, G - g0);       // query heads of this group
+        const int r1 = min(rows, tile1 * kAttTile);
+        const int32_t* table = a.cache.tables + static_cast<size_t>(b) * a.cache.max_pages;
+        const __nv_bfloat16* qh = a.q + (static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + g0) * D;
+        const size_t row_elems = static_cast<size_t>(a.Hkv) * D;
+        const __nv_bfloat16 *Kh = a.K + static_cast<size_t>(h) * D + 8 * t, *Vh = a.V + static_cast<size_t>(h) * D + 8 * g;
+
+        // lane l (and l + 16) looks up row l of a step
+        auto lookup = [&](int base) {
+            const int r = base + (lane & 15);
+            return r < r1 ? paged_row(a.cache, table, r) : -1;
+        };
+        uint4 kr[2][kCh], vr[4][kVh];
+        auto load_keys = [&](int at) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int row = __shfl_sync(kFull, at, 8 * j + g);
+                const __nv_bfloat16* p = Kh + static_cast<size_t>(max(row, 0)) * row_elems;
+#pragma unroll
+                for (int i = 0; i < kCh; ++i) kr[j][i] = row >= 0 ? load_once(p + 32 * i) : make_uint4(0, 0, 0, 0);
+            }
+        };
+        auto load_values = [&](int at) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = __shfl_sync(kFull, at, (j >> 1) * 8 + 2 * t + (j & 1));
+                const __nv_bfloat16* p = Vh + static_cast<size_t>(max(row, 0)) * row_elems;
+#pragma unroll
+                for (int i = 0; i < kVh; ++i) vr[j][i] = row >= 0 ? load_once(p + 64 * i) : make_uint4(0, 0, 0, 0);
+            }
+        };
+
+        int base = tile0 * kAttTile + warp * kAttStep;
+        int at = lookup(base);
+        load_keys(at);
+        load_values(at);
+        int at_next = lookup(base + kAttTile);
+        uint4 qr[NH][kCh];
+#pragma unroll
+        for (int n = 0; n < NH; ++n)
+#pragma unroll
+            for (int i = 0; i < kCh; ++i)
+                qr[n][i] = 8 * n + g < heads ? __ldg(reinterpret_cast<const uint4*>(qh + static_cast<size_t>(8 * n + g) * D + 32 * i + 8 * t)) : make_uint4(0, 0, 0, 0);
+
+        float m[NH], l[NH], o[NH][D / 16][4];
+#pragma unroll
+        for (int n = 0; n < NH; ++n) {
+            m[n] = -INFINITY;
+            l[n] = 0.f;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
+        }
+
+        for (; base < r1; base += kAttTile) {
+            // S: rows of the product are the query heads g and g + 8, columns the cache rows 2t and 2t + 1 of eight
+            float s[2][4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+#pragma unroll
+                for (int i = 0; i < kCh; ++i) {
+                    const uint4 k = kr[j][i];
+                    mma_bf16(s[j], qr[0][i].x, NH == 2 ? qr[NH - 1][i].x : 0u, qr[0][i].y, NH == 2 ? qr[NH - 1][i].y : 0u, k.x, k.y);
+                    mma_bf16(s[j], qr[0][i].z, NH == 2 ? qr[NH - 1][i].z : 0u, qr[0][i].w, NH == 2 ? qr[NH - 1][i].w : 0u, k.z, k.w);
+                }
+            }
+            unsigned seen = 0;                                  // bit 2j + e: row base + 8j + 2t + e
+#pragma unroll
+            for (int j = 0; j < 4; ++j) seen |= __shfl_sync(kFull, at, (j >> 1) * 8 + 2 * t + (j & 1)) >= 0 ? 1u << j : 0u;
+            load_keys(at_next);                                 // (the keys' registers are free)
+            const int at_after = lookup(base + 2 * kAttTile);
+
+            uint32_t hi[NH][2], lo[NH][2];
+            float factor[NH];
+            bool moved = false;
+#pragma unroll
+            for (int n = 0; n < NH; ++n) {
+                float v[2][2], mx = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        v[j][e] = seen >> (2 * j + e) & 1u ? s[j][2 * n + e] * a.scale_log2 : -INFINITY;
+                        mx = fmaxf(mx, v[j][e]);
+                    }
+                if constexpr (SUMS) {
+                    if (8 * n + g < heads) {
+                        float* lg = a.logits + (static_cast<size_t>(bh) * G + g0 + 8 * n + g) * a.logit_stride + base + 2 * t;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)             // (the stride is even and covers every row, so a pair fits)
+                            if (base + 8 * j + 2 * t < r1) *reinterpret_cast<float2*>(lg + 8 * j) = make_float2(v[j][0], v[j][1]);
+                    }
+                }
+                mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, 1));
+                mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, 2));
+                const float m_new = fmaxf(m[n], mx), ref = reference_of(m_new);
+                factor[n] = exp2_fast(m[n] - ref);
+                moved |= m_new != m[n];
+                m[n] = m_new;
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float p0 = exp2_fast(v[j][0] - ref), p1 = exp2_fast(v[j][1] - ref);
+                    sum += p0 + p1;
+                    hi[n][j] = pack_bf16(p0, p1);
+                    const float2 r = bf16_pair(hi[n][j]);
+                    lo[n][j] = pack_bf16(p0 - r.x, p1 - r.y);
+                }
+                l[n] = l[n] * factor[n] + sum;
+            }
+            if (__any_sync(kFull, moved)) {
+#pragma unroll
+                for (int n = 0; n < NH; ++n) {                  // O^T: columns are the heads 2t and 2t + 1
+                    const float f0 = __shfl_sync(kFull, factor[n], 8 * t), f1 = __shfl_sync(kFull, factor[n], 8 * t + 4);
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) { o[n][i][0] *= f0; o[n][i][1] *= f1; o[n][i][2] *= f0; o[n][i][3] *= f1; }
+                }
+            }
+            // O^T += V^T P^T: row g of the product's tile (hh, q) is dim 64 hh + 8 g + 2 q, row g + 8 the next dim
+#pragma unroll
+            for (int hh = 0; hh < kVh; ++hh) {
+                const uint32_t w0[4] = {vr[0][hh].x, vr[0][hh].y, vr[0][hh].z, vr[0][hh].w}, w1[4] = {vr[1][hh].x, vr[1][hh].y, vr[1][hh].z, vr[1][hh].w};
+                const uint32_t w2[4] = {vr[2][hh].x, vr[2][hh].y, vr[2][hh].z, vr[2][hh].w}, w3[4] = {vr[3][hh].x, vr[3][hh].y, vr[3][hh].z, vr[3][hh].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t a0 = __byte_perm(w0[q], w1[q], 0x5410), a1 = __byte_perm(w0[q], w1[q], 0x7632);
+                    const uint32_t a2 = __byte_perm(w2[q], w3[q], 0x5410), a3 = __byte_perm(w2[q], w3[q], 0x7632);
+#pragma unroll
+                    for (int n = 0; n < NH; ++n) {
+                        mma_bf16(o[n][4 * hh + q], a0, a1, a2, a3, hi[n][0], hi[n][1]);
+                        mma_bf16(o[n][4 * hh + q], a0, a1, a2, a3, lo[n][0], lo[n][1]);
+                    }
+                }
+            }
+            load_values(at_next);
+            at = at_next;
+            at_next = at_after;
+        }
+
+        // the warps' parts, joined: (max, sum) of a head from the four lanes that hold its columns, then over the warps
+        __syncthreads();                                        // (the unit before has been read)
+#pragma unroll
+        for (int n = 0; n < NH; ++n) {
+            l[n] += __shfl_xor_sync(kFull, l[n], 1);
+            l[n] += __shfl_xor_sync(kFull, l[n], 2);
+            if (t == 0) { sm.m[warp][8 * n + g] = m[n]; sm.l[warp][8 * n + g] = l[n]; }
+#pragma unroll
+            for (int hh = 0; hh < kVh; ++hh)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float* p = &sm.o[warp][8 * n + 2 * t + e][64 * hh + 8 * g];
+                    *reinterpret_cast<float4*>(p) = make_float4(o[n][4 * hh][e], o[n][4 * hh][e + 2], o[n][4 * hh + 1][e], o[n][4 * hh + 1][e + 2]);
+                    *reinterpret_cast<float4*>(p + 4) = make_float4(o[n][4 * hh + 2][e], o[n][4 * hh + 2][e + 2], o[n][4 * hh + 3][e], o[n][4 * hh + 3][e + 2]);
+                }
+        }
+        __syncthreads();
+        const bool begins = tile0 == 0, whole = begins && tile1 == tiles;
+        const size_t rec = record(cta, begins);
+        for (int e = threadIdx.x; e < heads * (D / 4); e += kAttThreads) {
+            const int hd = e / (D / 4), c4 = e % (D / 4) * 4;
+            float mm = sm.m[0][hd];
+#pragma unroll
+            for (int w = 1; w < kAttWarps; ++w) mm = fmaxf(mm, sm.m[w][hd]);
+            const float ref = reference_of(mm);
+            float ll = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kAttWarps; ++w) {
+                const float f = exp2_fast(sm.m[w][hd] - ref);
+                const float4 y = *reinterpret_cast<const float4*>(&sm.o[w][hd][c4]);
+                ll = fmaf(sm.l[w][hd], f, ll);
+                v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
+            }
+            if (whole) {
+                const float r = ll == 0.f ? 0.f : 1.f / ll;     // (nothing seen: zeros)
+                *reinterpret_cast<uint2*>(a.out + (static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + g0 + hd) * D + c4) =
+                    make_uint2(pack_bf16(v.x * r, v.y * r), pack_bf16(v.z * r, v.w * r));
+            } else {
+                *reinterpret_cast<float4*>(a.part_o + (rec * (8 * NH) + hd) * D + c4) = v;
+            }
+            if (c4 == 0) {
+                if (!whole) a.part_ml[rec * (8 * NH) + hd] = make_float2(mm, ll);
+                else if (SUMS) a.whole_ml[static_cast<size_t>(bh) * G + g0 + hd] = make_float2(mm, ll);   // (a CTA can have many)
+            }
+        }
+        x = unit0 + tile1;
+        if (grp + 1 == a.groups && tile1 == tiles) {            // on to the next unit that has rows
+            first = x;
+            do ++bh; while (bh < units && tiles_of(rows_of(a, bh)) == 0);
+        }
+    }
+}
+
+// Joins the records of the units that several CTAs worked on, a CTA of this kernel for every query head (blockIdx.x below `joiners`); writes zeros
+// for heads without rows; and adds every row's weights to the sums (the other CTAs: kJoinRows rows of a KV head each).
+template <int D, int NH, bool SUMS>
+__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs a, int ctas, int row_blocks) {
+    __shared__ DealSmem dsm;
+    __shared__ float2 ml[SUMS ? kJoinThreads : 1];              // (reference, factor) of the group's heads
+    const int G = a.Hq / a.Hkv, joiners = a.B * a.Hq;
+    const bool sums = SUMS && static_cast<int>(blockIdx.x) >= joiners;
+    const int idx = sums ? blockIdx.x - joiners : blockIdx.x;
+    const int bh = sums ? idx / row_blocks : idx / G;
+    // (the kernel ahead sets this one up after its own wait: what was there before it is there)
+    const Deal dl = deal(a, bh, 0, 1, dsm);
+    const int n_cta = dealt_to(dl.total, ctas);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int rows = rows_of(a, bh), tiles = tiles_of(rows);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // records of a group of query heads: the CTA that begins the unit, and those after it up to the unit's last tile
+    auto records = [&](int grp, int& c0, int& c1) {
+        const long long f = dl.first + static_cast<long long>(grp) * tiles;
+        c0 = owner_of(f, dl.total, n_cta);
+        c1 = owner_of(f + tiles - 1, dl.total, n_cta);
+    };
+    if (!sums) {
+        const int hq = idx - bh * G, grp = hq / (8 * NH), hd = hq - grp * 8 * NH;
+        const size_t row = (static_cast<size_t>(bh / a.Hkv) * a.Hq + static_cast<size_t>(bh % a.Hkv) * G + hq) * D;
+        if (rows == 0) {
+            for (int e = threadIdx.x; e < D; e += kJoinThreads) a.out[row + e] = __float2bfloat16(0.f);
+            return;
+        }
+        int c0, c1;
+        records(grp, c0, c1);
+        if (c0 == c1) return;                                   // one CTA had the whole unit and wrote it
+        for (int e = threadIdx.x; e < D; e += kJoinThreads) {
+            float mm = -INFINITY, ll = 0.f, v = 0.f;
+#pragma unroll 8
+            for (int c = c0; c <= c1; ++c) {
+                const size_t rec = record(c, c == c0) * (8 * NH) + hd;
+                const float2 s = a.part_ml[rec];
+                const float y = a.part_o[rec * D + e];
+                const float m_new = fmaxf(mm, s.x), ref = reference_of(m_new);
+                const float f0 = exp2_fast(mm - ref), f1 = exp2_fast(s.x - ref);
+                mm = m_new;
+                ll = ll * f0 + s.y * f1;
+                v = v * f0 + y * f1;
+            }
+            a.out[row + e] = __float2bfloat16(ll == 0.f ? 0.f : v / ll);
+        }
+        return;
+    }
+    if constexpr (SUMS) {
+        const int r0 = (idx - bh * row_blocks) * kJoinRows, r1 = min(rows, r0 + kJoinRows);
+        if (r0 >= r1) return;
+        float acc[kJoinRows / kJoinThreads];
+#pragma unroll
+        for (int i = 0; i < kJoinRows / kJoinThreads; ++i) acc[i] = 0.f;
+        for (int q0 = 0; q0 < G; q0 += kJoinThreads) {          // (more query heads than fit at once: in turns)
+            const int nq = min(kJoinThreads, G - q0);
+            __syncthreads();
+            for (int q = warp; q < nq; q += kJoinThreads / 32) {
+                const int grp = (q0 + q) / (8 * NH), hd = (q0 + q) - grp * 8 * NH;
+                int c0, c1;
+                records(grp, c0, c1);
+                if (c0 == c1) {
+                    const float2 s = a.whole_ml[static_cast<size_t>(bh) * G + q0 + q];
+                    if (lane == 0) ml[q] = make_float2(reference_of(s.x), s.y == 0.f ? 0.f : 1.f / s.y);
+                    continue;
+                }
+                float mm = -INFINITY;
+                for (int c = c0 + lane; c <= c1; c += 32) mm = fmaxf(mm, a.part_ml[record(c, c == c0) * (8 * NH) + hd].x);
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
+                const float ref = reference_of(mm);
+                float ll = 0.f;
+                for (int c = c0 + lane; c <= c1; c += 32) {
+                    const float2 s = a.part_ml[record(c, c == c0) * (8 * NH) + hd];
+                    ll += s.y * exp2_fast(s.x - ref);
+                }
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, off);
+                if (lane == 0) ml[q] = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
+            }
+            __syncthreads();
+            for (int q = 0; q < nq; ++q) {
+                const float2 s = ml[q];
+                const float* lg = a.logits + (static_cast<size_t>(bh) * G + q0 + q) * a.logit_stride;
+#pragma unroll
+                for (int i = 0; i < kJoinRows / kJoinThreads; ++i) {
+                    const int r = r0 + i * kJoinThreads + threadIdx.x;
+                    if (r < r1) acc[i] += exp2_fast(lg[r] - s.x) * s.y;
+                }
+            }
+        }
+        float* w = a.weights + static_cast<size_t>(bh) * a.cache.cap;
+#pragma unroll
+        for (int i = 0; i < kJoinRows / kJoinThreads; ++i) {
+            const int r = r0 + i * kJoinThreads + threadIdx.x;
+            if (r < r1) w[r] += acc[i];
+        }
+    }
+}
+
+template <int D, int NH, bool SUMS>
+cudaError_t launch_attend_t(const AttendArgs& a, int n_cta, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(n_cta);
+    cfg.blockDim = dim3(kAttThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, attend_kernel<D, NH, SUMS>, a);
+    if (e != cudaSuccess) return e;
+    const int row_blocks = SUMS ? (a.cache.cap + kJoinRows - 1) / kJoinRows : 0;
+    cfg.gridDim = dim3(static_cast<unsigned>(a.B * a.Hq + a.B * a.Hkv * row_blocks));
+    cfg.blockDim = dim3(kJoinThreads);
+    return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NH, SUMS>, a, n_cta, row_blocks);
+}
+
+}  // namespace
+
+// Scratch: (max, sum) and O of two records a CTA; where sums are asked for, (max, sum) of the units that one CTA had and the logits of all rows.
+AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
+    AttendPlan p;
+    const int G = Hq / Hkv;
+    p.nh = G > 8 ? 2 : 1;
+    p.groups = (G + 8 * p.nh - 1) / (8 * p.nh);
+    const long long tiles = static_cast<long long>(B) * Hkv * p.groups * ((cap + kAttTile - 1) / kAttTile);
+    p.max_ctas = static_cast<int>(tiles < kAttMaxCtas ? tiles : kAttMaxCtas);
+    const size_t heads = static_cast<size_t>(p.max_ctas) * 2 * 8 * p.nh;
+    p.logit_stride = (cap + 3) / 4 * 4;
+    p.off_o = (heads * sizeof(float2) + 255) / 256 * 256;
+    p.off_whole = p.off_o + heads * d * sizeof(float);
+    p.off_logits = p.off_whole + (sums ? (static_cast<size_t>(B) * Hq * sizeof(float2) + 255) / 256 * 256 : 0);
+    p.bytes = p.off_logits + (sums ? static_cast<size_t>(B) * Hq * p.logit_stride * sizeof(float) : 0);
+    return p;
+}
+
+cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d, char* scratch, int num_sms, cudaStream_t stream) {
+    if (args.B <= 0) return cudaSuccess;
+    AttendArgs a = args;
+    a.groups = plan.groups;
+    a.part_ml = reinterpret_cast<float2*>(scratch);
+    a.part_o = reinterpret_cast<float*>(scratch + plan.off_o);
+    a.whole_ml = reinterpret_cast<float2*>(scratch + plan.off_whole);
+    a.logits = reinterpret_cast<float*>(scratch + plan.off_logits);
+    a.logit_stride = plan.logit_stride;
+    const int resident = num_sms * (plan.nh == 1 ? 3 : 2);
+    const int n = resident < plan.max_ctas ? resident : plan.max_ctas;
+    const bool sums = a.weights != nullptr;
+#define CKV_ATTEND(D, NH) (sums ? launch_attend_t<D, NH, true>(a, n, stream) : launch_attend_t<D, NH, false>(a, n, stream))
+    if (d == 128) return plan.nh == 1 ? CKV_ATTEND(128, 1) : CKV_ATTEND(128, 2);
+    return plan.nh == 1 ? CKV_ATTEND(64, 1) : CKV_ATTEND(64, 2);
+#undef CKV_ATTEND
+}
+
+}  // namespace chunkkv

@@ -1,0 +1,77 @@
+// Host-side declarations of the kernels that work on the decode cache (rotate.cu, attend.cu, evict.cu).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace chunkkv {
+
+// A paged cache [num_pages, page_size, Hkv, d] and the block tables of the sequences in it.
+struct PagedCache {
+    const int32_t* tables;      // [B, max_pages]
+    int max_pages, page_size, num_pages;
+    int cap;                    // max_pages * page_size: rows that a sequence can have
+};
+
+// Queries and keys normalised and rotated (rotate.cu): into out_q / out_k (token and head strides in elements), or, with a cache, keys and values
+// into it.
+struct RotateArgs {
+    const __nv_bfloat16* qkv;
+    long long row_elems;
+    int T, Hq, Hkv;
+    const __nv_bfloat16 *gain_q, *gain_k;     // [d]; NULL: no norm
+    float eps;
+    const float *cos_t, *sin_t;               // [n_pos, d / 2]
+    int n_pos;
+    const int32_t* positions;                 // [T]
+    __nv_bfloat16 *out_q, *out_k;
+    long long q_token, q_head, k_token, k_head;
+    __nv_bfloat16 *cache_K, *cache_V;
+    const int32_t* lengths;                   // [T, Hkv], the token's row included
+    PagedCache cache;
+    int steps;                                // set by the launch
+};
+cudaError_t launch_rotate(const RotateArgs& args, int d, int num_sms, cudaStream_t stream);
+
+// Attention of one token a sequence over a paged cache (attend.cu).
+constexpr int kAttMaxCtas = 512;              // CTAs that leave records, at most
+struct AttendArgs {
+    const __nv_bfloat16 *q, *K, *V;
+    const int32_t* lengths;                   // [B, Hkv]
+    PagedCache cache;
+    int B, Hq, Hkv;
+    float scale_log2;                         // log2(e) / sqrt(d)
+    float* weights;                           // [B, Hkv, cap] or NULL
+    __nv_bfloat16* out;
+    int groups;                               // of query heads a KV head; these and what follows are set by the launch
+    float2 *part_ml, *whole_ml;
+    float *part_o, *logits;
+    long long logit_stride;
+};
+struct AttendPlan {
+    int nh, groups, max_ctas;
+    long long logit_stride;
+    size_t off_o, off_whole, off_logits, bytes;
+};
+AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums);
+cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d, char* scratch, int num_sms, cudaStream_t stream);
+
+// Eviction from a paged cache by sums of attention (evict.cu).
+struct EvictArgs {
+    float* weights;                           // [B, Hkv, cap]
+    int32_t* lengths;                         // [B, Hkv]
+    uint4 *K, *V;
+    PagedCache cache;
+    int Hkv, w, c, budget;
+    int32_t* out_idx;                         // [B, Hkv, budget]
+    int list_cap, key_cap;                    // set by the launch
+};
+struct EvictPlan {
+    bool fits;
+    int list_cap, key_cap, smem_bytes;
+};
+EvictPlan evict_plan(int cap, int c, int smem_limit);
+cudaError_t launch_evict(const EvictArgs& args, const EvictPlan& plan, int B, int d, int num_sms, cudaStream_t stream);
+
+}  // namespace chunkkv

@@ -1,0 +1,301 @@
+// Eviction from a paged cache by the sums of the attention that its rows received: every head with more than `budget` rows goes back to
+// at most that many. Of its first C chunks of c rows the k with the largest sums stay (ties to the lower chunk), and the r rows behind them, the window
+// among them, always do. Rows move as little as they can: kept chunks below place k stay where they are, the j-th kept chunk at or above it
+// fills the j-th free place below it, and the r rows follow, in their order. (Attention does not depend on the order of rows; with the chunks in
+// ascending order nearly every row behind the first evicted chunk would move.)
+//
+// A cluster of 1, 2, 4 or 8 CTAs works on a head. Each finds the selection itself - the k-th largest sum exactly, by an adaptive radix select, as
+// select.cuh does; a chain of latencies on a few thousand keys - and takes its part of the moves. Places in the way of one another are kept apart by cluster
+// barriers: nobody writes before all have read the sums; the chunks move before the rows behind them, whose new places may be those chunks'
+// old ones; those rows move in blocks from the lowest on, each read by all before any is written.
+#include "decode.cuh"
+#include "select.cuh"
+
+#include <cooperative_groups.h>
+
+namespace cg = cooperative_groups;
+
+namespace chunkkv {
+
+namespace {
+
+constexpr int kEvThreads = 512;
+constexpr int kEvWarps = kEvThreads / 32;
+constexpr int kEvAhead = 4;               // 16-byte pieces that a thread has in flight
+
+struct EvictSmem {
+    alignas(16) int hist[kSelBins];
+    int4 cnt[kEvWarps];                   // a warp's chunks: above the threshold, equal to it; the same below place k
+    uint2 range[kEvWarps];
+    int warp_tot[kEvWarps];
+    int2 found;
+};
+
+// Order of sums: not-a-number above everything (as torch sorts it), -0 as +0.
+__device__ __forceinline__ uint32_t evict_key(float x) { return x != x ? 0xffffffffu : select_order_key(x); }
+
+template <int VPR>
+__global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
+    constexpr unsigned kFull = 0xffffffffu;
+    extern __shared__ __align__(16) char smem_raw[];
+    EvictSmem& sm = *reinterpret_cast<EvictSmem*>(smem_raw);
+    unsigned short* from = reinterpret_cast<unsigned short*>(smem_raw + sizeof(EvictSmem));    // kept chunks at or above place k
+    unsigned short* to = from + a.list_cap;                                                    // free places below it
+    uint32_t* kbuf = reinterpret_cast<uint32_t*>(to + a.list_cap);                             // keys, where there is room for them
+    begin_dependent();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int n_cta = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
+    const int bh = blockIdx.x / n_cta, b = bh / a.Hkv, h = bh - b * a.Hkv;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int part = rank * kEvThreads + tid, parts = n_cta * kEvThreads;                      // this thread in the cluster
+    const int32_t* table = a.cache.tables + static_cast<size_t>(b) * a.cache.max_pages;
+    float* weights = a.weights + static_cast<size_t>(bh) * a.cache.cap;
+    int32_t* idx = a.out_idx + static_cast<size_t>(bh) * a.budget;
+    const int n = min(max(a.lengths[bh], 0), a.cache.cap), c = a.c;
+    if (n <= a.budget) {                                            // (the whole cluster)
+        for (int i = part; i < a.budget; i += parts) idx[i] = i < n ? i : -1;
+        return;
+    }
+    const int C = (n - a.w) / c, r = n - C * c, k = (a.budget - r) / c;     // k < C, as n is above the budget
+
+    // ---- the k-th largest sum: thresh, of which the first need_eq chunks are kept
+    auto key_of = [&](int ch) -> uint32_t {
+        if (c == 1) return evict_key(weights[ch]);
+        double sum = 0.0;                                           // (in order and 64 bits, rounded once: equal sums are equal)
+        for (int i = 0; i < c; ++i) sum += static_cast<double>(weights[static_cast<size_t>(ch) * c + i]);
+        return evict_key(static_cast<float>(sum));
+    };
+    const bool staged = C <= a.key_cap;
+    auto key_at = [&](int ch) { return staged ? kbuf[ch] : key_of(ch); };
+    uint32_t lo = 0xffffffffu, hi = 0u;
+    if (k > 0) {
+#pragma unroll 4
+        for (int ch = tid; ch < C; ch += kEvThreads) {
+            const uint32_t key = key_of(ch);
+            if (staged) kbuf[ch] = key;
+            lo = min(lo, key);
+            hi = max(hi, key);
+        }
+    }
+    lo = __reduce_min_sync(kFull, lo);
+    hi = __reduce_max_sync(kFull, hi);
+    if (lane == 0) sm.range[warp] = make_uint2(lo, hi);
+    for (int i = tid; i < kSelBins; i += kEvThreads) sm.hist[i] = 0;
+    __syncthreads();
+    uint32_t thresh = 0xffffffffu;
+    int need_eq = 0;                                                // (k = 0: nothing is kept)
+    if (k > 0) {
+        const uint2 mm = sm.range[lane & (kEvWarps - 1)];
+        uint32_t base = __reduce_min_sync(kFull, mm.x), span = __reduce_max_sync(kFull, mm.y) - base;
+        int need = k;                                               // the need-th largest key in [base, base + span]
+        for (int round = 0; span != 0u; ++round) {
+            const int shift = max(0, 21 - __clz(span));             // (span >> shift) < kSelBins
+            if (round > 0) {
+                for (int i = tid; i < kSelBins; i += kEvThreads) sm.hist[i] = 0;
+                __syncthreads();
+            }
+            for (int ch = tid; ch < C; ch += kEvThreads) {
+                const uint32_t dlt = key_at(ch) - base;             // (a key below base wraps to more than span)
+                if (dlt <= span) atomicAdd(&sm.hist[dlt >> shift], 1);
+            }
+            __syncthreads();
+            // thread t has the bins 2047 - 4t .. 2044 - 4t, so a prefix over threads counts from the top
+            const int4 b4 = *reinterpret_cast<const int4*>(sm.hist + kSelBins - 4 - 4 * tid);
+            const int cnt[4] = {b4.w, b4.z, b4.y, b4.x};
+            const int sum = (cnt[0] + cnt[1]) + (cnt[2] + cnt[3]);
+            int inc = sum;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int v = __shfl_up_sync(kFull, inc, off);
+                if (lane >= off) inc += v;
+            }
+            if (lane == 31) sm.warp_tot[warp] = inc;
+            __syncthreads();
+            inc += __reduce_add_sync(kFull, lane < warp ? sm.warp_tot[lane & (kEvWarps - 1)] : 0);
+            if (inc - sum < need && need <= inc) {                  // one thread
+                int above = inc - sum, q = 0;
+#pragma unroll
+                for (int i = 0; i < 3; ++i)                         // (unrolled: cnt stays in registers)
+                    if (q == i && above + cnt[i] < need) { above += cnt[i]; q = i + 1; }
+                sm.found = make_int2(kSelBins - 1 - 4 * tid - q, need - above);
+            }
+            __syncthreads();
+            const int2 f = sm.found;
+            need = f.y;
+            const uint32_t sub = static_cast<uint32_t>(f.x) << shift;
+            base += sub;
+            span = min((1u << shift) - 1u, span - sub);
+        }
+        thresh = base;
+        need_eq = need;
+    }
+
+    // ---- lists of the moves. A warp has a block of consecutive chunks and walks it 32 at a time.
+    const int rows = (C + kEvThreads - 1) / kEvThreads, first = warp * rows * 32;
+    const unsigned below = (1u << lane) - 1u;
+    int4 mine = make_int4(0, 0, 0, 0);
+    if (k > 0) {
+        for (int u = 0; u < rows; ++u) {
+            const int ch = first + 32 * u + lane;
+            const uint32_t key = ch < C ? key_at(ch) : 0u;
+            const unsigned gt = __ballot_sync(kFull, ch < C && key > thresh), eq = __ballot_sync(kFull, ch < C && key == thresh);
+            const unsigned low = __ballot_sync(kFull, ch < k);
+            mine.x += __popc(gt);
+            mine.y += __popc(eq);
+            mine.z += __popc(gt & low);
+            mine.w += __popc(eq & low);
+        }
+    }
+    if (lane == 0) sm.cnt[warp] = mine;
+    __syncthreads();
+    int gt_run = 0, eq_run = 0, low_gt = 0, low_eq = 0;
+#pragma unroll
+    for (int v = 0; v < kEvWarps; ++v) {
+        const int4 x = sm.cnt[v];
+        if (v < warp) { gt_run += x.x; eq_run += x.y; }
+        low_gt += x.z;
+        low_eq += x.w;
+    }
+    const int stay = low_gt + min(low_eq, need_eq), moves = k - stay;       // kept chunks that stay; as many move as places below k are free
+    if (k > 0) {
+        for (int u = 0; u < rows; ++u) {
+            const int ch = first + 32 * u + lane;
+            const uint32_t key = ch < C ? key_at(ch) : 0u;
+            const bool gt = ch < C && key > thresh, eq = ch < C && key == thresh;
+            const unsigned gtm = __ballot_sync(kFull, gt), eqm = __ballot_sync(kFull, eq);
+            const int eq_before = eq_run + __popc(eqm & below);
+            const int before = gt_run + __popc(gtm & below) + min(eq_before, need_eq);     // kept chunks before this one
+            const bool kept = gt || (eq && eq_before < need_eq);
+            if (ch < k) {
+                if (!kept) to[ch - before] = static_cast<unsigned short>(ch);
+                else if (n_cta == 1 || ch % n_cta == rank)
+                    for (int i = 0; i < c; ++i) idx[ch * c + i] = ch * c + i;
+            } else if (kept) {
+                from[before - stay] = static_cast<unsigned short>(ch);
+            }
+            gt_run += __popc(gtm);
+            eq_run += __popc(eqm);
+        }
+    }
+    cluster.sync();          // the lists are there, and every CTA has read the sums and the length
+
+    // ---- the chunks: a piece of 16 bytes of a row's keys or values an item
+    uint4 *K = a.K + static_cast<size_t>(h) * VPR, *V = a.V + static_cast<size_t>(h) * VPR;
+    const size_t row_vecs = static_cast<size_t>(a.Hkv) * VPR;
+    const int chunk_rows = moves * c, dst_r = k * c, src_r = C * c;
+    auto piece = [&](int row, int vec) -> uint4* {                 // NULL: the row's page is outside the cache
+        const int at = paged_row(a.cache, table, row);
+        if (at < 0) return nullptr;
+        return (vec < VPR ? K + vec : V + (vec - VPR)) + static_cast<size_t>(at) * row_vecs;
+    };
+    auto load_piece = [&](int row, int vec) {
+        const uint4* p = piece(row, vec);
+        return p != nullptr ? load_once(p) : make_uint4(0, 0, 0, 0);
+    };
+    auto store_piece = [&](int row, int vec, const uint4& v) {
+        uint4* p = piece(row, vec);
+        if (p != nullptr) *p = v;
+    };
+    for (long long i0 = part; i0 < static_cast<long long>(chunk_rows) * 2 * VPR; i0 += static_cast<long long>(kEvAhead) * parts) {
+        uint4 v[kEvAhead];
+        int dst[kEvAhead], vec[kEvAhead];
+#pragma unroll
+        for (int u = 0; u < kEvAhead; ++u) {
+            const long long i = i0 + static_cast<long long>(u) * parts;
+            dst[u] = -1;
+            if (i < static_cast<long long>(chunk_rows) * 2 * VPR) {
+                const int row = static_cast<int>(i / (2 * VPR)), j = row / c, off = row - j * c;
+                vec[u] = static_cast<int>(i % (2 * VPR));
+                dst[u] = to[j] * c + off;
+                v[u] = load_piece(from[j] * c + off, vec[u]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kEvAhead; ++u)
+            if (dst[u] >= 0) store_piece(dst[u], vec[u], v[u]);
+    }
+    for (int i = part; i < chunk_rows; i += parts) {
+        const int j = i / c, off = i - j * c, src = from[j] * c + off, dst = to[j] * c + off;
+        weights[dst] = weights[src];
+        idx[dst] = src;
+    }
+    cluster.sync();          // their places may be written now
+
+    // ---- the r rows behind the chunks, in blocks of kEvAhead pieces a thread (a piece more a row: its sum)
+    constexpr int kItems = 2 * VPR + 1;
+    for (long long i0 = 0; i0 < static_cast<long long>(r) * kItems; i0 += static_cast<long long>(kEvAhead) * parts) {
+        uint4 v[kEvAhead];
+#pragma unroll
+        for (int u = 0; u < kEvAhead; ++u) {
+            const long long i = i0 + static_cast<long long>(u) * parts + part;
+            if (i < static_cast<long long>(r) * kItems) {
+                const int row = static_cast<int>(i / kItems), vec = static_cast<int>(i % kItems);
+                if (vec < 2 * VPR) v[u] = load_piece(src_r + row, vec);
+                else v[u].x = __float_as_uint(weights[src_r + row]);
+            }
+        }
+        cluster.sync();
+#pragma unroll
+        for (int u = 0; u < kEvAhead; ++u) {
+            const long long i = i0 + static_cast<long long>(u) * parts + part;
+            if (i < static_cast<long long>(r) * kItems) {
+                const int row = static_cast<int>(i / kItems), vec = static_cast<int>(i % kItems);
+                if (vec < 2 * VPR) store_piece(dst_r + row, vec, v[u]);
+                else weights[dst_r + row] = __uint_as_float(v[u].x);
+            }
+        }
+    }
+    cluster.sync();          // (no block of sums is read any more: those behind the last row become zero)
+    const int len = dst_r + r;
+    for (int i = len + part; i < n; i += parts) weights[i] = 0.f;
+    for (int i = part; i < a.budget - dst_r; i += parts) idx[dst_r + i] = i < r ? src_r + i : -1;
+    if (part == 0) a.lengths[bh] = len;
+}
+
+}  // namespace
+
+EvictPlan evict_plan(int cap, int c, int smem_limit) {
+    EvictPlan p;
+    const long long chunks = cap / c;
+    // at most half the chunks move: as many as places below k are free, and k of C chunks are kept
+    const long long list = (chunks / 2 + 8) / 8 * 8;
+    p.fits = chunks <= kSelMaxChunks;
+    p.list_cap = p.fits ? static_cast<int>(list) : 0;
+    const long long fixed = sizeof(EvictSmem) + 4LL * p.list_cap;
+    const long long keys = (smem_limit - fixed) / 4;
+    p.key_cap = static_cast<int>(chunks <= keys ? chunks : 0);
+    p.smem_bytes = static_cast<int>(fixed + 4LL * p.key_cap);
+    return p;
+}
+
+cudaError_t launch_evict(const EvictArgs& args, const EvictPlan& plan, int B, int d, int num_sms, cudaStream_t stream) {
+    if (B <= 0) return cudaSuccess;
+    EvictArgs a = args;
+    a.list_cap = plan.list_cap;
+    a.key_cap = plan.key_cap;
+    auto kernel = d == 128 ? evict_kernel<16> : evict_kernel<8>;
+    if (plan.smem_bytes > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, plan.smem_bytes);
+        if (e != cudaSuccess) return e;
+    }
+    const long long units = static_cast<long long>(B) * a.Hkv;
+    int ctas = 1;
+    while (ctas < 8 && units * ctas * 2 <= 2LL * num_sms) ctas *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(units * ctas));
+    cfg.blockDim = dim3(kEvThreads);
+    cfg.dynamicSmemBytes = plan.smem_bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
+}  // namespace chunkkv

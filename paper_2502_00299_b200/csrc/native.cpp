@@ -393,10 +393,156 @@ PyObject* model(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// What the calls on the decode cache share: a paged cache [pages, page_size, Hkv, d], tables [B, max_pages], lengths [B, Hkv].
+struct Cache {
+    int pages, page_size, Hkv, d, B, max_pages;
+    const int32_t* tables;
+    int32_t* lengths;
+    void *K, *V;
+    Cache(PyObject* tables_, PyObject* lengths_, PyObject* K_, PyObject* V_) {
+        const at::Tensor &k = here(checked(K_, at::kBFloat16)), &v = here(checked(V_, at::kBFloat16));
+        const at::Tensor &bt = here(checked(tables_, at::kInt)), &ln = here(checked(lengths_, at::kInt));
+        if (k.dim() != 4 || v.sizes() != k.sizes() || bt.dim() != 2 || ln.dim() != 2 || ln.size(0) != bt.size(0) || ln.size(1) != k.size(2)) throw Decline{};
+        pages = narrow(k.size(0)); page_size = narrow(k.size(1)); Hkv = narrow(k.size(2)); d = narrow(k.size(3));
+        B = narrow(bt.size(0)); max_pages = narrow(bt.size(1));
+        tables = static_cast<const int32_t*>(bt.data_ptr());
+        lengths = static_cast<int32_t*>(ln.data_ptr());
+        K = k.data_ptr();
+        V = v.data_ptr();
+    }
+    // On the current device, where the call is queued.
+    static const at::Tensor& here(const at::Tensor& t) {
+        if (t.device().index() != c10::cuda::current_device()) throw Decline{};
+        return t;
+    }
+    float* sums(PyObject* o) const {
+        const at::Tensor& t = here(checked(o, at::kFloat));
+        if (t.dim() != 3 || t.size(0) != B || t.size(1) != Hkv || t.size(2) != static_cast<long long>(max_pages) * page_size) throw Decline{};
+        return static_cast<float*>(t.data_ptr());
+    }
+};
+// The angles, positions, gains and eps of a fused activation of `heads` heads of d.
+struct Angles {
+    int T, n_pos;
+    long long row;
+    float eps;
+    const void *x, *gq, *gk;
+    const float *co, *si;
+    const int32_t* pos;
+    Angles(PyObject* qkv, PyObject* cos, PyObject* sin, PyObject* positions, PyObject* q_gain, PyObject* k_gain, PyObject* eps_, long long heads, int d) {
+        const at::Tensor &t = Cache::here(checked(qkv, at::kBFloat16)), &c = Cache::here(checked(cos, at::kFloat)), &s = Cache::here(checked(sin, at::kFloat));
+        if (t.dim() != 2 || t.size(1) < heads * d || c.dim() != 2 || c.size(1) != d / 2 || s.sizes() != c.sizes() || !PyFloat_CheckExact(eps_)) throw Decline{};
+        T = narrow(t.size(0)); row = t.size(1); n_pos = narrow(c.size(0));
+        eps = static_cast<float>(PyFloat_AS_DOUBLE(eps_));
+        x = t.data_ptr();
+        co = static_cast<const float*>(c.data_ptr());
+        si = static_cast<const float*>(s.data_ptr());
+        pos = static_cast<const int32_t*>(Cache::here(sized(positions, at::kInt, T)).data_ptr());
+        gq = q_gain == Py_None ? nullptr : Cache::here(sized(q_gain, at::kBFloat16, d)).data_ptr();
+        gk = k_gain == Py_None ? nullptr : Cache::here(sized(k_gain, at::kBFloat16, d)).data_ptr();
+    }
+};
+// These calls take the current stream here, so that what they allocate belongs to it.
+void* current_stream(PyObject* o) {
+    if (o != Py_None) throw Decline{};
+    return stream_of(o);
+}
+
+// rotate_qk(qkv, Hq, Hkv, d, cos, sin, positions, q_gain, k_gain, eps, out_q, out_k, stream) -> (q, k); outputs given go the general way
+PyObject* rotate_qk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 13, [&]() -> PyObject* {
+        const int Hq = integer(a[1]), Hkv = integer(a[2]), d = integer(a[3]);
+        if (Hq < 1 || Hkv < 1 || d < 1 || a[10] != Py_None || a[11] != Py_None) throw Decline{};
+        const Angles x(a[0], a[4], a[5], a[6], a[7], a[8], a[9], static_cast<long long>(Hq) + Hkv, d);
+        void* s = current_stream(a[12]);
+        const at::Tensor& like = tensor(a[0]);
+        Ref oq, ok;
+        void* pq = oq.set(Py_None, at::kBFloat16, 0, [&] { return rows(like, x.T, Hq, d); });
+        void* pk = ok.set(Py_None, at::kBFloat16, 0, [&] { return rows(like, x.T, Hkv, d); });
+        const int st = unlocked([&] {
+            return chunkkv_rotate_qk(x.x, x.row, x.T, Hq, Hkv, d, x.gq, x.gk, x.eps, x.co, x.si, x.n_pos, x.pos, static_cast<long long>(Hq) * d, d,
+                                     static_cast<long long>(Hkv) * d, d, pq, pk, s);
+        });
+        if (st != 0) return PyLong_FromLong(st);
+        return PyTuple_Pack(2, oq.p, ok.p);
+    });
+}
+
+// append_paged(qkv, Hq, cos, sin, positions, block_tables, lengths, cache_K, cache_V, q_gain, k_gain, eps, out_q, stream) -> q
+PyObject* append_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 14, [&]() -> PyObject* {
+        const int Hq = integer(a[1]);
+        if (Hq < 1) throw Decline{};
+        const Cache c(a[5], a[6], a[7], a[8]);
+        const Angles x(a[0], a[2], a[3], a[4], a[9], a[10], a[11], static_cast<long long>(Hq) + 2LL * c.Hkv, c.d);
+        if (x.T != c.B) throw Decline{};
+        void* s = current_stream(a[13]);
+        if (a[12] != Py_None) Cache::here(checked(a[12], at::kBFloat16));
+        Ref oq;
+        void* pq = oq.set(a[12], at::kBFloat16, static_cast<long long>(c.B) * Hq * c.d, [&] { return rows(tensor(a[0]), c.B, Hq, c.d); });
+        const int st = unlocked([&] {
+            return chunkkv_append_paged(x.x, x.row, c.B, Hq, c.Hkv, c.d, x.gq, x.gk, x.eps, x.co, x.si, x.n_pos, x.pos, c.tables, c.max_pages, c.lengths,
+                                        c.page_size, c.pages, c.K, c.V, pq, s);
+        });
+        if (st != 0) return PyLong_FromLong(st);
+        Py_INCREF(oq.p);
+        return oq.p;
+    });
+}
+
+// attend_paged(q, block_tables, lengths, cache_K, cache_V, weights, out, stream) -> out
+PyObject* attend_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&]() -> PyObject* {
+        const Cache c(a[1], a[2], a[3], a[4]);
+        const at::Tensor& q = Cache::here(checked(a[0], at::kBFloat16));
+        if (q.dim() != 3 || q.size(0) != c.B || q.size(2) != c.d) throw Decline{};
+        const int Hq = narrow(q.size(1));
+        float* weights = a[5] == Py_None ? nullptr : c.sums(a[5]);
+        void* s = current_stream(a[7]);
+        if (a[6] != Py_None) Cache::here(checked(a[6], at::kBFloat16));
+        Ref o;
+        void* po = o.set(a[6], at::kBFloat16, static_cast<long long>(c.B) * Hq * c.d, [&] { return rows(q, c.B, Hq, c.d); });
+        const size_t need = chunkkv_attend_scratch_bytes(c.B, Hq, c.Hkv, c.d, c.max_pages, c.page_size, weights != nullptr);
+        at::Tensor scratch;                        // (freed behind the call on its stream: the allocator's blocks belong to streams)
+        if (need > 0) scratch = at::empty({static_cast<long long>(need)}, at::TensorOptions().dtype(at::kByte).device(q.device()));
+        const void* pq = q.data_ptr();
+        void* ps = need > 0 ? scratch.data_ptr() : nullptr;
+        const int st = unlocked([&] {
+            return chunkkv_attend_paged(pq, c.tables, c.max_pages, c.lengths, c.page_size, c.pages, c.K, c.V, c.B, Hq, c.Hkv, c.d, weights, po, ps, need, s);
+        });
+        if (st != 0) return PyLong_FromLong(st);
+        Py_INCREF(o.p);
+        return o.p;
+    });
+}
+
+// evict_paged(weights, block_tables, lengths, cache_K, cache_V, w, c, budget, out_idx, stream) -> idx
+PyObject* evict_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&]() -> PyObject* {
+        const Cache c(a[1], a[2], a[3], a[4]);
+        float* weights = c.sums(a[0]);
+        const int w = integer(a[5]), ch = integer(a[6]), budget = integer(a[7]);
+        if (budget < 1) throw Decline{};
+        void* s = current_stream(a[9]);
+        if (a[8] != Py_None) Cache::here(checked(a[8], at::kInt));
+        Ref o;
+        int32_t* po = static_cast<int32_t*>(o.set(a[8], at::kInt, static_cast<long long>(c.B) * c.Hkv * budget, [&] {
+            return at::empty({c.B, c.Hkv, budget}, at::TensorOptions().dtype(at::kInt).device(tensor(a[0]).device()));
+        }));
+        const int st = unlocked([&] {
+            return chunkkv_evict_paged(weights, c.tables, c.max_pages, c.lengths, c.page_size, c.pages, c.K, c.V, c.B, c.Hkv, c.d, w, ch, budget, po, s);
+        });
+        if (st != 0) return PyLong_FromLong(st);
+        Py_INCREF(o.p);
+        return o.p;
+    });
+}
+
 PyMethodDef kMethods[] = {
 #define CKV_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
     CKV_METHOD(scratch), CKV_METHOD(layer), CKV_METHOD(layer_strided), CKV_METHOD(layer_alg1), CKV_METHOD(layer_paged),
-    CKV_METHOD(window_queries), CKV_METHOD(score), CKV_METHOD(model), {nullptr, nullptr, 0, nullptr}};
+    CKV_METHOD(window_queries), CKV_METHOD(score), CKV_METHOD(model),
+    CKV_METHOD(rotate_qk), CKV_METHOD(append_paged), CKV_METHOD(attend_paged), CKV_METHOD(evict_paged), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "Per-call part of the binding (see binding.py).", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
