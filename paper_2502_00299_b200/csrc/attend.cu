@@ -1,16 +1,19 @@
 // Attention of one new token over a paged cache: out = softmax(q K^T / sqrt(d)) V for every query head, over the rows that its KV head
 // has (a length of its own), and, on request, the attention that every row received added to a running sum.
 //
-// What bounds it is the cache: every row is read once, 4 d bytes for 4 G d operations (G query heads of a KV head), so the product must not be what
-// the memory waits for. The products run on the tensor cores with the heads of a group as eight columns: a warp takes 16 rows at
-// a time, S = Q K^T as m16n8k16 (heads x rows; half of the 16 heads are zero up to G = 8) and O^T += V^T P^T (dims x heads). Keys and values go
-// from global memory to registers in 16-byte loads with no stop in shared memory: which 8 of a row's dims a lane holds is free as long
-// as queries (for the product over dims) or outputs (for the dims of O^T) are dealt the same way, and V^T comes out of two rows' registers by
-// byte permutes. P is split into two bf16 terms, so that its rounding (2^-16) is not seen beside that of the output.
+// What bounds it is the cache: every row is read once, 4 d bytes for 4 G d operations (G query heads of a KV head), so nothing else must be what
+// the memory waits for. A warp works on one KV head, 16 rows a step, with a ring of steps of its own in shared memory that asynchronous
+// copies fill (24 KB a warp, two thirds of it in flight: 128 KB an SM) - no warp waits for another. The eight warps of a CTA take neighbouring
+// heads of the same rows, which lie side by side in the cache, where there are as many; else several warps a head take rows in turn. The products run
+// on the tensor cores with the heads of a group as eight columns: S = Q K^T as m16n8k16 (heads x rows; half of the 16 heads are zero up
+// to G = 8) and O^T += V^T P^T (dims x heads), V^T out of two rows' registers by byte permutes. Which 8 of a row's dims a lane holds is
+// free as long as queries (for the product over dims) or outputs (for the dims of O^T) are dealt the same way, so every load from
+// shared memory is 16 bytes wide and, pieces of a row being exchanged, without conflicts. P is split into two bf16 terms, so that its rounding (2^-16)
+// is not seen beside that of the output.
 //
-// The rows of all (sequence, KV head) units are cut into tiles of 64 and dealt evenly to the CTAs in one line, so that lengths need not be
-// alike; a CTA walks the units in its share and leaves (max, sum, O) records for those that it shares with others, which a second launch joins in
-// the order of the CTAs (same result every time). The records live in scratch of the call's own: calls at the same time, and
+// The rows of all units (a sequence's heads that a CTA takes together) are cut into tiles and dealt evenly to the CTAs in one line, so that lengths
+// need not be alike; a CTA walks the units in its share and leaves (max, sum, O) records for those that it shares with others, which a second launch
+// joins in the order of the CTAs (same result every time). The records live in scratch of the call's own: calls at the same time, and
 // captured ones, have nothing in common.
 #include "decode.cuh"
 
@@ -18,13 +21,12 @@ namespace chunkkv {
 
 namespace {
 
-constexpr int kAttWarps = 4;
+constexpr int kAttWarps = 8;
 constexpr int kAttThreads = 32 * kAttWarps;
 constexpr int kAttStep = 16;                          // rows of a warp's step
-constexpr int kAttTile = kAttWarps * kAttStep;        // rows that are dealt together
+constexpr int kRingBytes = 24 * 1024;                 // of a warp
 constexpr int kJoinRows = 512;                        // rows of the sums that a CTA of the join takes
 constexpr int kJoinThreads = 128;
-static_assert(kJoinThreads == kAttThreads, "both kernels deal with as many threads");
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -36,32 +38,58 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// 16 bytes of global memory into shared memory, or zeros where `there` is false.
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_begin_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 load_shared(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
 // A maximum as the reference of exponents: 0 where nothing was seen.
 __device__ __forceinline__ float reference_of(float m) { return m == -INFINITY ? 0.f : m; }
 
+// Rows of a head and of a unit, the `block` heads from h0 on of a sequence.
 __device__ __forceinline__ int rows_of(const AttendArgs& a, int bh) { return min(max(__ldg(a.lengths + bh), 0), a.cache.cap); }
-__device__ __forceinline__ int tiles_of(int rows) { return (rows + kAttTile - 1) / kAttTile; }
+struct Unit {
+    int b, h0, heads;     // sequence, its KV heads [h0, h0 + heads)
+};
+__device__ __forceinline__ Unit unit_of(const AttendArgs& a, int u) {
+    const int b = u / a.blocks, h0 = (u - b * a.blocks) * a.block;
+    return {b, h0, min(a.block, a.Hkv - h0)};
+}
+__device__ __forceinline__ int tiles_of(const AttendArgs& a, int u) {
+    const Unit un = unit_of(a, u);
+    int n = 0;
+    for (int h = 0; h < un.heads; ++h) n = max(n, rows_of(a, un.b * a.Hkv + un.h0 + h));
+    return (n + a.tile - 1) / a.tile;
+}
 
-// The line of tiles: the units (sequence, KV head) in order, each `groups` times its tiles (one for each group of query heads).
+// The line of tiles: the units in order, each `groups` times its tiles (one for each group of query heads).
 struct Deal {
     long long total;      // tiles in all
-    int bh;               // the unit asked for, or the one that holds the tile asked for
+    int unit;             // the unit asked for, or the one that holds the tile asked for
     long long first;      // its first tile
 };
 struct DealSmem {
     long long warp[kAttWarps];
     long long first;
-    int bh;
+    int unit;
 };
 // CTAs that the line is dealt to: no more than it has tiles, so that each has one at least.
 __device__ __forceinline__ int dealt_to(long long total, int n_cta) { return static_cast<int>(min(total, static_cast<long long>(n_cta))); }
 
-// All threads. want >= 0: that unit; else the one that holds the first tile of CTA `cta` of a launch of n_cta.
+// All THREADS threads. want >= 0: that unit; else the one that holds the first tile of CTA `cta` of a launch of n_cta.
+template <int THREADS>
 __device__ __forceinline__ Deal deal(const AttendArgs& a, int want, int cta, int n_cta, DealSmem& sm) {
-    const int units = a.B * a.Hkv, per = (units + kAttThreads - 1) / kAttThreads;
+    const int units = a.B * a.blocks, per = (units + THREADS - 1) / THREADS;
     const int u0 = min(static_cast<int>(threadIdx.x) * per, units), u1 = min(u0 + per, units);
     long long mine = 0;
-    for (int u = u0; u < u1; ++u) mine += tiles_of(rows_of(a, u));
+    for (int u = u0; u < u1; ++u) mine += tiles_of(a, u);
     mine *= a.groups;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     long long inc = mine;
@@ -71,11 +99,11 @@ __device__ __forceinline__ Deal deal(const AttendArgs& a, int want, int cta, int
         if (lane >= off) inc += v;
     }
     if (lane == 31) sm.warp[warp] = inc;
-    if (threadIdx.x == 0) sm.bh = units;
+    if (threadIdx.x == 0) sm.unit = units;
     __syncthreads();
     long long total = 0;
 #pragma unroll
-    for (int w = 0; w < kAttWarps; ++w) {
+    for (int w = 0; w < THREADS / 32; ++w) {
         if (w < warp) inc += sm.warp[w];
         total += sm.warp[w];
     }
@@ -84,94 +112,110 @@ __device__ __forceinline__ Deal deal(const AttendArgs& a, int want, int cta, int
     long long at = inc - mine;
     if (want < 0 ? (at <= tile && tile < inc) : (u0 <= want && want < u1)) {       // one thread, if any
         for (int u = u0; u < u1; ++u) {
-            const long long t = static_cast<long long>(tiles_of(rows_of(a, u))) * a.groups;
-            if (want < 0 ? tile < at + t : u == want) { sm.bh = u; sm.first = at; break; }
+            const long long t = static_cast<long long>(tiles_of(a, u)) * a.groups;
+            if (want < 0 ? tile < at + t : u == want) { sm.unit = u; sm.first = at; break; }
             at += t;
         }
     }
     __syncthreads();
-    return {total, sm.bh, sm.first};
+    return {total, sm.unit, sm.first};
 }
 // The CTA of n that tile x falls to, where CTA i has the tiles [i total / n, (i + 1) total / n).
 __device__ __forceinline__ int owner_of(long long x, long long total, int n) { return static_cast<int>(((x + 1) * n - 1) / total); }
 
-// Where records of CTA `cta` are: one for a unit that an earlier CTA has begun, one for a unit that it begins itself.
-__device__ __forceinline__ size_t record(int cta, bool begins) { return static_cast<size_t>(cta) * 2 + (begins ? 1 : 0); }
+// Where records of CTA `cta` are: one for a unit that an earlier CTA has begun, one for a unit that it begins itself; each has a.block KV heads with
+// a.group query heads.
+__device__ __forceinline__ size_t record(const AttendArgs& a, int cta, bool begins, int h, int q) {
+    return (static_cast<size_t>(cta * 2 + (begins ? 1 : 0)) * a.block + h) * a.group + q;
+}
 
 template <int D, int NH>
 struct AttSmem {
     static constexpr int kPad = D + 4;
-    float o[kAttWarps][8 * NH][kPad];
+    union {
+        alignas(128) unsigned char ring[kAttWarps][kRingBytes];
+        float o[kAttWarps][8 * NH][kPad];       // where several warps work on a head (the ring is idle then)
+    };
     float m[kAttWarps][8 * NH], l[kAttWarps][8 * NH];
     DealSmem deal;
 };
 
 // D: head dim; NH: query heads of a group in eights.
 template <int D, int NH, bool SUMS>
-__global__ void __launch_bounds__(kAttThreads, NH == 1 ? 3 : 2) attend_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs a) {
     constexpr unsigned kFull = 0xffffffffu;
-    constexpr int kCh = D / 32;                   // 16-byte pieces of a key row that a lane holds
+    constexpr int kCh = D / 32;                   // 16-byte pieces of a key row that a lane takes
     constexpr int kVh = D / 64;                   // and of a value row
-    __shared__ __align__(16) AttSmem<D, NH> sm;
+    constexpr int kPieces = D / 8;                // of a row
+    constexpr int kRowsOnce = 32 / kPieces;       // rows that one copy instruction of a warp takes
+    constexpr int kHalf = kAttStep * D * 2;       // bytes of a step's keys
+    constexpr int kStages = kRingBytes / (2 * kHalf);
+    extern __shared__ __align__(128) char smem_raw[];
+    AttSmem<D, NH>& sm = *reinterpret_cast<AttSmem<D, NH>*>(smem_raw);
     begin_dependent();
-    const int cta = blockIdx.x, units = a.B * a.Hkv;
+    const int cta = blockIdx.x, units = a.B * a.blocks;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const Deal dl = deal(a, -1, cta, gridDim.x, sm.deal);
+    const Deal dl = deal<kAttThreads>(a, -1, cta, gridDim.x, sm.deal);
     const int n_cta = dealt_to(dl.total, gridDim.x);
     if (cta >= n_cta) return;
     long long x = dl.total * cta / n_cta;
     const long long x1 = dl.total * (cta + 1) / n_cta;
-    int bh = dl.bh;
+    int unit = dl.unit;
     long long first = dl.first;
-    while (x < x1 && bh < units) {
-        const int rows = rows_of(a, bh), tiles = tiles_of(rows);
+    // this warp's head in a unit and its rows among those of the head's warps
+    const int head = warp % a.block, turn = warp / a.block, turns = a.tile / kAttStep;
+    const int G = a.Hq / a.Hkv;
+    const size_t row_elems = static_cast<size_t>(a.Hkv) * D;
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(&sm.ring[warp][0]));
+    // what a lane copies of a step's rows: piece `piece` of the rows r0 + kRowsOnce i. Pieces are exchanged within 128 bytes so that the eight
+    // lanes of a load's quarter find theirs in different banks: keys are read four neighbouring pieces of two rows at a time, values two of four.
+    const int piece = lane % kPieces, r0 = lane / kPieces;
+    while (x < x1 && unit < units) {
+        const Unit un = unit_of(a, unit);
+        const int tiles = tiles_of(a, unit);
         const int grp = static_cast<int>((x - first) / tiles);
         const long long unit0 = first + static_cast<long long>(grp) * tiles;              // the unit's first tile
         const int tile0 = static_cast<int>(x - unit0), tile1 = static_cast<int>(min(x1 - unit0, static_cast<long long>(tiles)));
-        const int b = bh / a.Hkv, h = bh - b * a.Hkv;
-        const int G = a.Hq / a.Hkv, g0 = grp * 8 * NH, heads = min(8 * NH, G - g0);       // query heads of this group
-        const int r1 = min(rows, tile1 * kAttTile);
-        const int32_t* table = a.cache.tables + static_cast<size_t>(b) * a.cache.max_pages;
-        const __nv_bfloat16* qh = a.q + (static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + g0) * D;
-        const size_t row_elems = static_cast<size_t>(a.Hkv) * D;
-        const __nv_bfloat16 *Kh = a.K + static_cast<size_t>(h) * D + 8 * t, *Vh = a.V + static_cast<size_t>(h) * D + 8 * g;
+        const int h = un.h0 + head, bh = un.b * a.Hkv + h;
+        const bool on = head < un.heads && turn < turns;                                  // (else this warp has no head here)
+        const int rows = on ? rows_of(a, bh) : 0;
+        const int g0 = grp * 8 * NH, heads = min(8 * NH, G - g0);                         // query heads of this group
+        const int r1 = min(rows, tile1 * a.tile);
+        const int32_t* table = a.cache.tables + static_cast<size_t>(un.b) * a.cache.max_pages;
+        const size_t q_row = static_cast<size_t>(un.b) * a.Hq + static_cast<size_t>(h) * G + g0;
+        const __nv_bfloat16 *Kh = a.K + static_cast<size_t>(h) * D + 8 * piece, *Vh = a.V + static_cast<size_t>(h) * D + 8 * piece;
 
         // lane l (and l + 16) looks up row l of a step
         auto lookup = [&](int base) {
             const int r = base + (lane & 15);
             return r < r1 ? paged_row(a.cache, table, r) : -1;
         };
-        uint4 kr[2][kCh], vr[4][kVh];
-        auto load_keys = [&](int at) {
+        auto copy_step = [&](int at, uint32_t to) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int row = __shfl_sync(kFull, at, 8 * j + g);
-                const __nv_bfloat16* p = Kh + static_cast<size_t>(max(row, 0)) * row_elems;
-#pragma unroll
-                for (int i = 0; i < kCh; ++i) kr[j][i] = row >= 0 ? load_once(p + 32 * i) : make_uint4(0, 0, 0, 0);
-            }
-        };
-        auto load_values = [&](int at) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int row = __shfl_sync(kFull, at, (j >> 1) * 8 + 2 * t + (j & 1));
-                const __nv_bfloat16* p = Vh + static_cast<size_t>(max(row, 0)) * row_elems;
-#pragma unroll
-                for (int i = 0; i < kVh; ++i) vr[j][i] = row >= 0 ? load_once(p + 64 * i) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < kAttStep / kRowsOnce; ++i) {
+                const int r = i * kRowsOnce + r0, row = __shfl_sync(kFull, at, r);
+                const size_t off = static_cast<size_t>(max(row, 0)) * row_elems;
+                copy_async(to + r * (2 * D) + ((piece ^ (4 * (r & 1))) << 4), Kh + off, row >= 0);
+                copy_async(to + kHalf + r * (2 * D) + ((piece ^ (r & 6)) << 4), Vh + off, row >= 0);
             }
         };
 
-        int base = tile0 * kAttTile + warp * kAttStep;
-        int at = lookup(base);
-        load_keys(at);
-        load_values(at);
-        int at_next = lookup(base + kAttTile);
+        // at[i]: rows of the step i behind the one that is worked on. A group of copies a step, empty ones behind the last row.
+        int base = tile0 * a.tile + turn * kAttStep;
+        int at[kStages];
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) at[i] = lookup(base + i * a.tile);
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) {
+            if (base + i * a.tile < r1) copy_step(at[i], ring + i * 2 * kHalf);
+            copies_begin_group();
+        }
         uint4 qr[NH][kCh];
 #pragma unroll
         for (int n = 0; n < NH; ++n)
 #pragma unroll
             for (int i = 0; i < kCh; ++i)
-                qr[n][i] = 8 * n + g < heads ? __ldg(reinterpret_cast<const uint4*>(qh + static_cast<size_t>(8 * n + g) * D + 32 * i + 8 * t)) : make_uint4(0, 0, 0, 0);
+                qr[n][i] = on && 8 * n + g < heads ? __ldg(reinterpret_cast<const uint4*>(a.q + (q_row + 8 * n + g) * D + 32 * i + 8 * t)) : make_uint4(0, 0, 0, 0);
 
         float m[NH], l[NH], o[NH][D / 16][4];
 #pragma unroll
@@ -182,24 +226,33 @@ __global__ void __launch_bounds__(kAttThreads, NH == 1 ? 3 : 2) attend_kernel(co
             for (int i = 0; i < D / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
         }
 
-        for (; base < r1; base += kAttTile) {
+        int stage = 0;
+        for (; base < r1; base += a.tile) {
+            copies_wait<kStages - 2>();
+            __syncwarp();                                       // (this step has landed, and the one before has been read)
+            const int ahead = base + (kStages - 1) * a.tile;
+            if (ahead < r1) copy_step(at[kStages - 1], ring + (stage == 0 ? kStages - 1 : stage - 1) * 2 * kHalf);
+            copies_begin_group();
+            const uint32_t keys = ring + stage * 2 * kHalf, values = keys + kHalf;
+            stage = stage == kStages - 1 ? 0 : stage + 1;
             // S: rows of the product are the query heads g and g + 8, columns the cache rows 2t and 2t + 1 of eight
             float s[2][4];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+            for (int j = 0; j < 2; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
 #pragma unroll
-                for (int i = 0; i < kCh; ++i) {
-                    const uint4 k = kr[j][i];
+            for (int i = 0; i < kCh; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint4 k = load_shared(keys + (8 * j + g) * (2 * D) + (((4 * i + t) ^ (4 * (g & 1))) << 4));
                     mma_bf16(s[j], qr[0][i].x, NH == 2 ? qr[NH - 1][i].x : 0u, qr[0][i].y, NH == 2 ? qr[NH - 1][i].y : 0u, k.x, k.y);
                     mma_bf16(s[j], qr[0][i].z, NH == 2 ? qr[NH - 1][i].z : 0u, qr[0][i].w, NH == 2 ? qr[NH - 1][i].w : 0u, k.z, k.w);
                 }
-            }
             unsigned seen = 0;                                  // bit 2j + e: row base + 8j + 2t + e
 #pragma unroll
-            for (int j = 0; j < 4; ++j) seen |= __shfl_sync(kFull, at, (j >> 1) * 8 + 2 * t + (j & 1)) >= 0 ? 1u << j : 0u;
-            load_keys(at_next);                                 // (the keys' registers are free)
-            const int at_after = lookup(base + 2 * kAttTile);
+            for (int j = 0; j < 4; ++j) seen |= __shfl_sync(kFull, at[0], (j >> 1) * 8 + 2 * t + (j & 1)) >= 0 ? 1u << j : 0u;
+#pragma unroll
+            for (int i = 0; i < kStages - 1; ++i) at[i] = at[i + 1];
+            at[kStages - 1] = lookup(ahead + a.tile);
 
             uint32_t hi[NH][2], lo[NH][2];
             float factor[NH];
@@ -216,7 +269,7 @@ __global__ void __launch_bounds__(kAttThreads, NH == 1 ? 3 : 2) attend_kernel(co
                     }
                 if constexpr (SUMS) {
                     if (8 * n + g < heads) {
-                        float* lg = a.logits + (static_cast<size_t>(bh) * G + g0 + 8 * n + g) * a.logit_stride + base + 2 * t;
+                        float* lg = a.logits + (q_row + 8 * n + g) * a.logit_stride + base + 2 * t;
 #pragma unroll
                         for (int j = 0; j < 2; ++j)             // (the stride is even and covers every row, so a pair fits)
                             if (base + 8 * j + 2 * t < r1) *reinterpret_cast<float2*>(lg + 8 * j) = make_float2(v[j][0], v[j][1]);
@@ -250,12 +303,16 @@ __global__ void __launch_bounds__(kAttThreads, NH == 1 ? 3 : 2) attend_kernel(co
             // O^T += V^T P^T: row g of the product's tile (hh, q) is dim 64 hh + 8 g + 2 q, row g + 8 the next dim
 #pragma unroll
             for (int hh = 0; hh < kVh; ++hh) {
-                const uint32_t w0[4] = {vr[0][hh].x, vr[0][hh].y, vr[0][hh].z, vr[0][hh].w}, w1[4] = {vr[1][hh].x, vr[1][hh].y, vr[1][hh].z, vr[1][hh].w};
-                const uint32_t w2[4] = {vr[2][hh].x, vr[2][hh].y, vr[2][hh].z, vr[2][hh].w}, w3[4] = {vr[3][hh].x, vr[3][hh].y, vr[3][hh].z, vr[3][hh].w};
+                uint32_t w[4][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {                   // rows 2t, 2t + 1, 8 + 2t, 9 + 2t
+                    const uint4 v = load_shared(values + ((j >> 1) * 8 + 2 * t + (j & 1)) * (2 * D) + (((8 * hh + g) ^ (2 * t)) << 4));
+                    w[j][0] = v.x; w[j][1] = v.y; w[j][2] = v.z; w[j][3] = v.w;
+                }
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const uint32_t a0 = __byte_perm(w0[q], w1[q], 0x5410), a1 = __byte_perm(w0[q], w1[q], 0x7632);
-                    const uint32_t a2 = __byte_perm(w2[q], w3[q], 0x5410), a3 = __byte_perm(w2[q], w3[q], 0x7632);
+                    const uint32_t a0 = __byte_perm(w[0][q], w[1][q], 0x5410), a1 = __byte_perm(w[0][q], w[1][q], 0x7632);
+                    const uint32_t a2 = __byte_perm(w[2][q], w[3][q], 0x5410), a3 = __byte_perm(w[2][q], w[3][q], 0x7632);
 #pragma unroll
                     for (int n = 0; n < NH; ++n) {
                         mma_bf16(o[n][4 * hh + q], a0, a1, a2, a3, hi[n][0], hi[n][1]);
@@ -263,13 +320,10 @@ __global__ void __launch_bounds__(kAttThreads, NH == 1 ? 3 : 2) attend_kernel(co
                     }
                 }
             }
-            load_values(at_next);
-            at = at_next;
-            at_next = at_after;
         }
 
-        // the warps' parts, joined: (max, sum) of a head from the four lanes that hold its columns, then over the warps
-        __syncthreads();                                        // (the unit before has been read)
+        // the warps' parts of a head, joined: (max, sum) of a query head from the four lanes that hold its columns, then over the warps
+        __syncthreads();                                        // (every ring is idle)
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
             l[n] += __shfl_xor_sync(kFull, l[n], 1);
@@ -286,38 +340,38 @@ __global__ void __launch_bounds__(kAttThreads, NH == 1 ? 3 : 2) attend_kernel(co
         }
         __syncthreads();
         const bool begins = tile0 == 0, whole = begins && tile1 == tiles;
-        const size_t rec = record(cta, begins);
-        for (int e = threadIdx.x; e < heads * (D / 4); e += kAttThreads) {
-            const int hd = e / (D / 4), c4 = e % (D / 4) * 4;
-            float mm = sm.m[0][hd];
-#pragma unroll
-            for (int w = 1; w < kAttWarps; ++w) mm = fmaxf(mm, sm.m[w][hd]);
+        for (int e = threadIdx.x; e < un.heads * heads * (D / 4); e += kAttThreads) {
+            const int c4 = e % (D / 4) * 4, hq = e / (D / 4), hd = hq / heads, q = hq - hd * heads;
+            float mm = -INFINITY;
+            for (int w = 0; w < turns; ++w) mm = fmaxf(mm, sm.m[hd + w * a.block][q]);
             const float ref = reference_of(mm);
             float ll = 0.f;
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < kAttWarps; ++w) {
-                const float f = exp2_fast(sm.m[w][hd] - ref);
-                const float4 y = *reinterpret_cast<const float4*>(&sm.o[w][hd][c4]);
-                ll = fmaf(sm.l[w][hd], f, ll);
+            for (int w = 0; w < turns; ++w) {
+                const int of = hd + w * a.block;
+                const float f = exp2_fast(sm.m[of][q] - ref);
+                const float4 y = *reinterpret_cast<const float4*>(&sm.o[of][q][c4]);
+                ll = fmaf(sm.l[of][q], f, ll);
                 v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
             }
+            const size_t out_row = static_cast<size_t>(un.b) * a.Hq + static_cast<size_t>(un.h0 + hd) * G + g0 + q;
+            const size_t rec = record(a, cta, begins, hd, q);
             if (whole) {
                 const float r = ll == 0.f ? 0.f : 1.f / ll;     // (nothing seen: zeros)
-                *reinterpret_cast<uint2*>(a.out + (static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + g0 + hd) * D + c4) =
-                    make_uint2(pack_bf16(v.x * r, v.y * r), pack_bf16(v.z * r, v.w * r));
+                *reinterpret_cast<uint2*>(a.out + out_row * D + c4) = make_uint2(pack_bf16(v.x * r, v.y * r), pack_bf16(v.z * r, v.w * r));
             } else {
-                *reinterpret_cast<float4*>(a.part_o + (rec * (8 * NH) + hd) * D + c4) = v;
+                *reinterpret_cast<float4*>(a.part_o + rec * D + c4) = v;
             }
             if (c4 == 0) {
-                if (!whole) a.part_ml[rec * (8 * NH) + hd] = make_float2(mm, ll);
-                else if (SUMS) a.whole_ml[static_cast<size_t>(bh) * G + g0 + hd] = make_float2(mm, ll);   // (a CTA can have many)
+                if (!whole) a.part_ml[rec] = make_float2(mm, ll);
+                else if (SUMS) a.whole_ml[out_row] = make_float2(mm, ll);                 // (a CTA can have many)
             }
         }
+        __syncthreads();                                        // (read: the rings may be filled again)
         x = unit0 + tile1;
         if (grp + 1 == a.groups && tile1 == tiles) {            // on to the next unit that has rows
             first = x;
-            do ++bh; while (bh < units && tiles_of(rows_of(a, bh)) == 0);
+            do ++unit; while (unit < units && tiles_of(a, unit) == 0);
         }
     }
 }
@@ -332,7 +386,7 @@ struct JoinSmem {
 };
 
 // Joins the records of the units that several CTAs worked on, a CTA of this kernel for every query head (blockIdx.x below `joiners`); writes zeros
-// for heads without rows; and adds every row's weights to the sums (the other CTAs: kJoinRows rows of a KV head each).
+// for units without rows; and adds every row's weights to the sums (the other CTAs: kJoinRows rows of a KV head each).
 template <int D, int NH, bool SUMS>
 __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs a, int ctas, int row_blocks) {
     __shared__ JoinSmem<D> sm;
@@ -342,11 +396,12 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
     const int idx = sums ? blockIdx.x - joiners : blockIdx.x;
     const int bh = sums ? idx / row_blocks : idx / G;
     // (the kernel ahead sets this one up after its own wait: what was there before it is there)
-    const Deal dl = deal(a, bh, 0, 1, sm.deal);
+    const int b = bh / a.Hkv, h = bh - b * a.Hkv, blk = h / a.block, unit = b * a.blocks + blk, head = h - blk * a.block;
+    const Deal dl = deal<kJoinThreads>(a, unit, 0, 1, sm.deal);
     const int n_cta = dealt_to(dl.total, ctas);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int rows = rows_of(a, bh), tiles = tiles_of(rows);
+    const int tiles = tiles_of(a, unit);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     // records of a group of query heads: the CTA that begins the unit, and those after it up to the unit's last tile
     auto records = [&](int grp, int& c0, int& c1) {
@@ -356,8 +411,8 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
     };
     if (!sums) {
         const int hq = idx - bh * G, grp = hq / (8 * NH), hd = hq - grp * 8 * NH;
-        const size_t row = (static_cast<size_t>(bh / a.Hkv) * a.Hq + static_cast<size_t>(bh % a.Hkv) * G + hq) * D;
-        if (rows == 0) {
+        const size_t row = (static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + hq) * D;
+        if (tiles == 0) {
             for (int e = threadIdx.x; e < D; e += kJoinThreads) a.out[row + e] = __float2bfloat16(0.f);
             return;
         }
@@ -368,7 +423,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
         // of them are asked for before the factors that they wait for (one record after the other took 0.35 us each: 55 of them 20 us)
         constexpr int kParts = kJoinThreads / (D / 4), kAhead = 8;
         const int n_rec = c1 - c0 + 1, part = threadIdx.x / (D / 4), c4 = threadIdx.x % (D / 4) * 4;
-        auto row_of = [&](int r) { return record(c0 + r, r == 0) * (8 * NH) + hd; };
+        auto row_of = [&](int r) { return record(a, c0 + r, r == 0, head, hd); };
         auto values = [&](int r) { return *reinterpret_cast<const float4*>(a.part_o + row_of(r) * D + c4); };
         float4 y[kAhead];
 #pragma unroll
@@ -376,10 +431,11 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
             const int r = part + i * kParts;
             y[i] = r < n_rec ? values(r) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        float2 s[kAttMaxCtas / kJoinThreads];
+        constexpr int kOwn = (kAttMaxCtas + kJoinThreads - 1) / kJoinThreads;
+        float2 s[kOwn];
         float mm = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kAttMaxCtas / kJoinThreads; ++i) {
+        for (int i = 0; i < kOwn; ++i) {
             const int r = threadIdx.x + i * kJoinThreads;
             s[i] = r < n_rec ? a.part_ml[row_of(r)] : make_float2(-INFINITY, 0.f);
             mm = fmaxf(mm, s[i].x);
@@ -392,7 +448,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
         const float ref = reference_of(mm);
         float ll = 0.f;
 #pragma unroll
-        for (int i = 0; i < kAttMaxCtas / kJoinThreads; ++i) {
+        for (int i = 0; i < kOwn; ++i) {
             const int r = threadIdx.x + i * kJoinThreads;
             const float f = exp2_fast(s[i].x - ref);
             if (r < n_rec) sm.factor[r] = f;
@@ -426,7 +482,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
         return;
     }
     if constexpr (SUMS) {
-        const int r0 = (idx - bh * row_blocks) * kJoinRows, r1 = min(rows, r0 + kJoinRows);
+        const int r0 = (idx - bh * row_blocks) * kJoinRows, r1 = min(rows_of(a, bh), r0 + kJoinRows);
         if (r0 >= r1) return;
         float acc[kJoinRows / kJoinThreads];
 #pragma unroll
@@ -439,18 +495,18 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
                 int c0, c1;
                 records(grp, c0, c1);
                 if (c0 == c1) {
-                    const float2 s = a.whole_ml[static_cast<size_t>(bh) * G + q0 + q];
+                    const float2 s = a.whole_ml[static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + q0 + q];
                     if (lane == 0) ml[q] = make_float2(reference_of(s.x), s.y == 0.f ? 0.f : 1.f / s.y);
                     continue;
                 }
                 float mm = -INFINITY;
-                for (int c = c0 + lane; c <= c1; c += 32) mm = fmaxf(mm, a.part_ml[record(c, c == c0) * (8 * NH) + hd].x);
+                for (int c = c0 + lane; c <= c1; c += 32) mm = fmaxf(mm, a.part_ml[record(a, c, c == c0, head, hd)].x);
 #pragma unroll
                 for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
                 const float ref = reference_of(mm);
                 float ll = 0.f;
                 for (int c = c0 + lane; c <= c1; c += 32) {
-                    const float2 s = a.part_ml[record(c, c == c0) * (8 * NH) + hd];
+                    const float2 s = a.part_ml[record(a, c, c == c0, head, hd)];
                     ll += s.y * exp2_fast(s.x - ref);
                 }
 #pragma unroll
@@ -460,7 +516,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
             __syncthreads();
             for (int q = 0; q < nq; ++q) {
                 const float2 s = ml[q];
-                const float* lg = a.logits + (static_cast<size_t>(bh) * G + q0 + q) * a.logit_stride;
+                const float* lg = a.logits + (static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + q0 + q) * a.logit_stride;
 #pragma unroll
                 for (int i = 0; i < kJoinRows / kJoinThreads; ++i) {
                     const int r = r0 + i * kJoinThreads + threadIdx.x;
@@ -479,20 +535,26 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
 
 template <int D, int NH, bool SUMS>
 cudaError_t launch_attend_t(const AttendArgs& a, int n_cta, cudaStream_t stream) {
+    constexpr int smem = sizeof(AttSmem<D, NH>);
+    auto kernel = attend_kernel<D, NH, SUMS>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n_cta);
     cfg.blockDim = dim3(kAttThreads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, attend_kernel<D, NH, SUMS>, a);
+    e = cudaLaunchKernelEx(&cfg, kernel, a);
     if (e != cudaSuccess) return e;
     const int row_blocks = SUMS ? (a.cache.cap + kJoinRows - 1) / kJoinRows : 0;
     cfg.gridDim = dim3(static_cast<unsigned>(a.B * a.Hq + a.B * a.Hkv * row_blocks));
     cfg.blockDim = dim3(kJoinThreads);
+    cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NH, SUMS>, a, n_cta, row_blocks);
 }
 
@@ -504,9 +566,13 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     const int G = Hq / Hkv;
     p.nh = G > 8 ? 2 : 1;
     p.groups = (G + 8 * p.nh - 1) / (8 * p.nh);
-    const long long tiles = static_cast<long long>(B) * Hkv * p.groups * ((cap + kAttTile - 1) / kAttTile);
+    p.group = G < 8 * p.nh ? G : 8 * p.nh;
+    p.blocks = (Hkv + kAttWarps - 1) / kAttWarps;               // as many heads a CTA as it has warps, and blocks of heads alike
+    p.block = (Hkv + p.blocks - 1) / p.blocks;
+    p.tile = kAttWarps / p.block * kAttStep;
+    const long long tiles = static_cast<long long>(B) * p.blocks * p.groups * ((cap + p.tile - 1) / p.tile);
     p.max_ctas = static_cast<int>(tiles < kAttMaxCtas ? tiles : kAttMaxCtas);
-    const size_t heads = static_cast<size_t>(p.max_ctas) * 2 * 8 * p.nh;
+    const size_t heads = static_cast<size_t>(p.max_ctas) * 2 * p.block * p.group;
     p.logit_stride = (cap + 3) / 4 * 4;
     p.off_o = (heads * sizeof(float2) + 255) / 256 * 256;
     p.off_whole = p.off_o + heads * d * sizeof(float);
@@ -519,13 +585,16 @@ cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d,
     if (args.B <= 0) return cudaSuccess;
     AttendArgs a = args;
     a.groups = plan.groups;
+    a.group = plan.group;
+    a.blocks = plan.blocks;
+    a.block = plan.block;
+    a.tile = plan.tile;
     a.part_ml = reinterpret_cast<float2*>(scratch);
     a.part_o = reinterpret_cast<float*>(scratch + plan.off_o);
     a.whole_ml = reinterpret_cast<float2*>(scratch + plan.off_whole);
     a.logits = reinterpret_cast<float*>(scratch + plan.off_logits);
     a.logit_stride = plan.logit_stride;
-    const int resident = num_sms * (plan.nh == 1 ? 3 : 2);
-    const int n = resident < plan.max_ctas ? resident : plan.max_ctas;
+    const int n = num_sms < plan.max_ctas ? num_sms : plan.max_ctas;
     const bool sums = a.weights != nullptr;
 #define CKV_ATTEND(D, NH) (sums ? launch_attend_t<D, NH, true>(a, n, stream) : launch_attend_t<D, NH, false>(a, n, stream))
     if (d == 128) return plan.nh == 1 ? CKV_ATTEND(128, 1) : CKV_ATTEND(128, 2);

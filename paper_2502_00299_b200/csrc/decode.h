@@ -35,7 +35,7 @@ struct RotateArgs {
 cudaError_t launch_rotate(const RotateArgs& args, int d, int num_sms, cudaStream_t stream);
 
 // Attention of one token a sequence over a paged cache (attend.cu).
-constexpr int kAttMaxCtas = 512;              // CTAs that leave records, at most
+constexpr int kAttMaxCtas = 160;              // CTAs that leave records, at most
 struct AttendArgs {
     const __nv_bfloat16 *q, *K, *V;
     const int32_t* lengths;                   // [B, Hkv]
@@ -44,13 +44,15 @@ struct AttendArgs {
     float scale_log2;                         // log2(e) / sqrt(d)
     float* weights;                           // [B, Hkv, cap] or NULL
     __nv_bfloat16* out;
-    int groups;                               // of query heads a KV head; these and what follows are set by the launch
+    int groups, group;                        // groups of query heads of a KV head, and heads of one; these and what follows are set by the launch
+    int blocks, block;                        // blocks of KV heads that a CTA takes together, and heads of one
+    int tile;                                 // rows that are dealt together
     float2 *part_ml, *whole_ml;
     float *part_o, *logits;
     long long logit_stride;
 };
 struct AttendPlan {
-    int nh, groups, max_ctas;
+    int nh, groups, group, blocks, block, tile, max_ctas;
     long long logit_stride;
     size_t off_o, off_whole, off_logits, bytes;
 };
