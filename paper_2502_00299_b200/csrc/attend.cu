@@ -27,6 +27,8 @@ constexpr int kAttStep = 16;                          // rows of a warp's step
 constexpr int kRingBytes = 24 * 1024;                 // of a warp
 constexpr int kJoinRows = 512;                        // rows of the sums that a CTA of the join takes
 constexpr int kJoinThreads = 128;
+constexpr int kJoinFew = 256;                         // query heads of a call that are joined by a CTA for every 32 dims
+static_assert(kAttMaxCtas % 32 == 0, "records are looked at a warp at a time");
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -64,15 +66,20 @@ __device__ __forceinline__ Unit unit_of(const AttendArgs& a, int u) {
 }
 __device__ __forceinline__ int tiles_of(const AttendArgs& a, int u) {
     const Unit un = unit_of(a, u);
-    int n = 0;
-    for (int h = 0; h < un.heads; ++h) n = max(n, rows_of(a, un.b * a.Hkv + un.h0 + h));
-    return (n + a.tile - 1) / a.tile;
+    const int32_t* len = a.lengths + un.b * a.Hkv + un.h0;
+    int n[kAttWarps], most = 0;
+#pragma unroll
+    for (int h = 0; h < kAttWarps; ++h) n[h] = __ldg(len + min(h, un.heads - 1));       // (side by side: one after the other takes 0.3 us each)
+#pragma unroll
+    for (int h = 0; h < kAttWarps; ++h) most = max(most, n[h]);
+    return (min(most, a.cache.cap) + a.tile - 1) / a.tile;
 }
 
-// The line of tiles: the units in order, each `groups` times its tiles (one for each group of query heads).
+// The line of tiles: the units in order, each `groups` times its tiles (one for each group of query heads). CTA i of n has the tiles
+// [i total / n, (i + 1) total / n).
 struct Deal {
     long long total;      // tiles in all
-    int unit;             // the unit asked for, or the one that holds the tile asked for
+    int unit;             // the unit that holds the first tile of this CTA
     long long first;      // its first tile
 };
 struct DealSmem {
@@ -83,10 +90,8 @@ struct DealSmem {
 // CTAs that the line is dealt to: no more than it has tiles, so that each has one at least.
 __device__ __forceinline__ int dealt_to(long long total, int n_cta) { return static_cast<int>(min(total, static_cast<long long>(n_cta))); }
 
-// All THREADS threads. want >= 0: that unit; else the one that holds the first tile of CTA `cta` of a launch of n_cta.
-template <int THREADS>
-__device__ __forceinline__ Deal deal(const AttendArgs& a, int want, int cta, int n_cta, DealSmem& sm) {
-    const int units = a.B * a.blocks, per = (units + THREADS - 1) / THREADS;
+__device__ __forceinline__ Deal deal(const AttendArgs& a, int cta, int n_cta, DealSmem& sm) {
+    const int units = a.B * a.blocks, per = (units + kAttThreads - 1) / kAttThreads;
     const int u0 = min(static_cast<int>(threadIdx.x) * per, units), u1 = min(u0 + per, units);
     long long mine = 0;
     for (int u = u0; u < u1; ++u) mine += tiles_of(a, u);
@@ -103,24 +108,27 @@ __device__ __forceinline__ Deal deal(const AttendArgs& a, int want, int cta, int
     __syncthreads();
     long long total = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
+    for (int w = 0; w < kAttWarps; ++w) {
         if (w < warp) inc += sm.warp[w];
         total += sm.warp[w];
     }
     const int n = dealt_to(total, n_cta);
-    const long long tile = want < 0 ? (cta < n ? total * cta / n : total) : 0;
+    const long long tile = cta < n ? total * cta / n : total;
     long long at = inc - mine;
-    if (want < 0 ? (at <= tile && tile < inc) : (u0 <= want && want < u1)) {       // one thread, if any
-        for (int u = u0; u < u1; ++u) {
+    if (at <= tile && tile < inc) {                             // one thread, if any
+        int u = u0;
+        for (; u + 1 < u1; ++u) {
             const long long t = static_cast<long long>(tiles_of(a, u)) * a.groups;
-            if (want < 0 ? tile < at + t : u == want) { sm.unit = u; sm.first = at; break; }
+            if (tile < at + t) break;
             at += t;
         }
+        sm.unit = u;
+        sm.first = at;
     }
     __syncthreads();
     return {total, sm.unit, sm.first};
 }
-// The CTA of n that tile x falls to, where CTA i has the tiles [i total / n, (i + 1) total / n).
+// The CTA of n that tile x falls to.
 __device__ __forceinline__ int owner_of(long long x, long long total, int n) { return static_cast<int>(((x + 1) * n - 1) / total); }
 
 // Where records of CTA `cta` are: one for a unit that an earlier CTA has begun, one for a unit that it begins itself; each has a.block KV heads with
@@ -155,7 +163,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
     begin_dependent();
     const int cta = blockIdx.x, units = a.B * a.blocks;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const Deal dl = deal<kAttThreads>(a, -1, cta, gridDim.x, sm.deal);
+    const Deal dl = deal(a, cta, gridDim.x, sm.deal);
     const int n_cta = dealt_to(dl.total, gridDim.x);
     if (cta >= n_cta) return;
     long long x = dl.total * cta / n_cta;
@@ -340,6 +348,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
         }
         __syncthreads();
         const bool begins = tile0 == 0, whole = begins && tile1 == tiles;
+        if (begins && threadIdx.x == 0) a.shared_by[static_cast<size_t>(unit) * a.groups + grp] = make_int2(cta, owner_of(unit0 + tiles - 1, dl.total, n_cta));
         for (int e = threadIdx.x; e < un.heads * heads * (D / 4); e += kAttThreads) {
             const int c4 = e % (D / 4) * 4, hq = e / (D / 4), hd = hq / heads, q = hq - hd * heads;
             float mm = -INFINITY;
@@ -376,114 +385,120 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
     }
 }
 
-template <int D>
+// The join. A query head is joined by a team: with FEW query heads a CTA for every 32 dims of it, else a warp. The other CTAs add the rows' weights to
+// the sums, kJoinRows rows of a KV head each.
+template <int D, bool FEW>
+struct Team {
+    static constexpr int kThreads = FEW ? kJoinThreads : 32;
+    static constexpr int kDims = FEW ? 32 : D;                  // of a team
+    static constexpr int kParts = kThreads / (kDims / 4);       // groups of threads that take records in turn, 16 bytes of values a thread
+    static constexpr int kTeams = kJoinThreads / kThreads;      // in a CTA
+    static constexpr int kAhead = FEW ? 10 : 4;                 // values asked for before the factors that they wait for
+};
+template <int D, bool FEW>
 struct JoinSmem {
-    alignas(16) float o[kJoinThreads / (D / 4)][D];
-    float factor[kAttMaxCtas];
-    float part[kJoinThreads / 32], sum[kJoinThreads / 32];
+    alignas(16) float o[kJoinThreads][4];
+    float factor[Team<D, FEW>::kTeams][kAttMaxCtas];
+    float top[kJoinThreads / 32], sum[kJoinThreads / 32];
     float2 ml[kJoinThreads];          // (reference, factor) of query heads
-    DealSmem deal;
 };
 
-// Joins the records of the units that several CTAs worked on, a CTA of this kernel for every query head (blockIdx.x below `joiners`); writes zeros
-// for units without rows; and adds every row's weights to the sums (the other CTAs: kJoinRows rows of a KV head each).
-template <int D, int NH, bool SUMS>
-__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs a, int ctas, int row_blocks) {
-    __shared__ JoinSmem<D> sm;
-    float2* ml = sm.ml;
-    const int G = a.Hq / a.Hkv, joiners = a.B * a.Hq;
-    const bool sums = SUMS && static_cast<int>(blockIdx.x) >= joiners;
-    const int idx = sums ? blockIdx.x - joiners : blockIdx.x;
-    const int bh = sums ? idx / row_blocks : idx / G;
-    // (the kernel ahead sets this one up after its own wait: what was there before it is there)
-    const int b = bh / a.Hkv, h = bh - b * a.Hkv, blk = h / a.block, unit = b * a.blocks + blk, head = h - blk * a.block;
-    const Deal dl = deal<kJoinThreads>(a, unit, 0, 1, sm.deal);
-    const int n_cta = dealt_to(dl.total, ctas);
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int tiles = tiles_of(a, unit);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    // records of a group of query heads: the CTA that begins the unit, and those after it up to the unit's last tile
-    auto records = [&](int grp, int& c0, int& c1) {
-        const long long f = dl.first + static_cast<long long>(grp) * tiles;
-        c0 = owner_of(f, dl.total, n_cta);
-        c1 = owner_of(f + tiles - 1, dl.total, n_cta);
-    };
-    if (!sums) {
-        const int hq = idx - bh * G, grp = hq / (8 * NH), hd = hq - grp * 8 * NH;
-        const size_t row = (static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + hq) * D;
-        if (tiles == 0) {
-            for (int e = threadIdx.x; e < D; e += kJoinThreads) a.out[row + e] = __float2bfloat16(0.f);
+template <int D, int NH, bool SUMS, bool FEW>
+__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs a, int join_ctas, int row_blocks) {
+    using T = Team<D, FEW>;
+    constexpr unsigned kFull = 0xffffffffu;
+    __shared__ JoinSmem<D, FEW> sm;
+    const int G = a.Hq / a.Hkv, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    auto meet = [] { if constexpr (FEW) __syncthreads(); else __syncwarp(); };
+    // (the kernel ahead sets this one up after its own wait: lengths, which were there before it, may be read)
+    if (static_cast<int>(blockIdx.x) < join_ctas) {
+        const int team = threadIdx.x / T::kThreads, id = threadIdx.x % T::kThreads;
+        const int item = blockIdx.x * T::kTeams + team, cols = item % (D / T::kDims) * T::kDims, row = item / (D / T::kDims);   // row of q and out
+        const bool there = row < a.B * a.Hq;
+        const int b = row / a.Hq, hq = row - b * a.Hq, h = hq / G, q = hq - h * G, grp = q / (8 * NH), qg = q - grp * 8 * NH;
+        const int blk = h / a.block, unit = b * a.blocks + blk, head = h - blk * a.block;
+        const int tiles = there ? tiles_of(a, unit) : 0;
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (!there) return;                                     // (a whole team)
+        const int part = id / (T::kDims / 4), c4 = cols + id % (T::kDims / 4) * 4;
+        __nv_bfloat16* out = a.out + static_cast<size_t>(row) * D + c4;
+        if (tiles == 0) {                                       // no rows: zeros
+            if (part == 0) *reinterpret_cast<uint2*>(out) = make_uint2(0u, 0u);
             return;
         }
-        int c0, c1;
-        records(grp, c0, c1);
-        if (c0 == c1) return;                                   // one CTA had the whole unit and wrote it
-        // a record's values by D / 4 threads, 16 bytes each; the group of threads `part` takes the records part, part + kParts, ...; the first kAhead
-        // of them are asked for before the factors that they wait for (one record after the other took 0.35 us each: 55 of them 20 us)
-        constexpr int kParts = kJoinThreads / (D / 4), kAhead = 8;
-        const int n_rec = c1 - c0 + 1, part = threadIdx.x / (D / 4), c4 = threadIdx.x % (D / 4) * 4;
-        auto row_of = [&](int r) { return record(a, c0 + r, r == 0, head, hd); };
-        auto values = [&](int r) { return *reinterpret_cast<const float4*>(a.part_o + row_of(r) * D + c4); };
-        float4 y[kAhead];
+        const int2 by = a.shared_by[static_cast<size_t>(unit) * a.groups + grp];
+        const int n_rec = by.y - by.x + 1;
+        if (n_rec == 1) return;                                 // one CTA had the whole unit and wrote it
+        auto record_of = [&](int r) { return record(a, by.x + r, r == 0, head, qg); };
+        auto values = [&](int r) { return *reinterpret_cast<const float4*>(a.part_o + record_of(r) * D + c4); };
+        float4 y[T::kAhead];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int r = part + i * kParts;
+        for (int i = 0; i < T::kAhead; ++i) {
+            const int r = part + i * T::kParts;
             y[i] = r < n_rec ? values(r) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        constexpr int kOwn = (kAttMaxCtas + kJoinThreads - 1) / kJoinThreads;
+        constexpr int kOwn = (kAttMaxCtas + T::kThreads - 1) / T::kThreads;
         float2 s[kOwn];
         float mm = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
-            const int r = threadIdx.x + i * kJoinThreads;
-            s[i] = r < n_rec ? a.part_ml[row_of(r)] : make_float2(-INFINITY, 0.f);
+            const int r = id + i * T::kThreads;
+            s[i] = r < n_rec ? a.part_ml[record_of(r)] : make_float2(-INFINITY, 0.f);
             mm = fmaxf(mm, s[i].x);
         }
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
-        if (lane == 0) sm.part[warp] = mm;
-        __syncthreads();
-        mm = fmaxf(fmaxf(sm.part[0], sm.part[1]), fmaxf(sm.part[2], sm.part[3]));
+        for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(kFull, mm, off));
+        if constexpr (FEW) {
+            if (lane == 0) sm.top[warp] = mm;
+            __syncthreads();
+            mm = fmaxf(fmaxf(sm.top[0], sm.top[1]), fmaxf(sm.top[2], sm.top[3]));
+        }
         const float ref = reference_of(mm);
         float ll = 0.f;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
-            const int r = threadIdx.x + i * kJoinThreads;
+            const int r = id + i * T::kThreads;
             const float f = exp2_fast(s[i].x - ref);
-            if (r < n_rec) sm.factor[r] = f;
-            ll += r < n_rec ? s[i].y * f : 0.f;
+            if (r < n_rec) { sm.factor[team][r] = f; ll += s[i].y * f; }
         }
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, off);
-        if (lane == 0) sm.sum[warp] = ll;
-        __syncthreads();
-        ll = (sm.sum[0] + sm.sum[1]) + (sm.sum[2] + sm.sum[3]);
+        for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(kFull, ll, off);
+        if constexpr (FEW) {
+            if (lane == 0) sm.sum[warp] = ll;
+        }
+        meet();
+        if constexpr (FEW) ll = (sm.sum[0] + sm.sum[1]) + (sm.sum[2] + sm.sum[3]);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto add = [&](const float4& x, int r) {
-            const float f = sm.factor[r];
-            v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
-        };
+        auto add = [&](const float4& z, float f) { v.x = fmaf(z.x, f, v.x); v.y = fmaf(z.y, f, v.y); v.z = fmaf(z.z, f, v.z); v.w = fmaf(z.w, f, v.w); };
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            if (part + i * kParts < n_rec) add(y[i], part + i * kParts);
-#pragma unroll 8
-        for (int r = part + kAhead * kParts; r < n_rec; r += kParts) add(values(r), r);
-        *reinterpret_cast<float4*>(&sm.o[part][c4]) = v;
-        __syncthreads();
-        if (threadIdx.x < D / 2) {
-            const int e = 2 * threadIdx.x;
-            float v0 = 0.f, v1 = 0.f;
+        for (int i = 0; i < T::kAhead; ++i)
+            if (part + i * T::kParts < n_rec) add(y[i], sm.factor[team][part + i * T::kParts]);
+#pragma unroll 4
+        for (int r = part + T::kAhead * T::kParts; r < n_rec; r += T::kParts) add(values(r), sm.factor[team][r]);
+        if constexpr (T::kParts > 1) {                          // the parts, in their order
+            *reinterpret_cast<float4*>(sm.o[threadIdx.x]) = v;
+            meet();
+            if (part == 0) {
+                v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < kParts; ++i) { v0 += sm.o[i][e]; v1 += sm.o[i][e + 1]; }
-            const float r = ll == 0.f ? 0.f : 1.f / ll;
-            *reinterpret_cast<uint32_t*>(a.out + row + e) = pack_bf16(v0 * r, v1 * r);
+                for (int i = 0; i < T::kParts; ++i) add(*reinterpret_cast<const float4*>(sm.o[threadIdx.x + i * (T::kDims / 4)]), 1.f);
+            }
+        }
+        if (part == 0) {
+            const float r = ll == 0.f ? 0.f : 1.f / ll;         // (nothing seen: zeros)
+            *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16(v.x * r, v.y * r), pack_bf16(v.z * r, v.w * r));
         }
         return;
     }
     if constexpr (SUMS) {
+        const int idx = blockIdx.x - join_ctas, bh = idx / row_blocks, b = bh / a.Hkv, h = bh - b * a.Hkv;
+        const int blk = h / a.block, unit = b * a.blocks + blk, head = h - blk * a.block;
         const int r0 = (idx - bh * row_blocks) * kJoinRows, r1 = min(rows_of(a, bh), r0 + kJoinRows);
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        asm volatile("griddepcontrol.wait;" ::: "memory");
         if (r0 >= r1) return;
+        const size_t q_row = static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G;
         float acc[kJoinRows / kJoinThreads];
 #pragma unroll
         for (int i = 0; i < kJoinRows / kJoinThreads; ++i) acc[i] = 0.f;
@@ -491,32 +506,36 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
             const int nq = min(kJoinThreads, G - q0);
             __syncthreads();
             for (int q = warp; q < nq; q += kJoinThreads / 32) {
-                const int grp = (q0 + q) / (8 * NH), hd = (q0 + q) - grp * 8 * NH;
-                int c0, c1;
-                records(grp, c0, c1);
-                if (c0 == c1) {
-                    const float2 s = a.whole_ml[static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + q0 + q];
-                    if (lane == 0) ml[q] = make_float2(reference_of(s.x), s.y == 0.f ? 0.f : 1.f / s.y);
+                const int grp = (q0 + q) / (8 * NH), qg = (q0 + q) - grp * 8 * NH;
+                const int2 by = a.shared_by[static_cast<size_t>(unit) * a.groups + grp];
+                if (by.x == by.y) {
+                    const float2 s = a.whole_ml[q_row + q0 + q];
+                    if (lane == 0) sm.ml[q] = make_float2(reference_of(s.x), s.y == 0.f ? 0.f : 1.f / s.y);
                     continue;
                 }
+                constexpr int kOwn = kAttMaxCtas / 32;
+                float2 s[kOwn];
                 float mm = -INFINITY;
-                for (int c = c0 + lane; c <= c1; c += 32) mm = fmaxf(mm, a.part_ml[record(a, c, c == c0, head, hd)].x);
 #pragma unroll
-                for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
-                const float ref = reference_of(mm);
-                float ll = 0.f;
-                for (int c = c0 + lane; c <= c1; c += 32) {
-                    const float2 s = a.part_ml[record(a, c, c == c0, head, hd)];
-                    ll += s.y * exp2_fast(s.x - ref);
+                for (int i = 0; i < kOwn; ++i) {
+                    const int c = by.x + lane + 32 * i;
+                    s[i] = c <= by.y ? a.part_ml[record(a, c, c == by.x, head, qg)] : make_float2(-INFINITY, 0.f);
+                    mm = fmaxf(mm, s[i].x);
                 }
 #pragma unroll
-                for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, off);
-                if (lane == 0) ml[q] = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
+                for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(kFull, mm, off));
+                const float ref = reference_of(mm);
+                float ll = 0.f;
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) ll += by.x + lane + 32 * i <= by.y ? s[i].y * exp2_fast(s[i].x - ref) : 0.f;
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(kFull, ll, off);
+                if (lane == 0) sm.ml[q] = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
             }
             __syncthreads();
             for (int q = 0; q < nq; ++q) {
-                const float2 s = ml[q];
-                const float* lg = a.logits + (static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + q0 + q) * a.logit_stride;
+                const float2 s = sm.ml[q];
+                const float* lg = a.logits + (q_row + q0 + q) * a.logit_stride;
 #pragma unroll
                 for (int i = 0; i < kJoinRows / kJoinThreads; ++i) {
                     const int r = r0 + i * kJoinThreads + threadIdx.x;
@@ -552,15 +571,19 @@ cudaError_t launch_attend_t(const AttendArgs& a, int n_cta, cudaStream_t stream)
     e = cudaLaunchKernelEx(&cfg, kernel, a);
     if (e != cudaSuccess) return e;
     const int row_blocks = SUMS ? (a.cache.cap + kJoinRows - 1) / kJoinRows : 0;
-    cfg.gridDim = dim3(static_cast<unsigned>(a.B * a.Hq + a.B * a.Hkv * row_blocks));
+    const bool few = a.B * a.Hq <= kJoinFew;
+    const int join_ctas = few ? a.B * a.Hq * (D / Team<D, true>::kDims) : (a.B * a.Hq + Team<D, false>::kTeams - 1) / Team<D, false>::kTeams;
+    cfg.gridDim = dim3(static_cast<unsigned>(join_ctas + a.B * a.Hkv * row_blocks));
     cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NH, SUMS>, a, n_cta, row_blocks);
+    return few ? cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NH, SUMS, true>, a, join_ctas, row_blocks)
+               : cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NH, SUMS, false>, a, join_ctas, row_blocks);
 }
 
 }  // namespace
 
-// Scratch: (max, sum) and O of two records a CTA; where sums are asked for, (max, sum) of the units that one CTA had and the logits of all rows.
+// Scratch: (max, sum) and O of two records a CTA, the CTAs that share a unit; where sums are asked for, (max, sum) of the units that one CTA had and
+// the logits of all rows.
 AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     AttendPlan p;
     const int G = Hq / Hkv;
@@ -576,7 +599,8 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     p.logit_stride = (cap + 3) / 4 * 4;
     p.off_o = (heads * sizeof(float2) + 255) / 256 * 256;
     p.off_whole = p.off_o + heads * d * sizeof(float);
-    p.off_logits = p.off_whole + (sums ? (static_cast<size_t>(B) * Hq * sizeof(float2) + 255) / 256 * 256 : 0);
+    p.off_shared = p.off_whole + (sums ? (static_cast<size_t>(B) * Hq * sizeof(float2) + 255) / 256 * 256 : 0);
+    p.off_logits = p.off_shared + (static_cast<size_t>(B) * p.blocks * p.groups * sizeof(int2) + 255) / 256 * 256;
     p.bytes = p.off_logits + (sums ? static_cast<size_t>(B) * Hq * p.logit_stride * sizeof(float) : 0);
     return p;
 }
@@ -592,6 +616,7 @@ cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d,
     a.part_ml = reinterpret_cast<float2*>(scratch);
     a.part_o = reinterpret_cast<float*>(scratch + plan.off_o);
     a.whole_ml = reinterpret_cast<float2*>(scratch + plan.off_whole);
+    a.shared_by = reinterpret_cast<int2*>(scratch + plan.off_shared);
     a.logits = reinterpret_cast<float*>(scratch + plan.off_logits);
     a.logit_stride = plan.logit_stride;
     const int n = num_sms < plan.max_ctas ? num_sms : plan.max_ctas;

@@ -48,13 +48,14 @@ struct AttendArgs {
     int blocks, block;                        // blocks of KV heads that a CTA takes together, and heads of one
     int tile;                                 // rows that are dealt together
     float2 *part_ml, *whole_ml;
+    int2* shared_by;                          // first and last CTA with rows of a unit
     float *part_o, *logits;
     long long logit_stride;
 };
 struct AttendPlan {
     int nh, groups, group, blocks, block, tile, max_ctas;
     long long logit_stride;
-    size_t off_o, off_whole, off_logits, bytes;
+    size_t off_o, off_whole, off_shared, off_logits, bytes;
 };
 AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums);
 cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d, char* scratch, int num_sms, cudaStream_t stream);
