@@ -31,7 +31,7 @@ constexpr int kJoinFew = 256;                         // query heads of a call t
 static_assert(kAttMaxCtas % 32 == 0, "records are looked at a warp at a time");
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -47,11 +47,6 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool t
 __device__ __forceinline__ void copies_begin_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint4 load_shared(uint32_t at) {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
-}
 // A maximum as the reference of exponents: 0 where nothing was seen.
 __device__ __forceinline__ float reference_of(float m) { return m == -INFINITY ? 0.f : m; }
 
@@ -174,7 +169,8 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
     const int head = warp % a.block, turn = warp / a.block, turns = a.tile / kAttStep;
     const int G = a.Hq / a.Hkv;
     const size_t row_elems = static_cast<size_t>(a.Hkv) * D;
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(&sm.ring[warp][0]));
+    unsigned char* const slots = sm.ring[warp];
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(slots));
     // what a lane copies of a step's rows: piece `piece` of the rows r0 + kRowsOnce i. Pieces are exchanged within 128 bytes so that the eight
     // lanes of a load's quarter find theirs in different banks: keys are read four neighbouring pieces of two rows at a time, values two of four.
     const int piece = lane % kPieces, r0 = lane / kPieces;
@@ -241,17 +237,22 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
             const int ahead = base + (kStages - 1) * a.tile;
             if (ahead < r1) copy_step(at[kStages - 1], ring + (stage == 0 ? kStages - 1 : stage - 1) * 2 * kHalf);
             copies_begin_group();
-            const uint32_t keys = ring + stage * 2 * kHalf, values = keys + kHalf;
+            const unsigned char *keys = slots + stage * 2 * kHalf, *values = keys + kHalf;
             stage = stage == kStages - 1 ? 0 : stage + 1;
             // S: rows of the product are the query heads g and g + 8, columns the cache rows 2t and 2t + 1 of eight
             float s[2][4];
 #pragma unroll
             for (int j = 0; j < 2; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
+            uint4 kr[kCh][2];
+#pragma unroll
+            for (int i = 0; i < kCh; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) kr[i][j] = *reinterpret_cast<const uint4*>(keys + (8 * j + g) * (2 * D) + (((4 * i + t) ^ (4 * (g & 1))) << 4));
 #pragma unroll
             for (int i = 0; i < kCh; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint4 k = load_shared(keys + (8 * j + g) * (2 * D) + (((4 * i + t) ^ (4 * (g & 1))) << 4));
+                    const uint4 k = kr[i][j];
                     mma_bf16(s[j], qr[0][i].x, NH == 2 ? qr[NH - 1][i].x : 0u, qr[0][i].y, NH == 2 ? qr[NH - 1][i].y : 0u, k.x, k.y);
                     mma_bf16(s[j], qr[0][i].z, NH == 2 ? qr[NH - 1][i].z : 0u, qr[0][i].w, NH == 2 ? qr[NH - 1][i].w : 0u, k.z, k.w);
                 }
@@ -314,7 +315,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
                 uint32_t w[4][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {                   // rows 2t, 2t + 1, 8 + 2t, 9 + 2t
-                    const uint4 v = load_shared(values + ((j >> 1) * 8 + 2 * t + (j & 1)) * (2 * D) + (((8 * hh + g) ^ (2 * t)) << 4));
+                    const uint4 v = *reinterpret_cast<const uint4*>(values + ((j >> 1) * 8 + 2 * t + (j & 1)) * (2 * D) + (((8 * hh + g) ^ (2 * t)) << 4));
                     w[j][0] = v.x; w[j][1] = v.y; w[j][2] = v.z; w[j][3] = v.w;
                 }
 #pragma unroll
