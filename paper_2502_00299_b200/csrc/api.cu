@@ -753,9 +753,6 @@ static int check_decode_cache(int max_pages, int page_size, int num_pages) {
     return CHUNKKV_OK;
 }
 static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
-static PagedCache paged_cache(const int32_t* tables, int max_pages, int page_size, int num_pages) {
-    return {tables, max_pages, page_size, num_pages, max_pages * page_size};
-}
 
 int chunkkv_rotate_qk(const void* qkv, long long row_elems, int T, int Hq, int Hkv, int d, const void* q_gain, const void* k_gain, float eps,
                       const float* cos_t, const float* sin_t, int n_pos, const int32_t* positions, long long q_token_stride,
@@ -834,7 +831,8 @@ int chunkkv_attend_paged(const void* q, const int32_t* block_tables, int max_pag
     if (st == CHUNKKV_OK) st = check_decode_cache(max_pages, page_size, num_pages);
     if (st != CHUNKKV_OK) return st;
     const int cap = max_pages * page_size;
-    if (weights != nullptr && static_cast<long long>(B) * Hkv * (cap / 512 + 1) >= (1LL << 30)) return CHUNKKV_EINVAL_SHAPE;   // CTAs of a launch
+    // tiles of at least 16 rows are counted, and CTAs of a launch
+    if (static_cast<long long>(B) * Hq * (cap / 16 + 1) >= (1LL << 31)) return CHUNKKV_EINVAL_SHAPE;
     if (B == 0) return CHUNKKV_OK;
     if (q == nullptr || block_tables == nullptr || lengths == nullptr || cache_K == nullptr || cache_V == nullptr || out == nullptr) return CHUNKKV_EINVAL_NULL;
     if (!aligned16(q) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) || !aligned4(weights) || !aligned16(out))

@@ -67,53 +67,63 @@ __device__ __forceinline__ int tiles_of(const AttendArgs& a, int u) {
     for (int h = 0; h < kAttWarps; ++h) n[h] = __ldg(len + min(h, un.heads - 1));       // (side by side: one after the other takes 0.3 us each)
 #pragma unroll
     for (int h = 0; h < kAttWarps; ++h) most = max(most, n[h]);
-    return (min(most, a.cache.cap) + a.tile - 1) / a.tile;
+    const int last = min(most, a.cache.cap) + a.tile - 1;
+    return a.tile_shift >= 0 ? last >> a.tile_shift : last / a.tile;
 }
 
-// The line of tiles: the units in order, each `groups` times its tiles (one for each group of query heads). CTA i of n has the tiles
-// [i total / n, (i + 1) total / n).
+// The line of tiles: the units in order, each `groups` times its tiles (one for each group of query heads), dealt to n CTAs in shares
+// of `per`, the first `more` of them of one more.
+struct Share {
+    int n, per, more;
+    __device__ __forceinline__ Share(int total, int n_cta) {    // (no more CTAs than tiles, so that each has one at least)
+        n = min(total, n_cta);
+        per = n > 0 ? total / n : 0;
+        more = total - per * n;
+    }
+    __device__ __forceinline__ int begin(int cta) const { return cta * per + min(cta, more); }
+    __device__ __forceinline__ int owner(int x) const {         // the CTA that tile x falls to
+        const int wide = more * (per + 1);
+        return x < wide ? x / (per + 1) : more + (x - wide) / per;
+    }
+};
 struct Deal {
-    long long total;      // tiles in all
+    int total;            // tiles in all
     int unit;             // the unit that holds the first tile of this CTA
-    long long first;      // its first tile
+    int first;            // its first tile
 };
 struct DealSmem {
-    long long warp[kAttWarps];
-    long long first;
-    int unit;
+    int warp[kAttWarps];
+    int first, unit;
 };
-// CTAs that the line is dealt to: no more than it has tiles, so that each has one at least.
-__device__ __forceinline__ int dealt_to(long long total, int n_cta) { return static_cast<int>(min(total, static_cast<long long>(n_cta))); }
 
 __device__ __forceinline__ Deal deal(const AttendArgs& a, int cta, int n_cta, DealSmem& sm) {
     const int units = a.B * a.blocks, per = (units + kAttThreads - 1) / kAttThreads;
     const int u0 = min(static_cast<int>(threadIdx.x) * per, units), u1 = min(u0 + per, units);
-    long long mine = 0;
+    int mine = 0;
     for (int u = u0; u < u1; ++u) mine += tiles_of(a, u);
     mine *= a.groups;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    long long inc = mine;
+    int inc = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const long long v = __shfl_up_sync(0xffffffffu, inc, off);
+        const int v = __shfl_up_sync(0xffffffffu, inc, off);
         if (lane >= off) inc += v;
     }
     if (lane == 31) sm.warp[warp] = inc;
     if (threadIdx.x == 0) sm.unit = units;
     __syncthreads();
-    long long total = 0;
+    int total = 0;
 #pragma unroll
     for (int w = 0; w < kAttWarps; ++w) {
         if (w < warp) inc += sm.warp[w];
         total += sm.warp[w];
     }
-    const int n = dealt_to(total, n_cta);
-    const long long tile = cta < n ? total * cta / n : total;
-    long long at = inc - mine;
+    const int tile = Share(total, n_cta).begin(cta);
+    int at = inc - mine;
     if (at <= tile && tile < inc) {                             // one thread, if any
         int u = u0;
         for (; u + 1 < u1; ++u) {
-            const long long t = static_cast<long long>(tiles_of(a, u)) * a.groups;
+            const int t = tiles_of(a, u) * a.groups;
             if (tile < at + t) break;
             at += t;
         }
@@ -123,8 +133,6 @@ __device__ __forceinline__ Deal deal(const AttendArgs& a, int cta, int n_cta, De
     __syncthreads();
     return {total, sm.unit, sm.first};
 }
-// The CTA of n that tile x falls to.
-__device__ __forceinline__ int owner_of(long long x, long long total, int n) { return static_cast<int>(((x + 1) * n - 1) / total); }
 
 // Where records of CTA `cta` are: one for a unit that an earlier CTA has begun, one for a unit that it begins itself; each has a.block KV heads with
 // a.group query heads.
@@ -137,7 +145,7 @@ struct AttSmem {
     static constexpr int kPad = D + 4;
     union {
         alignas(128) unsigned char ring[kAttWarps][kRingBytes];
-        float o[kAttWarps][8 * NH][kPad];       // where several warps work on a head (the ring is idle then)
+        float o[kAttWarps][8 * NH][kPad];       // where several warps work on a head (the rings are idle then)
     };
     float m[kAttWarps][8 * NH], l[kAttWarps][8 * NH];
     DealSmem deal;
@@ -159,12 +167,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
     const int cta = blockIdx.x, units = a.B * a.blocks;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const Deal dl = deal(a, cta, gridDim.x, sm.deal);
-    const int n_cta = dealt_to(dl.total, gridDim.x);
-    if (cta >= n_cta) return;
-    long long x = dl.total * cta / n_cta;
-    const long long x1 = dl.total * (cta + 1) / n_cta;
-    int unit = dl.unit;
-    long long first = dl.first;
+    const Share share(dl.total, gridDim.x);
+    if (cta >= share.n || dl.unit >= units) return;
+    const int x1 = share.begin(cta + 1);
     // this warp's head in a unit and its rows among those of the head's warps
     const int head = warp % a.block, turn = warp / a.block, turns = a.tile / kAttStep;
     const int G = a.Hq / a.Hkv;
@@ -174,53 +179,73 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
     // what a lane copies of a step's rows: piece `piece` of the rows r0 + kRowsOnce i. Pieces are exchanged within 128 bytes so that the eight
     // lanes of a load's quarter find theirs in different banks: keys are read four neighbouring pieces of two rows at a time, values two of four.
     const int piece = lane % kPieces, r0 = lane / kPieces;
-    while (x < x1 && unit < units) {
-        const Unit un = unit_of(a, unit);
-        const int tiles = tiles_of(a, unit);
-        const int grp = static_cast<int>((x - first) / tiles);
-        const long long unit0 = first + static_cast<long long>(grp) * tiles;              // the unit's first tile
-        const int tile0 = static_cast<int>(x - unit0), tile1 = static_cast<int>(min(x1 - unit0, static_cast<long long>(tiles)));
-        const int h = un.h0 + head, bh = un.b * a.Hkv + h;
-        const bool on = head < un.heads && turn < turns;                                  // (else this warp has no head here)
-        const int rows = on ? rows_of(a, bh) : 0;
-        const int g0 = grp * 8 * NH, heads = min(8 * NH, G - g0);                         // query heads of this group
-        const int r1 = min(rows, tile1 * a.tile);
-        const int32_t* table = a.cache.tables + static_cast<size_t>(un.b) * a.cache.max_pages;
-        const size_t q_row = static_cast<size_t>(un.b) * a.Hq + static_cast<size_t>(h) * G + g0;
-        const __nv_bfloat16 *Kh = a.K + static_cast<size_t>(h) * D + 8 * piece, *Vh = a.V + static_cast<size_t>(h) * D + 8 * piece;
 
-        // lane l (and l + 16) looks up row l of a step
-        auto lookup = [&](int base) {
-            const int r = base + (lane & 15);
-            return r < r1 ? paged_row(a.cache, table, r) : -1;
-        };
-        auto copy_step = [&](int at, uint32_t to) {
+    // A part of this CTA's share: tiles [tile0, tile1) of a unit, for one group of query heads.
+    struct Part {
+        Unit un;
+        int unit, tiles, first, grp, tile0, tile1;
+        int rows_end;                // of this warp's head, within the part
+        __device__ __forceinline__ bool begins() const { return tile0 == 0; }
+        __device__ __forceinline__ bool whole() const { return tile0 == 0 && tile1 == tiles; }
+    };
+    auto part_at = [&](int x, int unit, int first) {            // first: the unit's first tile (of its first group)
+        Part p;
+        p.unit = unit;
+        p.first = first;
+        p.un = unit_of(a, unit);
+        p.tiles = tiles_of(a, unit);
+        p.grp = a.groups == 1 ? 0 : (x - first) / p.tiles;
+        const int begin = first + p.grp * p.tiles;
+        p.tile0 = x - begin;
+        p.tile1 = min(x1 - begin, p.tiles);
+        const bool on = head < p.un.heads && turn < turns;      // (else this warp has no head here)
+        p.rows_end = on ? min(rows_of(a, p.un.b * a.Hkv + p.un.h0 + head), p.tile1 * a.tile) : 0;
+        return p;
+    };
+    // lane l (and l + 16) looks up row l of a step
+    auto lookup = [&](const Part& p, int base) {
+        const int r = base + (lane & 15);
+        return r < p.rows_end ? paged_row(a.cache, a.cache.tables + static_cast<size_t>(p.un.b) * a.cache.max_pages, r) : -1;
+    };
+    auto copy_step = [&](const Part& p, int at, uint32_t to) {
+        const size_t off_h = static_cast<size_t>(p.un.h0 + head) * D + 8 * piece;
+        const __nv_bfloat16 *Kh = a.K + off_h, *Vh = a.V + off_h;
 #pragma unroll
-            for (int i = 0; i < kAttStep / kRowsOnce; ++i) {
-                const int r = i * kRowsOnce + r0, row = __shfl_sync(kFull, at, r);
-                const size_t off = static_cast<size_t>(max(row, 0)) * row_elems;
-                copy_async(to + r * (2 * D) + ((piece ^ (4 * (r & 1))) << 4), Kh + off, row >= 0);
-                copy_async(to + kHalf + r * (2 * D) + ((piece ^ (r & 6)) << 4), Vh + off, row >= 0);
-            }
-        };
-
-        // at[i]: rows of the step i behind the one that is worked on. A group of copies a step, empty ones behind the last row.
-        int base = tile0 * a.tile + turn * kAttStep;
-        int at[kStages];
-#pragma unroll
-        for (int i = 0; i < kStages; ++i) at[i] = lookup(base + i * a.tile);
-#pragma unroll
-        for (int i = 0; i < kStages - 1; ++i) {
-            if (base + i * a.tile < r1) copy_step(at[i], ring + i * 2 * kHalf);
-            copies_begin_group();
+        for (int i = 0; i < kAttStep / kRowsOnce; ++i) {
+            const int r = i * kRowsOnce + r0, row = __shfl_sync(kFull, at, r);
+            const size_t off = static_cast<size_t>(max(row, 0)) * row_elems;
+            copy_async(to + r * (2 * D) + ((piece ^ (4 * (r & 1))) << 4), Kh + off, row >= 0);
+            copy_async(to + kHalf + r * (2 * D) + ((piece ^ (r & 6)) << 4), Vh + off, row >= 0);
         }
-        uint4 qr[NH][kCh];
+    };
+    // at[i]: rows of the step i behind the one that is worked on. A group of copies a step, empty ones behind the last row.
+    int at[kStages];
+    uint4 qr[NH][kCh];
+    auto begin_part = [&](const Part& p) {
+        const int base = p.tile0 * a.tile + turn * kAttStep;
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) at[i] = lookup(p, base + i * a.tile);
+        const int heads = min(8 * NH, G - p.grp * 8 * NH);
+        const __nv_bfloat16* q = a.q + (static_cast<size_t>(p.un.b) * a.Hq + static_cast<size_t>(p.un.h0 + head) * G + p.grp * 8 * NH) * D;
 #pragma unroll
         for (int n = 0; n < NH; ++n)
 #pragma unroll
             for (int i = 0; i < kCh; ++i)
-                qr[n][i] = on && 8 * n + g < heads ? __ldg(reinterpret_cast<const uint4*>(a.q + (q_row + 8 * n + g) * D + 32 * i + 8 * t)) : make_uint4(0, 0, 0, 0);
+                qr[n][i] = p.rows_end > 0 && 8 * n + g < heads ? __ldg(reinterpret_cast<const uint4*>(q + static_cast<size_t>(8 * n + g) * D + 32 * i + 8 * t))
+                                                               : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) {
+            if (base + i * a.tile < p.rows_end) copy_step(p, at[i], ring + i * 2 * kHalf);
+            copies_begin_group();
+        }
+    };
 
+    Part p = part_at(share.begin(cta), dl.unit, dl.first);
+    begin_part(p);
+    for (;;) {
+        const int heads = min(8 * NH, G - p.grp * 8 * NH);      // query heads of this group
+        const int r1 = p.rows_end;
+        const size_t q_row = static_cast<size_t>(p.un.b) * a.Hq + static_cast<size_t>(p.un.h0 + head) * G + p.grp * 8 * NH;
         float m[NH], l[NH], o[NH][D / 16][4];
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
@@ -231,11 +256,11 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
         }
 
         int stage = 0;
-        for (; base < r1; base += a.tile) {
+        for (int base = p.tile0 * a.tile + turn * kAttStep; base < r1; base += a.tile) {
             copies_wait<kStages - 2>();
             __syncwarp();                                       // (this step has landed, and the one before has been read)
             const int ahead = base + (kStages - 1) * a.tile;
-            if (ahead < r1) copy_step(at[kStages - 1], ring + (stage == 0 ? kStages - 1 : stage - 1) * 2 * kHalf);
+            if (ahead < r1) copy_step(p, at[kStages - 1], ring + (stage == 0 ? kStages - 1 : stage - 1) * 2 * kHalf);
             copies_begin_group();
             const unsigned char *keys = slots + stage * 2 * kHalf, *values = keys + kHalf;
             stage = stage == kStages - 1 ? 0 : stage + 1;
@@ -261,7 +286,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
             for (int j = 0; j < 4; ++j) seen |= __shfl_sync(kFull, at[0], (j >> 1) * 8 + 2 * t + (j & 1)) >= 0 ? 1u << j : 0u;
 #pragma unroll
             for (int i = 0; i < kStages - 1; ++i) at[i] = at[i + 1];
-            at[kStages - 1] = lookup(ahead + a.tile);
+            at[kStages - 1] = lookup(p, ahead + a.tile);
 
             uint32_t hi[NH][2], lo[NH][2];
             float factor[NH];
@@ -331,58 +356,113 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
             }
         }
 
-        // the warps' parts of a head, joined: (max, sum) of a query head from the four lanes that hold its columns, then over the warps
-        __syncthreads();                                        // (every ring is idle)
+        // the part behind this one, if any: where no other warp's values are joined in the rings' place its first rows are asked for at once
+        const int x = p.first + p.grp * p.tiles + p.tile1;
+        Part next = p;
+        bool more = x < x1;
+        if (more) {
+            int unit = p.unit, first = p.first;
+            if (p.grp + 1 == a.groups) {                        // on to the next unit that has rows
+                first = x;
+                do ++unit; while (unit < units && tiles_of(a, unit) == 0);
+            }
+            more = unit < units;
+            if (more) next = part_at(x, unit, first);
+        }
+        __syncwarp();                                           // (the last step has been read)
+        if (more && turns == 1) begin_part(next);
+
 #pragma unroll
-        for (int n = 0; n < NH; ++n) {
+        for (int n = 0; n < NH; ++n) {                          // (max, sum) of a query head from the four lanes that hold its columns
             l[n] += __shfl_xor_sync(kFull, l[n], 1);
             l[n] += __shfl_xor_sync(kFull, l[n], 2);
-            if (t == 0) { sm.m[warp][8 * n + g] = m[n]; sm.l[warp][8 * n + g] = l[n]; }
+        }
+        if (p.begins() && threadIdx.x == 0)
+            a.shared_by[static_cast<size_t>(p.unit) * a.groups + p.grp] = make_int2(cta, share.owner(p.first + (p.grp + 1) * p.tiles - 1));
+        const bool whole = p.whole();
+        if (turns == 1) {
+            // a lane holds eight neighbouring dims (of each 64) of the heads 2t and 2t + 1
+            if (head < p.un.heads) {
 #pragma unroll
-            for (int hh = 0; hh < kVh; ++hh)
+                for (int n = 0; n < NH; ++n) {
+                    if (t == 0 && 8 * n + g < heads) {
+                        if (!whole) a.part_ml[record(a, cta, p.begins(), head, 8 * n + g)] = make_float2(m[n], l[n]);
+                        else if (SUMS) a.whole_ml[q_row + 8 * n + g] = make_float2(m[n], l[n]);        // (a CTA can have many)
+                    }
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float* p = &sm.o[warp][8 * n + 2 * t + e][64 * hh + 8 * g];
-                    *reinterpret_cast<float4*>(p) = make_float4(o[n][4 * hh][e], o[n][4 * hh][e + 2], o[n][4 * hh + 1][e], o[n][4 * hh + 1][e + 2]);
-                    *reinterpret_cast<float4*>(p + 4) = make_float4(o[n][4 * hh + 2][e], o[n][4 * hh + 2][e + 2], o[n][4 * hh + 3][e], o[n][4 * hh + 3][e + 2]);
+                    for (int e = 0; e < 2; ++e) {
+                        const float ll = __shfl_sync(kFull, l[n], 8 * t + 4 * e);
+                        const int q = 8 * n + 2 * t + e;
+                        if (q >= heads) continue;
+                        if (whole) {
+                            const float r = ll == 0.f ? 0.f : 1.f / ll;     // (nothing seen: zeros)
+                            __nv_bfloat16* to = a.out + (q_row + q) * D + 8 * g;
+#pragma unroll
+                            for (int hh = 0; hh < kVh; ++hh) {
+                                uint32_t w[4];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) w[i] = pack_bf16(o[n][4 * hh + i][e] * r, o[n][4 * hh + i][e + 2] * r);
+                                *reinterpret_cast<uint4*>(to + 64 * hh) = make_uint4(w[0], w[1], w[2], w[3]);
+                            }
+                        } else {
+                            float* to = a.part_o + record(a, cta, p.begins(), head, q) * D + 8 * g;
+#pragma unroll
+                            for (int hh = 0; hh < kVh; ++hh) {
+                                *reinterpret_cast<float4*>(to + 64 * hh) = make_float4(o[n][4 * hh][e], o[n][4 * hh][e + 2], o[n][4 * hh + 1][e], o[n][4 * hh + 1][e + 2]);
+                                *reinterpret_cast<float4*>(to + 64 * hh + 4) = make_float4(o[n][4 * hh + 2][e], o[n][4 * hh + 2][e + 2], o[n][4 * hh + 3][e], o[n][4 * hh + 3][e + 2]);
+                            }
+                        }
+                    }
                 }
-        }
-        __syncthreads();
-        const bool begins = tile0 == 0, whole = begins && tile1 == tiles;
-        if (begins && threadIdx.x == 0) a.shared_by[static_cast<size_t>(unit) * a.groups + grp] = make_int2(cta, owner_of(unit0 + tiles - 1, dl.total, n_cta));
-        for (int e = threadIdx.x; e < un.heads * heads * (D / 4); e += kAttThreads) {
-            const int c4 = e % (D / 4) * 4, hq = e / (D / 4), hd = hq / heads, q = hq - hd * heads;
-            float mm = -INFINITY;
-            for (int w = 0; w < turns; ++w) mm = fmaxf(mm, sm.m[hd + w * a.block][q]);
-            const float ref = reference_of(mm);
-            float ll = 0.f;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = 0; w < turns; ++w) {
-                const int of = hd + w * a.block;
-                const float f = exp2_fast(sm.m[of][q] - ref);
-                const float4 y = *reinterpret_cast<const float4*>(&sm.o[of][q][c4]);
-                ll = fmaf(sm.l[of][q], f, ll);
-                v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
             }
-            const size_t out_row = static_cast<size_t>(un.b) * a.Hq + static_cast<size_t>(un.h0 + hd) * G + g0 + q;
-            const size_t rec = record(a, cta, begins, hd, q);
-            if (whole) {
-                const float r = ll == 0.f ? 0.f : 1.f / ll;     // (nothing seen: zeros)
-                *reinterpret_cast<uint2*>(a.out + out_row * D + c4) = make_uint2(pack_bf16(v.x * r, v.y * r), pack_bf16(v.z * r, v.w * r));
-            } else {
-                *reinterpret_cast<float4*>(a.part_o + rec * D + c4) = v;
+        } else {
+            __syncthreads();                                    // (every ring is idle)
+#pragma unroll
+            for (int n = 0; n < NH; ++n) {
+                if (t == 0) { sm.m[warp][8 * n + g] = m[n]; sm.l[warp][8 * n + g] = l[n]; }
+#pragma unroll
+                for (int hh = 0; hh < kVh; ++hh)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float* to = &sm.o[warp][8 * n + 2 * t + e][64 * hh + 8 * g];
+                        *reinterpret_cast<float4*>(to) = make_float4(o[n][4 * hh][e], o[n][4 * hh][e + 2], o[n][4 * hh + 1][e], o[n][4 * hh + 1][e + 2]);
+                        *reinterpret_cast<float4*>(to + 4) = make_float4(o[n][4 * hh + 2][e], o[n][4 * hh + 2][e + 2], o[n][4 * hh + 3][e], o[n][4 * hh + 3][e + 2]);
+                    }
             }
-            if (c4 == 0) {
-                if (!whole) a.part_ml[rec] = make_float2(mm, ll);
-                else if (SUMS) a.whole_ml[out_row] = make_float2(mm, ll);                 // (a CTA can have many)
+            __syncthreads();
+            const int c4 = threadIdx.x % (D / 4) * 4;
+            for (int hq = threadIdx.x / (D / 4); hq < p.un.heads * heads; hq += kAttThreads / (D / 4)) {
+                const int hd = hq / heads, q = hq - hd * heads;
+                float mm = -INFINITY;
+                for (int w = 0; w < turns; ++w) mm = fmaxf(mm, sm.m[hd + w * a.block][q]);
+                const float ref = reference_of(mm);
+                float ll = 0.f;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int w = 0; w < turns; ++w) {
+                    const int of = hd + w * a.block;
+                    const float f = exp2_fast(sm.m[of][q] - ref);
+                    const float4 y = *reinterpret_cast<const float4*>(&sm.o[of][q][c4]);
+                    ll = fmaf(sm.l[of][q], f, ll);
+                    v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
+                }
+                const size_t out_row = static_cast<size_t>(p.un.b) * a.Hq + static_cast<size_t>(p.un.h0 + hd) * G + p.grp * 8 * NH + q;
+                const size_t rec = record(a, cta, p.begins(), hd, q);
+                if (whole) {
+                    const float r = ll == 0.f ? 0.f : 1.f / ll;
+                    *reinterpret_cast<uint2*>(a.out + out_row * D + c4) = make_uint2(pack_bf16(v.x * r, v.y * r), pack_bf16(v.z * r, v.w * r));
+                } else {
+                    *reinterpret_cast<float4*>(a.part_o + rec * D + c4) = v;
+                }
+                if (c4 == 0) {
+                    if (!whole) a.part_ml[rec] = make_float2(mm, ll);
+                    else if (SUMS) a.whole_ml[out_row] = make_float2(mm, ll);
+                }
             }
+            __syncthreads();                                    // (read: the rings may be filled again)
+            if (more) begin_part(next);
         }
-        __syncthreads();                                        // (read: the rings may be filled again)
-        x = unit0 + tile1;
-        if (grp + 1 == a.groups && tile1 == tiles) {            // on to the next unit that has rows
-            first = x;
-            do ++unit; while (unit < units && tiles_of(a, unit) == 0);
-        }
+        if (!more) return;
+        p = next;
     }
 }
 
@@ -594,6 +674,9 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     p.blocks = (Hkv + kAttWarps - 1) / kAttWarps;               // as many heads a CTA as it has warps, and blocks of heads alike
     p.block = (Hkv + p.blocks - 1) / p.blocks;
     p.tile = kAttWarps / p.block * kAttStep;
+    p.tile_shift = -1;
+    for (int s = 0; s < 31; ++s)
+        if (p.tile == 1 << s) p.tile_shift = s;
     const long long tiles = static_cast<long long>(B) * p.blocks * p.groups * ((cap + p.tile - 1) / p.tile);
     p.max_ctas = static_cast<int>(tiles < kAttMaxCtas ? tiles : kAttMaxCtas);
     const size_t heads = static_cast<size_t>(p.max_ctas) * 2 * p.block * p.group;
@@ -614,6 +697,7 @@ cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d,
     a.blocks = plan.blocks;
     a.block = plan.block;
     a.tile = plan.tile;
+    a.tile_shift = plan.tile_shift;
     a.part_ml = reinterpret_cast<float2*>(scratch);
     a.part_o = reinterpret_cast<float*>(scratch + plan.off_o);
     a.whole_ml = reinterpret_cast<float2*>(scratch + plan.off_whole);

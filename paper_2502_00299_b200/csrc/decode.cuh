@@ -12,7 +12,7 @@ namespace chunkkv {
 
 // Row `row` (below cap) of the sequence with table `table` as a row of the cache, page * page_size + slot; -1: its page is outside the cache.
 __device__ __forceinline__ int paged_row(const PagedCache& c, const int32_t* table, int row) {
-    const int p = row / c.page_size;
+    const int p = static_cast<int>((__umulhi(c.magic, static_cast<uint32_t>(row)) + static_cast<uint32_t>(row)) >> c.shift);
     const int page = __ldg(table + p);
     return static_cast<unsigned>(page) < static_cast<unsigned>(c.num_pages) ? page * c.page_size + (row - p * c.page_size) : -1;
 }

@@ -12,7 +12,15 @@ struct PagedCache {
     const int32_t* tables;      // [B, max_pages]
     int max_pages, page_size, num_pages;
     int cap;                    // max_pages * page_size: rows that a sequence can have
+    uint32_t magic;             // row / page_size = (mulhi(magic, row) + row) >> shift for rows below 2^31
+    int shift;
 };
+inline PagedCache paged_cache(const int32_t* tables, int max_pages, int page_size, int num_pages) {
+    int shift = 0;
+    while ((1LL << shift) < page_size) ++shift;
+    const uint64_t over = (1ULL << shift) - static_cast<uint64_t>(page_size);
+    return {tables, max_pages, page_size, num_pages, max_pages * page_size, static_cast<uint32_t>((over << 32) / page_size + 1), shift};
+}
 
 // Queries and keys normalised and rotated (rotate.cu): into out_q / out_k (token and head strides in elements), or, with a cache, keys and values
 // into it.
@@ -46,14 +54,14 @@ struct AttendArgs {
     __nv_bfloat16* out;
     int groups, group;                        // groups of query heads of a KV head, and heads of one; these and what follows are set by the launch
     int blocks, block;                        // blocks of KV heads that a CTA takes together, and heads of one
-    int tile;                                 // rows that are dealt together
+    int tile, tile_shift;                     // rows that are dealt together; log2 where it is a power of two, else -1
     float2 *part_ml, *whole_ml;
     int2* shared_by;                          // first and last CTA with rows of a unit
     float *part_o, *logits;
     long long logit_stride;
 };
 struct AttendPlan {
-    int nh, groups, group, blocks, block, tile, max_ctas;
+    int nh, groups, group, blocks, block, tile, tile_shift, max_ctas;
     long long logit_stride;
     size_t off_o, off_whole, off_shared, off_logits, bytes;
 };

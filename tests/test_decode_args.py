@@ -49,8 +49,8 @@ def test_sizes_are_refused():
         assert _rotate(**bad) == SHAPE, bad
     for bad in (dict(row=1535), dict(n_pos=0), dict(eps=-1.0), dict(eps=float("nan"))):
         assert _append(**bad) == SHAPE, bad
-    assert _attend(B=1, Hkv=8, Hq=8, per=1 << 29, page=1, weights=P) == NOWS
-    assert _attend(B=1 << 12, Hkv=8, Hq=8, per=1 << 29, page=1, weights=P) == SHAPE
+    assert _attend(B=1, Hkv=8, Hq=8, per=1 << 29, page=1) == NOWS
+    assert _attend(B=8, Hkv=8, Hq=8, per=1 << 29, page=1) == SHAPE      # 2^31 steps of 16 rows and heads
 
 
 def test_missing_and_unaligned_pointers_are_refused():
