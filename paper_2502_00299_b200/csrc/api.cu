@@ -832,7 +832,7 @@ int chunkkv_attend_paged(const void* q, const int32_t* block_tables, int max_pag
     if (st != CHUNKKV_OK) return st;
     const int cap = max_pages * page_size;
     // tiles of at least 16 rows are counted, and CTAs of a launch
-    if (static_cast<long long>(B) * Hq * (cap / 16 + 1) >= (1LL << 31)) return CHUNKKV_EINVAL_SHAPE;
+    if (static_cast<long long>(B) * Hq * (cap / 16 + 8) >= (1LL << 31)) return CHUNKKV_EINVAL_SHAPE;
     if (B == 0) return CHUNKKV_OK;
     if (q == nullptr || block_tables == nullptr || lengths == nullptr || cache_K == nullptr || cache_V == nullptr || out == nullptr) return CHUNKKV_EINVAL_NULL;
     if (!aligned16(q) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) || !aligned4(weights) || !aligned16(out))
@@ -854,7 +854,8 @@ int chunkkv_attend_paged(const void* q, const int32_t* block_tables, int max_pag
     a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(d)));
     a.weights = weights;
     a.out = static_cast<__nv_bfloat16*>(out);
-    const cudaError_t e = launch_attend(a, plan, d, static_cast<char*>(scratch), ctx->num_sms, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_attend(a, plan, d, static_cast<char*>(scratch), ctx->num_sms, static_cast<int>(ctx - g_ctx),
+                                        static_cast<cudaStream_t>(stream));
     return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
 }
 

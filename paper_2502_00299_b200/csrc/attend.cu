@@ -25,9 +25,9 @@ constexpr int kAttWarps = 8;
 constexpr int kAttThreads = 32 * kAttWarps;
 constexpr int kAttStep = 16;                          // rows of a warp's step
 constexpr int kRingBytes = 24 * 1024;                 // of a warp
-constexpr int kJoinRows = 512;                        // rows of the sums that a CTA of the join takes
+constexpr int kJoinRows = 256;                        // rows of the sums that a CTA of the join takes
 constexpr int kJoinThreads = 128;
-constexpr int kJoinFew = 256;                         // query heads of a call that are joined by a CTA for every 32 dims
+constexpr int kJoinHeads = 8;                         // query heads whose weights are added together
 static_assert(kAttMaxCtas % 32 == 0, "records are looked at a warp at a time");
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -140,15 +140,23 @@ __device__ __forceinline__ size_t record(const AttendArgs& a, int cta, bool begi
     return (static_cast<size_t>(cta * 2 + (begins ? 1 : 0)) * a.block + h) * a.group + q;
 }
 
+// What a warp leaves for the one that joins its head's warps: every lane's (max, sum) and O.
+template <int D, int NH>
+struct Left {
+    float4 o[NH * D / 16][32];
+    float2 ml[NH][32];
+};
 template <int D, int NH>
 struct AttSmem {
-    static constexpr int kPad = D + 4;
-    union {
-        alignas(128) unsigned char ring[kAttWarps][kRingBytes];
-        float o[kAttWarps][8 * NH][kPad];       // where several warps work on a head (the rings are idle then)
-    };
-    float m[kAttWarps][8 * NH], l[kAttWarps][8 * NH];
+    // apart from the rings where there is room (a warp's ring can then be filled for the next part while others join), else in the rings' place
+    static constexpr bool kApart = kAttWarps * kRingBytes + (kAttWarps - 1) * sizeof(Left<D, NH>) + 1024 <= 227 * 1024;
+    alignas(128) unsigned char ring[kAttWarps][kRingBytes];
+    alignas(16) unsigned char left_[kApart ? (kAttWarps - 1) * sizeof(Left<D, NH>) : 16];
     DealSmem deal;
+    __device__ __forceinline__ Left<D, NH>& left(int warp, int block) {     // of a warp that is not the first of its head
+        if constexpr (kApart) return reinterpret_cast<Left<D, NH>*>(left_)[warp - block];
+        else return *reinterpret_cast<Left<D, NH>*>(ring[warp]);
+    }
 };
 
 // D: head dim; NH: query heads of a group in eights.
@@ -370,127 +378,122 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
             if (more) next = part_at(x, unit, first);
         }
         __syncwarp();                                           // (the last step has been read)
-        if (more && turns == 1) begin_part(next);
+        constexpr bool kApart = AttSmem<D, NH>::kApart;
+        if (more && (kApart || turns == 1)) begin_part(next);
 
+        if (turns > 1) {                                        // the warps of a head, joined by its first one in their order
+            __syncthreads();                                    // (what was left before has been read)
+            if (turn > 0 && turn < turns) {
+                Left<D, NH>& mine = sm.left(warp, a.block);
 #pragma unroll
-        for (int n = 0; n < NH; ++n) {                          // (max, sum) of a query head from the four lanes that hold its columns
+                for (int n = 0; n < NH; ++n) {
+                    mine.ml[n][lane] = make_float2(m[n], l[n]);
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) mine.o[n * (D / 16) + i][lane] = make_float4(o[n][i][0], o[n][i][1], o[n][i][2], o[n][i][3]);
+                }
+            }
+            __syncthreads();
+            if (turn == 0) {
+                for (int w = 1; w < turns; ++w) {
+                    const Left<D, NH>& other = sm.left(warp + w * a.block, a.block);
+#pragma unroll
+                    for (int n = 0; n < NH; ++n) {
+                        const float2 s = other.ml[n][lane];
+                        const float m_new = fmaxf(m[n], s.x), ref = reference_of(m_new);
+                        const float own = exp2_fast(m[n] - ref), its = exp2_fast(s.x - ref);
+                        m[n] = m_new;
+                        l[n] = l[n] * own + s.y * its;
+                        const float a0 = __shfl_sync(kFull, own, 8 * t), a1 = __shfl_sync(kFull, own, 8 * t + 4);
+                        const float b0 = __shfl_sync(kFull, its, 8 * t), b1 = __shfl_sync(kFull, its, 8 * t + 4);
+#pragma unroll
+                        for (int i = 0; i < D / 16; ++i) {
+                            const float4 v = other.o[n * (D / 16) + i][lane];
+                            o[n][i][0] = o[n][i][0] * a0 + v.x * b0;
+                            o[n][i][1] = o[n][i][1] * a1 + v.y * b1;
+                            o[n][i][2] = o[n][i][2] * a0 + v.z * b0;
+                            o[n][i][3] = o[n][i][3] * a1 + v.w * b1;
+                        }
+                    }
+                }
+            }
+            if (!kApart) {
+                __syncthreads();
+                if (more) begin_part(next);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NH; ++n) {                          // the sum of a query head from the four lanes that hold its columns
             l[n] += __shfl_xor_sync(kFull, l[n], 1);
             l[n] += __shfl_xor_sync(kFull, l[n], 2);
         }
         if (p.begins() && threadIdx.x == 0)
             a.shared_by[static_cast<size_t>(p.unit) * a.groups + p.grp] = make_int2(cta, share.owner(p.first + (p.grp + 1) * p.tiles - 1));
         const bool whole = p.whole();
-        if (turns == 1) {
-            // a lane holds eight neighbouring dims (of each 64) of the heads 2t and 2t + 1
-            if (head < p.un.heads) {
+        if (turn == 0 && head < p.un.heads) {                   // a lane holds eight neighbouring dims (of each 64) of the heads 2t and 2t + 1
 #pragma unroll
-                for (int n = 0; n < NH; ++n) {
-                    if (t == 0 && 8 * n + g < heads) {
-                        if (!whole) a.part_ml[record(a, cta, p.begins(), head, 8 * n + g)] = make_float2(m[n], l[n]);
-                        else if (SUMS) a.whole_ml[q_row + 8 * n + g] = make_float2(m[n], l[n]);        // (a CTA can have many)
-                    }
+            for (int n = 0; n < NH; ++n) {
+                if (t == 0 && 8 * n + g < heads) {
+                    if (!whole) a.part_ml[record(a, cta, p.begins(), head, 8 * n + g)] = make_float2(m[n], l[n]);
+                    else if (SUMS) a.whole_ml[q_row + 8 * n + g] = make_float2(m[n], l[n]);        // (a CTA can have many)
+                }
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float ll = __shfl_sync(kFull, l[n], 8 * t + 4 * e);
-                        const int q = 8 * n + 2 * t + e;
-                        if (q >= heads) continue;
-                        if (whole) {
-                            const float r = ll == 0.f ? 0.f : 1.f / ll;     // (nothing seen: zeros)
-                            __nv_bfloat16* to = a.out + (q_row + q) * D + 8 * g;
+                for (int e = 0; e < 2; ++e) {
+                    const float ll = __shfl_sync(kFull, l[n], 8 * t + 4 * e);
+                    const int q = 8 * n + 2 * t + e;
+                    if (q >= heads) continue;
+                    if (whole) {
+                        const float r = ll == 0.f ? 0.f : 1.f / ll;     // (nothing seen: zeros)
+                        __nv_bfloat16* to = a.out + (q_row + q) * D + 8 * g;
 #pragma unroll
-                            for (int hh = 0; hh < kVh; ++hh) {
-                                uint32_t w[4];
+                        for (int hh = 0; hh < kVh; ++hh) {
+                            uint32_t w[4];
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) w[i] = pack_bf16(o[n][4 * hh + i][e] * r, o[n][4 * hh + i][e + 2] * r);
-                                *reinterpret_cast<uint4*>(to + 64 * hh) = make_uint4(w[0], w[1], w[2], w[3]);
-                            }
-                        } else {
-                            float* to = a.part_o + record(a, cta, p.begins(), head, q) * D + 8 * g;
+                            for (int i = 0; i < 4; ++i) w[i] = pack_bf16(o[n][4 * hh + i][e] * r, o[n][4 * hh + i][e + 2] * r);
+                            *reinterpret_cast<uint4*>(to + 64 * hh) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    } else {
+                        float* to = a.part_o + record(a, cta, p.begins(), head, q) * D + 8 * g;
 #pragma unroll
-                            for (int hh = 0; hh < kVh; ++hh) {
-                                *reinterpret_cast<float4*>(to + 64 * hh) = make_float4(o[n][4 * hh][e], o[n][4 * hh][e + 2], o[n][4 * hh + 1][e], o[n][4 * hh + 1][e + 2]);
-                                *reinterpret_cast<float4*>(to + 64 * hh + 4) = make_float4(o[n][4 * hh + 2][e], o[n][4 * hh + 2][e + 2], o[n][4 * hh + 3][e], o[n][4 * hh + 3][e + 2]);
-                            }
+                        for (int hh = 0; hh < kVh; ++hh) {
+                            *reinterpret_cast<float4*>(to + 64 * hh) = make_float4(o[n][4 * hh][e], o[n][4 * hh][e + 2], o[n][4 * hh + 1][e], o[n][4 * hh + 1][e + 2]);
+                            *reinterpret_cast<float4*>(to + 64 * hh + 4) = make_float4(o[n][4 * hh + 2][e], o[n][4 * hh + 2][e + 2], o[n][4 * hh + 3][e], o[n][4 * hh + 3][e + 2]);
                         }
                     }
                 }
             }
-        } else {
-            __syncthreads();                                    // (every ring is idle)
-#pragma unroll
-            for (int n = 0; n < NH; ++n) {
-                if (t == 0) { sm.m[warp][8 * n + g] = m[n]; sm.l[warp][8 * n + g] = l[n]; }
-#pragma unroll
-                for (int hh = 0; hh < kVh; ++hh)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float* to = &sm.o[warp][8 * n + 2 * t + e][64 * hh + 8 * g];
-                        *reinterpret_cast<float4*>(to) = make_float4(o[n][4 * hh][e], o[n][4 * hh][e + 2], o[n][4 * hh + 1][e], o[n][4 * hh + 1][e + 2]);
-                        *reinterpret_cast<float4*>(to + 4) = make_float4(o[n][4 * hh + 2][e], o[n][4 * hh + 2][e + 2], o[n][4 * hh + 3][e], o[n][4 * hh + 3][e + 2]);
-                    }
-            }
-            __syncthreads();
-            const int c4 = threadIdx.x % (D / 4) * 4;
-            for (int hq = threadIdx.x / (D / 4); hq < p.un.heads * heads; hq += kAttThreads / (D / 4)) {
-                const int hd = hq / heads, q = hq - hd * heads;
-                float mm = -INFINITY;
-                for (int w = 0; w < turns; ++w) mm = fmaxf(mm, sm.m[hd + w * a.block][q]);
-                const float ref = reference_of(mm);
-                float ll = 0.f;
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-                for (int w = 0; w < turns; ++w) {
-                    const int of = hd + w * a.block;
-                    const float f = exp2_fast(sm.m[of][q] - ref);
-                    const float4 y = *reinterpret_cast<const float4*>(&sm.o[of][q][c4]);
-                    ll = fmaf(sm.l[of][q], f, ll);
-                    v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
-                }
-                const size_t out_row = static_cast<size_t>(p.un.b) * a.Hq + static_cast<size_t>(p.un.h0 + hd) * G + p.grp * 8 * NH + q;
-                const size_t rec = record(a, cta, p.begins(), hd, q);
-                if (whole) {
-                    const float r = ll == 0.f ? 0.f : 1.f / ll;
-                    *reinterpret_cast<uint2*>(a.out + out_row * D + c4) = make_uint2(pack_bf16(v.x * r, v.y * r), pack_bf16(v.z * r, v.w * r));
-                } else {
-                    *reinterpret_cast<float4*>(a.part_o + rec * D + c4) = v;
-                }
-                if (c4 == 0) {
-                    if (!whole) a.part_ml[rec] = make_float2(mm, ll);
-                    else if (SUMS) a.whole_ml[out_row] = make_float2(mm, ll);
-                }
-            }
-            __syncthreads();                                    // (read: the rings may be filled again)
-            if (more) begin_part(next);
         }
         if (!more) return;
         p = next;
     }
 }
 
-// The join. A query head is joined by a team: with FEW query heads a CTA for every 32 dims of it, else a warp. The other CTAs add the rows' weights to
-// the sums, kJoinRows rows of a KV head each.
-template <int D, bool FEW>
+// The join. A query head's records are joined by a team: a warp where few CTAs share a unit, else a CTA, or, of many CTAs, one for every 32 dims.
+// The other CTAs add the rows' weights to the sums, kJoinRows rows of a KV head each.
+enum TeamOf { kTeamWarp, kTeamCta, kTeamCtas };
+template <int D, TeamOf TEAM>
 struct Team {
-    static constexpr int kThreads = FEW ? kJoinThreads : 32;
-    static constexpr int kDims = FEW ? 32 : D;                  // of a team
+    static constexpr bool kCta = TEAM != kTeamWarp;
+    static constexpr int kThreads = kCta ? kJoinThreads : 32;
+    static constexpr int kDims = TEAM == kTeamCtas ? 32 : D;    // of a team
     static constexpr int kParts = kThreads / (kDims / 4);       // groups of threads that take records in turn, 16 bytes of values a thread
     static constexpr int kTeams = kJoinThreads / kThreads;      // in a CTA
-    static constexpr int kAhead = FEW ? 10 : 4;                 // values asked for before the factors that they wait for
+    static constexpr int kAhead = TEAM == kTeamCtas ? 10 : (TEAM == kTeamCta ? 8 : 4);     // values asked for before the factors that they wait for
 };
-template <int D, bool FEW>
+template <int D, TeamOf TEAM>
 struct JoinSmem {
     alignas(16) float o[kJoinThreads][4];
-    float factor[Team<D, FEW>::kTeams][kAttMaxCtas];
+    float factor[Team<D, TEAM>::kTeams][kAttMaxCtas];
     float top[kJoinThreads / 32], sum[kJoinThreads / 32];
-    float2 ml[kJoinThreads];          // (reference, factor) of query heads
+    float2 ml[kJoinHeads];            // (reference, factor) of query heads
 };
 
-template <int D, int NH, bool SUMS, bool FEW>
+template <int D, int NH, bool SUMS, TeamOf TEAM>
 __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs a, int join_ctas, int row_blocks) {
-    using T = Team<D, FEW>;
+    using T = Team<D, TEAM>;
     constexpr unsigned kFull = 0xffffffffu;
-    __shared__ JoinSmem<D, FEW> sm;
+    __shared__ JoinSmem<D, TEAM> sm;
     const int G = a.Hq / a.Hkv, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    auto meet = [] { if constexpr (FEW) __syncthreads(); else __syncwarp(); };
+    auto meet = [] { if constexpr (T::kCta) __syncthreads(); else __syncwarp(); };
     // (the kernel ahead sets this one up after its own wait: lengths, which were there before it, may be read)
     if (static_cast<int>(blockIdx.x) < join_ctas) {
         const int team = threadIdx.x / T::kThreads, id = threadIdx.x % T::kThreads;
@@ -530,7 +533,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
         }
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(kFull, mm, off));
-        if constexpr (FEW) {
+        if constexpr (T::kCta) {
             if (lane == 0) sm.top[warp] = mm;
             __syncthreads();
             mm = fmaxf(fmaxf(sm.top[0], sm.top[1]), fmaxf(sm.top[2], sm.top[3]));
@@ -545,11 +548,11 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
         }
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(kFull, ll, off);
-        if constexpr (FEW) {
+        if constexpr (T::kCta) {
             if (lane == 0) sm.sum[warp] = ll;
         }
         meet();
-        if constexpr (FEW) ll = (sm.sum[0] + sm.sum[1]) + (sm.sum[2] + sm.sum[3]);
+        if constexpr (T::kCta) ll = (sm.sum[0] + sm.sum[1]) + (sm.sum[2] + sm.sum[3]);
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         auto add = [&](const float4& z, float f) { v.x = fmaf(z.x, f, v.x); v.y = fmaf(z.y, f, v.y); v.z = fmaf(z.z, f, v.z); v.w = fmaf(z.w, f, v.w); };
 #pragma unroll
@@ -580,65 +583,88 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
         asm volatile("griddepcontrol.wait;" ::: "memory");
         if (r0 >= r1) return;
         const size_t q_row = static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G;
-        float acc[kJoinRows / kJoinThreads];
+        constexpr int kOwnRows = kJoinRows / kJoinThreads;
+        float acc[kOwnRows];
 #pragma unroll
-        for (int i = 0; i < kJoinRows / kJoinThreads; ++i) acc[i] = 0.f;
-        for (int q0 = 0; q0 < G; q0 += kJoinThreads) {          // (more query heads than fit at once: in turns)
-            const int nq = min(kJoinThreads, G - q0);
+        for (int i = 0; i < kOwnRows; ++i) acc[i] = 0.f;
+        for (int q0 = 0; q0 < G; q0 += kJoinHeads) {
+            float lg[kJoinHeads][kOwnRows];                     // (asked for before the statistics that they wait for)
+#pragma unroll
+            for (int q = 0; q < kJoinHeads; ++q)
+#pragma unroll
+                for (int i = 0; i < kOwnRows; ++i) {
+                    const int r = r0 + i * kJoinThreads + threadIdx.x;
+                    lg[q][i] = q0 + q < G && r < r1 ? a.logits[(q_row + q0 + q) * a.logit_stride + r] : -INFINITY;
+                }
             __syncthreads();
-            for (int q = warp; q < nq; q += kJoinThreads / 32) {
-                const int grp = (q0 + q) / (8 * NH), qg = (q0 + q) - grp * 8 * NH;
-                const int2 by = a.shared_by[static_cast<size_t>(unit) * a.groups + grp];
-                if (by.x == by.y) {
-                    const float2 s = a.whole_ml[q_row + q0 + q];
-                    if (lane == 0) sm.ml[q] = make_float2(reference_of(s.x), s.y == 0.f ? 0.f : 1.f / s.y);
-                    continue;
+#pragma unroll
+            for (int qw = 0; qw < kJoinHeads; qw += kJoinThreads / 32) {
+                const int q = q0 + qw + warp;
+                float2 f = make_float2(0.f, 0.f);
+                if (q < G) {
+                    const int grp = q / (8 * NH), qg = q - grp * 8 * NH;
+                    const int2 by = a.shared_by[static_cast<size_t>(unit) * a.groups + grp];
+                    constexpr int kOwn = kAttMaxCtas / 32;
+                    float2 s[kOwn];
+                    float mm = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < kOwn; ++i) {
+                        const int c = by.x + lane + 32 * i;
+                        s[i] = c > by.y ? make_float2(-INFINITY, 0.f) : by.x == by.y ? a.whole_ml[q_row + q] : a.part_ml[record(a, c, c == by.x, head, qg)];
+                        mm = fmaxf(mm, s[i].x);
+                    }
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(kFull, mm, off));
+                    const float ref = reference_of(mm);
+                    float ll = 0.f;
+#pragma unroll
+                    for (int i = 0; i < kOwn; ++i) ll += by.x + lane + 32 * i <= by.y ? s[i].y * exp2_fast(s[i].x - ref) : 0.f;
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(kFull, ll, off);
+                    f = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
                 }
-                constexpr int kOwn = kAttMaxCtas / 32;
-                float2 s[kOwn];
-                float mm = -INFINITY;
-#pragma unroll
-                for (int i = 0; i < kOwn; ++i) {
-                    const int c = by.x + lane + 32 * i;
-                    s[i] = c <= by.y ? a.part_ml[record(a, c, c == by.x, head, qg)] : make_float2(-INFINITY, 0.f);
-                    mm = fmaxf(mm, s[i].x);
-                }
-#pragma unroll
-                for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(kFull, mm, off));
-                const float ref = reference_of(mm);
-                float ll = 0.f;
-#pragma unroll
-                for (int i = 0; i < kOwn; ++i) ll += by.x + lane + 32 * i <= by.y ? s[i].y * exp2_fast(s[i].x - ref) : 0.f;
-#pragma unroll
-                for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(kFull, ll, off);
-                if (lane == 0) sm.ml[q] = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
+                if (lane == 0) sm.ml[qw + warp] = f;
             }
             __syncthreads();
-            for (int q = 0; q < nq; ++q) {
-                const float2 s = sm.ml[q];
-                const float* lg = a.logits + (q_row + q0 + q) * a.logit_stride;
 #pragma unroll
-                for (int i = 0; i < kJoinRows / kJoinThreads; ++i) {
-                    const int r = r0 + i * kJoinThreads + threadIdx.x;
-                    if (r < r1) acc[i] += exp2_fast(lg[r] - s.x) * s.y;
+            for (int q = 0; q < kJoinHeads; ++q) {
+                const float2 f = sm.ml[q];
+                if (q0 + q < G) {
+#pragma unroll
+                    for (int i = 0; i < kOwnRows; ++i) acc[i] += exp2_fast(lg[q][i] - f.x) * f.y;
                 }
             }
         }
         float* w = a.weights + static_cast<size_t>(bh) * a.cache.cap;
 #pragma unroll
-        for (int i = 0; i < kJoinRows / kJoinThreads; ++i) {
+        for (int i = 0; i < kOwnRows; ++i) {
             const int r = r0 + i * kJoinThreads + threadIdx.x;
             if (r < r1) w[r] += acc[i];
         }
     }
 }
 
+template <int D, int NH, bool SUMS, TeamOf TEAM>
+cudaError_t launch_join(const AttendArgs& a, cudaLaunchConfig_t cfg, int row_blocks) {
+    using T = Team<D, TEAM>;
+    const int join_ctas = (a.B * a.Hq * (D / T::kDims) + T::kTeams - 1) / T::kTeams;
+    cfg.gridDim = dim3(static_cast<unsigned>(join_ctas + a.B * a.Hkv * row_blocks));
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NH, SUMS, TEAM>, a, join_ctas, row_blocks);
+}
+
 template <int D, int NH, bool SUMS>
-cudaError_t launch_attend_t(const AttendArgs& a, int n_cta, cudaStream_t stream) {
+cudaError_t launch_attend_t(const AttendArgs& a, int n_cta, int device, cudaStream_t stream) {
     constexpr int smem = sizeof(AttSmem<D, NH>);
+    static_assert(smem <= 227 * 1024, "an SM's shared memory");
     auto kernel = attend_kernel<D, NH, SUMS>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
+    static uint64_t set_on = 0;                                 // devices; the caller holds the library's lock
+    if ((set_on >> device & 1u) == 0) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        set_on |= 1ull << device;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(n_cta);
     cfg.blockDim = dim3(kAttThreads);
@@ -649,16 +675,14 @@ cudaError_t launch_attend_t(const AttendArgs& a, int n_cta, cudaStream_t stream)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, a);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
     if (e != cudaSuccess) return e;
     const int row_blocks = SUMS ? (a.cache.cap + kJoinRows - 1) / kJoinRows : 0;
-    const bool few = a.B * a.Hq <= kJoinFew;
-    const int join_ctas = few ? a.B * a.Hq * (D / Team<D, true>::kDims) : (a.B * a.Hq + Team<D, false>::kTeams - 1) / Team<D, false>::kTeams;
-    cfg.gridDim = dim3(static_cast<unsigned>(join_ctas + a.B * a.Hkv * row_blocks));
-    cfg.blockDim = dim3(kJoinThreads);
-    cfg.dynamicSmemBytes = 0;
-    return few ? cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NH, SUMS, true>, a, join_ctas, row_blocks)
-               : cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NH, SUMS, false>, a, join_ctas, row_blocks);
+    // records of a unit, where lengths are alike: up to 4 a warp has in flight at once, up to 32 a CTA
+    const int records = n_cta / (a.B * a.blocks * a.groups) + 2;
+    if (records <= 4) return launch_join<D, NH, SUMS, kTeamWarp>(a, cfg, row_blocks);
+    if (records <= 36) return launch_join<D, NH, SUMS, kTeamCta>(a, cfg, row_blocks);
+    return launch_join<D, NH, SUMS, kTeamCtas>(a, cfg, row_blocks);
 }
 
 }  // namespace
@@ -689,7 +713,7 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     return p;
 }
 
-cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d, char* scratch, int num_sms, cudaStream_t stream) {
+cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d, char* scratch, int num_sms, int device, cudaStream_t stream) {
     if (args.B <= 0) return cudaSuccess;
     AttendArgs a = args;
     a.groups = plan.groups;
@@ -706,7 +730,7 @@ cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d,
     a.logit_stride = plan.logit_stride;
     const int n = num_sms < plan.max_ctas ? num_sms : plan.max_ctas;
     const bool sums = a.weights != nullptr;
-#define CKV_ATTEND(D, NH) (sums ? launch_attend_t<D, NH, true>(a, n, stream) : launch_attend_t<D, NH, false>(a, n, stream))
+#define CKV_ATTEND(D, NH) (sums ? launch_attend_t<D, NH, true>(a, n, device, stream) : launch_attend_t<D, NH, false>(a, n, device, stream))
     if (d == 128) return plan.nh == 1 ? CKV_ATTEND(128, 1) : CKV_ATTEND(128, 2);
     return plan.nh == 1 ? CKV_ATTEND(64, 1) : CKV_ATTEND(64, 2);
 #undef CKV_ATTEND

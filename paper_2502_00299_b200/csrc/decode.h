@@ -66,7 +66,7 @@ struct AttendPlan {
     size_t off_o, off_whole, off_shared, off_logits, bytes;
 };
 AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums);
-cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d, char* scratch, int num_sms, cudaStream_t stream);
+cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d, char* scratch, int num_sms, int device, cudaStream_t stream);
 
 // Eviction from a paged cache by sums of attention (evict.cu).
 struct EvictArgs {
