@@ -18,5 +18,6 @@ __all__ = list(_EXPORTS)
 def __getattr__(name):
     if name in _EXPORTS:
         from . import binding
-        return getattr(binding, name)
+        globals()[name] = value = getattr(binding, name)         # (found here from now on: a look-up less a call)
+        return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -13,8 +13,11 @@ namespace chunkkv {
 
 namespace {
 
-constexpr int kRotThreads = 256;
-constexpr int kRotAhead = 4;        // rows a lane has in flight
+// 28 warps an SM with two rows of every lane in flight: 32768 tokens of 40 heads 110 us; 24 warps 115, 32 warps (spills) 112, 16 warps with four
+// rows 121; CTAs of 256 threads, whose last wave is coarser, 114 to 117.
+constexpr int kRotThreads = 128;
+constexpr int kRotCtas = 7;         // of an SM
+constexpr int kRotAhead = 2;        // rows a lane has in flight
 
 template <int D>
 struct Rot {
@@ -22,48 +25,44 @@ struct Rot {
     static constexpr int kRows = 32 / kLanes;       // rows of a warp's step
 };
 
-__device__ __forceinline__ void unpack8(const uint4& v, float* o) {
-    const float2 a = bf16_pair(v.x), b = bf16_pair(v.y), c = bf16_pair(v.z), d = bf16_pair(v.w);
-    o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y; o[4] = c.x; o[5] = c.y; o[6] = d.x; o[7] = d.y;
-}
-__device__ __forceinline__ uint4 pack8(const float* o) {
-    return make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
-}
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// One row: both halves of this lane's elements, normalised and turned.
+// One row: both halves of this lane's elements, normalised and turned, a pair of neighbours at a time (few values are live beside the rows in flight).
 template <int D>
 __device__ __forceinline__ void turn(uint4& lo, uint4& hi, bool norm, float eps, const uint4& gain_lo, const uint4& gain_hi, const float* co,
                                      const float* si) {
-    float a[8], b[8];
-    unpack8(lo, a);
-    unpack8(hi, b);
+    float r = 1.f;
     if (norm) {
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(a[i], a[i], fmaf(b[i], b[i], sum));
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = bf16_pair(word(lo, i)), b = bf16_pair(word(hi, i));
+            sum = fmaf(a.x, a.x, fmaf(a.y, a.y, fmaf(b.x, b.x, fmaf(b.y, b.y, sum))));
+        }
 #pragma unroll
         for (int off = 1; off < Rot<D>::kLanes; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-        const float r = rsqrtf(sum * (1.f / D) + eps);
-        float ga[8], gb[8];
-        unpack8(gain_lo, ga);
-        unpack8(gain_hi, gb);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) { a[i] *= r * ga[i]; b[i] *= r * gb[i]; }
+        r = rsqrtf(sum * (1.f / D) + eps);
     }
-    float x[8], y[8];
+    uint32_t x[4], y[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x[i] = a[i] * co[i] - b[i] * si[i];
-        y[i] = b[i] * co[i] + a[i] * si[i];
+    for (int i = 0; i < 4; ++i) {
+        float2 a = bf16_pair(word(lo, i)), b = bf16_pair(word(hi, i));
+        if (norm) {
+            const float2 ga = bf16_pair(word(gain_lo, i)), gb = bf16_pair(word(gain_hi, i));
+            a.x *= r * ga.x; a.y *= r * ga.y; b.x *= r * gb.x; b.y *= r * gb.y;
+        }
+        const float c0 = co[2 * i], c1 = co[2 * i + 1], s0 = si[2 * i], s1 = si[2 * i + 1];
+        x[i] = pack_bf16(a.x * c0 - b.x * s0, a.y * c1 - b.y * s1);
+        y[i] = pack_bf16(b.x * c0 + a.x * s0, b.y * c1 + a.y * s1);
     }
-    lo = pack8(x);
-    hi = pack8(y);
+    lo = make_uint4(x[0], x[1], x[2], x[3]);
+    hi = make_uint4(y[0], y[1], y[2], y[3]);
 }
 
 // Work item: `steps` steps of kRows heads of one token, out of ceil(Hq / kRows) steps of queries, then as many as the KV heads take of
 // keys and, with a cache, of values.
 template <int D, bool CACHE>
-__global__ void __launch_bounds__(kRotThreads) rotate_kernel(const RotateArgs a) {
+__global__ void __launch_bounds__(kRotThreads, kRotCtas) rotate_kernel(const RotateArgs a) {
     constexpr int kL = Rot<D>::kLanes, kR = Rot<D>::kRows;
     begin_dependent();
     const int lane = threadIdx.x & 31, l = lane & (kL - 1), slot = lane / kL;
