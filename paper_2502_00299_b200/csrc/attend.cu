@@ -17,6 +17,10 @@
 // captured ones, have nothing in common.
 #include "decode.cuh"
 
+#include <cooperative_groups.h>
+
+namespace cg = cooperative_groups;
+
 namespace chunkkv {
 
 namespace {
@@ -27,6 +31,8 @@ constexpr int kAttStep = 16;                          // rows of a warp's step
 constexpr int kRingBytes = 24 * 1024;                 // of a warp
 constexpr int kJoinRows = 256;                        // rows of the sums that a CTA of the join takes
 constexpr int kJoinThreads = 128;
+constexpr int kSmallSmem = 113 * 1024;                // shared memory of a CTA of the form for short caches, two an SM
+constexpr int kSmallRows = 512;                       // rows of a CTA of it, at most
 constexpr int kJoinHeads = 8;                         // query heads whose weights are added together
 static_assert(kAttMaxCtas % 32 == 0, "records are looked at a warp at a time");
 
@@ -140,121 +146,75 @@ __device__ __forceinline__ size_t record(const AttendArgs& a, int cta, bool begi
     return (static_cast<size_t>(cta * 2 + (begins ? 1 : 0)) * a.block + h) * a.group + q;
 }
 
-// What a warp leaves for the one that joins its head's warps: every lane's (max, sum) and O.
+// A warp's walk over rows of one KV head, kAttStep at a time and `stride` rows from one step to the next, for up to 8 NH query heads.
 template <int D, int NH>
-struct Left {
-    float4 o[NH * D / 16][32];
-    float2 ml[NH][32];
-};
-template <int D, int NH>
-struct AttSmem {
-    // apart from the rings where there is room (a warp's ring can then be filled for the next part while others join), else in the rings' place
-    static constexpr bool kApart = kAttWarps * kRingBytes + (kAttWarps - 1) * sizeof(Left<D, NH>) + 1024 <= 227 * 1024;
-    alignas(128) unsigned char ring[kAttWarps][kRingBytes];
-    alignas(16) unsigned char left_[kApart ? (kAttWarps - 1) * sizeof(Left<D, NH>) : 16];
-    DealSmem deal;
-    __device__ __forceinline__ Left<D, NH>& left(int warp, int block) {     // of a warp that is not the first of its head
-        if constexpr (kApart) return reinterpret_cast<Left<D, NH>*>(left_)[warp - block];
-        else return *reinterpret_cast<Left<D, NH>*>(ring[warp]);
+struct Walk {
+    static constexpr int kCh = D / 32;                  // 16-byte pieces of a key row that a lane takes
+    static constexpr int kVh = D / 64;                  // and of a value row
+    static constexpr int kPieces = D / 8;               // of a row
+    static constexpr int kRowsOnce = 32 / kPieces;      // rows that one copy instruction of a warp takes
+    static constexpr int kHalf = kAttStep * D * 2;      // bytes of a step's keys
+    static constexpr int kStages = kRingBytes / (2 * kHalf);
+
+    const PagedCache cache;
+    const float scale_log2;
+    const size_t row_elems;                             // from a row of the cache to the next
+    unsigned char* const slots;                         // kRingBytes of shared memory
+    const uint32_t ring;
+    const int32_t* table;
+    const __nv_bfloat16 *Kh, *Vh;                       // the head's part of the cache's first row, at this lane's piece
+    int base, end, stride, heads;                       // rows base, base + 1, ... of a step, up to `end`
+    int at[kStages];                                    // rows of the cache of the steps ahead: lane l (and l + 16) row l of a step, -1: none
+    uint4 qr[NH][kCh];
+    float m[NH], l[NH], o[NH][D / 16][4];               // of the query heads g and 8 + g: running maximum, this lane's part of the sum; O^T
+
+    __device__ __forceinline__ Walk(const AttendArgs& a, unsigned char* slots_)
+        : cache(a.cache), scale_log2(a.scale_log2), row_elems(static_cast<size_t>(a.Hkv) * D), slots(slots_),
+          ring(static_cast<uint32_t>(__cvta_generic_to_shared(slots_))) {}
+
+    __device__ __forceinline__ int lookup(int from) const {
+        const int r = from + (threadIdx.x & 15);
+        return r < end ? paged_row(cache, table, r) : -1;
     }
-};
-
-// D: head dim; NH: query heads of a group in eights.
-template <int D, int NH, bool SUMS>
-__global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs a) {
-    constexpr unsigned kFull = 0xffffffffu;
-    constexpr int kCh = D / 32;                   // 16-byte pieces of a key row that a lane takes
-    constexpr int kVh = D / 64;                   // and of a value row
-    constexpr int kPieces = D / 8;                // of a row
-    constexpr int kRowsOnce = 32 / kPieces;       // rows that one copy instruction of a warp takes
-    constexpr int kHalf = kAttStep * D * 2;       // bytes of a step's keys
-    constexpr int kStages = kRingBytes / (2 * kHalf);
-    extern __shared__ __align__(128) char smem_raw[];
-    AttSmem<D, NH>& sm = *reinterpret_cast<AttSmem<D, NH>*>(smem_raw);
-    begin_dependent();
-    const int cta = blockIdx.x, units = a.B * a.blocks;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const Deal dl = deal(a, cta, gridDim.x, sm.deal);
-    const Share share(dl.total, gridDim.x);
-    if (cta >= share.n || dl.unit >= units) return;
-    const int x1 = share.begin(cta + 1);
-    // this warp's head in a unit and its rows among those of the head's warps
-    const int head = warp % a.block, turn = warp / a.block, turns = a.tile / kAttStep;
-    const int G = a.Hq / a.Hkv;
-    const size_t row_elems = static_cast<size_t>(a.Hkv) * D;
-    unsigned char* const slots = sm.ring[warp];
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(slots));
-    // what a lane copies of a step's rows: piece `piece` of the rows r0 + kRowsOnce i. Pieces are exchanged within 128 bytes so that the eight
-    // lanes of a load's quarter find theirs in different banks: keys are read four neighbouring pieces of two rows at a time, values two of four.
-    const int piece = lane % kPieces, r0 = lane / kPieces;
-
-    // A part of this CTA's share: tiles [tile0, tile1) of a unit, for one group of query heads.
-    struct Part {
-        Unit un;
-        int unit, tiles, first, grp, tile0, tile1;
-        int rows_end;                // of this warp's head, within the part
-        __device__ __forceinline__ bool begins() const { return tile0 == 0; }
-        __device__ __forceinline__ bool whole() const { return tile0 == 0 && tile1 == tiles; }
-    };
-    auto part_at = [&](int x, int unit, int first) {            // first: the unit's first tile (of its first group)
-        Part p;
-        p.unit = unit;
-        p.first = first;
-        p.un = unit_of(a, unit);
-        p.tiles = tiles_of(a, unit);
-        p.grp = a.groups == 1 ? 0 : (x - first) / p.tiles;
-        const int begin = first + p.grp * p.tiles;
-        p.tile0 = x - begin;
-        p.tile1 = min(x1 - begin, p.tiles);
-        const bool on = head < p.un.heads && turn < turns;      // (else this warp has no head here)
-        p.rows_end = on ? min(rows_of(a, p.un.b * a.Hkv + p.un.h0 + head), p.tile1 * a.tile) : 0;
-        return p;
-    };
-    // lane l (and l + 16) looks up row l of a step
-    auto lookup = [&](const Part& p, int base) {
-        const int r = base + (lane & 15);
-        return r < p.rows_end ? paged_row(a.cache, a.cache.tables + static_cast<size_t>(p.un.b) * a.cache.max_pages, r) : -1;
-    };
-    auto copy_step = [&](const Part& p, int at, uint32_t to) {
-        const size_t off_h = static_cast<size_t>(p.un.h0 + head) * D + 8 * piece;
-        const __nv_bfloat16 *Kh = a.K + off_h, *Vh = a.V + off_h;
+    // Pieces are exchanged within 128 bytes so that the eight lanes of a load's quarter find theirs in different banks: keys are read four
+    // neighbouring pieces of two rows at a time, values two of four. A lane copies piece `piece` of every kRowsOnce-th row.
+    __device__ __forceinline__ void copy_step(int rows, uint32_t to) const {
+        const int lane = threadIdx.x & 31, piece = lane % kPieces;
 #pragma unroll
         for (int i = 0; i < kAttStep / kRowsOnce; ++i) {
-            const int r = i * kRowsOnce + r0, row = __shfl_sync(kFull, at, r);
+            const int r = i * kRowsOnce + lane / kPieces, row = __shfl_sync(0xffffffffu, rows, r);
             const size_t off = static_cast<size_t>(max(row, 0)) * row_elems;
             copy_async(to + r * (2 * D) + ((piece ^ (4 * (r & 1))) << 4), Kh + off, row >= 0);
             copy_async(to + kHalf + r * (2 * D) + ((piece ^ (r & 6)) << 4), Vh + off, row >= 0);
         }
-    };
-    // at[i]: rows of the step i behind the one that is worked on. A group of copies a step, empty ones behind the last row.
-    int at[kStages];
-    uint4 qr[NH][kCh];
-    auto begin_part = [&](const Part& p) {
-        const int base = p.tile0 * a.tile + turn * kAttStep;
+    }
+    // Asks for the first steps. b: sequence, h: KV head, q_row: first of the query heads among all. A group of copies a step, empty ones behind `end`.
+    __device__ __forceinline__ void begin(const AttendArgs& a, int b, int h, size_t q_row, int heads_, int base_, int end_, int stride_) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        table = cache.tables + static_cast<size_t>(b) * cache.max_pages;
+        const size_t off = static_cast<size_t>(h) * D + 8 * (lane % kPieces);
+        Kh = a.K + off;
+        Vh = a.V + off;
+        base = base_; end = end_; stride = stride_; heads = heads_;
 #pragma unroll
-        for (int i = 0; i < kStages; ++i) at[i] = lookup(p, base + i * a.tile);
-        const int heads = min(8 * NH, G - p.grp * 8 * NH);
-        const __nv_bfloat16* q = a.q + (static_cast<size_t>(p.un.b) * a.Hq + static_cast<size_t>(p.un.h0 + head) * G + p.grp * 8 * NH) * D;
+        for (int i = 0; i < kStages; ++i) at[i] = lookup(base + i * stride);
+        const __nv_bfloat16* q = a.q + q_row * D + 8 * t;
 #pragma unroll
         for (int n = 0; n < NH; ++n)
 #pragma unroll
             for (int i = 0; i < kCh; ++i)
-                qr[n][i] = p.rows_end > 0 && 8 * n + g < heads ? __ldg(reinterpret_cast<const uint4*>(q + static_cast<size_t>(8 * n + g) * D + 32 * i + 8 * t))
-                                                               : make_uint4(0, 0, 0, 0);
+                qr[n][i] = base < end && 8 * n + g < heads ? __ldg(reinterpret_cast<const uint4*>(q + static_cast<size_t>(8 * n + g) * D + 32 * i)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) {
-            if (base + i * a.tile < p.rows_end) copy_step(p, at[i], ring + i * 2 * kHalf);
+            if (base + i * stride < end) copy_step(at[i], ring + i * 2 * kHalf);
             copies_begin_group();
         }
-    };
-
-    Part p = part_at(share.begin(cta), dl.unit, dl.first);
-    begin_part(p);
-    for (;;) {
-        const int heads = min(8 * NH, G - p.grp * 8 * NH);      // query heads of this group
-        const int r1 = p.rows_end;
-        const size_t q_row = static_cast<size_t>(p.un.b) * a.Hq + static_cast<size_t>(p.un.h0 + head) * G + p.grp * 8 * NH;
-        float m[NH], l[NH], o[NH][D / 16][4];
+    }
+    // keep(n, base, v): the logits v[j][e] of query head 8 n + g and rows base + 8 j + 2 t + e (in powers of two; -inf: not seen).
+    template <class Keep>
+    __device__ __forceinline__ void run(Keep keep) {
+        constexpr unsigned kFull = 0xffffffffu;
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
             m[n] = -INFINITY;
@@ -262,13 +222,12 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
         }
-
         int stage = 0;
-        for (int base = p.tile0 * a.tile + turn * kAttStep; base < r1; base += a.tile) {
+        for (; base < end; base += stride) {
             copies_wait<kStages - 2>();
             __syncwarp();                                       // (this step has landed, and the one before has been read)
-            const int ahead = base + (kStages - 1) * a.tile;
-            if (ahead < r1) copy_step(p, at[kStages - 1], ring + (stage == 0 ? kStages - 1 : stage - 1) * 2 * kHalf);
+            const int ahead = base + (kStages - 1) * stride;
+            if (ahead < end) copy_step(at[kStages - 1], ring + (stage == 0 ? kStages - 1 : stage - 1) * 2 * kHalf);
             copies_begin_group();
             const unsigned char *keys = slots + stage * 2 * kHalf, *values = keys + kHalf;
             stage = stage == kStages - 1 ? 0 : stage + 1;
@@ -294,7 +253,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
             for (int j = 0; j < 4; ++j) seen |= __shfl_sync(kFull, at[0], (j >> 1) * 8 + 2 * t + (j & 1)) >= 0 ? 1u << j : 0u;
 #pragma unroll
             for (int i = 0; i < kStages - 1; ++i) at[i] = at[i + 1];
-            at[kStages - 1] = lookup(p, ahead + a.tile);
+            at[kStages - 1] = lookup(ahead + stride);
 
             uint32_t hi[NH][2], lo[NH][2];
             float factor[NH];
@@ -306,17 +265,10 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        v[j][e] = seen >> (2 * j + e) & 1u ? s[j][2 * n + e] * a.scale_log2 : -INFINITY;
+                        v[j][e] = seen >> (2 * j + e) & 1u ? s[j][2 * n + e] * scale_log2 : -INFINITY;
                         mx = fmaxf(mx, v[j][e]);
                     }
-                if constexpr (SUMS) {
-                    if (8 * n + g < heads) {
-                        float* lg = a.logits + (q_row + 8 * n + g) * a.logit_stride + base + 2 * t;
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)             // (the stride is even and covers every row, so a pair fits)
-                            if (base + 8 * j + 2 * t < r1) *reinterpret_cast<float2*>(lg + 8 * j) = make_float2(v[j][0], v[j][1]);
-                    }
-                }
+                if (8 * n + g < heads) keep(n, base, v);
                 mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, 1));
                 mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, 2));
                 const float m_new = fmaxf(m[n], mx), ref = reference_of(m_new);
@@ -363,6 +315,133 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
                 }
             }
         }
+        __syncwarp();                                           // (the last step has been read)
+    }
+    // Another warp's walk over the same head (its values as left by leave) joined to this one.
+    template <class From>
+    __device__ __forceinline__ void join(const From& other) {
+        constexpr unsigned kFull = 0xffffffffu;
+        const int lane = threadIdx.x & 31, t = lane & 3;
+#pragma unroll
+        for (int n = 0; n < NH; ++n) {
+            const float2 s = other.ml[n][lane];
+            const float m_new = fmaxf(m[n], s.x), ref = reference_of(m_new);
+            const float own = exp2_fast(m[n] - ref), its = exp2_fast(s.x - ref);
+            m[n] = m_new;
+            l[n] = l[n] * own + s.y * its;
+            const float a0 = __shfl_sync(kFull, own, 8 * t), a1 = __shfl_sync(kFull, own, 8 * t + 4);
+            const float b0 = __shfl_sync(kFull, its, 8 * t), b1 = __shfl_sync(kFull, its, 8 * t + 4);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                const float4 v = other.o[n * (D / 16) + i][lane];
+                o[n][i][0] = o[n][i][0] * a0 + v.x * b0;
+                o[n][i][1] = o[n][i][1] * a1 + v.y * b1;
+                o[n][i][2] = o[n][i][2] * a0 + v.z * b0;
+                o[n][i][3] = o[n][i][3] * a1 + v.w * b1;
+            }
+        }
+    }
+    template <class To>
+    __device__ __forceinline__ void leave(To& to) const {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int n = 0; n < NH; ++n) {
+            to.ml[n][lane] = make_float2(m[n], l[n]);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) to.o[n * (D / 16) + i][lane] = make_float4(o[n][i][0], o[n][i][1], o[n][i][2], o[n][i][3]);
+        }
+    }
+    // The sum of a query head from the four lanes that hold its columns.
+    __device__ __forceinline__ void add_up() {
+#pragma unroll
+        for (int n = 0; n < NH; ++n) {
+            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
+            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
+        }
+    }
+    // This lane's values of query head 8 n + 2 t + e: the dims 64 hh + 8 g, ..., + 7.
+    __device__ __forceinline__ float value(int n, int e, int hh, int i) const { return o[n][4 * hh + i / 2][e + 2 * (i & 1)]; }
+};
+
+// What a warp leaves for the one that joins its head's warps: every lane's (max, sum) and O.
+template <int D, int NH>
+struct Left {
+    float4 o[NH * D / 16][32];
+    float2 ml[NH][32];
+};
+template <int D, int NH>
+struct AttSmem {
+    // apart from the rings where there is room (a warp's ring can then be filled for the next part while others join), else in the rings' place
+    static constexpr bool kApart = kAttWarps * kRingBytes + (kAttWarps - 1) * sizeof(Left<D, NH>) + 1024 <= 227 * 1024;
+    alignas(128) unsigned char ring[kAttWarps][kRingBytes];
+    alignas(16) unsigned char left_[kApart ? (kAttWarps - 1) * sizeof(Left<D, NH>) : 16];
+    DealSmem deal;
+    __device__ __forceinline__ Left<D, NH>& left(int warp, int block) {     // of a warp that is not the first of its head
+        if constexpr (kApart) return reinterpret_cast<Left<D, NH>*>(left_)[warp - block];
+        else return *reinterpret_cast<Left<D, NH>*>(ring[warp]);
+    }
+};
+
+// D: head dim; NH: query heads of a group in eights.
+template <int D, int NH, bool SUMS>
+__global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs a) {
+    constexpr unsigned kFull = 0xffffffffu;
+    constexpr int kVh = D / 64;
+    extern __shared__ __align__(128) char smem_raw[];
+    AttSmem<D, NH>& sm = *reinterpret_cast<AttSmem<D, NH>*>(smem_raw);
+    begin_dependent();
+    const int cta = blockIdx.x, units = a.B * a.blocks;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const Deal dl = deal(a, cta, gridDim.x, sm.deal);
+    const Share share(dl.total, gridDim.x);
+    if (cta >= share.n || dl.unit >= units) return;
+    const int x1 = share.begin(cta + 1);
+    // this warp's head in a unit and its rows among those of the head's warps
+    const int head = warp % a.block, turn = warp / a.block, turns = a.tile / kAttStep;
+    const int G = a.Hq / a.Hkv;
+    Walk<D, NH> walk(a, sm.ring[warp]);
+
+    // A part of this CTA's share: tiles [tile0, tile1) of a unit, for one group of query heads.
+    struct Part {
+        Unit un;
+        int unit, tiles, first, grp, tile0, tile1;
+        int rows_end;                // of this warp's head, within the part
+        __device__ __forceinline__ bool begins() const { return tile0 == 0; }
+        __device__ __forceinline__ bool whole() const { return tile0 == 0 && tile1 == tiles; }
+    };
+    auto part_at = [&](int x, int unit, int first) {            // first: the unit's first tile (of its first group)
+        Part p;
+        p.unit = unit;
+        p.first = first;
+        p.un = unit_of(a, unit);
+        p.tiles = tiles_of(a, unit);
+        p.grp = a.groups == 1 ? 0 : (x - first) / p.tiles;
+        const int begin = first + p.grp * p.tiles;
+        p.tile0 = x - begin;
+        p.tile1 = min(x1 - begin, p.tiles);
+        const bool on = head < p.un.heads && turn < turns;      // (else this warp has no head here)
+        p.rows_end = on ? min(rows_of(a, p.un.b * a.Hkv + p.un.h0 + head), p.tile1 * a.tile) : 0;
+        return p;
+    };
+    auto row_of_q = [&](const Part& p) { return static_cast<size_t>(p.un.b) * a.Hq + static_cast<size_t>(p.un.h0 + head) * G + p.grp * 8 * NH; };
+    auto begin_part = [&](const Part& p) {
+        walk.begin(a, p.un.b, p.un.h0 + head, row_of_q(p), min(8 * NH, G - p.grp * 8 * NH), p.tile0 * a.tile + turn * kAttStep, p.rows_end, a.tile);
+    };
+
+    Part p = part_at(share.begin(cta), dl.unit, dl.first);
+    begin_part(p);
+    for (;;) {
+        const int heads = walk.heads;                           // query heads of this group
+        const size_t q_row = row_of_q(p);
+        const int r1 = p.rows_end;
+        walk.run([&](int n, int base, const float (&v)[2][2]) {
+            if constexpr (SUMS) {
+                float* lg = a.logits + (q_row + 8 * n + g) * a.logit_stride + base + 2 * t;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)                     // (the stride is even and covers every row, so a pair fits)
+                    if (base + 8 * j + 2 * t < r1) *reinterpret_cast<float2*>(lg + 8 * j) = make_float2(v[j][0], v[j][1]);
+            }
+        });
 
         // the part behind this one, if any: where no other warp's values are joined in the rings' place its first rows are asked for at once
         const int x = p.first + p.grp * p.tiles + p.tile1;
@@ -377,68 +456,34 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
             more = unit < units;
             if (more) next = part_at(x, unit, first);
         }
-        __syncwarp();                                           // (the last step has been read)
         constexpr bool kApart = AttSmem<D, NH>::kApart;
         if (more && (kApart || turns == 1)) begin_part(next);
 
         if (turns > 1) {                                        // the warps of a head, joined by its first one in their order
             __syncthreads();                                    // (what was left before has been read)
-            if (turn > 0 && turn < turns) {
-                Left<D, NH>& mine = sm.left(warp, a.block);
-#pragma unroll
-                for (int n = 0; n < NH; ++n) {
-                    mine.ml[n][lane] = make_float2(m[n], l[n]);
-#pragma unroll
-                    for (int i = 0; i < D / 16; ++i) mine.o[n * (D / 16) + i][lane] = make_float4(o[n][i][0], o[n][i][1], o[n][i][2], o[n][i][3]);
-                }
-            }
+            if (turn > 0 && turn < turns) walk.leave(sm.left(warp, a.block));
             __syncthreads();
-            if (turn == 0) {
-                for (int w = 1; w < turns; ++w) {
-                    const Left<D, NH>& other = sm.left(warp + w * a.block, a.block);
-#pragma unroll
-                    for (int n = 0; n < NH; ++n) {
-                        const float2 s = other.ml[n][lane];
-                        const float m_new = fmaxf(m[n], s.x), ref = reference_of(m_new);
-                        const float own = exp2_fast(m[n] - ref), its = exp2_fast(s.x - ref);
-                        m[n] = m_new;
-                        l[n] = l[n] * own + s.y * its;
-                        const float a0 = __shfl_sync(kFull, own, 8 * t), a1 = __shfl_sync(kFull, own, 8 * t + 4);
-                        const float b0 = __shfl_sync(kFull, its, 8 * t), b1 = __shfl_sync(kFull, its, 8 * t + 4);
-#pragma unroll
-                        for (int i = 0; i < D / 16; ++i) {
-                            const float4 v = other.o[n * (D / 16) + i][lane];
-                            o[n][i][0] = o[n][i][0] * a0 + v.x * b0;
-                            o[n][i][1] = o[n][i][1] * a1 + v.y * b1;
-                            o[n][i][2] = o[n][i][2] * a0 + v.z * b0;
-                            o[n][i][3] = o[n][i][3] * a1 + v.w * b1;
-                        }
-                    }
-                }
-            }
+            if (turn == 0)
+                for (int w = 1; w < turns; ++w) walk.join(sm.left(warp + w * a.block, a.block));
             if (!kApart) {
                 __syncthreads();
                 if (more) begin_part(next);
             }
         }
-#pragma unroll
-        for (int n = 0; n < NH; ++n) {                          // the sum of a query head from the four lanes that hold its columns
-            l[n] += __shfl_xor_sync(kFull, l[n], 1);
-            l[n] += __shfl_xor_sync(kFull, l[n], 2);
-        }
+        walk.add_up();
         if (p.begins() && threadIdx.x == 0)
             a.shared_by[static_cast<size_t>(p.unit) * a.groups + p.grp] = make_int2(cta, share.owner(p.first + (p.grp + 1) * p.tiles - 1));
         const bool whole = p.whole();
-        if (turn == 0 && head < p.un.heads) {                   // a lane holds eight neighbouring dims (of each 64) of the heads 2t and 2t + 1
+        if (turn == 0 && head < p.un.heads) {
 #pragma unroll
             for (int n = 0; n < NH; ++n) {
                 if (t == 0 && 8 * n + g < heads) {
-                    if (!whole) a.part_ml[record(a, cta, p.begins(), head, 8 * n + g)] = make_float2(m[n], l[n]);
-                    else if (SUMS) a.whole_ml[q_row + 8 * n + g] = make_float2(m[n], l[n]);        // (a CTA can have many)
+                    if (!whole) a.part_ml[record(a, cta, p.begins(), head, 8 * n + g)] = make_float2(walk.m[n], walk.l[n]);
+                    else if (SUMS) a.whole_ml[q_row + 8 * n + g] = make_float2(walk.m[n], walk.l[n]);      // (a CTA can have many)
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float ll = __shfl_sync(kFull, l[n], 8 * t + 4 * e);
+                    const float ll = __shfl_sync(kFull, walk.l[n], 8 * t + 4 * e);
                     const int q = 8 * n + 2 * t + e;
                     if (q >= heads) continue;
                     if (whole) {
@@ -448,16 +493,17 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
                         for (int hh = 0; hh < kVh; ++hh) {
                             uint32_t w[4];
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) w[i] = pack_bf16(o[n][4 * hh + i][e] * r, o[n][4 * hh + i][e + 2] * r);
+                            for (int i = 0; i < 4; ++i) w[i] = pack_bf16(walk.value(n, e, hh, 2 * i) * r, walk.value(n, e, hh, 2 * i + 1) * r);
                             *reinterpret_cast<uint4*>(to + 64 * hh) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
                     } else {
                         float* to = a.part_o + record(a, cta, p.begins(), head, q) * D + 8 * g;
 #pragma unroll
-                        for (int hh = 0; hh < kVh; ++hh) {
-                            *reinterpret_cast<float4*>(to + 64 * hh) = make_float4(o[n][4 * hh][e], o[n][4 * hh][e + 2], o[n][4 * hh + 1][e], o[n][4 * hh + 1][e + 2]);
-                            *reinterpret_cast<float4*>(to + 64 * hh + 4) = make_float4(o[n][4 * hh + 2][e], o[n][4 * hh + 2][e + 2], o[n][4 * hh + 3][e], o[n][4 * hh + 3][e + 2]);
-                        }
+                        for (int hh = 0; hh < kVh; ++hh)
+#pragma unroll
+                            for (int i = 0; i < 8; i += 4)
+                                *reinterpret_cast<float4*>(to + 64 * hh + i) = make_float4(walk.value(n, e, hh, i), walk.value(n, e, hh, i + 1),
+                                                                                           walk.value(n, e, hh, i + 2), walk.value(n, e, hh, i + 3));
                     }
                 }
             }
@@ -644,6 +690,160 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
     }
 }
 
+// The form for short caches: a cluster of CTAs works on one (sequence, KV head, group of query heads), each CTA on an even share of its rows, and the
+// parts are joined through distributed shared memory: one launch and no scratch. Logits that the sums need stay in shared memory.
+constexpr int kSmallWarps = 4;
+constexpr int kSmallThreads = 32 * kSmallWarps;
+constexpr int kSmallMaxCtas = 16;                     // of a cluster
+
+template <int D, int NH>
+struct SmallSmem {
+    union {
+        alignas(128) unsigned char ring[kSmallWarps][kRingBytes];
+        float o[kSmallWarps][8 * NH][D + 4];          // the warps' parts (the rings are idle then)
+    };
+    float2 warp_ml[kSmallWarps][8 * NH];
+    alignas(16) float cta_o[8 * NH][D];               // this CTA's part, which the others read
+    float2 cta_ml[8 * NH];
+    float2 all[8 * NH];                               // (reference, factor) of the query heads
+    // float logits[8 * NH][a.small_rows] behind it
+};
+
+template <int D, int NH, bool SUMS>
+__global__ void __launch_bounds__(kSmallThreads, 2) attend_small_kernel(const AttendArgs a) {
+    constexpr int kVh = D / 64;
+    extern __shared__ __align__(128) char smem_raw[];
+    SmallSmem<D, NH>& sm = *reinterpret_cast<SmallSmem<D, NH>*>(smem_raw);
+    float* logits = reinterpret_cast<float*>(smem_raw + sizeof(SmallSmem<D, NH>));
+    begin_dependent();
+    cg::cluster_group cluster = cg::this_cluster();
+    const int n_cta = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int item = blockIdx.x / n_cta, bh = item / a.groups, grp = item - bh * a.groups, b = bh / a.Hkv, h = bh - b * a.Hkv;
+    const int G = a.Hq / a.Hkv, heads = min(8 * NH, G - grp * 8 * NH);
+    const size_t q_row = static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + grp * 8 * NH;
+    const int n = rows_of(a, bh), steps = (n + kAttStep - 1) / kAttStep;
+    const int r0 = rank * steps / n_cta * kAttStep, r1 = min((rank + 1) * steps / n_cta * kAttStep, n);
+    Walk<D, NH> walk(a, sm.ring[warp]);
+    walk.begin(a, b, h, q_row, heads, r0 + warp * kAttStep, r1, kSmallWarps * kAttStep);
+    walk.run([&](int nn, int base, const float (&v)[2][2]) {
+        if constexpr (SUMS) {                         // (rows of a CTA and their pairs: an even number)
+            float* lg = logits + (8 * nn + g) * a.small_rows + (base - r0) + 2 * t;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) *reinterpret_cast<float2*>(lg + 8 * j) = make_float2(v[j][0], v[j][1]);
+        }
+    });
+    walk.add_up();
+    __syncthreads();                                  // (every ring is idle)
+#pragma unroll
+    for (int nn = 0; nn < NH; ++nn) {
+        if (t == 0) sm.warp_ml[warp][8 * nn + g] = make_float2(walk.m[nn], walk.l[nn]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int hh = 0; hh < kVh; ++hh)
+#pragma unroll
+                for (int i = 0; i < 8; i += 4)
+                    *reinterpret_cast<float4*>(&sm.o[warp][8 * nn + 2 * t + e][64 * hh + 8 * g + i]) =
+                        make_float4(walk.value(nn, e, hh, i), walk.value(nn, e, hh, i + 1), walk.value(nn, e, hh, i + 2), walk.value(nn, e, hh, i + 3));
+    }
+    __syncthreads();
+    for (int e = tid; e < heads * (D / 4); e += kSmallThreads) {
+        const int q = e / (D / 4), c4 = e % (D / 4) * 4;
+        float2 s[kSmallWarps];
+        float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+        for (int w = 0; w < kSmallWarps; ++w) { s[w] = sm.warp_ml[w][q]; mm = fmaxf(mm, s[w].x); }
+        const float ref = reference_of(mm);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kSmallWarps; ++w) {
+            const float f = exp2_fast(s[w].x - ref);
+            const float4 y = *reinterpret_cast<const float4*>(&sm.o[w][q][c4]);
+            ll = fmaf(s[w].y, f, ll);
+            v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
+        }
+        *reinterpret_cast<float4*>(&sm.cta_o[q][c4]) = v;
+        if (c4 == 0) sm.cta_ml[q] = make_float2(mm, ll);
+    }
+    cluster.sync();
+    // the CTAs' parts, in their order: a query head's (max, sum), then the values, an even share of them by every CTA
+    auto joined = [&](int q, float2 (&s)[kSmallMaxCtas], float& ref) {
+        float mm = -INFINITY, ll = 0.f;
+#pragma unroll
+        for (int c = 0; c < kSmallMaxCtas; ++c) {
+            s[c] = c < n_cta ? *cluster.map_shared_rank(&sm.cta_ml[q], c) : make_float2(-INFINITY, 0.f);
+            mm = fmaxf(mm, s[c].x);
+        }
+        ref = reference_of(mm);
+#pragma unroll
+        for (int c = 0; c < kSmallMaxCtas; ++c) {
+            s[c].x = exp2_fast(s[c].x - ref);
+            ll += c < n_cta ? s[c].y * s[c].x : 0.f;
+        }
+        return ll == 0.f ? 0.f : 1.f / ll;            // (nothing seen: zeros)
+    };
+    for (int e = rank * kSmallThreads + tid; e < heads * (D / 4); e += n_cta * kSmallThreads) {
+        const int q = e / (D / 4), c4 = e % (D / 4) * 4;
+        float4 y[kSmallMaxCtas];
+#pragma unroll
+        for (int c = 0; c < kSmallMaxCtas; ++c)
+            y[c] = c < n_cta ? *reinterpret_cast<const float4*>(cluster.map_shared_rank(&sm.cta_o[q][c4], c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        float2 s[kSmallMaxCtas];
+        float ref;
+        const float r = joined(q, s, ref);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < kSmallMaxCtas; ++c)
+            if (c < n_cta) { v.x = fmaf(y[c].x, s[c].x, v.x); v.y = fmaf(y[c].y, s[c].x, v.y); v.z = fmaf(y[c].z, s[c].x, v.z); v.w = fmaf(y[c].w, s[c].x, v.w); }
+        *reinterpret_cast<uint2*>(a.out + (q_row + q) * D + c4) = make_uint2(pack_bf16(v.x * r, v.y * r), pack_bf16(v.z * r, v.w * r));
+    }
+    if constexpr (SUMS) {
+        if (tid < heads) {
+            float2 s[kSmallMaxCtas];
+            float ref;
+            const float r = joined(tid, s, ref);
+            sm.all[tid] = make_float2(ref, r);
+        }
+        __syncthreads();
+        float* w = a.weights + static_cast<size_t>(bh) * a.cache.cap;
+        for (int r = r0 + tid; r < r1; r += kSmallThreads) {
+            float sum = 0.f;
+            for (int q = 0; q < heads; ++q) sum += exp2_fast(logits[q * a.small_rows + r - r0] - sm.all[q].x) * sm.all[q].y;
+            w[r] += sum;
+        }
+    }
+    cluster.sync();                                   // (a CTA's part is there until all have read it)
+}
+
+template <int D, int NH, bool SUMS>
+cudaError_t launch_small(const AttendArgs& a, const AttendPlan& plan, int device, cudaStream_t stream) {
+    const int smem = static_cast<int>(sizeof(SmallSmem<D, NH>)) + (SUMS ? 8 * NH * plan.small_rows * 4 : 0);
+    auto kernel = attend_small_kernel<D, NH, SUMS>;
+    static uint64_t set_on = 0;                                 // devices; the caller holds the library's lock
+    if ((set_on >> device & 1u) == 0) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+        set_on |= 1ull << device;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.B * a.Hkv * a.groups * plan.cluster));
+    cfg.blockDim = dim3(kSmallThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = plan.cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 template <int D, int NH, bool SUMS, TeamOf TEAM>
 cudaError_t launch_join(const AttendArgs& a, cudaLaunchConfig_t cfg, int row_blocks) {
     using T = Team<D, TEAM>;
@@ -703,6 +903,21 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
         if (p.tile == 1 << s) p.tile_shift = s;
     const long long tiles = static_cast<long long>(B) * p.blocks * p.groups * ((cap + p.tile - 1) / p.tile);
     p.max_ctas = static_cast<int>(tiles < kAttMaxCtas ? tiles : kAttMaxCtas);
+    // short caches: as many CTAs a head as are resident (the cluster sizes that fit beside each other), each with few rows
+    const long long items = static_cast<long long>(B) * Hkv * p.groups;
+    p.cluster = items <= 14 ? 16 : items <= 33 ? 8 : items <= 71 ? 4 : items <= 148 ? 2 : items <= 296 ? 1 : 0;
+    if (p.cluster > 0) {
+        const int steps = (cap + kAttStep - 1) / kAttStep;
+        p.small_rows = (steps + p.cluster - 1) / p.cluster * kAttStep;
+        const size_t fixed = d == 128 ? (p.nh == 1 ? sizeof(SmallSmem<128, 1>) : sizeof(SmallSmem<128, 2>)) : (p.nh == 1 ? sizeof(SmallSmem<64, 1>) : sizeof(SmallSmem<64, 2>));
+        const bool fits = !sums || (p.groups == 1 && fixed + 8ull * p.nh * p.small_rows * 4 <= kSmallSmem);
+        if (p.small_rows > kSmallRows || !fits) p.cluster = 0;
+    }
+    if (p.cluster > 0) {                                        // (no scratch: a byte, so that every call has some)
+        p.off_o = p.off_whole = p.off_shared = p.off_logits = 0;
+        p.bytes = 256;
+        return p;
+    }
     const size_t heads = static_cast<size_t>(p.max_ctas) * 2 * p.block * p.group;
     p.logit_stride = (cap + 3) / 4 * 4;
     p.off_o = (heads * sizeof(float2) + 255) / 256 * 256;
@@ -730,6 +945,13 @@ cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d,
     a.logit_stride = plan.logit_stride;
     const int n = num_sms < plan.max_ctas ? num_sms : plan.max_ctas;
     const bool sums = a.weights != nullptr;
+    if (plan.cluster > 0) {
+        a.small_rows = plan.small_rows;
+#define CKV_SMALL(D, NH) (sums ? launch_small<D, NH, true>(a, plan, device, stream) : launch_small<D, NH, false>(a, plan, device, stream))
+        if (d == 128) return plan.nh == 1 ? CKV_SMALL(128, 1) : CKV_SMALL(128, 2);
+        return plan.nh == 1 ? CKV_SMALL(64, 1) : CKV_SMALL(64, 2);
+#undef CKV_SMALL
+    }
 #define CKV_ATTEND(D, NH) (sums ? launch_attend_t<D, NH, true>(a, n, device, stream) : launch_attend_t<D, NH, false>(a, n, device, stream))
     if (d == 128) return plan.nh == 1 ? CKV_ATTEND(128, 1) : CKV_ATTEND(128, 2);
     return plan.nh == 1 ? CKV_ATTEND(64, 1) : CKV_ATTEND(64, 2);

@@ -59,9 +59,11 @@ struct AttendArgs {
     int2* shared_by;                          // first and last CTA with rows of a unit
     float *part_o, *logits;
     long long logit_stride;
+    int small_rows;                           // rows of a CTA of a cluster, at most
 };
 struct AttendPlan {
     int nh, groups, group, blocks, block, tile, tile_shift, max_ctas;
+    int cluster, small_rows;                  // CTAs of a cluster of the form for short caches (0: the other form), rows of one
     long long logit_stride;
     size_t off_o, off_whole, off_shared, off_logits, bytes;
 };

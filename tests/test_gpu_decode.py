@@ -194,19 +194,23 @@ EDGES = [0, 1, 2, 7, 8, 9, 15, 16, 17, 31, 33, 63, 64, 65, 127, 128, 129, 191, 2
 
 @pytest.mark.parametrize("Hq,Hkv,d", SHAPES + [(9, 1, 128), (16, 1, 64), (24, 2, 128), (17, 1, 128), (40, 1, 64), (33, 1, 128)])
 @pytest.mark.parametrize("page", [1, 3, 16, 100])
-def test_attention_at_every_edge(Hq, Hkv, d, page):
+@pytest.mark.parametrize("room", [0, 9000])
+def test_attention_at_every_edge(Hq, Hkv, d, page, room):
+    """Both forms: one launch where no sequence can have many rows, two (and shares of CTAs) where the tables have room for more."""
     per = -(-200 // page)
     B = -(-len(EDGES) // Hkv)
     rng = np.random.default_rng(Hq * page)
     lengths = np.resize(rng.permutation(EDGES), (B, Hkv)).astype(np.int32)
     K, V, tables = new_cache(rng, B, Hkv, d, page, per)
     q = rand_bits(rng, (B, Hq, d), 2.0)
+    tables = np.concatenate([tables, np.full((B, room // page), -1, dtype=np.int32)], 1)
     check_attention(q, K, V, tables, lengths)
-    check_attention(q, K, V, tables, lengths, rng.random((B, Hkv, per * page)).astype(np.float32))
+    check_attention(q, K, V, tables, lengths, rng.random((B, Hkv, tables.shape[1] * page)).astype(np.float32))
 
 
 @pytest.mark.parametrize("d", [64, 128])
-def test_attention_sees_no_row_that_is_not_there(d):
+@pytest.mark.parametrize("room", [0, 1200])
+def test_attention_sees_no_row_that_is_not_there(d, room):
     """Not-a-number and infinities behind a head's last row, in other heads' rows and in pages of nobody; pages outside the cache; lengths out of range."""
     Hq, Hkv, page, per, B = 6, 2, 8, 6, 5
     rng = np.random.default_rng(5)
@@ -226,12 +230,14 @@ def test_attention_sees_no_row_that_is_not_there(d):
                 if (p, s, h) not in used:
                     K[p, s, h], V[p, s, h] = rng.choice([0x7FC0, 0x7F80, 0xFF80, 0x7F7F, 0xFF7F], 2).astype(np.uint16)
     q = rand_bits(rng, (B, Hq, d))
-    out, _ = check_attention(q, K, V, tables, lengths, rng.random((B, Hkv, per * page)).astype(np.float32))
+    tables = np.concatenate([tables, np.full((B, room), -1, dtype=np.int32)], 1)
+    out, _ = check_attention(q, K, V, tables, lengths, rng.random((B, Hkv, tables.shape[1] * page)).astype(np.float32))
     assert not out[3].any() and not out[1, 3:].any() and not out[4, 3:].any()          # heads that see nothing: zeros
 
 
 @pytest.mark.parametrize("d,G", [(64, 3), (128, 8), (128, 12)])
-def test_attention_of_infinite_and_extreme_logits(d, G):
+@pytest.mark.parametrize("room", [0, 600])
+def test_attention_of_infinite_and_extreme_logits(d, G, room):
     """Keys that no query attends to (logit -inf) weigh nothing, a head of nothing else gets zeros; +inf and not-a-number go the formula's way;
     logits of +-1e4 neither overflow nor lose the largest."""
     page, per, Hkv = 16, 8, 6
@@ -251,7 +257,8 @@ def test_attention_of_infinite_and_extreme_logits(d, G):
         K[p, s, 3, 0] = 0x47C3 if j == 77 else 0xC7C3                        # +-99840: logits of 1e4
     K[at[50][0], at[50][1], 2, 0] = 0x7F80                                   # a logit of +inf
     K[at[70][0], at[70][1], 4, 3] = 0x7FC0                                   # not a number
-    w = np.zeros((1, Hkv, per * page), dtype=np.float32)
+    tables = np.concatenate([tables, np.full((1, room), -1, dtype=np.int32)], 1)
+    w = np.zeros((1, Hkv, tables.shape[1] * page), dtype=np.float32)
     out, sums = check_attention(q, K, V, tables, lengths, w)
     assert not out[0, G:2 * G].any() and not sums[0, 1].any()
     assert torch.isnan(out[0, 2 * G:3 * G]).all() and torch.isnan(out[0, 4 * G:5 * G]).all() and torch.isfinite(out[0, 5 * G:]).all()
