@@ -31,8 +31,7 @@ constexpr int kAttStep = 16;                          // rows of a warp's step
 constexpr int kRingBytes = 24 * 1024;                 // of a warp
 constexpr int kJoinRows = 256;                        // rows of the sums that a CTA of the join takes
 constexpr int kJoinThreads = 128;
-constexpr int kSmallSmem = 113 * 1024;                // shared memory of a CTA of the form for short caches, two an SM
-constexpr int kSmallRows = 512;                       // rows of a CTA of it, at most
+constexpr int kSmallSmem = 227 * 1024;                // shared memory of a CTA of the form for short caches, one an SM
 constexpr int kJoinHeads = 8;                         // query heads whose weights are added together
 static_assert(kAttMaxCtas % 32 == 0, "records are looked at a warp at a time");
 
@@ -692,9 +691,8 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
 
 // The form for short caches: a cluster of CTAs works on one (sequence, KV head, group of query heads), each CTA on an even share of its rows, and the
 // parts are joined through distributed shared memory: one launch and no scratch. Logits that the sums need stay in shared memory.
-constexpr int kSmallWarps = 4;
+constexpr int kSmallWarps = 8;
 constexpr int kSmallThreads = 32 * kSmallWarps;
-constexpr int kSmallMaxCtas = 16;                     // of a cluster
 
 template <int D, int NH>
 struct SmallSmem {
@@ -706,11 +704,11 @@ struct SmallSmem {
     alignas(16) float cta_o[8 * NH][D];               // this CTA's part, which the others read
     float2 cta_ml[8 * NH];
     float2 all[8 * NH];                               // (reference, factor) of the query heads
-    // float logits[8 * NH][a.small_rows] behind it
+    // float logits[a.group][a.small_rows] behind it
 };
 
 template <int D, int NH, bool SUMS>
-__global__ void __launch_bounds__(kSmallThreads, 2) attend_small_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(kSmallThreads, 1) attend_small_kernel(const AttendArgs a) {
     constexpr int kVh = D / 64;
     extern __shared__ __align__(128) char smem_raw[];
     SmallSmem<D, NH>& sm = *reinterpret_cast<SmallSmem<D, NH>*>(smem_raw);
@@ -767,43 +765,31 @@ __global__ void __launch_bounds__(kSmallThreads, 2) attend_small_kernel(const At
         if (c4 == 0) sm.cta_ml[q] = make_float2(mm, ll);
     }
     cluster.sync();
-    // the CTAs' parts, in their order: a query head's (max, sum), then the values, an even share of them by every CTA
-    auto joined = [&](int q, float2 (&s)[kSmallMaxCtas], float& ref) {
-        float mm = -INFINITY, ll = 0.f;
-#pragma unroll
-        for (int c = 0; c < kSmallMaxCtas; ++c) {
-            s[c] = c < n_cta ? *cluster.map_shared_rank(&sm.cta_ml[q], c) : make_float2(-INFINITY, 0.f);
-            mm = fmaxf(mm, s[c].x);
-        }
-        ref = reference_of(mm);
-#pragma unroll
-        for (int c = 0; c < kSmallMaxCtas; ++c) {
-            s[c].x = exp2_fast(s[c].x - ref);
-            ll += c < n_cta ? s[c].y * s[c].x : 0.f;
-        }
-        return ll == 0.f ? 0.f : 1.f / ll;            // (nothing seen: zeros)
+    // the CTAs' parts: a lane takes one of them, n_cta neighbouring lanes join an item (one thread for all of them took 2.9 us of reads from afar)
+    const int c = tid & (n_cta - 1), slot = tid / n_cta, slots = kSmallThreads / n_cta;
+    auto top = [&](float x) {
+        for (int off = 1; off < n_cta; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+        return x;
     };
-    for (int e = rank * kSmallThreads + tid; e < heads * (D / 4); e += n_cta * kSmallThreads) {
-        const int q = e / (D / 4), c4 = e % (D / 4) * 4;
-        float4 y[kSmallMaxCtas];
-#pragma unroll
-        for (int c = 0; c < kSmallMaxCtas; ++c)
-            y[c] = c < n_cta ? *reinterpret_cast<const float4*>(cluster.map_shared_rank(&sm.cta_o[q][c4], c)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        float2 s[kSmallMaxCtas];
-        float ref;
-        const float r = joined(q, s, ref);
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int c = 0; c < kSmallMaxCtas; ++c)
-            if (c < n_cta) { v.x = fmaf(y[c].x, s[c].x, v.x); v.y = fmaf(y[c].y, s[c].x, v.y); v.z = fmaf(y[c].z, s[c].x, v.z); v.w = fmaf(y[c].w, s[c].x, v.w); }
-        *reinterpret_cast<uint2*>(a.out + (q_row + q) * D + c4) = make_uint2(pack_bf16(v.x * r, v.y * r), pack_bf16(v.z * r, v.w * r));
+    auto sum = [&](float x) {
+        for (int off = 1; off < n_cta; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+        return x;
+    };
+    for (int e0 = 0; e0 < heads * (D / 4); e0 += kSmallThreads) {       // every CTA an even share of the items
+        const int e = min(e0 + rank * slots + slot, heads * (D / 4) - 1), q = e / (D / 4), c4 = e % (D / 4) * 4;
+        const float2 s = *cluster.map_shared_rank(&sm.cta_ml[q], c);
+        const float4 y = *reinterpret_cast<const float4*>(cluster.map_shared_rank(&sm.cta_o[q][c4], c));
+        const float f = exp2_fast(s.x - reference_of(top(s.x))), ll = sum(s.y * f);
+        const float r = ll == 0.f ? 0.f : 1.f / ll;                     // (nothing seen: zeros)
+        const float v0 = sum(y.x * f), v1 = sum(y.y * f), v2 = sum(y.z * f), v3 = sum(y.w * f);
+        if (c == 0) *reinterpret_cast<uint2*>(a.out + (q_row + q) * D + c4) = make_uint2(pack_bf16(v0 * r, v1 * r), pack_bf16(v2 * r, v3 * r));
     }
     if constexpr (SUMS) {
-        if (tid < heads) {
-            float2 s[kSmallMaxCtas];
-            float ref;
-            const float r = joined(tid, s, ref);
-            sm.all[tid] = make_float2(ref, r);
+        for (int q0 = 0; q0 < heads; q0 += slots) {
+            const int q = min(q0 + slot, heads - 1);
+            const float2 s = *cluster.map_shared_rank(&sm.cta_ml[q], c);
+            const float ref = reference_of(top(s.x)), ll = sum(s.y * exp2_fast(s.x - ref));
+            if (c == 0) sm.all[q] = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
         }
         __syncthreads();
         float* w = a.weights + static_cast<size_t>(bh) * a.cache.cap;
@@ -818,12 +804,11 @@ __global__ void __launch_bounds__(kSmallThreads, 2) attend_small_kernel(const At
 
 template <int D, int NH, bool SUMS>
 cudaError_t launch_small(const AttendArgs& a, const AttendPlan& plan, int device, cudaStream_t stream) {
-    const int smem = static_cast<int>(sizeof(SmallSmem<D, NH>)) + (SUMS ? 8 * NH * plan.small_rows * 4 : 0);
+    const int smem = static_cast<int>(sizeof(SmallSmem<D, NH>)) + (SUMS ? plan.group * plan.small_rows * 4 : 0);
     auto kernel = attend_small_kernel<D, NH, SUMS>;
     static uint64_t set_on = 0;                                 // devices; the caller holds the library's lock
     if ((set_on >> device & 1u) == 0) {
-        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
         if (e != cudaSuccess) return e;
         set_on |= 1ull << device;
     }
@@ -903,15 +888,19 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
         if (p.tile == 1 << s) p.tile_shift = s;
     const long long tiles = static_cast<long long>(B) * p.blocks * p.groups * ((cap + p.tile - 1) / p.tile);
     p.max_ctas = static_cast<int>(tiles < kAttMaxCtas ? tiles : kAttMaxCtas);
-    // short caches: as many CTAs a head as are resident (the cluster sizes that fit beside each other), each with few rows
+    // Short caches: as many CTAs a head as are resident beside each other, where they do not have many more rows each than in even shares of all
+    // SMs. The second launch and its records cost 2 us; 128 rows of a CTA 0.8 (64 dims) to 1.2 us. One KV head of 8, 128 dims, 100 / 2000 / 4000 / 8000
+    // rows: 4.7 / 6.2 / 8.3 / 13.0 us with one launch, 6.2 / 8.4 / 8.4 / 12.0 with two; 2 heads, 64 dims, 4000 / 8000 rows 6.7 / 9.8 and 6.7 / 6.9; 16
+    // sequences of 8 heads, 600 / 1000 rows 11.6 / 15.7 and 15.1 / 18.6. At most 768 rows each, as sequences need not be alike.
     const long long items = static_cast<long long>(B) * Hkv * p.groups;
-    p.cluster = items <= 14 ? 16 : items <= 33 ? 8 : items <= 71 ? 4 : items <= 148 ? 2 : items <= 296 ? 1 : 0;
+    p.cluster = items <= 15 ? 8 : items <= 33 ? 4 : items <= 74 ? 2 : items <= 148 ? 1 : 0;
+    p.small_rows = 0;
     if (p.cluster > 0) {
-        const int steps = (cap + kAttStep - 1) / kAttStep;
-        p.small_rows = (steps + p.cluster - 1) / p.cluster * kAttStep;
+        const long long steps = (cap + kAttStep - 1) / kAttStep, rows = (steps + p.cluster - 1) / p.cluster * kAttStep;
         const size_t fixed = d == 128 ? (p.nh == 1 ? sizeof(SmallSmem<128, 1>) : sizeof(SmallSmem<128, 2>)) : (p.nh == 1 ? sizeof(SmallSmem<64, 1>) : sizeof(SmallSmem<64, 2>));
-        const bool fits = !sums || (p.groups == 1 && fixed + 8ull * p.nh * p.small_rows * 4 <= kSmallSmem);
-        if (p.small_rows > kSmallRows || !fits) p.cluster = 0;
+        const bool few = rows <= 768 && rows - items * cap / 148 <= 300;
+        if (few && (!sums || (p.groups == 1 && fixed + 4ull * p.group * rows <= kSmallSmem))) p.small_rows = static_cast<int>(rows);
+        else p.cluster = 0;
     }
     if (p.cluster > 0) {                                        // (no scratch: a byte, so that every call has some)
         p.off_o = p.off_whole = p.off_shared = p.off_logits = 0;
