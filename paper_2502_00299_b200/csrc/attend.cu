@@ -5,11 +5,11 @@
 // the memory waits for. A warp works on one KV head, 16 rows a step, with a ring of steps of its own in shared memory that asynchronous
 // copies fill (24 KB a warp, two thirds of it in flight: 128 KB an SM) - no warp waits for another. The eight warps of a CTA take neighbouring
 // heads of the same rows, which lie side by side in the cache, where there are as many; else several warps a head take rows in turn. The products run
-// on the tensor cores with the heads of a group as eight columns: S = Q K^T as m16n8k16 (heads x rows; half of the 16 heads are zero up
-// to G = 8) and O^T += V^T P^T (dims x heads), V^T out of two rows' registers by byte permutes. Which 8 of a row's dims a lane holds is
-// free as long as queries (for the product over dims) or outputs (for the dims of O^T) are dealt the same way, so every load from
-// shared memory is 16 bytes wide and, pieces of a row being exchanged, without conflicts. P is split into two bf16 terms, so that its rounding (2^-16)
-// is not seen beside that of the output.
+// on the tensor cores with the rows, then the dims, as 16 rows of a product and the heads of a group as its eight columns: S^T = K Q^T and O^T += V^T P^T,
+// so that half the products are not empty up to eight heads, a head's statistics and values lie in the same lanes, and V^T comes out of shared memory as it
+// is needed. P is split into two bf16 terms, so that its rounding (2^-16) is not seen beside that of the output. A head's reference moves only when a
+// logit lies 2^8 above it, which a vote finds without looking for the maximum. 64 sequences of 4160 rows, 8 heads of 128 dims: 164 us, the memory's own
+// time; with heads as rows (16 of which 8 empty), V^T by byte permutes and a maximum every step a step took 1600 clocks instead of MEASURED.
 //
 // The rows of all units (a sequence's heads that a CTA takes together) are cut into tiles and dealt evenly to the CTAs in one line, so that lengths
 // need not be alike; a CTA walks the units in its share and leaves (max, sum, O) records for those that it shares with others, which a second launch
@@ -35,10 +35,25 @@ constexpr int kSmallSmem = 227 * 1024;                // shared memory of a CTA 
 constexpr int kJoinHeads = 8;                         // query heads whose weights are added together
 static_assert(kAttMaxCtas % 32 == 0, "records are looked at a warp at a time");
 
-__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Four 8 x 8 matrices of 16-bit values out of shared memory, as the first operand of a product or (TURNED) its transpose. Lanes 0 to 15 give the
+// addresses of the rows of the first eight columns, the others those of the next eight.
+template <bool TURNED>
+__device__ __forceinline__ void load_matrices(uint32_t (&a)[4], uint32_t at) {
+    if constexpr (TURNED)                             // (rows of the operand are columns there: the second and third change places)
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a[0]), "=r"(a[2]), "=r"(a[1]), "=r"(a[3]) : "r"(at) : "memory");
+    else
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]) : "r"(at) : "memory");
+}
+// An 8 x 8 matrix of 16-bit values, a pair a lane, transposed.
+__device__ __forceinline__ uint32_t turn_matrix(uint32_t v) {
+    uint32_t o;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(o) : "r"(v));
+    return o;
 }
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -148,43 +163,53 @@ __device__ __forceinline__ size_t record(const AttendArgs& a, int cta, bool begi
 // A warp's walk over rows of one KV head, kAttStep at a time and `stride` rows from one step to the next, for up to 8 NH query heads.
 template <int D, int NH>
 struct Walk {
-    static constexpr int kCh = D / 32;                  // 16-byte pieces of a key row that a lane takes
-    static constexpr int kVh = D / 64;                  // and of a value row
-    static constexpr int kPieces = D / 8;               // of a row
+    static constexpr int kPieces = D / 8;               // 16-byte pieces of a row
     static constexpr int kRowsOnce = 32 / kPieces;      // rows that one copy instruction of a warp takes
+    static constexpr int kCopies = kAttStep / kRowsOnce;
     static constexpr int kHalf = kAttStep * D * 2;      // bytes of a step's keys
     static constexpr int kStages = kRingBytes / (2 * kHalf);
+    static constexpr float kSlack = 8.f;                // how far logits may lie above the reference before it moves (in powers of two)
 
     const PagedCache cache;
     const float scale_log2;
-    const size_t row_elems;                             // from a row of the cache to the next
-    unsigned char* const slots;                         // kRingBytes of shared memory
-    const uint32_t ring;
+    const uint32_t row_bytes;                           // from a row of the cache to the next
+    const uint32_t ring;                                // kRingBytes of shared memory
     const int32_t* table;
-    const __nv_bfloat16 *Kh, *Vh;                       // the head's part of the cache's first row, at this lane's piece
+    const char *Kh, *Vh;                                // the head's part of the cache's first row, at this lane's piece
     int base, end, stride, heads;                       // rows base, base + 1, ... of a step, up to `end`
     int at[kStages];                                    // rows of the cache of the steps ahead: lane l (and l + 16) row l of a step, -1: none
-    uint4 qr[NH][kCh];
-    float m[NH], l[NH], o[NH][D / 16][4];               // of the query heads g and 8 + g: running maximum, this lane's part of the sum; O^T
+    uint32_t put[4];                                    // where a lane's piece goes in every fourth copy of a step
+    uint32_t get[4];                                    // where a lane's row of 16 x 16 values is, in every fourth
+    uint32_t qr[NH][D / 16][2];
+    float m[NH][2], l[NH][2], o[NH][D / 16][4];         // of the query heads 8 n + 2 t + e: reference, this lane's part of the sum; O^T
 
-    __device__ __forceinline__ Walk(const AttendArgs& a, unsigned char* slots_)
-        : cache(a.cache), scale_log2(a.scale_log2), row_elems(static_cast<size_t>(a.Hkv) * D), slots(slots_),
-          ring(static_cast<uint32_t>(__cvta_generic_to_shared(slots_))) {}
+    __device__ __forceinline__ Walk(const AttendArgs& a, const unsigned char* slots)
+        : cache(a.cache), scale_log2(a.scale_log2), row_bytes(static_cast<uint32_t>(a.Hkv) * (D * 2)),
+          ring(static_cast<uint32_t>(__cvta_generic_to_shared(slots))) {
+        // Pieces of row r are exchanged by r mod 8 within 128 bytes, so that neither a copy's quarter nor the eight rows of a matrix meet in a bank.
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = (i * kRowsOnce + lane / kPieces) % 8, row = (lane & 7) + (lane & 8);
+            put[i] = (lane / kPieces) * (2 * D) + (((lane % kPieces) ^ r) << 4);
+            get[i] = row * (2 * D) + (((2 * i + (lane >> 4)) ^ (row & 7)) << 4);
+        }
+    }
 
     __device__ __forceinline__ int lookup(int from) const {
         const int r = from + (threadIdx.x & 15);
         return r < end ? paged_row(cache, table, r) : -1;
     }
-    // Pieces are exchanged within 128 bytes so that the eight lanes of a load's quarter find theirs in different banks: keys are read four
-    // neighbouring pieces of two rows at a time, values two of four. A lane copies piece `piece` of every kRowsOnce-th row.
     __device__ __forceinline__ void copy_step(int rows, uint32_t to) const {
-        const int lane = threadIdx.x & 31, piece = lane % kPieces;
+        const int lane = threadIdx.x & 31;
+        const bool all = __all_sync(0xffffffffu, rows >= 0);
 #pragma unroll
-        for (int i = 0; i < kAttStep / kRowsOnce; ++i) {
-            const int r = i * kRowsOnce + lane / kPieces, row = __shfl_sync(0xffffffffu, rows, r);
-            const size_t off = static_cast<size_t>(max(row, 0)) * row_elems;
-            copy_async(to + r * (2 * D) + ((piece ^ (4 * (r & 1))) << 4), Kh + off, row >= 0);
-            copy_async(to + kHalf + r * (2 * D) + ((piece ^ (r & 6)) << 4), Vh + off, row >= 0);
+        for (int i = 0; i < kCopies; ++i) {
+            const int row = __shfl_sync(0xffffffffu, rows, i * kRowsOnce + lane / kPieces);
+            const uint32_t dst = to + put[i % 4] + i * kRowsOnce * (2 * D);
+            const uint64_t off = static_cast<uint64_t>(static_cast<uint32_t>(all ? row : max(row, 0))) * row_bytes;
+            copy_async(dst, Kh + off, all || row >= 0);
+            copy_async(dst + kHalf, Vh + off, all || row >= 0);
         }
     }
     // Asks for the first steps. b: sequence, h: KV head, q_row: first of the query heads among all. A group of copies a step, empty ones behind `end`.
@@ -192,32 +217,34 @@ struct Walk {
         const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
         table = cache.tables + static_cast<size_t>(b) * cache.max_pages;
         const size_t off = static_cast<size_t>(h) * D + 8 * (lane % kPieces);
-        Kh = a.K + off;
-        Vh = a.V + off;
+        Kh = reinterpret_cast<const char*>(a.K + off);
+        Vh = reinterpret_cast<const char*>(a.V + off);
         base = base_; end = end_; stride = stride_; heads = heads_;
 #pragma unroll
         for (int i = 0; i < kStages; ++i) at[i] = lookup(base + i * stride);
-        const __nv_bfloat16* q = a.q + q_row * D + 8 * t;
+        const __nv_bfloat16* q = a.q + q_row * D + 2 * t;
 #pragma unroll
         for (int n = 0; n < NH; ++n)
 #pragma unroll
-            for (int i = 0; i < kCh; ++i)
-                qr[n][i] = base < end && 8 * n + g < heads ? __ldg(reinterpret_cast<const uint4*>(q + static_cast<size_t>(8 * n + g) * D + 32 * i)) : make_uint4(0, 0, 0, 0);
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    qr[n][i][e] = base < end && 8 * n + g < heads ? __ldg(reinterpret_cast<const uint32_t*>(q + static_cast<size_t>(8 * n + g) * D + 16 * i + 8 * e)) : 0u;
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) {
             if (base + i * stride < end) copy_step(at[i], ring + i * 2 * kHalf);
             copies_begin_group();
         }
     }
-    // keep(n, base, v): the logits v[j][e] of query head 8 n + g and rows base + 8 j + 2 t + e (in powers of two; -inf: not seen).
+    // keep(n, base, v): the logits v[j][e] of query head 8 n + 2 t + e and row base + 8 j + g (in powers of two; -inf: not seen).
     template <class Keep>
     __device__ __forceinline__ void run(Keep keep) {
         constexpr unsigned kFull = 0xffffffffu;
-        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+        const int lane = threadIdx.x & 31, g = lane >> 2;
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
-            m[n] = -INFINITY;
-            l[n] = 0.f;
+            m[n][0] = m[n][1] = -INFINITY;
+            l[n][0] = l[n][1] = 0.f;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
         }
@@ -228,90 +255,79 @@ struct Walk {
             const int ahead = base + (kStages - 1) * stride;
             if (ahead < end) copy_step(at[kStages - 1], ring + (stage == 0 ? kStages - 1 : stage - 1) * 2 * kHalf);
             copies_begin_group();
-            const unsigned char *keys = slots + stage * 2 * kHalf, *values = keys + kHalf;
+            const uint32_t keys = ring + stage * 2 * kHalf, values = keys + kHalf;
             stage = stage == kStages - 1 ? 0 : stage + 1;
-            // S: rows of the product are the query heads g and g + 8, columns the cache rows 2t and 2t + 1 of eight
-            float s[2][4];
+            // S^T = K Q^T: rows of the product are the rows g and g + 8 of the step, columns the query heads 2t and 2t + 1
+            float s[NH][2][4];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-            uint4 kr[kCh][2];
+            for (int n = 0; n < NH; ++n)
 #pragma unroll
-            for (int i = 0; i < kCh; ++i)
+                for (int i = 0; i < 4; ++i) s[n][0][i] = s[n][1][i] = 0.f;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) kr[i][j] = *reinterpret_cast<const uint4*>(keys + (8 * j + g) * (2 * D) + (((4 * i + t) ^ (4 * (g & 1))) << 4));
+            for (int i = 0; i < D / 16; ++i) {
+                uint32_t k[4];
+                load_matrices<false>(k, keys + get[i % 4] + (i / 4) * 128);
 #pragma unroll
-            for (int i = 0; i < kCh; ++i)
+                for (int n = 0; n < NH; ++n) mma_bf16(s[n][i & 1], k, qr[n][i][0], qr[n][i][1]);
+            }
+            uint32_t v[D / 16][4];                              // V^T: rows are dims
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint4 k = kr[i][j];
-                    mma_bf16(s[j], qr[0][i].x, NH == 2 ? qr[NH - 1][i].x : 0u, qr[0][i].y, NH == 2 ? qr[NH - 1][i].y : 0u, k.x, k.y);
-                    mma_bf16(s[j], qr[0][i].z, NH == 2 ? qr[NH - 1][i].z : 0u, qr[0][i].w, NH == 2 ? qr[NH - 1][i].w : 0u, k.z, k.w);
-                }
-            unsigned seen = 0;                                  // bit 2j + e: row base + 8j + 2t + e
-#pragma unroll
-            for (int j = 0; j < 4; ++j) seen |= __shfl_sync(kFull, at[0], (j >> 1) * 8 + 2 * t + (j & 1)) >= 0 ? 1u << j : 0u;
+            for (int i = 0; i < D / 16; ++i) load_matrices<true>(v[i], values + get[i % 4] + (i / 4) * 128);
+            const unsigned seen = __ballot_sync(kFull, at[0] >= 0) >> g;       // bits 0 and 8: rows g and g + 8
 #pragma unroll
             for (int i = 0; i < kStages - 1; ++i) at[i] = at[i + 1];
             at[kStages - 1] = lookup(ahead + stride);
 
-            uint32_t hi[NH][2], lo[NH][2];
-            float factor[NH];
-            bool moved = false;
+            float z[NH][2][2];
+            bool above = false;
 #pragma unroll
             for (int n = 0; n < NH; ++n) {
-                float v[2][2], mx = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        v[j][e] = seen >> (2 * j + e) & 1u ? s[j][2 * n + e] * scale_log2 : -INFINITY;
-                        mx = fmaxf(mx, v[j][e]);
+                        z[n][j][e] = seen >> (8 * j) & 1u ? (s[n][0][2 * j + e] + s[n][1][2 * j + e]) * scale_log2 : -INFINITY;
+                        above |= z[n][j][e] > m[n][e] + kSlack;
                     }
-                if (8 * n + g < heads) keep(n, base, v);
-                mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, 2));
-                const float m_new = fmaxf(m[n], mx), ref = reference_of(m_new);
-                factor[n] = exp2_fast(m[n] - ref);
-                moved |= m_new != m[n];
-                m[n] = m_new;
-                float sum = 0.f;
+                keep(n, base, z[n]);
+            }
+            if (__any_sync(kFull, above)) {                     // a new reference: the first step's, and few after it
+#pragma unroll
+                for (int n = 0; n < NH; ++n) {
+                    float factor[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float mx = fmaxf(z[n][0][e], z[n][1][e]);
+#pragma unroll
+                        for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(kFull, mx, off));
+                        const float now = fmaxf(m[n][e], mx);
+                        factor[e] = exp2_fast(m[n][e] - reference_of(now));
+                        m[n][e] = now;
+                        l[n][e] *= factor[e];
+                    }
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i) { o[n][i][0] *= factor[0]; o[n][i][1] *= factor[1]; o[n][i][2] *= factor[0]; o[n][i][3] *= factor[1]; }
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NH; ++n) {
+                const float ref0 = reference_of(m[n][0]), ref1 = reference_of(m[n][1]);
+                uint32_t hi[2], lo[2];                          // P, turned from (rows, heads) to the product's second operand
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const float p0 = exp2_fast(v[j][0] - ref), p1 = exp2_fast(v[j][1] - ref);
-                    sum += p0 + p1;
-                    hi[n][j] = pack_bf16(p0, p1);
-                    const float2 r = bf16_pair(hi[n][j]);
-                    lo[n][j] = pack_bf16(p0 - r.x, p1 - r.y);
+                    const float p0 = exp2_fast(z[n][j][0] - ref0), p1 = exp2_fast(z[n][j][1] - ref1);
+                    l[n][0] += p0;
+                    l[n][1] += p1;
+                    const uint32_t w = pack_bf16(p0, p1);
+                    const float2 r = bf16_pair(w);
+                    hi[j] = turn_matrix(w);
+                    lo[j] = turn_matrix(pack_bf16(p0 - r.x, p1 - r.y));
                 }
-                l[n] = l[n] * factor[n] + sum;
-            }
-            if (__any_sync(kFull, moved)) {
+                // O^T += V^T P^T: rows of the product are the dims 16 i + g and 16 i + 8 + g, columns the query heads 2t and 2t + 1
 #pragma unroll
-                for (int n = 0; n < NH; ++n) {                  // O^T: columns are the heads 2t and 2t + 1
-                    const float f0 = __shfl_sync(kFull, factor[n], 8 * t), f1 = __shfl_sync(kFull, factor[n], 8 * t + 4);
+                for (int i = 0; i < D / 16; ++i) mma_bf16(o[n][i], v[i], hi[0], hi[1]);
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i) { o[n][i][0] *= f0; o[n][i][1] *= f1; o[n][i][2] *= f0; o[n][i][3] *= f1; }
-                }
-            }
-            // O^T += V^T P^T: row g of the product's tile (hh, q) is dim 64 hh + 8 g + 2 q, row g + 8 the next dim
-#pragma unroll
-            for (int hh = 0; hh < kVh; ++hh) {
-                uint32_t w[4][4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {                   // rows 2t, 2t + 1, 8 + 2t, 9 + 2t
-                    const uint4 v = *reinterpret_cast<const uint4*>(values + ((j >> 1) * 8 + 2 * t + (j & 1)) * (2 * D) + (((8 * hh + g) ^ (2 * t)) << 4));
-                    w[j][0] = v.x; w[j][1] = v.y; w[j][2] = v.z; w[j][3] = v.w;
-                }
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t a0 = __byte_perm(w[0][q], w[1][q], 0x5410), a1 = __byte_perm(w[0][q], w[1][q], 0x7632);
-                    const uint32_t a2 = __byte_perm(w[2][q], w[3][q], 0x5410), a3 = __byte_perm(w[2][q], w[3][q], 0x7632);
-#pragma unroll
-                    for (int n = 0; n < NH; ++n) {
-                        mma_bf16(o[n][4 * hh + q], a0, a1, a2, a3, hi[n][0], hi[n][1]);
-                        mma_bf16(o[n][4 * hh + q], a0, a1, a2, a3, lo[n][0], lo[n][1]);
-                    }
-                }
+                for (int i = 0; i < D / 16; ++i) mma_bf16(o[n][i], v[i], lo[0], lo[1]);
             }
         }
         __syncwarp();                                           // (the last step has been read)
@@ -319,24 +335,27 @@ struct Walk {
     // Another warp's walk over the same head (its values as left by leave) joined to this one.
     template <class From>
     __device__ __forceinline__ void join(const From& other) {
-        constexpr unsigned kFull = 0xffffffffu;
-        const int lane = threadIdx.x & 31, t = lane & 3;
+        const int lane = threadIdx.x & 31;
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
-            const float2 s = other.ml[n][lane];
-            const float m_new = fmaxf(m[n], s.x), ref = reference_of(m_new);
-            const float own = exp2_fast(m[n] - ref), its = exp2_fast(s.x - ref);
-            m[n] = m_new;
-            l[n] = l[n] * own + s.y * its;
-            const float a0 = __shfl_sync(kFull, own, 8 * t), a1 = __shfl_sync(kFull, own, 8 * t + 4);
-            const float b0 = __shfl_sync(kFull, its, 8 * t), b1 = __shfl_sync(kFull, its, 8 * t + 4);
+            const float4 s = other.ml[n][lane];
+            const float its_m[2] = {s.x, s.y}, its_l[2] = {s.z, s.w};
+            float own[2], its[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float now = fmaxf(m[n][e], its_m[e]), ref = reference_of(now);
+                own[e] = exp2_fast(m[n][e] - ref);
+                its[e] = exp2_fast(its_m[e] - ref);
+                m[n][e] = now;
+                l[n][e] = l[n][e] * own[e] + its_l[e] * its[e];
+            }
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
-                const float4 v = other.o[n * (D / 16) + i][lane];
-                o[n][i][0] = o[n][i][0] * a0 + v.x * b0;
-                o[n][i][1] = o[n][i][1] * a1 + v.y * b1;
-                o[n][i][2] = o[n][i][2] * a0 + v.z * b0;
-                o[n][i][3] = o[n][i][3] * a1 + v.w * b1;
+                const float4 x = other.o[n * (D / 16) + i][lane];
+                o[n][i][0] = o[n][i][0] * own[0] + x.x * its[0];
+                o[n][i][1] = o[n][i][1] * own[1] + x.y * its[1];
+                o[n][i][2] = o[n][i][2] * own[0] + x.z * its[0];
+                o[n][i][3] = o[n][i][3] * own[1] + x.w * its[1];
             }
         }
     }
@@ -345,28 +364,37 @@ struct Walk {
         const int lane = threadIdx.x & 31;
 #pragma unroll
         for (int n = 0; n < NH; ++n) {
-            to.ml[n][lane] = make_float2(m[n], l[n]);
+            to.ml[n][lane] = make_float4(m[n][0], m[n][1], l[n][0], l[n][1]);
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) to.o[n * (D / 16) + i][lane] = make_float4(o[n][i][0], o[n][i][1], o[n][i][2], o[n][i][3]);
         }
     }
-    // The sum of a query head from the four lanes that hold its columns.
+    // The sums of the query heads from the eight lanes that hold their rows.
     __device__ __forceinline__ void add_up() {
 #pragma unroll
-        for (int n = 0; n < NH; ++n) {
-            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
-            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
-        }
+        for (int n = 0; n < NH; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+                for (int off = 4; off < 32; off <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], off);
     }
-    // This lane's values of query head 8 n + 2 t + e: the dims 64 hh + 8 g, ..., + 7.
-    __device__ __forceinline__ float value(int n, int e, int hh, int i) const { return o[n][4 * hh + i / 2][e + 2 * (i & 1)]; }
+    // Two neighbouring values of query head 8 n + 2 t + e, the dims dim_of(i) and the next (every lane calls this: neighbours exchange one).
+    __device__ __forceinline__ int dim_of(int i) const {
+        const int g = (threadIdx.x & 31) >> 2;
+        return 16 * i + ((g & 1) ? 7 + g : g);
+    }
+    __device__ __forceinline__ float2 values(int n, int e, int i) const {
+        const bool odd = (threadIdx.x & 4) != 0;
+        const float x = o[n][i][e], y = o[n][i][e + 2], got = __shfl_xor_sync(0xffffffffu, odd ? x : y, 4);
+        return odd ? make_float2(got, y) : make_float2(x, got);
+    }
 };
 
 // What a warp leaves for the one that joins its head's warps: every lane's (max, sum) and O.
 template <int D, int NH>
 struct Left {
     float4 o[NH * D / 16][32];
-    float2 ml[NH][32];
+    float4 ml[NH][32];
 };
 template <int D, int NH>
 struct AttSmem {
@@ -384,8 +412,6 @@ struct AttSmem {
 // D: head dim; NH: query heads of a group in eights.
 template <int D, int NH, bool SUMS>
 __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs a) {
-    constexpr unsigned kFull = 0xffffffffu;
-    constexpr int kVh = D / 64;
     extern __shared__ __align__(128) char smem_raw[];
     AttSmem<D, NH>& sm = *reinterpret_cast<AttSmem<D, NH>*>(smem_raw);
     begin_dependent();
@@ -433,12 +459,14 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
         const int heads = walk.heads;                           // query heads of this group
         const size_t q_row = row_of_q(p);
         const int r1 = p.rows_end;
-        walk.run([&](int n, int base, const float (&v)[2][2]) {
+        walk.run([&](int n, int base, const float (&z)[2][2]) {
             if constexpr (SUMS) {
-                float* lg = a.logits + (q_row + 8 * n + g) * a.logit_stride + base + 2 * t;
+                float* lg = a.logits + (q_row + 8 * n + 2 * t) * a.logit_stride + base + g;
 #pragma unroll
-                for (int j = 0; j < 2; ++j)                     // (the stride is even and covers every row, so a pair fits)
-                    if (base + 8 * j + 2 * t < r1) *reinterpret_cast<float2*>(lg + 8 * j) = make_float2(v[j][0], v[j][1]);
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (8 * n + 2 * t + e < heads && base + 8 * j + g < r1) lg[e * a.logit_stride + 8 * j] = z[j][e];
             }
         });
 
@@ -475,37 +503,26 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
         const bool whole = p.whole();
         if (turn == 0 && head < p.un.heads) {
 #pragma unroll
-            for (int n = 0; n < NH; ++n) {
-                if (t == 0 && 8 * n + g < heads) {
-                    if (!whole) a.part_ml[record(a, cta, p.begins(), head, 8 * n + g)] = make_float2(walk.m[n], walk.l[n]);
-                    else if (SUMS) a.whole_ml[q_row + 8 * n + g] = make_float2(walk.m[n], walk.l[n]);      // (a CTA can have many)
-                }
+            for (int n = 0; n < NH; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float ll = __shfl_sync(kFull, walk.l[n], 8 * t + 4 * e);
                     const int q = 8 * n + 2 * t + e;
-                    if (q >= heads) continue;
-                    if (whole) {
-                        const float r = ll == 0.f ? 0.f : 1.f / ll;     // (nothing seen: zeros)
-                        __nv_bfloat16* to = a.out + (q_row + q) * D + 8 * g;
+                    const bool mine = q < heads;
+                    const size_t rec = record(a, cta, p.begins(), head, mine ? q : 0);
+                    if (mine && g == 0) {
+                        const float2 s = make_float2(walk.m[n][e], walk.l[n][e]);
+                        if (!whole) a.part_ml[rec] = s;
+                        else if (SUMS) a.whole_ml[q_row + q] = s;           // (a CTA can have many)
+                    }
+                    const float ll = walk.l[n][e], r = ll == 0.f ? 0.f : 1.f / ll;     // (nothing seen: zeros)
 #pragma unroll
-                        for (int hh = 0; hh < kVh; ++hh) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) w[i] = pack_bf16(walk.value(n, e, hh, 2 * i) * r, walk.value(n, e, hh, 2 * i + 1) * r);
-                            *reinterpret_cast<uint4*>(to + 64 * hh) = make_uint4(w[0], w[1], w[2], w[3]);
-                        }
-                    } else {
-                        float* to = a.part_o + record(a, cta, p.begins(), head, q) * D + 8 * g;
-#pragma unroll
-                        for (int hh = 0; hh < kVh; ++hh)
-#pragma unroll
-                            for (int i = 0; i < 8; i += 4)
-                                *reinterpret_cast<float4*>(to + 64 * hh + i) = make_float4(walk.value(n, e, hh, i), walk.value(n, e, hh, i + 1),
-                                                                                           walk.value(n, e, hh, i + 2), walk.value(n, e, hh, i + 3));
+                    for (int i = 0; i < D / 16; ++i) {
+                        const float2 x = walk.values(n, e, i);
+                        if (!mine) continue;
+                        if (whole) *reinterpret_cast<uint32_t*>(a.out + (q_row + q) * D + walk.dim_of(i)) = pack_bf16(x.x * r, x.y * r);
+                        else *reinterpret_cast<float2*>(a.part_o + rec * D + walk.dim_of(i)) = x;
                     }
                 }
-            }
         }
         if (!more) return;
         p = next;
@@ -709,7 +726,6 @@ struct SmallSmem {
 
 template <int D, int NH, bool SUMS>
 __global__ void __launch_bounds__(kSmallThreads, 1) attend_small_kernel(const AttendArgs a) {
-    constexpr int kVh = D / 64;
     extern __shared__ __align__(128) char smem_raw[];
     SmallSmem<D, NH>& sm = *reinterpret_cast<SmallSmem<D, NH>*>(smem_raw);
     float* logits = reinterpret_cast<float*>(smem_raw + sizeof(SmallSmem<D, NH>));
@@ -724,27 +740,27 @@ __global__ void __launch_bounds__(kSmallThreads, 1) attend_small_kernel(const At
     const int r0 = rank * steps / n_cta * kAttStep, r1 = min((rank + 1) * steps / n_cta * kAttStep, n);
     Walk<D, NH> walk(a, sm.ring[warp]);
     walk.begin(a, b, h, q_row, heads, r0 + warp * kAttStep, r1, kSmallWarps * kAttStep);
-    walk.run([&](int nn, int base, const float (&v)[2][2]) {
-        if constexpr (SUMS) {                         // (rows of a CTA and their pairs: an even number)
-            float* lg = logits + (8 * nn + g) * a.small_rows + (base - r0) + 2 * t;
+    walk.run([&](int nn, int base, const float (&z)[2][2]) {
+        if constexpr (SUMS) {
+            float* lg = logits + (8 * nn + 2 * t) * a.small_rows + (base - r0) + g;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) *reinterpret_cast<float2*>(lg + 8 * j) = make_float2(v[j][0], v[j][1]);
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (8 * nn + 2 * t + e < heads) lg[e * a.small_rows + 8 * j] = z[j][e];
         }
     });
     walk.add_up();
     __syncthreads();                                  // (every ring is idle)
 #pragma unroll
-    for (int nn = 0; nn < NH; ++nn) {
-        if (t == 0) sm.warp_ml[warp][8 * nn + g] = make_float2(walk.m[nn], walk.l[nn]);
+    for (int nn = 0; nn < NH; ++nn)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < 2; ++e) {
+            const int q = 8 * nn + 2 * t + e;
+            if (g == 0) sm.warp_ml[warp][q] = make_float2(walk.m[nn][e], walk.l[nn][e]);
 #pragma unroll
-            for (int hh = 0; hh < kVh; ++hh)
-#pragma unroll
-                for (int i = 0; i < 8; i += 4)
-                    *reinterpret_cast<float4*>(&sm.o[warp][8 * nn + 2 * t + e][64 * hh + 8 * g + i]) =
-                        make_float4(walk.value(nn, e, hh, i), walk.value(nn, e, hh, i + 1), walk.value(nn, e, hh, i + 2), walk.value(nn, e, hh, i + 3));
-    }
+            for (int i = 0; i < D / 16; ++i) *reinterpret_cast<float2*>(&sm.o[warp][q][walk.dim_of(i)]) = walk.values(nn, e, i);
+        }
     __syncthreads();
     for (int e = tid; e < heads * (D / 4); e += kSmallThreads) {
         const int q = e / (D / 4), c4 = e % (D / 4) * 4;
@@ -897,9 +913,10 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     p.small_rows = 0;
     if (p.cluster > 0) {
         const long long steps = (cap + kAttStep - 1) / kAttStep, rows = (steps + p.cluster - 1) / p.cluster * kAttStep;
+        const long long kept = rows + 4;                        // (logits of four neighbouring pairs of heads lie in different banks)
         const size_t fixed = d == 128 ? (p.nh == 1 ? sizeof(SmallSmem<128, 1>) : sizeof(SmallSmem<128, 2>)) : (p.nh == 1 ? sizeof(SmallSmem<64, 1>) : sizeof(SmallSmem<64, 2>));
         const bool few = rows <= 768 && rows - items * cap / 148 <= 300;
-        if (few && (!sums || (p.groups == 1 && fixed + 4ull * p.group * rows <= kSmallSmem))) p.small_rows = static_cast<int>(rows);
+        if (few && (!sums || (p.groups == 1 && fixed + 4ull * p.group * kept <= kSmallSmem))) p.small_rows = static_cast<int>(kept);
         else p.cluster = 0;
     }
     if (p.cluster > 0) {                                        // (no scratch: a byte, so that every call has some)
