@@ -4,10 +4,11 @@
 // fills the j-th free place below it, and the r rows follow, in their order. (Attention does not depend on the order of rows; with the chunks in
 // ascending order nearly every row behind the first evicted chunk would move.)
 //
-// A cluster of 1, 2, 4 or 8 CTAs works on a head. Each finds the selection itself - the k-th largest sum exactly, by an adaptive radix select, as
-// select.cuh does; a chain of latencies on a few thousand keys - and takes its part of the moves. Places in the way of one another are kept apart by cluster
-// barriers: nobody writes before all have read the sums; the chunks move before the rows behind them, whose new places may be those chunks'
-// old ones; those rows move in blocks from the lowest on, each read by all before any is written.
+// A cluster of 1, 2, 4 or 8 CTAs works on a head. Each finds the selection itself - a chain of latencies on a few thousand keys: select.cuh's body with keys
+// in registers up to 24 a thread, beyond that (or for more kept chunks than it lists) a radix select that reads them again - and takes its
+// part of the moves. Places in the way of one another are kept apart by cluster barriers: nobody writes before all have read the sums; the chunks
+// move before the rows behind them, whose new places may be those chunks' old ones; those rows move in blocks from the lowest on, each read by
+// all before any is written, the first of them (mostly the only one) before the chunks move.
 #include "decode.cuh"
 #include "select.cuh"
 
@@ -23,19 +24,24 @@ constexpr int kEvThreads = 512;
 constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvAhead = 4;               // 16-byte pieces that a thread has in flight
 
-struct EvictSmem {
+struct RadixSmem {
     alignas(16) int hist[kSelBins];
     int4 cnt[kEvWarps];                   // a warp's chunks: above the threshold, equal to it; the same below place k
     uint2 range[kEvWarps];
     int warp_tot[kEvWarps];
     int2 found;
 };
+union EvictSmem {
+    SelectSmem sel;
+    RadixSmem radix;
+};
+constexpr int kEvMaxKeys = 24;            // keys of a thread in registers, at most
 
 // Order of sums: not-a-number above everything (as torch sorts it), -0 as +0.
 __device__ __forceinline__ uint32_t evict_key(float x) { return x != x ? 0xffffffffu : select_order_key(x); }
 
 template <int VPR>
-__global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
+__global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictArgs a) {
     constexpr unsigned kFull = 0xffffffffu;
     extern __shared__ __align__(16) char smem_raw[];
     EvictSmem& sm = *reinterpret_cast<EvictSmem*>(smem_raw);
@@ -58,17 +64,64 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
     }
     const int C = (n - a.w) / c, r = n - C * c, k = (a.budget - r) / c;     // k < C, as n is above the budget
 
-    // ---- the k-th largest sum: thresh, of which the first need_eq chunks are kept
+    // ---- which chunks stay: lists of those that move and of the places that are free
     auto key_of = [&](int ch) -> uint32_t {
         if (c == 1) return evict_key(weights[ch]);
+        const float* w = weights + static_cast<size_t>(ch) * c;
         double sum = 0.0;                                           // (in order and 64 bits, rounded once: equal sums are equal)
-        for (int i = 0; i < c; ++i) sum += static_cast<double>(weights[static_cast<size_t>(ch) * c + i]);
+        for (int i0 = 0; i0 < c; i0 += 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i0 + i < c ? w[i0 + i] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += static_cast<double>(v[i]);
+        }
         return evict_key(static_cast<float>(sum));
     };
-    const bool staged = C <= a.key_cap;
-    auto key_at = [&](int ch) { return staged ? kbuf[ch] : key_of(ch); };
-    uint32_t lo = 0xffffffffu, hi = 0u;
-    if (k > 0) {
+    for (int i = part; i < k * c; i += parts) idx[i] = i;           // (rows that move overwrite theirs behind the barrier)
+    const unsigned short* moved = from;
+    int stay = 0;
+    if (k > 0 && C <= kEvMaxKeys * kEvThreads && C <= a.key_cap && k <= kSelCap) {
+        uint32_t lo = 0xffffffffu, hi = 0u;
+#pragma unroll 4
+        for (int ch = tid; ch < C; ch += kEvThreads) {
+            const uint32_t key = key_of(ch);
+            kbuf[ch] = key;
+            lo = min(lo, key);
+            hi = max(hi, key);
+        }
+        lo = __reduce_min_sync(kFull, lo);
+        hi = __reduce_max_sync(kFull, hi);
+        if (lane == 0) sm.sel.warp_sums[warp] = static_cast<unsigned long long>(hi) << 32 | lo;
+        select_clear(sm.sel);
+        __syncthreads();
+        const int per = (C + kEvThreads - 1) / kEvThreads;
+        if (per <= 2) select_staged<2>(kbuf, C, k, sm.sel);
+        else if (per <= 4) select_staged<4>(kbuf, C, k, sm.sel);
+        else if (per <= 6) select_staged<6>(kbuf, C, k, sm.sel);
+        else if (per <= 8) select_staged<8>(kbuf, C, k, sm.sel);
+        else if (per <= 10) select_staged<10>(kbuf, C, k, sm.sel);
+        else if (per <= 12) select_staged<12>(kbuf, C, k, sm.sel);
+        else select_staged<kEvMaxKeys>(kbuf, C, k, sm.sel);
+        // The kept chunks are in ascending order: `stay` of them lie below k, and the j-th free place below k is j + i, where i of them lie below it.
+        const unsigned short* kept = sm.sel.sel;
+        auto count = [&](int most, auto before) {                   // of the first `most`, those that come first and of which that holds
+            int lo_i = 0, hi_i = most;
+            while (lo_i < hi_i) {
+                const int mid = (lo_i + hi_i) >> 1;
+                if (before(mid)) lo_i = mid + 1;
+                else hi_i = mid;
+            }
+            return lo_i;
+        };
+        stay = count(k, [&](int i) { return kept[i] < k; });
+        for (int j = tid; j < k - stay; j += kEvThreads) to[j] = static_cast<unsigned short>(j + count(stay, [&](int i) { return kept[i] - i <= j; }));
+        __syncthreads();
+        moved = kept + stay;
+    } else if (k > 0) {
+        const bool staged = C <= a.key_cap;
+        auto key_at = [&](int ch) { return staged ? kbuf[ch] : key_of(ch); };
+        uint32_t lo = 0xffffffffu, hi = 0u;
 #pragma unroll 4
         for (int ch = tid; ch < C; ch += kEvThreads) {
             const uint32_t key = key_of(ch);
@@ -76,31 +129,27 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
             lo = min(lo, key);
             hi = max(hi, key);
         }
-    }
-    lo = __reduce_min_sync(kFull, lo);
-    hi = __reduce_max_sync(kFull, hi);
-    if (lane == 0) sm.range[warp] = make_uint2(lo, hi);
-    for (int i = tid; i < kSelBins; i += kEvThreads) sm.hist[i] = 0;
-    __syncthreads();
-    uint32_t thresh = 0xffffffffu;
-    int need_eq = 0;                                                // (k = 0: nothing is kept)
-    if (k > 0) {
-        const uint2 mm = sm.range[lane & (kEvWarps - 1)];
+        lo = __reduce_min_sync(kFull, lo);
+        hi = __reduce_max_sync(kFull, hi);
+        if (lane == 0) sm.radix.range[warp] = make_uint2(lo, hi);
+        for (int i = tid; i < kSelBins; i += kEvThreads) sm.radix.hist[i] = 0;
+        __syncthreads();
+        const uint2 mm = sm.radix.range[lane & (kEvWarps - 1)];
         uint32_t base = __reduce_min_sync(kFull, mm.x), span = __reduce_max_sync(kFull, mm.y) - base;
         int need = k;                                               // the need-th largest key in [base, base + span]
         for (int round = 0; span != 0u; ++round) {
             const int shift = max(0, 21 - __clz(span));             // (span >> shift) < kSelBins
             if (round > 0) {
-                for (int i = tid; i < kSelBins; i += kEvThreads) sm.hist[i] = 0;
+                for (int i = tid; i < kSelBins; i += kEvThreads) sm.radix.hist[i] = 0;
                 __syncthreads();
             }
             for (int ch = tid; ch < C; ch += kEvThreads) {
                 const uint32_t dlt = key_at(ch) - base;             // (a key below base wraps to more than span)
-                if (dlt <= span) atomicAdd(&sm.hist[dlt >> shift], 1);
+                if (dlt <= span) atomicAdd(&sm.radix.hist[dlt >> shift], 1);
             }
             __syncthreads();
             // thread t has the bins 2047 - 4t .. 2044 - 4t, so a prefix over threads counts from the top
-            const int4 b4 = *reinterpret_cast<const int4*>(sm.hist + kSelBins - 4 - 4 * tid);
+            const int4 b4 = *reinterpret_cast<const int4*>(sm.radix.hist + kSelBins - 4 - 4 * tid);
             const int cnt[4] = {b4.w, b4.z, b4.y, b4.x};
             const int sum = (cnt[0] + cnt[1]) + (cnt[2] + cnt[3]);
             int inc = sum;
@@ -109,32 +158,30 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
                 const int v = __shfl_up_sync(kFull, inc, off);
                 if (lane >= off) inc += v;
             }
-            if (lane == 31) sm.warp_tot[warp] = inc;
+            if (lane == 31) sm.radix.warp_tot[warp] = inc;
             __syncthreads();
-            inc += __reduce_add_sync(kFull, lane < warp ? sm.warp_tot[lane & (kEvWarps - 1)] : 0);
+            inc += __reduce_add_sync(kFull, lane < warp ? sm.radix.warp_tot[lane & (kEvWarps - 1)] : 0);
             if (inc - sum < need && need <= inc) {                  // one thread
                 int above = inc - sum, q = 0;
 #pragma unroll
                 for (int i = 0; i < 3; ++i)                         // (unrolled: cnt stays in registers)
                     if (q == i && above + cnt[i] < need) { above += cnt[i]; q = i + 1; }
-                sm.found = make_int2(kSelBins - 1 - 4 * tid - q, need - above);
+                sm.radix.found = make_int2(kSelBins - 1 - 4 * tid - q, need - above);
             }
             __syncthreads();
-            const int2 f = sm.found;
+            const int2 f = sm.radix.found;
             need = f.y;
             const uint32_t sub = static_cast<uint32_t>(f.x) << shift;
             base += sub;
             span = min((1u << shift) - 1u, span - sub);
         }
-        thresh = base;
-        need_eq = need;
-    }
+        const uint32_t thresh = base;
+        const int need_eq = need;                                   // of those equal to it, the first so many are kept
 
-    // ---- lists of the moves. A warp has a block of consecutive chunks and walks it 32 at a time.
-    const int rows = (C + kEvThreads - 1) / kEvThreads, first = warp * rows * 32;
-    const unsigned below = (1u << lane) - 1u;
-    int4 mine = make_int4(0, 0, 0, 0);
-    if (k > 0) {
+        // ---- lists of the moves. A warp has a block of consecutive chunks and walks it 32 at a time.
+        const int rows = (C + kEvThreads - 1) / kEvThreads, first = warp * rows * 32;
+        const unsigned below = (1u << lane) - 1u;
+        int4 mine = make_int4(0, 0, 0, 0);
         for (int u = 0; u < rows; ++u) {
             const int ch = first + 32 * u + lane;
             const uint32_t key = ch < C ? key_at(ch) : 0u;
@@ -145,19 +192,17 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
             mine.z += __popc(gt & low);
             mine.w += __popc(eq & low);
         }
-    }
-    if (lane == 0) sm.cnt[warp] = mine;
-    __syncthreads();
-    int gt_run = 0, eq_run = 0, low_gt = 0, low_eq = 0;
+        if (lane == 0) sm.radix.cnt[warp] = mine;
+        __syncthreads();
+        int gt_run = 0, eq_run = 0, low_gt = 0, low_eq = 0;
 #pragma unroll
-    for (int v = 0; v < kEvWarps; ++v) {
-        const int4 x = sm.cnt[v];
-        if (v < warp) { gt_run += x.x; eq_run += x.y; }
-        low_gt += x.z;
-        low_eq += x.w;
-    }
-    const int stay = low_gt + min(low_eq, need_eq), moves = k - stay;       // kept chunks that stay; as many move as places below k are free
-    if (k > 0) {
+        for (int v = 0; v < kEvWarps; ++v) {
+            const int4 x = sm.radix.cnt[v];
+            if (v < warp) { gt_run += x.x; eq_run += x.y; }
+            low_gt += x.z;
+            low_eq += x.w;
+        }
+        stay = low_gt + min(low_eq, need_eq);
         for (int u = 0; u < rows; ++u) {
             const int ch = first + 32 * u + lane;
             const uint32_t key = ch < C ? key_at(ch) : 0u;
@@ -168,8 +213,6 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
             const bool kept = gt || (eq && eq_before < need_eq);
             if (ch < k) {
                 if (!kept) to[ch - before] = static_cast<unsigned short>(ch);
-                else if (n_cta == 1 || ch % n_cta == rank)
-                    for (int i = 0; i < c; ++i) idx[ch * c + i] = ch * c + i;
             } else if (kept) {
                 from[before - stay] = static_cast<unsigned short>(ch);
             }
@@ -177,6 +220,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
             eq_run += __popc(eqm);
         }
     }
+    const int moves = k - stay;                                     // as many move as places below k are free
     cluster.sync();          // the lists are there, and every CTA has read the sums and the length
 
     // ---- the chunks: a piece of 16 bytes of a row's keys or values an item
@@ -196,6 +240,33 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
         uint4* p = piece(row, vec);
         if (p != nullptr) *p = v;
     };
+    // the r rows behind the chunks go in blocks of kEvAhead pieces a thread (a piece more a row: its sum)
+    constexpr int kItems = 2 * VPR + 1;
+    const long long items = static_cast<long long>(r) * kItems, block = static_cast<long long>(kEvAhead) * parts;
+    uint4 w[kEvAhead];
+    auto load_block = [&](long long i0) {
+#pragma unroll
+        for (int u = 0; u < kEvAhead; ++u) {
+            const long long i = i0 + static_cast<long long>(u) * parts + part;
+            if (i < items) {
+                const int row = static_cast<int>(i / kItems), vec = static_cast<int>(i % kItems);
+                if (vec < 2 * VPR) w[u] = load_piece(src_r + row, vec);
+                else w[u].x = __float_as_uint(weights[src_r + row]);
+            }
+        }
+    };
+    auto store_block = [&](long long i0) {
+#pragma unroll
+        for (int u = 0; u < kEvAhead; ++u) {
+            const long long i = i0 + static_cast<long long>(u) * parts + part;
+            if (i < items) {
+                const int row = static_cast<int>(i / kItems), vec = static_cast<int>(i % kItems);
+                if (vec < 2 * VPR) store_piece(dst_r + row, vec, w[u]);
+                else weights[dst_r + row] = __uint_as_float(w[u].x);
+            }
+        }
+    };
+    load_block(0);
     for (long long i0 = part; i0 < static_cast<long long>(chunk_rows) * 2 * VPR; i0 += static_cast<long long>(kEvAhead) * parts) {
         uint4 v[kEvAhead];
         int dst[kEvAhead], vec[kEvAhead];
@@ -207,7 +278,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
                 const int row = static_cast<int>(i / (2 * VPR)), j = row / c, off = row - j * c;
                 vec[u] = static_cast<int>(i % (2 * VPR));
                 dst[u] = to[j] * c + off;
-                v[u] = load_piece(from[j] * c + off, vec[u]);
+                v[u] = load_piece(moved[j] * c + off, vec[u]);
             }
         }
 #pragma unroll
@@ -215,37 +286,18 @@ __global__ void __launch_bounds__(kEvThreads) evict_kernel(const EvictArgs a) {
             if (dst[u] >= 0) store_piece(dst[u], vec[u], v[u]);
     }
     for (int i = part; i < chunk_rows; i += parts) {
-        const int j = i / c, off = i - j * c, src = from[j] * c + off, dst = to[j] * c + off;
+        const int j = i / c, off = i - j * c, src = moved[j] * c + off, dst = to[j] * c + off;
         weights[dst] = weights[src];
         idx[dst] = src;
     }
-    cluster.sync();          // their places may be written now
-
-    // ---- the r rows behind the chunks, in blocks of kEvAhead pieces a thread (a piece more a row: its sum)
-    constexpr int kItems = 2 * VPR + 1;
-    for (long long i0 = 0; i0 < static_cast<long long>(r) * kItems; i0 += static_cast<long long>(kEvAhead) * parts) {
-        uint4 v[kEvAhead];
-#pragma unroll
-        for (int u = 0; u < kEvAhead; ++u) {
-            const long long i = i0 + static_cast<long long>(u) * parts + part;
-            if (i < static_cast<long long>(r) * kItems) {
-                const int row = static_cast<int>(i / kItems), vec = static_cast<int>(i % kItems);
-                if (vec < 2 * VPR) v[u] = load_piece(src_r + row, vec);
-                else v[u].x = __float_as_uint(weights[src_r + row]);
-            }
-        }
+    cluster.sync();          // the chunks' old places may be written now, and those of the first block
+    store_block(0);
+    for (long long i0 = block; i0 < items; i0 += block) {
+        load_block(i0);
         cluster.sync();
-#pragma unroll
-        for (int u = 0; u < kEvAhead; ++u) {
-            const long long i = i0 + static_cast<long long>(u) * parts + part;
-            if (i < static_cast<long long>(r) * kItems) {
-                const int row = static_cast<int>(i / kItems), vec = static_cast<int>(i % kItems);
-                if (vec < 2 * VPR) store_piece(dst_r + row, vec, v[u]);
-                else weights[dst_r + row] = __uint_as_float(v[u].x);
-            }
-        }
+        store_block(i0);
     }
-    cluster.sync();          // (no block of sums is read any more: those behind the last row become zero)
+    if (items > block) cluster.sync();       // (no block of sums is read any more: those behind the last row become zero)
     const int len = dst_r + r;
     for (int i = len + part; i < n; i += parts) weights[i] = 0.f;
     for (int i = part; i < a.budget - dst_r; i += parts) idx[dst_r + i] = i < r ? src_r + i : -1;
@@ -258,12 +310,12 @@ EvictPlan evict_plan(int cap, int c, int smem_limit) {
     EvictPlan p;
     const long long chunks = cap / c;
     // at most half the chunks move: as many as places below k are free, and k of C chunks are kept
-    const long long list = (chunks / 2 + 8) / 8 * 8;
+    const long long list = (chunks / 2 + 8) / 8 * 8;        // (kbuf behind the lists is 16-byte aligned)
     p.fits = chunks <= kSelMaxChunks;
     p.list_cap = p.fits ? static_cast<int>(list) : 0;
     const long long fixed = sizeof(EvictSmem) + 4LL * p.list_cap;
     const long long keys = (smem_limit - fixed) / 4;
-    p.key_cap = static_cast<int>(chunks <= keys ? chunks : 0);
+    p.key_cap = static_cast<int>(chunks + 4 <= keys ? (chunks + 3) / 4 * 4 : 0);
     p.smem_bytes = static_cast<int>(fixed + 4LL * p.key_cap);
     return p;
 }
