@@ -29,7 +29,6 @@ constexpr int kAttWarps = 8;
 constexpr int kAttThreads = 32 * kAttWarps;
 constexpr int kAttStep = 16;                          // rows of a warp's step
 constexpr int kRingBytes = 24 * 1024;                 // of a warp
-constexpr int kJoinRows = 256;                        // rows of the sums that a CTA of the join takes
 constexpr int kJoinThreads = 128;
 constexpr int kSmallSmem = 227 * 1024;                // shared memory of a CTA of the form for short caches, one an SM
 constexpr int kJoinHeads = 8;                         // query heads whose weights are added together
@@ -530,7 +529,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
 }
 
 // The join. A query head's records are joined by a team: a warp where few CTAs share a unit, else a CTA, or, of many CTAs, one for every 32 dims.
-// The other CTAs add the rows' weights to the sums, kJoinRows rows of a KV head each.
+// The other CTAs add the rows' weights to the sums, kJoinThreads RPT rows of a KV head each.
 enum TeamOf { kTeamWarp, kTeamCta, kTeamCtas };
 template <int D, TeamOf TEAM>
 struct Team {
@@ -549,7 +548,8 @@ struct JoinSmem {
     float2 ml[kJoinHeads];            // (reference, factor) of query heads
 };
 
-template <int D, int NH, bool SUMS, TeamOf TEAM>
+// RPT: rows of the sums a thread takes; 0: no sums.
+template <int D, int NH, int RPT, TeamOf TEAM>
 __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendArgs a, int join_ctas, int row_blocks) {
     using T = Team<D, TEAM>;
     constexpr unsigned kFull = 0xffffffffu;
@@ -637,7 +637,8 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
         }
         return;
     }
-    if constexpr (SUMS) {
+    if constexpr (RPT > 0) {
+        constexpr int kJoinRows = RPT * kJoinThreads;
         const int idx = blockIdx.x - join_ctas, bh = idx / row_blocks, b = bh / a.Hkv, h = bh - b * a.Hkv;
         const int blk = h / a.block, unit = b * a.blocks + blk, head = h - blk * a.block;
         const int r0 = (idx - bh * row_blocks) * kJoinRows, r1 = min(rows_of(a, bh), r0 + kJoinRows);
@@ -645,16 +646,20 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
         asm volatile("griddepcontrol.wait;" ::: "memory");
         if (r0 >= r1) return;
         const size_t q_row = static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G;
-        constexpr int kOwnRows = kJoinRows / kJoinThreads;
-        float acc[kOwnRows];
+        float* w = a.weights + static_cast<size_t>(bh) * a.cache.cap;
+        float acc[RPT], was[RPT];
 #pragma unroll
-        for (int i = 0; i < kOwnRows; ++i) acc[i] = 0.f;
+        for (int i = 0; i < RPT; ++i) {
+            const int r = r0 + i * kJoinThreads + threadIdx.x;
+            acc[i] = 0.f;
+            was[i] = r < r1 ? w[r] : 0.f;
+        }
         for (int q0 = 0; q0 < G; q0 += kJoinHeads) {
-            float lg[kJoinHeads][kOwnRows];                     // (asked for before the statistics that they wait for)
+            float lg[kJoinHeads][RPT];                     // (asked for before the statistics that they wait for)
 #pragma unroll
             for (int q = 0; q < kJoinHeads; ++q)
 #pragma unroll
-                for (int i = 0; i < kOwnRows; ++i) {
+                for (int i = 0; i < RPT; ++i) {
                     const int r = r0 + i * kJoinThreads + threadIdx.x;
                     lg[q][i] = q0 + q < G && r < r1 ? a.logits[(q_row + q0 + q) * a.logit_stride + r] : -INFINITY;
                 }
@@ -693,15 +698,14 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
                 const float2 f = sm.ml[q];
                 if (q0 + q < G) {
 #pragma unroll
-                    for (int i = 0; i < kOwnRows; ++i) acc[i] += exp2_fast(lg[q][i] - f.x) * f.y;
+                    for (int i = 0; i < RPT; ++i) acc[i] += exp2_fast(lg[q][i] - f.x) * f.y;
                 }
             }
         }
-        float* w = a.weights + static_cast<size_t>(bh) * a.cache.cap;
 #pragma unroll
-        for (int i = 0; i < kOwnRows; ++i) {
+        for (int i = 0; i < RPT; ++i) {
             const int r = r0 + i * kJoinThreads + threadIdx.x;
-            if (r < r1) w[r] += acc[i];
+            if (r < r1) w[r] = was[i] + acc[i];
         }
     }
 }
@@ -845,14 +849,24 @@ cudaError_t launch_small(const AttendArgs& a, const AttendPlan& plan, int device
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <int D, int NH, bool SUMS, TeamOf TEAM>
-cudaError_t launch_join(const AttendArgs& a, cudaLaunchConfig_t cfg, int row_blocks) {
+template <int D, int NH, int RPT, TeamOf TEAM>
+cudaError_t launch_join(const AttendArgs& a, cudaLaunchConfig_t cfg) {
     using T = Team<D, TEAM>;
+    const int row_blocks = RPT > 0 ? (a.cache.cap + RPT * kJoinThreads - 1) / (RPT > 0 ? RPT * kJoinThreads : 1) : 0;
     const int join_ctas = (a.B * a.Hq * (D / T::kDims) + T::kTeams - 1) / T::kTeams;
     cfg.gridDim = dim3(static_cast<unsigned>(join_ctas + a.B * a.Hkv * row_blocks));
     cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NH, SUMS, TEAM>, a, join_ctas, row_blocks);
+    return cudaLaunchKernelEx(&cfg, attend_join_kernel<D, NH, RPT, TEAM>, a, join_ctas, row_blocks);
+}
+
+template <int D, int NH, int RPT>
+cudaError_t launch_teams(const AttendArgs& a, const cudaLaunchConfig_t& cfg, int n_cta) {
+    // records of a unit, where lengths are alike: up to 4 a warp has in flight at once, up to 32 a CTA
+    const int records = n_cta / (a.B * a.blocks * a.groups) + 2;
+    if (records <= 4) return launch_join<D, NH, RPT, kTeamWarp>(a, cfg);
+    if (records <= 36) return launch_join<D, NH, RPT, kTeamCta>(a, cfg);
+    return launch_join<D, NH, RPT, kTeamCtas>(a, cfg);
 }
 
 template <int D, int NH, bool SUMS>
@@ -878,12 +892,13 @@ cudaError_t launch_attend_t(const AttendArgs& a, int n_cta, int device, cudaStre
     cfg.numAttrs = 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
     if (e != cudaSuccess) return e;
-    const int row_blocks = SUMS ? (a.cache.cap + kJoinRows - 1) / kJoinRows : 0;
-    // records of a unit, where lengths are alike: up to 4 a warp has in flight at once, up to 32 a CTA
-    const int records = n_cta / (a.B * a.blocks * a.groups) + 2;
-    if (records <= 4) return launch_join<D, NH, SUMS, kTeamWarp>(a, cfg, row_blocks);
-    if (records <= 36) return launch_join<D, NH, SUMS, kTeamCta>(a, cfg, row_blocks);
-    return launch_join<D, NH, SUMS, kTeamCtas>(a, cfg, row_blocks);
+    // few rows a CTA where there are few of them (two threads' worth of loads in flight then), else enough for about one wave
+    if constexpr (SUMS) {
+        const long long rows = static_cast<long long>(a.B) * a.Hkv * a.cache.cap;
+        return rows <= 2LL * kJoinThreads * 8 * n_cta ? launch_teams<D, NH, 2>(a, cfg, n_cta) : launch_teams<D, NH, 8>(a, cfg, n_cta);
+    } else {
+        return launch_teams<D, NH, 0>(a, cfg, n_cta);
+    }
 }
 
 }  // namespace
