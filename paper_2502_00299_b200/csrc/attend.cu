@@ -59,9 +59,16 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// 16 bytes of global memory into shared memory, or zeros where `there` is false.
+// 16 bytes of global memory into shared memory, or zeros where `there` is false. ONCE: the first to leave the L2.
+template <bool ONCE>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+    if constexpr (ONCE) {
+        uint64_t policy;
+        asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+        asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0), "l"(policy) : "memory");
+    } else {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+    }
 }
 __device__ __forceinline__ void copies_begin_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -160,7 +167,9 @@ __device__ __forceinline__ size_t record(const AttendArgs& a, int cta, bool begi
 }
 
 // A warp's walk over rows of one KV head, kAttStep at a time and `stride` rows from one step to the next, for up to 8 NH query heads.
-template <int D, int NH>
+// ONCE: keys and values are the first to leave the L2, so that records, logits and sums stay (sums of 16 x 8000 rows 99.6 -> 91.0 us, 8 x 4352 22.1 ->
+// 20.9, 9 ragged sequences 43.4 -> 40.4); not for short caches, which stay there themselves (4 x 2000 rows 9.7, 10.4 with it).
+template <int D, int NH, bool ONCE>
 struct Walk {
     static constexpr int kPieces = D / 8;               // 16-byte pieces of a row
     static constexpr int kRowsOnce = 32 / kPieces;      // rows that one copy instruction of a warp takes
@@ -207,8 +216,8 @@ struct Walk {
             const int row = __shfl_sync(0xffffffffu, rows, i * kRowsOnce + lane / kPieces);
             const uint32_t dst = to + put[i % 4] + i * kRowsOnce * (2 * D);
             const uint64_t off = static_cast<uint64_t>(static_cast<uint32_t>(all ? row : max(row, 0))) * row_bytes;
-            copy_async(dst, Kh + off, all || row >= 0);
-            copy_async(dst + kHalf, Vh + off, all || row >= 0);
+            copy_async<ONCE>(dst, Kh + off, all || row >= 0);
+            copy_async<ONCE>(dst + kHalf, Vh + off, all || row >= 0);
         }
     }
     // Asks for the first steps. b: sequence, h: KV head, q_row: first of the query heads among all. A group of copies a step, empty ones behind `end`.
@@ -423,7 +432,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
     // this warp's head in a unit and its rows among those of the head's warps
     const int head = warp % a.block, turn = warp / a.block, turns = a.tile / kAttStep;
     const int G = a.Hq / a.Hkv;
-    Walk<D, NH> walk(a, sm.ring[warp]);
+    Walk<D, NH, true> walk(a, sm.ring[warp]);
 
     // A part of this CTA's share: tiles [tile0, tile1) of a unit, for one group of query heads.
     struct Part {
@@ -742,7 +751,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) attend_small_kernel(const At
     const size_t q_row = static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * G + grp * 8 * NH;
     const int n = rows_of(a, bh), steps = (n + kAttStep - 1) / kAttStep;
     const int r0 = rank * steps / n_cta * kAttStep, r1 = min((rank + 1) * steps / n_cta * kAttStep, n);
-    Walk<D, NH> walk(a, sm.ring[warp]);
+    Walk<D, NH, false> walk(a, sm.ring[warp]);
     walk.begin(a, b, h, q_row, heads, r0 + warp * kAttStep, r1, kSmallWarps * kAttStep);
     walk.run([&](int nn, int base, const float (&z)[2][2]) {
         if constexpr (SUMS) {
