@@ -336,7 +336,7 @@ CHUNKKV_API int chunkkv_compress_layer_alg1(const void* q_obs, const void* K, co
  * chunkkv_attend_paged: attention of one new token a sequence, q [B, Hq, d] bf16 (rotated), over the rows j < lengths[b, h] of
  *   its KV head: out [B, Hq, d] bf16 = softmax(q K^T / sqrt(d)) V, in 32 bits, rounded once. A head with no row to see, or none
  *   with a logit above -inf, gets zeros; other infinite or not-a-number products go the way of the formula. weights != NULL:
- *   weights[b, h, j] += the row's attention, summed over the query heads of KV head h. scratch: device memory of the call's own
+ *   weights[b, h, j] += the row's attention, summed over the query heads of KV head h (0 for a logit of -inf). scratch: device memory of the call's own
  *   until it has finished, 256-byte aligned, chunkkv_attend_scratch_bytes(...) bytes (0: invalid sizes; its contents do not
  *   matter); CHUNKKV_ENOWORKSPACE when smaller. Same result every time: sums are taken in a fixed order.
  *

@@ -75,6 +75,8 @@ template <int N>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 // A maximum as the reference of exponents: 0 where nothing was seen.
 __device__ __forceinline__ float reference_of(float m) { return m == -INFINITY ? 0.f : m; }
+// A row's weight from its logit and its head's (reference, factor): nothing for a row that was not seen, whatever became of the head.
+__device__ __forceinline__ float weight_of(float logit, const float2& f) { return logit == -INFINITY ? 0.f : exp2_fast(logit - f.x) * f.y; }
 
 // Rows of a head and of a unit, the `block` heads from h0 on of a sequence.
 __device__ __forceinline__ int rows_of(const AttendArgs& a, int bh) { return min(max(__ldg(a.lengths + bh), 0), a.cache.cap); }
@@ -707,7 +709,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
                 const float2 f = sm.ml[q];
                 if (q0 + q < G) {
 #pragma unroll
-                    for (int i = 0; i < RPT; ++i) acc[i] += exp2_fast(lg[q][i] - f.x) * f.y;
+                    for (int i = 0; i < RPT; ++i) acc[i] += weight_of(lg[q][i], f);
                 }
             }
         }
@@ -824,7 +826,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) attend_small_kernel(const At
         float* w = a.weights + static_cast<size_t>(bh) * a.cache.cap;
         for (int r = r0 + tid; r < r1; r += kSmallThreads) {
             float sum = 0.f;
-            for (int q = 0; q < heads; ++q) sum += exp2_fast(logits[q * a.small_rows + r - r0] - sm.all[q].x) * sm.all[q].y;
+            for (int q = 0; q < heads; ++q) sum += weight_of(logits[q * a.small_rows + r - r0], sm.all[q]);
             w[r] += sum;
         }
     }

@@ -42,9 +42,8 @@ def angles(n, d, seed=0):
 
 
 def rotated(x, gain, eps, cos, sin):
-    """(the formula's values, the tolerance's scale) of x [T, H, d] with cos, sin [T, d / 2]."""
+    """The formula's values and the tolerance, of x [T, H, d] with cos, sin [T, d / 2]."""
     ref = ora.rotate(x, gain, eps, cos[:, None], sin[:, None])
-    scale = ora.rotate(np.abs(x), None if gain is None else np.abs(gain), eps, np.abs(cos[:, None]), -np.abs(sin[:, None]))
     a, b = np.split(np.abs(x) if gain is None else np.abs(ora.rotate(x, gain, eps, np.ones_like(cos[:, None]), np.zeros_like(sin[:, None]))), 2, -1)
     c, s = np.abs(cos[:, None]), np.abs(sin[:, None])
     scale = np.concatenate([a * c + b * s, b * c + a * s], -1)
@@ -154,7 +153,7 @@ def test_append(Hq, Hkv, d, page):
 
 
 # ------------------------------------------------------------------------------------------------ attention
-def check_attention(q, K, V, tables, lengths, weights=None, q_bits=True, runs=1):
+def check_attention(q, K, V, tables, lengths, weights=None):
     """One call against the formula; K, V, q as bf16 bits. Returns (out, weights)."""
     page, (B, Hq, d) = K.shape[1], q.shape
     Hkv, cap = K.shape[2], tables.shape[1] * page
@@ -276,6 +275,80 @@ def test_attention_over_long_and_many_caches(Hq, Hkv, d, B, n, page):
     check_attention(rand_bits(rng, (B, Hq, d), 3.0), K, V, tables, lengths, np.zeros((B, Hkv, per * page), dtype=np.float32))
 
 
+@pytest.mark.parametrize("Hkv,B,d", [(1, 1, 128), (3, 5, 64), (2, 8, 128), (8, 4, 64), (1, 60, 128), (6, 20, 64), (148, 1, 64), (149, 1, 64)])
+def test_attention_with_every_size_of_cluster(Hkv, B, d):
+    """Short caches: a head's rows go to 8, 4, 2 or 1 CTAs, or (149 heads) to shares of CTAs; with fewer steps of 16 rows than CTAs among them."""
+    rng = np.random.default_rng(Hkv * B)
+    page, per = 16, 9
+    K, V, tables = new_cache(rng, B, Hkv, d, page, per)
+    lengths = rng.integers(0, page * per + 1, (B, Hkv)).astype(np.int32)
+    lengths[0, 0] = page * per
+    check_attention(rand_bits(rng, (B, 2 * Hkv, d), 2.0), K, V, tables, lengths, rng.random((B, Hkv, per * page)).astype(np.float32))
+
+
+def test_attention_reads_pages_that_sequences_share():
+    rng = np.random.default_rng(21)
+    K, V, tables = new_cache(rng, 3, 2, 64, 16, 5)
+    tables[1, :3] = tables[0, :3]                                            # a common prefix
+    tables[2, 4] = tables[2, 0]                                              # a page twice
+    check_attention(rand_bits(rng, (3, 4, 64)), K, V, tables, np.array([[80, 70], [66, 48], [79, 80]], dtype=np.int32), np.zeros((3, 2, 80), dtype=np.float32))
+
+
+@pytest.mark.parametrize("room", [0, 600])
+def test_rows_that_are_not_seen_get_no_weight_whatever_becomes_of_the_head(room):
+    rng = np.random.default_rng(22)
+    K, V, tables = new_cache(rng, 1, 1, 64, 16, 4)
+    tables[0, 1] = -1
+    K[tables[0, 2], 3, 0, 5] = 0x7FC0                                        # not a number: so are the outputs
+    tables = np.concatenate([tables, np.full((1, room), -1, dtype=np.int32)], 1)
+    w = torch.full((1, 1, tables.shape[1] * 16), 0.5, device="cuda")
+    out = ck.attend_paged(to_dev(rand_bits(rng, (1, 2, 64))), i32(tables), i32([[60]]), to_dev(K), to_dev(V), w)
+    assert torch.isnan(out).all() and (w[0, 0, 16:32] == 0.5).all() and (w[0, 0, 60:] == 0.5).all() and torch.isnan(w[0, 0, :16]).all()
+
+
+def test_native_and_general_calls_are_the_same(monkeypatch):
+    """The binding's general way (other streams, given outputs, declined arguments) queues what the native one does."""
+    from paper_2502_00299_b200 import binding
+    rng = np.random.default_rng(23)
+    Hq, Hkv, d, page, per, B = 8, 2, 64, 16, 5, 3
+    K, V, tables = new_cache(rng, B, Hkv, d, page, per)
+    lengths = np.array([[70, 33], [1, 80], [0, 5]], dtype=np.int32)
+    qkv, gain = to_dev(rand_bits(rng, (B, (Hq + 2 * Hkv) * d))), to_dev(rand_bits(rng, (d,)))
+    cos, sin = (torch.tensor(x).cuda() for x in angles(9, d))
+    pos = i32([3, 8, 0])
+
+    def all_of_them(**k):
+        dK, dV, dl, w = to_dev(K), to_dev(V), i32(lengths), torch.rand(B, Hkv, per * page, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+        torch.cuda.synchronize()
+        r = list(ck.rotate_qk(qkv, Hq, Hkv, d, cos, sin, pos, gain, None, 1e-6, **k))
+        r.append(ck.append_paged(qkv, Hq, cos, sin, pos, i32(tables), dl, dK, dV, gain, gain, 1e-6, **k))
+        r.append(ck.attend_paged(r[2], i32(tables), dl, dK, dV, **k))
+        r.append(ck.attend_paged(r[2], i32(tables), dl, dK, dV, w, **k))
+        r.append(ck.evict_paged(w, i32(tables), dl, dK, dV, 4, 3, 20, **k))
+        torch.cuda.synchronize()
+        return r + [dK, dV, dl, w]
+
+    taken = []
+    with monkeypatch.context() as m:
+        for name in ("rotate_qk", "append_paged", "attend_paged", "evict_paged"):
+            was = getattr(binding._native, name)
+            m.setattr(binding._native, name, lambda *a, was=was: taken.append(was(*a)) or taken[-1])
+        native = all_of_them()
+    assert len(taken) == 5 and all(t is not None and type(t) is not int for t in taken)
+    side = torch.cuda.Stream()
+    with monkeypatch.context() as m:
+        for name in ("rotate_qk", "append_paged", "attend_paged", "evict_paged"):
+            m.setattr(binding._native, name, lambda *a: None)
+        general = all_of_them()
+    other = all_of_them(stream=side)
+    for a, b, c in zip(native, general, other):
+        assert torch.equal(a, b) and torch.equal(a, c)
+    with pytest.raises(ck.ChunkKVError):
+        ck.evict_paged(native[-1], i32(tables), native[-2], native[-4], native[-3], 4, 3, 5)       # budget below w + c - 1
+    with pytest.raises(ck.ChunkKVError):
+        ck.rotate_qk(qkv, Hq, Hkv, d, cos, sin, pos, eps=-1.0)
+
+
 def test_attention_beyond_32_bit_offsets():
     """A cache of more than 2^32 elements: its last pages are read and written."""
     Hkv, d, page, Hq, B = 8, 128, 16, 8, 1
@@ -357,7 +430,7 @@ def check_eviction(rng, B, Hkv, d, page, per, lengths, w, c, budget, weights, ho
     for b, p, v in holes:
         tables[b, p] = v
     cap = per * page
-    weights = (weights * (np.arange(cap) < np.clip(lengths, 0, cap)[..., None])).astype(np.float32)
+    weights = np.where(np.arange(cap) < np.clip(lengths, 0, cap)[..., None], weights, 0).astype(np.float32)
     dK, dV = Guarded(K.shape, torch.bfloat16), Guarded(V.shape, torch.bfloat16)
     dK.t.copy_(to_dev(K)), dV.t.copy_(to_dev(V))
     dw, dl, di = Guarded(weights.shape, torch.float32), Guarded(lengths.shape, torch.int32), Guarded((B, Hkv, budget), torch.int32)
