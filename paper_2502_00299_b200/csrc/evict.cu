@@ -37,6 +37,9 @@ union EvictSmem {
 };
 constexpr int kEvMaxKeys = 24;            // keys of a thread in registers, at most
 
+template <int N>
+struct Keys { static constexpr int value = N; };     // of a thread
+
 // Order of sums: not-a-number above everything (as torch sorts it), -0 as +0.
 __device__ __forceinline__ uint32_t evict_key(float x) { return x != x ? 0xffffffffu : select_order_key(x); }
 
@@ -78,31 +81,47 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictArgs a)
         }
         return evict_key(static_cast<float>(sum));
     };
-    for (int i = part; i < k * c; i += parts) idx[i] = i;           // (rows that move overwrite theirs behind the barrier)
+    auto stay_put = [&] {                                           // (rows that move overwrite theirs behind the barrier)
+        for (int i = part; i < k * c; i += parts) idx[i] = i;
+    };
     const unsigned short* moved = from;
     int stay = 0;
     if (k > 0 && C <= kEvMaxKeys * kEvThreads && C <= a.key_cap && k <= kSelCap) {
-        uint32_t lo = 0xffffffffu, hi = 0u;
-#pragma unroll 4
-        for (int ch = tid; ch < C; ch += kEvThreads) {
-            const uint32_t key = key_of(ch);
-            kbuf[ch] = key;
-            lo = min(lo, key);
-            hi = max(hi, key);
-        }
-        lo = __reduce_min_sync(kFull, lo);
-        hi = __reduce_max_sync(kFull, hi);
-        if (lane == 0) sm.sel.warp_sums[warp] = static_cast<unsigned long long>(hi) << 32 | lo;
-        select_clear(sm.sel);
-        __syncthreads();
         const int per = (C + kEvThreads - 1) / kEvThreads;
-        if (per <= 2) select_staged<2>(kbuf, C, k, sm.sel);
-        else if (per <= 4) select_staged<4>(kbuf, C, k, sm.sel);
-        else if (per <= 6) select_staged<6>(kbuf, C, k, sm.sel);
-        else if (per <= 8) select_staged<8>(kbuf, C, k, sm.sel);
-        else if (per <= 10) select_staged<10>(kbuf, C, k, sm.sel);
-        else if (per <= 12) select_staged<12>(kbuf, C, k, sm.sel);
-        else select_staged<kEvMaxKeys>(kbuf, C, k, sm.sel);
+        auto select = [&](auto keys_of_thread) {
+            constexpr int KPT = decltype(keys_of_thread)::value;
+            uint32_t lo = 0xffffffffu, hi = 0u;
+            auto take = [&](int ch, uint32_t key) {
+                kbuf[ch] = key;
+                lo = min(lo, key);
+                hi = max(hi, key);
+            };
+            if (c == 1) {                                           // (all loads before the first use)
+                float v[KPT];
+#pragma unroll
+                for (int u = 0; u < KPT; ++u) v[u] = tid + u * kEvThreads < C ? weights[tid + u * kEvThreads] : 0.f;
+                stay_put();
+#pragma unroll
+                for (int u = 0; u < KPT; ++u)
+                    if (tid + u * kEvThreads < C) take(tid + u * kEvThreads, evict_key(v[u]));
+            } else {
+                for (int ch = tid; ch < C; ch += kEvThreads) take(ch, key_of(ch));
+                stay_put();
+            }
+            lo = __reduce_min_sync(kFull, lo);
+            hi = __reduce_max_sync(kFull, hi);
+            if (lane == 0) sm.sel.warp_sums[warp] = static_cast<unsigned long long>(hi) << 32 | lo;
+            select_clear(sm.sel);
+            __syncthreads();
+            select_staged<KPT>(kbuf, C, k, sm.sel);
+        };
+        if (per <= 2) select(Keys<2>{});
+        else if (per <= 4) select(Keys<4>{});
+        else if (per <= 6) select(Keys<6>{});
+        else if (per <= 8) select(Keys<8>{});
+        else if (per <= 10) select(Keys<10>{});
+        else if (per <= 12) select(Keys<12>{});
+        else select(Keys<kEvMaxKeys>{});
         // The kept chunks are in ascending order: `stay` of them lie below k, and the j-th free place below k is j + i, where i of them lie below it.
         const unsigned short* kept = sm.sel.sel;
         auto count = [&](int most, auto before) {                   // of the first `most`, those that come first and of which that holds
@@ -119,6 +138,7 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictArgs a)
         __syncthreads();
         moved = kept + stay;
     } else if (k > 0) {
+        stay_put();
         const bool staged = C <= a.key_cap;
         auto key_at = [&](int ch) { return staged ? kbuf[ch] : key_of(ch); };
         uint32_t lo = 0xffffffffu, hi = 0u;
