@@ -9,7 +9,7 @@
 // so that half the products are not empty up to eight heads, a head's statistics and values lie in the same lanes, and V^T comes out of shared memory as it
 // is needed. P is split into two bf16 terms, so that its rounding (2^-16) is not seen beside that of the output. A head's reference moves only when a
 // logit lies 2^8 above it, which a vote finds without looking for the maximum. 64 sequences of 4160 rows, 8 heads of 128 dims: 164 us, the memory's own
-// time; with heads as rows (16 of which 8 empty), V^T by byte permutes and a maximum every step a step took 1600 clocks instead of MEASURED.
+// time (what a step takes is what an SM gets out of the L2, 62 GB/s, or the memory: half the instructions did not change it).
 //
 // The rows of all units (a sequence's heads that a CTA takes together) are cut into tiles and dealt evenly to the CTAs in one line, so that lengths
 // need not be alike; a CTA walks the units in its share and leaves (max, sum, O) records for those that it shares with others, which a second launch
@@ -30,6 +30,7 @@ constexpr int kAttThreads = 32 * kAttWarps;
 constexpr int kAttStep = 16;                          // rows of a warp's step
 constexpr int kRingBytes = 24 * 1024;                 // of a warp
 constexpr int kJoinThreads = 128;
+constexpr int kSmallRows = 1152;                      // rows of a CTA of the form for short caches, at most
 constexpr int kSmallSmem = 227 * 1024;                // shared memory of a CTA of the form for short caches, one an SM
 constexpr int kJoinHeads = 8;                         // query heads whose weights are added together
 static_assert(kAttMaxCtas % 32 == 0, "records are looked at a warp at a time");
@@ -765,6 +766,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1) attend_small_kernel(const At
                     if (8 * nn + 2 * t + e < heads) lg[e * a.small_rows + 8 * j] = z[j][e];
         }
     });
+    constexpr int kOwnRows = SUMS ? (kSmallRows + kSmallThreads - 1) / kSmallThreads : 1;
+    float* sums = SUMS ? a.weights + static_cast<size_t>(bh) * a.cache.cap : nullptr;
+    float was[kOwnRows];                              // (asked for before the joining)
+    if constexpr (SUMS) {
+#pragma unroll
+        for (int i = 0; i < kOwnRows; ++i) was[i] = r0 + tid + i * kSmallThreads < r1 ? sums[r0 + tid + i * kSmallThreads] : 0.f;
+    }
     walk.add_up();
     __syncthreads();                                  // (every ring is idle)
 #pragma unroll
@@ -823,11 +831,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1) attend_small_kernel(const At
             if (c == 0) sm.all[q] = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
         }
         __syncthreads();
-        float* w = a.weights + static_cast<size_t>(bh) * a.cache.cap;
-        for (int r = r0 + tid; r < r1; r += kSmallThreads) {
-            float sum = 0.f;
-            for (int q = 0; q < heads; ++q) sum += weight_of(logits[q * a.small_rows + r - r0], sm.all[q]);
-            w[r] += sum;
+#pragma unroll
+        for (int i = 0; i < kOwnRows; ++i) {
+            const int r = r0 + tid + i * kSmallThreads;
+            if (r >= r1) break;
+            float add = 0.f;
+#pragma unroll 4
+            for (int q = 0; q < heads; ++q) add += weight_of(logits[q * a.small_rows + r - r0], sm.all[q]);
+            sums[r] = was[i] + add;
         }
     }
     cluster.sync();                                   // (a CTA's part is there until all have read it)
@@ -931,9 +942,10 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     const long long tiles = static_cast<long long>(B) * p.blocks * p.groups * ((cap + p.tile - 1) / p.tile);
     p.max_ctas = static_cast<int>(tiles < kAttMaxCtas ? tiles : kAttMaxCtas);
     // Short caches: as many CTAs a head as are resident beside each other, where they do not have many more rows each than in even shares of all
-    // SMs. The second launch and its records cost 2 us; 128 rows of a CTA 0.8 (64 dims) to 1.2 us. One KV head of 8, 128 dims, 100 / 2000 / 4000 / 8000
-    // rows: 4.7 / 6.2 / 8.3 / 13.0 us with one launch, 6.2 / 8.4 / 8.4 / 12.0 with two; 2 heads, 64 dims, 4000 / 8000 rows 6.7 / 9.8 and 6.7 / 6.9; 16
-    // sequences of 8 heads, 600 / 1000 rows 11.6 / 15.7 and 15.1 / 18.6. At most 768 rows each, as sequences need not be alike.
+    // SMs. The second launch and its records cost 3 to 5 us; 128 rows of a CTA 0.8 (64 dims) to 1.2 us. One launch and two, us: one sequence of 8 heads,
+    // 128 dims, 100 / 2000 / 4000 / 8000 rows 4.7 and 6.2 / 6.2 and 8.4 / 8.3 and 8.4 / 13.0 and 12.0; of 2 heads, 64 dims, 4000 / 8000 rows 6.7 and 6.7 /
+    // 9.8 and 6.9; 16 of 8 heads, 1000 rows 15.7 and 17.3, unlike lengths 13.1 and 15.4; 8 of 4 heads, 4352 rows, sums, 20.2 and 20.8, unlike 17.7 and 17.3.
+    // At most kSmallRows each, as sequences need not be alike (128 CTAs of 2000 rows: 25.9 and 29.6 where they are).
     const long long items = static_cast<long long>(B) * Hkv * p.groups;
     p.cluster = items <= 15 ? 8 : items <= 33 ? 4 : items <= 74 ? 2 : items <= 148 ? 1 : 0;
     p.small_rows = 0;
@@ -941,7 +953,7 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
         const long long steps = (cap + kAttStep - 1) / kAttStep, rows = (steps + p.cluster - 1) / p.cluster * kAttStep;
         const long long kept = rows + 4;                        // (logits of four neighbouring pairs of heads lie in different banks)
         const size_t fixed = d == 128 ? (p.nh == 1 ? sizeof(SmallSmem<128, 1>) : sizeof(SmallSmem<128, 2>)) : (p.nh == 1 ? sizeof(SmallSmem<64, 1>) : sizeof(SmallSmem<64, 2>));
-        const bool few = rows <= 768 && rows - items * cap / 148 <= 300;
+        const bool few = rows <= kSmallRows && rows - items * cap / 148 <= 300;
         if (few && (!sums || (p.groups == 1 && fixed + 4ull * p.group * kept <= kSmallSmem))) p.small_rows = static_cast<int>(kept);
         else p.cluster = 0;
     }
