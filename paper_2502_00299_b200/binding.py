@@ -628,9 +628,9 @@ def attend_paged(q: torch.Tensor, block_tables: torch.Tensor, lengths: torch.Ten
             out = torch.empty((B, Hq, d), dtype=torch.bfloat16, device=q.device)
         # scratch of this call: the allocator hands it out again only behind it on its stream
         need = int(lib.chunkkv_attend_scratch_bytes(B, Hq, Hkv, d, max_pages, page_size, int(weights is not None)))
-        scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+        scratch = torch.empty(need, dtype=torch.uint8, device=q.device) if need > 256 else None
         _check(lib.chunkkv_attend_paged(q.data_ptr(), block_tables.data_ptr(), max_pages, lengths.data_ptr(), page_size, pages, cache_K.data_ptr(),
-                                        cache_V.data_ptr(), B, Hq, Hkv, d, _ptr(weights), out.data_ptr(), scratch.data_ptr(), need, _stream(stream)),
+                                        cache_V.data_ptr(), B, Hq, Hkv, d, _ptr(weights), out.data_ptr(), _ptr(scratch), need, _stream(stream)),
                "chunkkv_attend_paged")
     return out
 

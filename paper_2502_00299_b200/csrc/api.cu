@@ -838,8 +838,10 @@ int chunkkv_attend_paged(const void* q, const int32_t* block_tables, int max_pag
     if (!aligned16(q) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) || !aligned4(weights) || !aligned16(out))
         return CHUNKKV_EINVAL_ALIGN;
     const AttendPlan plan = attend_plan(B, Hq, Hkv, d, cap, weights != nullptr);
-    if (scratch == nullptr || scratch_bytes < plan.bytes) return CHUNKKV_ENOWORKSPACE;
-    if ((reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return CHUNKKV_EINVAL_ALIGN;
+    if (plan.bytes > kAttNoScratch) {
+        if (scratch == nullptr || scratch_bytes < plan.bytes) return CHUNKKV_ENOWORKSPACE;
+        if ((reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return CHUNKKV_EINVAL_ALIGN;
+    }
     std::lock_guard<std::mutex> lk(g_mu);
     DeviceCtx* ctx;
     st = get_ctx(&ctx);

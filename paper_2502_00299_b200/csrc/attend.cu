@@ -957,9 +957,9 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
         if (few && (!sums || (p.groups == 1 && fixed + 4ull * p.group * kept <= kSmallSmem))) p.small_rows = static_cast<int>(kept);
         else p.cluster = 0;
     }
-    if (p.cluster > 0) {                                        // (no scratch: a byte, so that every call has some)
+    if (p.cluster > 0) {
         p.off_o = p.off_whole = p.off_shared = p.off_logits = 0;
-        p.bytes = 256;
+        p.bytes = kAttNoScratch;
         return p;
     }
     const size_t heads = static_cast<size_t>(p.max_ctas) * 2 * p.block * p.group;

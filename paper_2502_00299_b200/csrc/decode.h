@@ -43,6 +43,7 @@ struct RotateArgs {
 cudaError_t launch_rotate(const RotateArgs& args, int d, int num_sms, cudaStream_t stream);
 
 // Attention of one token a sequence over a paged cache (attend.cu).
+constexpr size_t kAttNoScratch = 256;         // said of calls that need none
 constexpr int kAttMaxCtas = 160;              // CTAs that leave records, at most
 struct AttendArgs {
     const __nv_bfloat16 *q, *K, *V;

@@ -504,9 +504,9 @@ PyObject* attend_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
         void* po = o.set(a[6], at::kBFloat16, static_cast<long long>(c.B) * Hq * c.d, [&] { return rows(q, c.B, Hq, c.d); });
         const size_t need = chunkkv_attend_scratch_bytes(c.B, Hq, c.Hkv, c.d, c.max_pages, c.page_size, weights != nullptr);
         at::Tensor scratch;                        // (freed behind the call on its stream: the allocator's blocks belong to streams)
-        if (need > 0) scratch = at::empty({static_cast<long long>(need)}, at::TensorOptions().dtype(at::kByte).device(q.device()));
+        if (need > 256) scratch = at::empty({static_cast<long long>(need)}, at::TensorOptions().dtype(at::kByte).device(q.device()));
         const void* pq = q.data_ptr();
-        void* ps = need > 0 ? scratch.data_ptr() : nullptr;
+        void* ps = need > 256 ? scratch.data_ptr() : nullptr;
         const int st = unlocked([&] {
             return chunkkv_attend_paged(pq, c.tables, c.max_pages, c.lengths, c.page_size, c.pages, c.K, c.V, c.B, Hq, c.Hkv, c.d, weights, po, ps, need, s);
         });

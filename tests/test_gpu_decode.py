@@ -500,6 +500,22 @@ def test_eviction_again_changes_nothing():
     assert torch.equal(idx, torch.arange(80, device="cuda", dtype=torch.int32).expand(2, 2, 80))
 
 
+def test_calls_with_nothing_to_do():
+    """No sequence at all, and a batch of padding: nothing is written but zeros and what stays."""
+    Hq, Hkv, d = 4, 2, 64
+    K, V = (torch.full((3, 16, Hkv, d), 7.0, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    cos, sin = (torch.tensor(x).cuda() for x in angles(4, d))
+    for B in (0, 2):
+        table, lengths = torch.zeros(B, 2, device="cuda", dtype=torch.int32), torch.zeros(B, Hkv, device="cuda", dtype=torch.int32)
+        w = torch.zeros(B, Hkv, 32, device="cuda")
+        q = ck.append_paged(torch.ones(B, (Hq + 2 * Hkv) * d, device="cuda", dtype=torch.bfloat16), Hq, cos, sin, torch.zeros(B, device="cuda", dtype=torch.int32),
+                            table, lengths, K, V)
+        out = ck.attend_paged(q, table, lengths, K, V, w)
+        idx = ck.evict_paged(w, table, lengths, K, V, 2, 1, 4)
+        assert q.shape == out.shape == (B, Hq, d) and not out.any() and not w.any() and not lengths.any()
+        assert idx.shape == (B, Hkv, 4) and (idx == -1).all() and (K == 7).all() and (V == 7).all()
+
+
 # ------------------------------------------------------------------------------------------------ together
 @pytest.mark.parametrize("captured", [False, True])
 def test_decoding_on_a_compressed_cache(captured):
