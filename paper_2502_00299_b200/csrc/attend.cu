@@ -31,7 +31,7 @@ constexpr int kAttStep = 16;                          // rows of a warp's step
 constexpr int kRingBytes = 24 * 1024;                 // of a warp
 constexpr int kJoinThreads = 128;
 constexpr int kSmallRows = 1152;                      // rows of a CTA of the form for short caches, at most
-constexpr int kSmallSmem = 227 * 1024;                // shared memory of a CTA of the form for short caches, one an SM
+constexpr int kSmallItems = 2048;                     // heads of a call that takes it, at most
 constexpr int kJoinHeads = 8;                         // query heads whose weights are added together
 static_assert(kAttMaxCtas % 32 == 0, "records are looked at a warp at a time");
 
@@ -723,28 +723,27 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendA
 }
 
 // The form for short caches: a cluster of CTAs works on one (sequence, KV head, group of query heads), each CTA on an even share of its rows, and the
-// parts are joined through distributed shared memory: one launch and no scratch. Logits that the sums need stay in shared memory.
-constexpr int kSmallWarps = 8;
-constexpr int kSmallThreads = 32 * kSmallWarps;
-
-template <int D, int NH>
+// parts are joined through distributed shared memory: one launch and no scratch. Logits that the sums need stay in shared memory. W: warps of a CTA,
+// eight, one CTA an SM, or (more heads than SMs, a CTA each) four, two an SM, so that one's first loads travel while the other works.
+template <int D, int NH, int W>
 struct SmallSmem {
     union {
-        alignas(128) unsigned char ring[kSmallWarps][kRingBytes];
-        float o[kSmallWarps][8 * NH][D + 4];          // the warps' parts (the rings are idle then)
+        alignas(128) unsigned char ring[W][kRingBytes];
+        float o[W][8 * NH][D + 4];                    // the warps' parts (the rings are idle then)
     };
-    float2 warp_ml[kSmallWarps][8 * NH];
+    float2 warp_ml[W][8 * NH];
     alignas(16) float cta_o[8 * NH][D];               // this CTA's part, which the others read
     float2 cta_ml[8 * NH];
     float2 all[8 * NH];                               // (reference, factor) of the query heads
     // float logits[a.group][a.small_rows] behind it
 };
 
-template <int D, int NH, bool SUMS>
-__global__ void __launch_bounds__(kSmallThreads, 1) attend_small_kernel(const AttendArgs a) {
+template <int D, int NH, bool SUMS, int W>
+__global__ void __launch_bounds__(32 * W, 8 / W) attend_small_kernel(const AttendArgs a) {
+    constexpr int kSmallWarps = W, kSmallThreads = 32 * W;
     extern __shared__ __align__(128) char smem_raw[];
-    SmallSmem<D, NH>& sm = *reinterpret_cast<SmallSmem<D, NH>*>(smem_raw);
-    float* logits = reinterpret_cast<float*>(smem_raw + sizeof(SmallSmem<D, NH>));
+    SmallSmem<D, NH, W>& sm = *reinterpret_cast<SmallSmem<D, NH, W>*>(smem_raw);
+    float* logits = reinterpret_cast<float*>(smem_raw + sizeof(SmallSmem<D, NH, W>));
     begin_dependent();
     cg::cluster_group cluster = cg::this_cluster();
     const int n_cta = static_cast<int>(cluster.num_blocks()), rank = static_cast<int>(cluster.block_rank());
@@ -844,19 +843,22 @@ __global__ void __launch_bounds__(kSmallThreads, 1) attend_small_kernel(const At
     cluster.sync();                                   // (a CTA's part is there until all have read it)
 }
 
-template <int D, int NH, bool SUMS>
+// Shared memory that a CTA of that form may have.
+constexpr int small_smem(int warps) { return warps == 8 ? 227 * 1024 : 113 * 1024; }
+
+template <int D, int NH, bool SUMS, int W>
 cudaError_t launch_small(const AttendArgs& a, const AttendPlan& plan, int device, cudaStream_t stream) {
-    const int smem = static_cast<int>(sizeof(SmallSmem<D, NH>)) + (SUMS ? plan.group * plan.small_rows * 4 : 0);
-    auto kernel = attend_small_kernel<D, NH, SUMS>;
+    const int smem = static_cast<int>(sizeof(SmallSmem<D, NH, W>)) + (SUMS ? plan.group * plan.small_rows * 4 : 0);
+    auto kernel = attend_small_kernel<D, NH, SUMS, W>;
     static uint64_t set_on = 0;                                 // devices; the caller holds the library's lock
     if ((set_on >> device & 1u) == 0) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(W));
         if (e != cudaSuccess) return e;
         set_on |= 1ull << device;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(a.B * a.Hkv * a.groups * plan.cluster));
-    cfg.blockDim = dim3(kSmallThreads);
+    cfg.blockDim = dim3(32 * W);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -925,6 +927,11 @@ cudaError_t launch_attend_t(const AttendArgs& a, int n_cta, int device, cudaStre
 
 }  // namespace
 
+template <int W>
+static size_t small_bytes(int d, int nh) {
+    return d == 128 ? (nh == 1 ? sizeof(SmallSmem<128, 1, W>) : sizeof(SmallSmem<128, 2, W>)) : (nh == 1 ? sizeof(SmallSmem<64, 1, W>) : sizeof(SmallSmem<64, 2, W>));
+}
+
 // Scratch: (max, sum) and O of two records a CTA, the CTAs that share a unit; where sums are asked for, (max, sum) of the units that one CTA had and
 // the logits of all rows.
 AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
@@ -945,18 +952,18 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     // SMs. The second launch and its records cost 3 to 5 us; 128 rows of a CTA 0.8 (64 dims) to 1.2 us. One launch and two, us: one sequence of 8 heads,
     // 128 dims, 100 / 2000 / 4000 / 8000 rows 4.7 and 6.2 / 6.2 and 8.4 / 8.3 and 8.4 / 13.0 and 12.0; of 2 heads, 64 dims, 4000 / 8000 rows 6.7 and 6.7 /
     // 9.8 and 6.9; 16 of 8 heads, 1000 rows 15.7 and 17.3, unlike lengths 13.1 and 15.4; 8 of 4 heads, 4352 rows, sums, 20.2 and 20.8, unlike 17.7 and 17.3.
-    // At most kSmallRows each, as sequences need not be alike (128 CTAs of 2000 rows: 25.9 and 29.6 where they are).
+    // At most kSmallRows each, as sequences need not be alike (128 CTAs of 2000 rows: 25.9 and 29.6 where they are). More heads than SMs, a CTA of
+    // four warps each: 24 sequences of 8 heads, 70 / 300 / 600 rows 5.2 and 9.0 / 8.7 and 14.0 / 14.7 and 18.1; more than are resident, 40 of 8, 70 / 150 /
+    // 300 / 600 rows 8.7 and 12.2 / 10.7 and 14.0 / 17.8 and 18.2 / 27.8 and 24.8, with sums of 64 of 8, 70 / 150 rows 10.7 and 12.7 / 17.0 and 15.0.
     const long long items = static_cast<long long>(B) * Hkv * p.groups;
-    p.cluster = items <= 15 ? 8 : items <= 33 ? 4 : items <= 74 ? 2 : items <= 148 ? 1 : 0;
-    p.small_rows = 0;
-    if (p.cluster > 0) {
-        const long long steps = (cap + kAttStep - 1) / kAttStep, rows = (steps + p.cluster - 1) / p.cluster * kAttStep;
-        const long long kept = rows + 4;                        // (logits of four neighbouring pairs of heads lie in different banks)
-        const size_t fixed = d == 128 ? (p.nh == 1 ? sizeof(SmallSmem<128, 1>) : sizeof(SmallSmem<128, 2>)) : (p.nh == 1 ? sizeof(SmallSmem<64, 1>) : sizeof(SmallSmem<64, 2>));
-        const bool few = rows <= kSmallRows && rows - items * cap / 148 <= 300;
-        if (few && (!sums || (p.groups == 1 && fixed + 4ull * p.group * kept <= kSmallSmem))) p.small_rows = static_cast<int>(kept);
-        else p.cluster = 0;
-    }
+    p.cluster = items <= 15 ? 8 : items <= 33 ? 4 : items <= 74 ? 2 : 1;
+    p.warps = items <= 148 ? 8 : 4;
+    const long long steps = (cap + kAttStep - 1) / kAttStep, rows = (steps + p.cluster - 1) / p.cluster * kAttStep;
+    const long long kept = rows + 4;                            // (logits of four neighbouring pairs of heads lie in different banks)
+    const size_t fixed = p.warps == 8 ? small_bytes<8>(d, p.nh) : small_bytes<4>(d, p.nh);
+    const bool few = items <= 148 ? rows <= kSmallRows && rows - items * cap / 148 <= 300 : items <= 296 ? rows <= kSmallRows : items <= kSmallItems && rows <= 128;
+    p.small_rows = static_cast<int>(few ? kept : 0);
+    if (!few || (sums && (p.groups > 1 || fixed + 4ull * p.group * kept > static_cast<size_t>(small_smem(p.warps))))) p.cluster = 0;
     if (p.cluster > 0) {
         p.off_o = p.off_whole = p.off_shared = p.off_logits = 0;
         p.bytes = kAttNoScratch;
@@ -991,10 +998,12 @@ cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d,
     const bool sums = a.weights != nullptr;
     if (plan.cluster > 0) {
         a.small_rows = plan.small_rows;
-#define CKV_SMALL(D, NH) (sums ? launch_small<D, NH, true>(a, plan, device, stream) : launch_small<D, NH, false>(a, plan, device, stream))
+#define CKV_SMALL_W(D, NH, W) (sums ? launch_small<D, NH, true, W>(a, plan, device, stream) : launch_small<D, NH, false, W>(a, plan, device, stream))
+#define CKV_SMALL(D, NH) (plan.warps == 8 ? CKV_SMALL_W(D, NH, 8) : CKV_SMALL_W(D, NH, 4))
         if (d == 128) return plan.nh == 1 ? CKV_SMALL(128, 1) : CKV_SMALL(128, 2);
         return plan.nh == 1 ? CKV_SMALL(64, 1) : CKV_SMALL(64, 2);
 #undef CKV_SMALL
+#undef CKV_SMALL_W
     }
 #define CKV_ATTEND(D, NH) (sums ? launch_attend_t<D, NH, true>(a, n, device, stream) : launch_attend_t<D, NH, false>(a, n, device, stream))
     if (d == 128) return plan.nh == 1 ? CKV_ATTEND(128, 1) : CKV_ATTEND(128, 2);

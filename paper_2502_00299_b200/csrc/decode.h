@@ -64,7 +64,7 @@ struct AttendArgs {
 };
 struct AttendPlan {
     int nh, groups, group, blocks, block, tile, tile_shift, max_ctas;
-    int cluster, small_rows;                  // CTAs of a cluster of the form for short caches (0: the other form), rows of one
+    int cluster, warps, small_rows;           // CTAs of a cluster of the form for short caches (0: the other form), warps and rows of one
     long long logit_stride;
     size_t off_o, off_whole, off_shared, off_logits, bytes;
 };
