@@ -852,7 +852,8 @@ cudaError_t launch_small(const AttendArgs& a, const AttendPlan& plan, int device
     auto kernel = attend_small_kernel<D, NH, SUMS, W>;
     static uint64_t set_on = 0;                                 // devices; the caller holds the library's lock
     if ((set_on >> device & 1u) == 0) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(W));
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(W));
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);     // (of 16)
         if (e != cudaSuccess) return e;
         set_on |= 1ull << device;
     }
@@ -952,11 +953,12 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     // SMs. The second launch and its records cost 3 to 5 us; 128 rows of a CTA 0.8 (64 dims) to 1.2 us. One launch and two, us: one sequence of 8 heads,
     // 128 dims, 100 / 2000 / 4000 / 8000 rows 4.7 and 6.2 / 6.2 and 8.4 / 8.3 and 8.4 / 13.0 and 12.0; of 2 heads, 64 dims, 4000 / 8000 rows 6.7 and 6.7 /
     // 9.8 and 6.9; 16 of 8 heads, 1000 rows 15.7 and 17.3, unlike lengths 13.1 and 15.4; 8 of 4 heads, 4352 rows, sums, 20.2 and 20.8, unlike 17.7 and 17.3.
+    // Clusters of 16 take 0.5 us longer to launch: 3 sequences of 2 heads, 12 query heads each, 300 / 4000 rows 7.5 / 9.9 us with 16, 6.8 / 15.6 without.
     // At most kSmallRows each, as sequences need not be alike (128 CTAs of 2000 rows: 25.9 and 29.6 where they are). More heads than SMs, a CTA of
     // four warps each: 24 sequences of 8 heads, 70 / 300 / 600 rows 5.2 and 9.0 / 8.7 and 14.0 / 14.7 and 18.1; more than are resident, 40 of 8, 70 / 150 /
     // 300 / 600 rows 8.7 and 12.2 / 10.7 and 14.0 / 17.8 and 18.2 / 27.8 and 24.8, with sums of 64 of 8, 70 / 150 rows 10.7 and 12.7 / 17.0 and 15.0.
     const long long items = static_cast<long long>(B) * Hkv * p.groups;
-    p.cluster = items <= 15 ? 8 : items <= 33 ? 4 : items <= 74 ? 2 : 1;
+    p.cluster = items <= 7 && cap > 1536 ? 16 : items <= 15 ? 8 : items <= 33 ? 4 : items <= 74 ? 2 : 1;
     p.warps = items <= 148 ? 8 : 4;
     const long long steps = (cap + kAttStep - 1) / kAttStep, rows = (steps + p.cluster - 1) / p.cluster * kAttStep;
     const long long kept = rows + 4;                            // (logits of four neighbouring pairs of heads lie in different banks)
