@@ -729,9 +729,9 @@ template <int D, int NH, int W>
 struct SmallSmem {
     union {
         alignas(128) unsigned char ring[W][kRingBytes];
-        float o[W][8 * NH][D + 4];                    // the warps' parts (the rings are idle then)
+        float4 o[W][NH * D / 16][33];                 // the warps' parts as their lanes hold them (the rings are idle then)
     };
-    float2 warp_ml[W][8 * NH];
+    alignas(16) float2 warp_ml[W][8 * NH];
     alignas(16) float cta_o[8 * NH][D];               // this CTA's part, which the others read
     float2 cta_ml[8 * NH];
     float2 all[8 * NH];                               // (reference, factor) of the query heads
@@ -775,14 +775,12 @@ __global__ void __launch_bounds__(32 * W, 8 / W) attend_small_kernel(const Atten
     walk.add_up();
     __syncthreads();                                  // (every ring is idle)
 #pragma unroll
-    for (int nn = 0; nn < NH; ++nn)
+    for (int nn = 0; nn < NH; ++nn) {
+        if (g == 0) *reinterpret_cast<float4*>(&sm.warp_ml[warp][8 * nn + 2 * t]) = make_float4(walk.m[nn][0], walk.l[nn][0], walk.m[nn][1], walk.l[nn][1]);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int q = 8 * nn + 2 * t + e;
-            if (g == 0) sm.warp_ml[warp][q] = make_float2(walk.m[nn][e], walk.l[nn][e]);
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) *reinterpret_cast<float2*>(&sm.o[warp][q][walk.dim_of(i)]) = walk.values(nn, e, i);
-        }
+        for (int i = 0; i < D / 16; ++i)
+            sm.o[warp][nn * (D / 16) + i][lane] = make_float4(walk.o[nn][i][0], walk.o[nn][i][1], walk.o[nn][i][2], walk.o[nn][i][3]);
+    }
     __syncthreads();
     for (int e = tid; e < heads * (D / 4); e += kSmallThreads) {
         const int q = e / (D / 4), c4 = e % (D / 4) * 4;
@@ -795,7 +793,8 @@ __global__ void __launch_bounds__(32 * W, 8 / W) attend_small_kernel(const Atten
 #pragma unroll
         for (int w = 0; w < kSmallWarps; ++w) {
             const float f = exp2_fast(s[w].x - ref);
-            const float4 y = *reinterpret_cast<const float4*>(&sm.o[w][q][c4]);
+            const float* o = reinterpret_cast<const float*>(&sm.o[w][q / 8 * (D / 16) + c4 / 16][4 * (c4 % 8) + q % 8 / 2]) + (q & 1) + c4 / 8 % 2 * 2;
+            const float4 y = make_float4(o[0], o[16], o[32], o[48]);       // (the next dim is four lanes further)
             ll = fmaf(s[w].y, f, ll);
             v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w);
         }
