@@ -502,6 +502,8 @@ def compress_layer_paged(q_obs: Optional[torch.Tensor], K: torch.Tensor, V: torc
 @contextlib.contextmanager
 def _on(dev: torch.device, stream: Optional[torch.cuda.Stream]):
     """The device of a call's tensors and its stream as the current ones: what is allocated inside belongs to that stream."""
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"stream must be one of {dev}")
     with torch.cuda.device(dev), torch.cuda.stream(stream):
         yield
 

@@ -137,3 +137,12 @@ def test_tensors_on_the_host_are_refused():
     for name in ("rotate_qk", "append_paged", "attend_paged", "evict_paged"):
         with pytest.raises(TypeError):
             getattr(binding._native, name)(1, 2, 3)
+
+
+def test_a_stream_of_another_device_is_refused():
+    class Stream:
+        device = torch.device("cuda", 1)
+
+    with pytest.raises(ValueError, match="stream must be one of cuda:0"):
+        with binding._on(torch.device("cuda", 0), Stream()):
+            pass
