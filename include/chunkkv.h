@@ -335,10 +335,12 @@ CHUNKKV_API int chunkkv_compress_layer_alg1(const void* q_obs, const void* K, co
  *
  * chunkkv_attend_paged: attention of one new token a sequence, q [B, Hq, d] bf16 (rotated), over the rows j < lengths[b, h] of
  *   its KV head: out [B, Hq, d] bf16 = softmax(q K^T / sqrt(d)) V, in 32 bits, rounded once. A head with no row to see, or none
- *   with a logit above -inf, gets zeros; other infinite or not-a-number products go the way of the formula. weights != NULL:
- *   weights[b, h, j] += the row's attention, summed over the query heads of KV head h (0 for a logit of -inf). scratch: device memory of the call's own
- *   until it has finished, 256-byte aligned, chunkkv_attend_scratch_bytes(...) bytes (0: invalid sizes; 256: none is needed and
- *   scratch may be NULL; its contents do not matter); CHUNKKV_ENOWORKSPACE when smaller. Same result every time: sums are taken in a fixed order.
+ *   with a logit above -inf, gets zeros; other infinite or not-a-number logits go the way of the formula. Values are added up before
+ *   they are divided by the sum of weights: they may be as large as 2^88, and an infinite one, in a row that is seen, makes its
+ *   dim of the output infinite or not a number. weights != NULL: weights[b, h, j] += the row's attention, summed over the query
+ *   heads of KV head h (0 for a logit of -inf). scratch: device memory of the call's own until it has finished, 256-byte
+ *   aligned, chunkkv_attend_scratch_bytes(...) bytes (0: invalid sizes; 256: none is needed and scratch may be NULL; its contents
+ *   do not matter); CHUNKKV_ENOWORKSPACE when smaller. Same result every time: sums are taken in a fixed order.
  *
  * chunkkv_evict_paged: heads with n = lengths[b, h] > budget rows go back to at most budget: C = floor((n - w) / c) chunks of c
  *   rows from row 0, r = n - C c rows behind them (w <= r < w + c), k = floor((budget - r) / c) of the chunks stay, those with

@@ -264,6 +264,27 @@ def test_attention_of_infinite_and_extreme_logits(d, G, room):
     assert torch.equal(out[0, 3 * G], to_dev(V[at[77][0], at[77][1], 3]))
 
 
+@pytest.mark.parametrize("room", [0, 600])
+def test_attention_over_large_and_infinite_values(room):
+    """Values of up to 2^88 are not too large (products with powers of two are exact: the same output, times as much); an infinite one reaches
+    its own dim alone."""
+    rng = np.random.default_rng(31)
+    K, V, tables = new_cache(rng, 2, 2, 64, 16, 8)
+    q, lengths = rand_bits(rng, (2, 6, 64)), np.full((2, 2), 120, dtype=np.int32)
+    lengths[1, 1] = 0
+    tables = np.concatenate([tables, np.full((2, room), -1, dtype=np.int32)], 1)
+    v = to_dev(V).clamp(-3.9, 3.9)
+    args = to_dev(q), torch.from_numpy(tables).cuda(), torch.from_numpy(lengths).cuda(), to_dev(K)
+    out = ck.attend_paged(*args, v)
+    assert torch.equal(ck.attend_paged(*args, v * 2.0**86), out * 2.0**86)
+    p, s = ora.place(tables[0], 77, 16, len(K))
+    v[p, s, 1, 5] = float("inf")
+    got = ck.attend_paged(*args, v)
+    rest = torch.arange(64, device=got.device) != 5
+    assert not torch.isfinite(got[0, 3:, 5]).any()
+    assert torch.equal(got[..., rest], out[..., rest]) and torch.equal(got[1], out[1]) and torch.equal(got[0, :3], out[0, :3])
+
+
 @pytest.mark.parametrize("Hq,Hkv,d,B,n,page", [(8, 2, 64, 1, 20011, 16), (32, 8, 128, 1, 3501, 16), (12, 1, 128, 2, 9001, 64), (28, 4, 128, 3, 2500, 7),
                                                (4, 4, 64, 40, 300, 32), (2, 1, 128, 300, 90, 16)])
 def test_attention_over_long_and_many_caches(Hq, Hkv, d, B, n, page):
