@@ -8,7 +8,7 @@
 // on the tensor cores with the rows, then the dims, as 16 rows of a product and the heads of a group as its eight columns: S^T = K Q^T and O^T += V^T P^T,
 // so that half the products are not empty up to eight heads, a head's statistics and values lie in the same lanes, and V^T comes out of shared memory as it
 // is needed. P is split into two bf16 terms, so that its rounding (2^-16) is not seen beside that of the output. A head's reference moves only when a
-// logit lies 2^8 above it, which a vote finds without looking for the maximum. 64 sequences of 4160 rows, 8 heads of 128 dims: 164 us, the memory's own
+// logit lies 2^8 above it, which a vote finds without looking for the maximum. 64 sequences of 4160 rows, 8 heads of 128 dims: 166 us, the memory's own
 // time (what a step takes is what an SM gets out of the L2, 62 GB/s, or the memory: half the instructions did not change it).
 //
 // The rows of all units (a sequence's heads that a CTA takes together) are cut into tiles and dealt evenly to the CTAs in one line, so that lengths
@@ -812,6 +812,10 @@ __global__ void __launch_bounds__(32 * W, 8 / W) attend_small_kernel(const Atten
         for (int off = 1; off < n_cta; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
         return x;
     };
+    static_assert(8 * NH * 16 <= 32 * 8, "a slot for every head in clusters of 16, which have 8 warps");
+    const int own = min(slot, heads - 1);
+    float2 own_s = make_float2(0.f, 0.f);
+    if constexpr (SUMS) own_s = *cluster.map_shared_rank(&sm.cta_ml[own], c);           // (on its way beside the first item's)
     for (int e0 = 0; e0 < heads * (D / 4); e0 += kSmallThreads) {       // every CTA an even share of the items
         const int e = min(e0 + rank * slots + slot, heads * (D / 4) - 1), q = e / (D / 4), c4 = e % (D / 4) * 4;
         const float2 s = *cluster.map_shared_rank(&sm.cta_ml[q], c);
@@ -822,12 +826,8 @@ __global__ void __launch_bounds__(32 * W, 8 / W) attend_small_kernel(const Atten
         if (c == 0) *reinterpret_cast<uint2*>(a.out + (q_row + q) * D + c4) = make_uint2(pack_bf16(v0 * r, v1 * r), pack_bf16(v2 * r, v3 * r));
     }
     if constexpr (SUMS) {
-        for (int q0 = 0; q0 < heads; q0 += slots) {
-            const int q = min(q0 + slot, heads - 1);
-            const float2 s = *cluster.map_shared_rank(&sm.cta_ml[q], c);
-            const float ref = reference_of(top(s.x)), ll = sum(s.y * exp2_fast(s.x - ref));
-            if (c == 0) sm.all[q] = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
-        }
+        const float ref = reference_of(top(own_s.x)), ll = sum(own_s.y * exp2_fast(own_s.x - ref));
+        if (c == 0) sm.all[own] = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kOwnRows; ++i) {
@@ -951,7 +951,7 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     // Short caches: as many CTAs a head as are resident beside each other, where they do not have many more rows each than in even shares of all
     // SMs. The second launch and its records cost 3 to 5 us; 128 rows of a CTA 0.8 (64 dims) to 1.2 us. One launch and two, us: one sequence of 8 heads,
     // 128 dims, 100 / 2000 / 4000 / 8000 rows 4.7 and 6.2 / 6.2 and 8.4 / 8.3 and 8.4 / 13.0 and 12.0; of 2 heads, 64 dims, 4000 / 8000 rows 6.7 and 6.7 /
-    // 9.8 and 6.9; 16 of 8 heads, 1000 rows 15.7 and 17.3, unlike lengths 13.1 and 15.4; 8 of 4 heads, 4352 rows, sums, 20.2 and 20.8, unlike 17.7 and 17.3.
+    // 9.8 and 6.9; 16 of 8 heads, 1000 rows 15.7 and 17.3, unlike lengths 13.1 and 15.4; 8 of 4 heads, 4352 rows, sums, 19.7 and 20.8, unlike 17.7 and 17.3.
     // Clusters of 16 take 0.5 us longer to launch: 3 sequences of 2 heads, 12 query heads each, 300 / 4000 rows 7.5 / 9.9 us with 16, 6.8 / 15.6 without.
     // At most kSmallRows each, as sequences need not be alike (128 CTAs of 2000 rows: 25.9 and 29.6 where they are). More heads than SMs, a CTA of
     // four warps each: 24 sequences of 8 heads, 70 / 300 / 600 rows 5.2 and 9.0 / 8.7 and 14.0 / 14.7 and 18.1; more than are resident, 40 of 8, 70 / 150 /
