@@ -11,6 +11,8 @@ Tolerances (u = 2^-8: half a step of bf16, relative; e = 2^-24: of fp32)
              value, plus half a step of fp32 of the sum before and after.
   eviction   exact.
 """
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -445,6 +447,33 @@ def test_attention_is_the_same_every_time_and_beside_others():
     assert torch.equal(outs[0], ck.attend_paged(*sets[0]))
 
 
+def test_calls_of_several_threads():
+    """Four host threads, a stream each, at the same time: what one call alone gives (short and long form, whose scratch is each call's own)."""
+    rng = np.random.default_rng(12)
+    jobs = []
+    for i, (Hq, Hkv, d, B, n) in enumerate([(32, 8, 128, 3, 1500), (8, 2, 64, 2, 200), (12, 1, 128, 5, 2500), (8, 8, 64, 40, 700)]):
+        K, V, tables = new_cache(rng, B, Hkv, d, 16, -(-n // 16))
+        jobs.append((to_dev(rand_bits(rng, (B, Hq, d))), i32(tables), i32(rng.integers(1, n, (B, Hkv))), to_dev(K), to_dev(V)))
+    want = [ck.attend_paged(*j) for j in jobs]
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    got = [[] for _ in jobs]
+
+    def work(i):
+        with torch.cuda.stream(streams[i]):
+            for k in range(50):
+                got[i].append(ck.attend_paged(*jobs[i], stream=streams[i] if k % 2 else None))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(jobs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert len(g) == 50 and all(torch.equal(x, w) for x in g)
+
+
 # ------------------------------------------------------------------------------------------------ eviction
 def check_eviction(rng, B, Hkv, d, page, per, lengths, w, c, budget, weights, holes=()):
     K, V, tables = new_cache(rng, B, Hkv, d, page, per)
@@ -535,6 +564,29 @@ def test_calls_with_nothing_to_do():
         idx = ck.evict_paged(w, table, lengths, K, V, 2, 1, 4)
         assert q.shape == out.shape == (B, Hq, d) and not out.any() and not w.any() and not lengths.any()
         assert idx.shape == (B, Hkv, 4) and (idx == -1).all() and (K == 7).all() and (V == 7).all()
+
+
+@pytest.mark.parametrize("B,Hq,Hkv", [(1, 65535, 1), (1, 4099, 4099), (9001, 1, 1), (2, 65534, 32767)])
+def test_very_many_heads_and_sequences(B, Hq, Hkv):
+    """As many query heads as there may be, of one KV head and of many; more sequences than any launch has CTAs at once."""
+    rng = np.random.default_rng(B + Hkv)
+    d, page, per = 64, 4, 2
+    K, V, tables = new_cache(rng, B, Hkv, d, page, per, spare=1)
+    lengths = rng.integers(0, page * per + 1, (B, Hkv)).astype(np.int32)
+    check_attention(rand_bits(rng, (B, Hq, d)), K, V, tables, lengths, rng.random((B, Hkv, page * per)).astype(np.float32))
+    # appended: every head's last row is the token's, and nothing else changed
+    dK, dV, cos, sin = to_dev(K), to_dev(V), torch.ones(1, d // 2, device="cuda"), torch.zeros(1, d // 2, device="cuda")
+    qkv, zeros = to_dev(rand_bits(rng, (B, (Hq + 2 * Hkv) * d))), torch.zeros(B, device="cuda", dtype=torch.int32)
+    q = ck.append_paged(qkv, Hq, cos, sin, zeros, i32(tables), i32(lengths), dK, dV)
+    assert torch.equal(q.flatten(1), qkv[:, :Hq * d])
+    b, h = np.nonzero(lengths)
+    at = lengths[b, h] - 1
+    p, s = tables[b, at // page], at % page
+    want_K, want_V = to_dev(K), to_dev(V)
+    heads = qkv.view(B, -1, d)
+    want_K[p, s, h], want_V[p, s, h] = heads[b, Hq + h], heads[b, Hq + Hkv + h]
+    assert torch.equal(dK, want_K) and torch.equal(dV, want_V)
+    check_eviction(rng, B, Hkv, d, page, per, lengths, 1, 1, 5, rng.random((B, Hkv, page * per)))
 
 
 # ------------------------------------------------------------------------------------------------ together
