@@ -101,7 +101,11 @@ __device__ __forceinline__ int tiles_of(const AttendArgs& a, int u) {
 }
 
 // The line of tiles: the units in order, each `groups` times its tiles (one for each group of query heads), dealt to n CTAs in shares
-// of `per`, the first `more` of them of one more.
+// of `per`, the first `more` of them of one more. In front of a unit's tiles stand kBegin that hold no rows, for the time that a CTA takes to
+// begin with another unit (table, queries, first rows: 2 to 3 us, as long as 2 to 4 tiles take). us without them, with 2, 3 and 4: 64 sequences of 8
+// heads, 300 rows 21.1, 20.5, 20.3, 20.3; 24 of 1200 26.7, 25.5, 25.3, 25.3; of 2 heads, 64 dims, 64 of 2400 21.6, 20.9, 21.1, 21.2.
+constexpr int kBegin = 3;
+__device__ __forceinline__ int span_of(int tiles) { return tiles > 0 ? tiles + kBegin : 0; }
 struct Share {
     int n, per, more;
     __device__ __forceinline__ Share(int total, int n_cta) {    // (no more CTAs than tiles, so that each has one at least)
@@ -116,7 +120,7 @@ struct Share {
     }
 };
 struct Deal {
-    int total;            // tiles in all
+    int total;            // the line's length
     int unit;             // the unit that holds the first tile of this CTA
     int first;            // its first tile
 };
@@ -129,7 +133,7 @@ __device__ __forceinline__ Deal deal(const AttendArgs& a, int cta, int n_cta, De
     const int units = a.B * a.blocks, per = (units + kAttThreads - 1) / kAttThreads;
     const int u0 = min(static_cast<int>(threadIdx.x) * per, units), u1 = min(u0 + per, units);
     int mine = 0;
-    for (int u = u0; u < u1; ++u) mine += tiles_of(a, u);
+    for (int u = u0; u < u1; ++u) mine += span_of(tiles_of(a, u));
     mine *= a.groups;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int inc = mine;
@@ -152,7 +156,7 @@ __device__ __forceinline__ Deal deal(const AttendArgs& a, int cta, int n_cta, De
     if (at <= tile && tile < inc) {                             // one thread, if any
         int u = u0;
         for (; u + 1 < u1; ++u) {
-            const int t = tiles_of(a, u) * a.groups;
+            const int t = span_of(tiles_of(a, u)) * a.groups;
             if (tile < at + t) break;
             at += t;
         }
@@ -440,7 +444,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
     // A part of this CTA's share: tiles [tile0, tile1) of a unit, for one group of query heads.
     struct Part {
         Unit un;
-        int unit, tiles, first, grp, tile0, tile1;
+        int unit, tiles, first, grp, tile0, tile1;     // (none, where tile1 <= tile0)
         int rows_end;                // of this warp's head, within the part
         __device__ __forceinline__ bool begins() const { return tile0 == 0; }
         __device__ __forceinline__ bool whole() const { return tile0 == 0 && tile1 == tiles; }
@@ -451,9 +455,9 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
         p.first = first;
         p.un = unit_of(a, unit);
         p.tiles = tiles_of(a, unit);
-        p.grp = a.groups == 1 ? 0 : (x - first) / p.tiles;
-        const int begin = first + p.grp * p.tiles;
-        p.tile0 = x - begin;
+        p.grp = a.groups == 1 ? 0 : (x - first) / span_of(p.tiles);
+        const int begin = first + p.grp * span_of(p.tiles) + kBegin;
+        p.tile0 = max(x - begin, 0);
         p.tile1 = min(x1 - begin, p.tiles);
         const bool on = head < p.un.heads && turn < turns;      // (else this warp has no head here)
         p.rows_end = on ? min(rows_of(a, p.un.b * a.Hkv + p.un.h0 + head), p.tile1 * a.tile) : 0;
@@ -465,6 +469,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
     };
 
     Part p = part_at(share.begin(cta), dl.unit, dl.first);
+    if (p.tile1 <= p.tile0) return;
     begin_part(p);
     for (;;) {
         const int heads = walk.heads;                           // query heads of this group
@@ -482,7 +487,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
         });
 
         // the part behind this one, if any: where no other warp's values are joined in the rings' place its first rows are asked for at once
-        const int x = p.first + p.grp * p.tiles + p.tile1;
+        const int x = p.first + p.grp * span_of(p.tiles) + kBegin + p.tile1;
         Part next = p;
         bool more = x < x1;
         if (more) {
@@ -493,6 +498,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
             }
             more = unit < units;
             if (more) next = part_at(x, unit, first);
+            more = more && next.tile0 < next.tile1;
         }
         constexpr bool kApart = AttSmem<D, NH>::kApart;
         if (more && (kApart || turns == 1)) begin_part(next);
@@ -510,7 +516,7 @@ __global__ void __launch_bounds__(kAttThreads, 1) attend_kernel(const AttendArgs
         }
         walk.add_up();
         if (p.begins() && threadIdx.x == 0)
-            a.shared_by[static_cast<size_t>(p.unit) * a.groups + p.grp] = make_int2(cta, share.owner(p.first + (p.grp + 1) * p.tiles - 1));
+            a.shared_by[static_cast<size_t>(p.unit) * a.groups + p.grp] = make_int2(cta, share.owner(p.first + (p.grp + 1) * span_of(p.tiles) - 1));
         const bool whole = p.whole();
         if (turn == 0 && head < p.un.heads) {
 #pragma unroll
@@ -812,10 +818,6 @@ __global__ void __launch_bounds__(32 * W, 8 / W) attend_small_kernel(const Atten
         for (int off = 1; off < n_cta; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
         return x;
     };
-    static_assert(8 * NH * 16 <= 32 * 8, "a slot for every head in clusters of 16, which have 8 warps");
-    const int own = min(slot, heads - 1);
-    float2 own_s = make_float2(0.f, 0.f);
-    if constexpr (SUMS) own_s = *cluster.map_shared_rank(&sm.cta_ml[own], c);           // (on its way beside the first item's)
     for (int e0 = 0; e0 < heads * (D / 4); e0 += kSmallThreads) {       // every CTA an even share of the items
         const int e = min(e0 + rank * slots + slot, heads * (D / 4) - 1), q = e / (D / 4), c4 = e % (D / 4) * 4;
         const float2 s = *cluster.map_shared_rank(&sm.cta_ml[q], c);
@@ -826,8 +828,12 @@ __global__ void __launch_bounds__(32 * W, 8 / W) attend_small_kernel(const Atten
         if (c == 0) *reinterpret_cast<uint2*>(a.out + (q_row + q) * D + c4) = make_uint2(pack_bf16(v0 * r, v1 * r), pack_bf16(v2 * r, v3 * r));
     }
     if constexpr (SUMS) {
-        const float ref = reference_of(top(own_s.x)), ll = sum(own_s.y * exp2_fast(own_s.x - ref));
-        if (c == 0) sm.all[own] = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
+        for (int q0 = 0; q0 < heads; q0 += slots) {
+            const int q = min(q0 + slot, heads - 1);
+            const float2 s = *cluster.map_shared_rank(&sm.cta_ml[q], c);
+            const float ref = reference_of(top(s.x)), ll = sum(s.y * exp2_fast(s.x - ref));
+            if (c == 0) sm.all[q] = make_float2(ref, ll == 0.f ? 0.f : 1.f / ll);
+        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kOwnRows; ++i) {
