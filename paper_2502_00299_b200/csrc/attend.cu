@@ -954,21 +954,29 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
         if (p.tile == 1 << s) p.tile_shift = s;
     const long long tiles = static_cast<long long>(B) * p.blocks * p.groups * ((cap + p.tile - 1) / p.tile);
     p.max_ctas = static_cast<int>(tiles < kAttMaxCtas ? tiles : kAttMaxCtas);
-    // Short caches: as many CTAs a head as are resident beside each other, where they do not have many more rows each than in even shares of all
-    // SMs. The second launch and its records cost 3 to 5 us; 128 rows of a CTA 0.8 (64 dims) to 1.2 us. One launch and two, us: one sequence of 8 heads,
-    // 128 dims, 100 / 2000 / 4000 / 8000 rows 4.7 and 6.2 / 6.2 and 8.4 / 8.3 and 8.4 / 13.0 and 12.0; of 2 heads, 64 dims, 4000 / 8000 rows 6.7 and 6.7 /
-    // 9.8 and 6.9; 16 of 8 heads, 1000 rows 15.7 and 17.3, unlike lengths 13.1 and 15.4; 8 of 4 heads, 4352 rows, sums, 19.7 and 20.8, unlike 17.7 and 17.3.
+    // Short caches: as many CTAs a head as are resident beside each other, up to 1024 rows each (sequences need not be alike), or, where even shares of
+    // all SMs would not be many rows less, kSmallRows. us in one launch and
+    // in two, 128 dims: one sequence of 8 heads, 100 / 2000 / 4352 / 6000 / 9000 rows 4.7 and 6.8 / 6.2 and 9.2 / 9.0 and 11.8 / 10.4 and 13.2 / 14.0 and 16.0;
+    // 16 of them, 300 / 1000 rows 6.2 and 10.1 / 15.5 and 17.7, of unlike lengths 5.9 and 9.4 / 12.8 and 14.4; 8 of 4 heads, 7 query heads each, 4352 rows 17.3 and 18.7,
+    // unlike 15.1 and 15.7, with sums 19.9 and 19.9, unlike 17.3 and 16.3; 4 of them, sums, 4352 rows (1088 a CTA, 64 CTAs) 15.2 and 14.3;
+    // one of 2 heads, 64 dims, 4352 / 9000 rows 6.2 and 7.3 / 7.7 and 8.2.
     // Clusters of 16 take 0.5 us longer to launch: 3 sequences of 2 heads, 12 query heads each, 300 / 4000 rows 7.5 / 9.9 us with 16, 6.8 / 15.6 without.
-    // At most kSmallRows each, as sequences need not be alike (128 CTAs of 2000 rows: 25.9 and 29.6 where they are). More heads than SMs, a CTA of
-    // four warps each: 24 sequences of 8 heads, 70 / 300 / 600 rows 5.2 and 9.0 / 8.7 and 14.0 / 14.7 and 18.1; more than are resident, 40 of 8, 70 / 150 /
-    // 300 / 600 rows 8.7 and 12.2 / 10.7 and 14.0 / 17.8 and 18.2 / 27.8 and 24.8, with sums of 64 of 8, 70 / 150 rows 10.7 and 12.7 / 17.0 and 15.0.
+    // More heads than SMs, a CTA of four warps each: 24 sequences of 8 heads, 100 / 300 / 600 / 1000 rows 5.3 and 9.4 / 8.6 and 12.3 / 14.6 and 16.7 / 20.6 and
+    // 22.6. More than are resident: a CTA of the long form takes a sequence's heads, up to eight, together, so it depends on them. One launch against two: 64
+    // sequences of 8 heads, 160 / 240 rows -13 / -4 %, with sums +4 / +10 %, 111 sequences +4 to +30 %; 256 of 2 heads, 64 dims, 320 / 480 rows -22 / -5 %,
+    // 444 sequences, 160 / 320 rows -15 / -2 %.
     const long long items = static_cast<long long>(B) * Hkv * p.groups;
     p.cluster = items <= 7 && cap > 1536 ? 16 : items <= 15 ? 8 : items <= 33 ? 4 : items <= 74 ? 2 : 1;
     p.warps = items <= 148 ? 8 : 4;
     const long long steps = (cap + kAttStep - 1) / kAttStep, rows = (steps + p.cluster - 1) / p.cluster * kAttStep;
     const long long kept = rows + 4;                            // (logits of four neighbouring pairs of heads lie in different banks)
     const size_t fixed = p.warps == 8 ? small_bytes<8>(d, p.nh) : small_bytes<4>(d, p.nh);
-    const bool few = items <= 148 ? rows <= kSmallRows && rows - items * cap / 148 <= 300 : items <= 296 ? rows <= kSmallRows : items <= kSmallItems && rows <= 128;
+    const long long most = items <= 148 && rows - items * cap / 148 > 300 ? 1024
+                           : items <= 296                                 ? kSmallRows
+                           : items <= 592                                 ? (p.block > 4 ? 160 : 400)
+                           : items <= kSmallItems && p.block <= 4         ? 160
+                                                                          : 0;
+    const bool few = rows <= most;
     p.small_rows = static_cast<int>(few ? kept : 0);
     if (!few || (sums && (p.groups > 1 || fixed + 4ull * p.group * kept > static_cast<size_t>(small_smem(p.warps))))) p.cluster = 0;
     if (p.cluster > 0) {
