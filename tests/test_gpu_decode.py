@@ -300,7 +300,7 @@ def test_attention_over_long_and_many_caches(Hq, Hkv, d, B, n, page):
 
 @pytest.mark.parametrize("Hkv,B,d", [(1, 1, 128), (5, 1, 64), (3, 2, 64), (3, 5, 64), (2, 8, 128), (8, 4, 64), (1, 60, 128), (6, 20, 64), (148, 1, 64), (149, 1, 64)])
 def test_attention_with_every_size_of_cluster(Hkv, B, d):
-    """Short caches: a head's rows go to 16, 8, 4, 2 or 1 CTAs, or (149 heads) to shares of CTAs; with fewer steps of 16 rows than CTAs among them."""
+    """Short caches: a head's rows go to 16, 8, 4, 2 or 1 CTAs, of four warps with 149 heads; with fewer steps of 16 rows than CTAs among them."""
     rng = np.random.default_rng(Hkv * B)
     page, per = (16, 9) if B > 1 or Hkv > 5 else (16, 110)                   # (more than 1536 rows: 16)
     K, V, tables = new_cache(rng, B, Hkv, d, page, per)
