@@ -80,7 +80,7 @@ __device__ __forceinline__ float reference_of(float m) { return m == -INFINITY ?
 __device__ __forceinline__ float weight_of(float logit, const float2& f) { return logit == -INFINITY ? 0.f : exp2_fast(logit - f.x) * f.y; }
 
 // Rows of a head and of a unit, the `block` heads from h0 on of a sequence.
-__device__ __forceinline__ int rows_of(const AttendArgs& a, int bh) { return min(max(__ldg(a.lengths + bh), 0), a.cache.cap); }
+__device__ __forceinline__ int rows_of(const AttendArgs& a, int bh) { return min(max(a.lengths[bh], 0), a.cache.cap); }
 struct Unit {
     int b, h0, heads;     // sequence, its KV heads [h0, h0 + heads)
 };
@@ -93,7 +93,7 @@ __device__ __forceinline__ int tiles_of(const AttendArgs& a, int u) {
     const int32_t* len = a.lengths + un.b * a.Hkv + un.h0;
     int n[kAttWarps], most = 0;
 #pragma unroll
-    for (int h = 0; h < kAttWarps; ++h) n[h] = __ldg(len + min(h, un.heads - 1));       // (side by side: one after the other takes 0.3 us each)
+    for (int h = 0; h < kAttWarps; ++h) n[h] = len[min(h, un.heads - 1)];       // (side by side: one after the other takes 0.3 us each)
 #pragma unroll
     for (int h = 0; h < kAttWarps; ++h) most = max(most, n[h]);
     const int last = min(most, a.cache.cap) + a.tile - 1;
@@ -244,7 +244,7 @@ struct Walk {
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
-                    qr[n][i][e] = base < end && 8 * n + g < heads ? __ldg(reinterpret_cast<const uint32_t*>(q + static_cast<size_t>(8 * n + g) * D + 16 * i + 8 * e)) : 0u;
+                    qr[n][i][e] = base < end && 8 * n + g < heads ? *reinterpret_cast<const uint32_t*>(q + static_cast<size_t>(8 * n + g) * D + 16 * i + 8 * e) : 0u;
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) {
             if (base + i * stride < end) copy_step(at[i], ring + i * 2 * kHalf);

@@ -1,6 +1,11 @@
 // Device helpers shared by the kernels that work on the decode cache (rotate.cu, attend.cu, evict.cu): rows of a paged cache
 // [num_pages, page_size, Hkv, d] found through a sequence's block table, bf16 pairs, vector loads, and the ordering against the
 // kernel ahead.
+//
+// These kernels are on the SMs while the kernel ahead, which may be one of them, still writes what they read: queries, lengths, sums, rows, and, from a
+// program's own kernels, tables, positions and angles. All of that is therefore read with coherent loads (plain ones, asynchronous copies,
+// load_once), which stay behind the wait. The read-only path (the intrinsic and the .nc loads) is for data that nothing writes as long as a kernel
+// lives: the compiler may move such a load to the front of the wait, and no wait makes it see what was written meanwhile.
 #pragma once
 #include "decode.h"
 
@@ -13,7 +18,7 @@ namespace chunkkv {
 // Row `row` (below cap) of the sequence with table `table` as a row of the cache, page * page_size + slot; -1: its page is outside the cache.
 __device__ __forceinline__ int paged_row(const PagedCache& c, const int32_t* table, int row) {
     const int p = static_cast<int>((__umulhi(c.magic, static_cast<uint32_t>(row)) + static_cast<uint32_t>(row)) >> c.shift);
-    const int page = __ldg(table + p);
+    const int page = table[p];
     return static_cast<unsigned>(page) < static_cast<unsigned>(c.num_pages) ? page * c.page_size + (row - p * c.page_size) : -1;
 }
 

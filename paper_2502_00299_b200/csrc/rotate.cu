@@ -77,12 +77,12 @@ __global__ void __launch_bounds__(kRotThreads, kRotCtas) rotate_kernel(const Rot
     const __nv_bfloat16* x = a.qkv + static_cast<size_t>(t) * a.row_elems + 8 * l;
 
     float co[8], si[8];
-    const int pos = __ldg(a.positions + t);
+    const int pos = a.positions[t];
     const bool known = static_cast<unsigned>(pos) < static_cast<unsigned>(a.n_pos);
     {
         const size_t at = static_cast<size_t>(known ? pos : 0) * (D / 2) + 8 * l;
         const float4 *c4 = reinterpret_cast<const float4*>(a.cos_t + at), *s4 = reinterpret_cast<const float4*>(a.sin_t + at);
-        const float4 c0 = __ldg(c4), c1 = __ldg(c4 + 1), n0 = __ldg(s4), n1 = __ldg(s4 + 1);
+        const float4 c0 = c4[0], c1 = c4[1], n0 = s4[0], n1 = s4[1];
         co[0] = c0.x; co[1] = c0.y; co[2] = c0.z; co[3] = c0.w; co[4] = c1.x; co[5] = c1.y; co[6] = c1.z; co[7] = c1.w;
         si[0] = n0.x; si[1] = n0.y; si[2] = n0.z; si[3] = n0.w; si[4] = n1.x; si[5] = n1.y; si[6] = n1.z; si[7] = n1.w;
     }
@@ -93,8 +93,8 @@ __global__ void __launch_bounds__(kRotThreads, kRotCtas) rotate_kernel(const Rot
         const bool norm = gain != nullptr;
         uint4 g_lo = make_uint4(0, 0, 0, 0), g_hi = g_lo;
         if (norm) {
-            g_lo = __ldg(reinterpret_cast<const uint4*>(gain + 8 * l));
-            g_hi = __ldg(reinterpret_cast<const uint4*>(gain + D / 2 + 8 * l));
+            g_lo = *reinterpret_cast<const uint4*>(gain + 8 * l);
+            g_hi = *reinterpret_cast<const uint4*>(gain + D / 2 + 8 * l);
         }
         for (int s = b; s < e; s += kRotAhead) {
             uint4 lo[kRotAhead], hi[kRotAhead];
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kRotThreads, kRotCtas) rotate_kernel(const Rot
     };
     // this token's place in the cache for head h, or NULL
     auto cached = [&](__nv_bfloat16* cache, int h) -> __nv_bfloat16* {
-        const int row = __ldg(a.lengths + static_cast<size_t>(t) * a.Hkv + h) - 1;
+        const int row = a.lengths[static_cast<size_t>(t) * a.Hkv + h] - 1;
         if (row < 0 || row >= a.cache.cap) return nullptr;
         const int at = paged_row(a.cache, a.cache.tables + static_cast<size_t>(t) * a.cache.max_pages, row);
         return at < 0 ? nullptr : cache + (static_cast<size_t>(at) * a.Hkv + h) * D + 8 * l;
