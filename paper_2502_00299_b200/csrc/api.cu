@@ -819,20 +819,27 @@ int chunkkv_append_paged(const void* qkv, long long row_elems, int B, int Hq, in
     return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
 }
 
+// The sizes that attention takes. Its kernels count tiles of at least 16 rows, three more for every beginning of one, and CTAs in 32 bits: a CTA
+// takes at most eight KV heads of a sequence and 16 query heads of each together, so there are no more of either than counted here.
+static int check_attend(int B, int Hq, int Hkv, int d, int max_pages, int page_size, int num_pages) {
+    int st = check_decode_heads(B, Hq, Hkv, d);
+    if (st == CHUNKKV_OK) st = check_decode_cache(max_pages, page_size, num_pages);
+    if (st != CHUNKKV_OK) return st;
+    const long long walks = static_cast<long long>(B) * Hkv * ((Hq / Hkv + 7) / 8);       // (below 2^30)
+    return walks * (max_pages * page_size / 16 + 8) >= (1LL << 31) ? CHUNKKV_EINVAL_SHAPE : CHUNKKV_OK;
+}
+
 size_t chunkkv_attend_scratch_bytes(int B, int Hq, int Hkv, int d, int max_pages, int page_size, int with_weights) {
-    if (B < 1 || check_decode_heads(B, Hq, Hkv, d) != CHUNKKV_OK || check_decode_cache(max_pages, page_size, 1) != CHUNKKV_OK) return 0;
+    if (B < 1 || check_attend(B, Hq, Hkv, d, max_pages, page_size, 1) != CHUNKKV_OK) return 0;
     return attend_plan(B, Hq, Hkv, d, max_pages * page_size, with_weights != 0).bytes;
 }
 
 int chunkkv_attend_paged(const void* q, const int32_t* block_tables, int max_pages, const int32_t* lengths, int page_size, int num_pages,
                          const void* cache_K, const void* cache_V, int B, int Hq, int Hkv, int d, float* weights, void* out, void* scratch,
                          size_t scratch_bytes, void* stream) {
-    int st = check_decode_heads(B, Hq, Hkv, d);
-    if (st == CHUNKKV_OK) st = check_decode_cache(max_pages, page_size, num_pages);
+    int st = check_attend(B, Hq, Hkv, d, max_pages, page_size, num_pages);
     if (st != CHUNKKV_OK) return st;
     const int cap = max_pages * page_size;
-    // tiles of at least 16 rows are counted, and CTAs of a launch
-    if (static_cast<long long>(B) * Hq * (cap / 16 + 8) >= (1LL << 31)) return CHUNKKV_EINVAL_SHAPE;
     if (B == 0) return CHUNKKV_OK;
     if (q == nullptr || block_tables == nullptr || lengths == nullptr || cache_K == nullptr || cache_V == nullptr || out == nullptr) return CHUNKKV_EINVAL_NULL;
     if (!aligned16(q) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) || !aligned4(weights) || !aligned16(out))
