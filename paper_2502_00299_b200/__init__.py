@@ -13,11 +13,15 @@ _EXPORTS = (
     "profile_read", "score", "select", "set_workspace", "strerror", "workspace_bytes",
 )
 __all__ = list(_EXPORTS)
+_NAMES = frozenset(_EXPORTS)
 
 
 def __getattr__(name):
-    if name in _EXPORTS:
-        from . import binding
-        globals()[name] = value = getattr(binding, name)         # (found here from now on: a look-up less a call)
-        return value
+    # Names are looked up in the binding every time: what is put in its place there (a hook, a test's patch, a reload) is what callers get.
+    # Loaded, the binding is an attribute of this package, which is found in half the time that an import statement takes.
+    if name in _NAMES:
+        module = globals().get("binding")
+        if module is None:
+            from . import binding as module
+        return getattr(module, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
