@@ -339,8 +339,8 @@ CHUNKKV_API int chunkkv_compress_layer_alg1(const void* q_obs, const void* K, co
  *   they are divided by the sum of weights: they may be as large as 2^88, and an infinite one, in a row that is seen, makes its
  *   dim of the output infinite or not a number. weights != NULL: weights[b, h, j] += the row's attention, summed over the query
  *   heads of KV head h (0 for a logit of -inf). scratch: device memory of the call's own until it has finished, 256-byte
- *   aligned, chunkkv_attend_scratch_bytes(...) bytes (0: invalid sizes; 256: none is needed and scratch may be NULL; its contents
- *   do not matter); CHUNKKV_ENOWORKSPACE when smaller. Same result every time: sums are taken in a fixed order.
+ *   aligned, chunkkv_attend_scratch_bytes(...) bytes on the call's device (0: invalid sizes; 256: none is needed and scratch may be
+ *   NULL; its contents do not matter); CHUNKKV_ENOWORKSPACE when smaller. Same result every time: sums are taken in a fixed order.
  *   Beyond the limits above, B * Hkv * ceil(Hq / Hkv / 8) * (max_pages * page_size / 16 + 8) < 2^31 (else CHUNKKV_EINVAL_SHAPE, and 0 bytes).
  *
  * chunkkv_evict_paged: heads with n = lengths[b, h] > budget rows go back to at most budget: C = floor((n - w) / c) chunks of c

@@ -30,6 +30,7 @@ struct ProfileRec {
 struct DeviceCtx {
     bool init = false;
     int num_sms = 0;
+    int wide_clusters = -1;          // whether attend_paged can have clusters of 16; -1: not asked yet
     int smem_optin = 0;
     void* ws = nullptr;        // scratch handed over with chunkkv_set_workspace (header + payload)
     size_t ws_bytes = 0;
@@ -829,9 +830,24 @@ static int check_attend(int B, int Hq, int Hkv, int d, int max_pages, int page_s
     return walks * (max_pages * page_size / 16 + 8) >= (1LL << 31) ? CHUNKKV_EINVAL_SHAPE : CHUNKKV_OK;
 }
 
+// The plan of a call on the current device. Without one there is nothing to launch, and the sizes are those of a whole B200.
+static AttendPlan attend_plan_here(int B, int Hq, int Hkv, int d, int cap, bool sums) {
+    const AttendPlan plan = attend_plan(B, Hq, Hkv, d, cap, sums, true);
+    if (plan.cluster <= 8) return plan;
+    std::lock_guard<std::mutex> lk(g_mu);
+    const int last = g_last_cuda_error;
+    DeviceCtx* ctx;
+    if (get_ctx(&ctx) != CHUNKKV_OK) {
+        g_last_cuda_error = last;
+        return plan;
+    }
+    if (ctx->wide_clusters < 0) ctx->wide_clusters = attend_wide_clusters();
+    return ctx->wide_clusters != 0 ? plan : attend_plan(B, Hq, Hkv, d, cap, sums, false);
+}
+
 size_t chunkkv_attend_scratch_bytes(int B, int Hq, int Hkv, int d, int max_pages, int page_size, int with_weights) {
     if (B < 1 || check_attend(B, Hq, Hkv, d, max_pages, page_size, 1) != CHUNKKV_OK) return 0;
-    return attend_plan(B, Hq, Hkv, d, max_pages * page_size, with_weights != 0).bytes;
+    return attend_plan_here(B, Hq, Hkv, d, max_pages * page_size, with_weights != 0).bytes;
 }
 
 int chunkkv_attend_paged(const void* q, const int32_t* block_tables, int max_pages, const int32_t* lengths, int page_size, int num_pages,
@@ -844,7 +860,7 @@ int chunkkv_attend_paged(const void* q, const int32_t* block_tables, int max_pag
     if (q == nullptr || block_tables == nullptr || lengths == nullptr || cache_K == nullptr || cache_V == nullptr || out == nullptr) return CHUNKKV_EINVAL_NULL;
     if (!aligned16(q) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) || !aligned4(weights) || !aligned16(out))
         return CHUNKKV_EINVAL_ALIGN;
-    const AttendPlan plan = attend_plan(B, Hq, Hkv, d, cap, weights != nullptr);
+    const AttendPlan plan = attend_plan_here(B, Hq, Hkv, d, cap, weights != nullptr);
     if (plan.bytes > kAttNoScratch) {
         if (scratch == nullptr || scratch_bytes < plan.bytes) return CHUNKKV_ENOWORKSPACE;
         if ((reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return CHUNKKV_EINVAL_ALIGN;

@@ -851,6 +851,15 @@ __global__ void __launch_bounds__(32 * W, 8 / W) attend_small_kernel(const Atten
 // Shared memory that a CTA of that form may have.
 constexpr int small_smem(int warps) { return warps == 8 ? 227 * 1024 : 113 * 1024; }
 
+cudaLaunchAttribute cluster_of(int ctas) {
+    cudaLaunchAttribute a;
+    a.id = cudaLaunchAttributeClusterDimension;
+    a.val.clusterDim.x = ctas;
+    a.val.clusterDim.y = 1;
+    a.val.clusterDim.z = 1;
+    return a;
+}
+
 template <int D, int NH, bool SUMS, int W>
 cudaError_t launch_small(const AttendArgs& a, const AttendPlan& plan, int device, cudaStream_t stream) {
     const int smem = static_cast<int>(sizeof(SmallSmem<D, NH, W>)) + (SUMS ? plan.group * plan.small_rows * 4 : 0);
@@ -870,10 +879,7 @@ cudaError_t launch_small(const AttendArgs& a, const AttendPlan& plan, int device
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = plan.cluster;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
+    attr[1] = cluster_of(plan.cluster);
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, a);
@@ -940,7 +946,7 @@ static size_t small_bytes(int d, int nh) {
 
 // Scratch: (max, sum) and O of two records a CTA, the CTAs that share a unit; where sums are asked for, (max, sum) of the units that one CTA had and
 // the logits of all rows.
-AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
+AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums, bool wide) {
     AttendPlan p;
     const int G = Hq / Hkv;
     p.nh = G > 8 ? 2 : 1;
@@ -966,7 +972,7 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     // sequences of 8 heads, 160 / 240 rows -13 / -4 %, with sums +4 / +10 %, 111 sequences +4 to +30 %; 256 of 2 heads, 64 dims, 320 / 480 rows -22 / -5 %,
     // 444 sequences, 160 / 320 rows -15 / -2 %.
     const long long items = static_cast<long long>(B) * Hkv * p.groups;
-    p.cluster = items <= 7 && cap > 1536 ? 16 : items <= 15 ? 8 : items <= 33 ? 4 : items <= 74 ? 2 : 1;
+    p.cluster = items <= 7 && cap > 1536 && wide ? 16 : items <= 15 ? 8 : items <= 33 ? 4 : items <= 74 ? 2 : 1;
     p.warps = items <= 148 ? 8 : 4;
     const long long steps = (cap + kAttStep - 1) / kAttStep, rows = (steps + p.cluster - 1) / p.cluster * kAttStep;
     const long long kept = rows + 4;                            // (logits of four neighbouring pairs of heads lie in different banks)
@@ -992,6 +998,25 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums) {
     p.off_logits = p.off_shared + (static_cast<size_t>(B) * p.blocks * p.groups * sizeof(int2) + 255) / 256 * 256;
     p.bytes = p.off_logits + (sums ? static_cast<size_t>(B) * Hq * p.logit_stride * sizeof(float) : 0);
     return p;
+}
+
+// A cluster of 16 CTAs, an SM's shared memory each, needs 16 SMs of one GPC, which parts of a device may not have. (One instantiation answers for all:
+// a CTA an SM is what each of them takes.)
+bool attend_wide_clusters() {
+    auto kernel = attend_small_kernel<128, 1, false, 8>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(16);
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = small_smem(8);
+    cudaLaunchAttribute attr[1] = {cluster_of(16)};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, small_smem(8));
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg);
+    if (e != cudaSuccess) cudaGetLastError();                   // (said to nobody: the other forms run)
+    return e == cudaSuccess && clusters > 0;
 }
 
 cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d, char* scratch, int num_sms, int device, cudaStream_t stream) {

@@ -68,7 +68,9 @@ struct AttendPlan {
     long long logit_stride;
     size_t off_o, off_whole, off_shared, off_logits, bytes;
 };
-AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums);
+// wide: clusters of 16 CTAs can be launched (more than the eight that every device takes).
+AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums, bool wide);
+bool attend_wide_clusters();                  // on the current device
 cudaError_t launch_attend(const AttendArgs& args, const AttendPlan& plan, int d, char* scratch, int num_sms, int device, cudaStream_t stream);
 
 // Eviction from a paged cache by sums of attention (evict.cu).
