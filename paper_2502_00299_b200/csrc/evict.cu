@@ -64,7 +64,8 @@ __global__ void __launch_bounds__(kEvThreads, 2) evict_kernel(const EvictArgs a)
     int32_t* idx = a.out_idx + static_cast<size_t>(bh) * a.budget;
     const int n = min(max(a.lengths[bh], 0), a.cache.cap), c = a.c;
     if (n <= a.budget) {                                            // (the whole cluster)
-        for (int i = part; i < a.budget; i += parts) idx[i] = i < n ? i : -1;
+        // (a budget may be any number up to 2^31 - 1, so that the last step of the index goes beyond it; all other counts here are below 2^30)
+        for (unsigned i = part; i < static_cast<unsigned>(a.budget); i += parts) idx[i] = i < static_cast<unsigned>(n) ? static_cast<int>(i) : -1;
         return;
     }
     const int C = (n - a.w) / c, r = n - C * c, k = (a.budget - r) / c;     // k < C, as n is above the budget
