@@ -8,6 +8,8 @@ With S_j the sum of the |q_i k_ji| of row j, s_j its logit, n the rows seen, all
   weight   both ends of a ratio have that error, so twice; a weight is a product of at most 16 exponentials (its own, moves of the reference, joins) of 2^-22 each;
            the sum of weights has n / 8 terms a lane and 200 joins, 2^-24 each.
   output   the terms of p in bf16 twice: 2^-16. A step of 16 rows cuts 2 * 17 terms at 2^-23 of sum p |v| and may scale what is there (2^-24); 200 joins.
+           A warp takes at most n / 16 + 1 steps of a head. In one launch they are 18 at most (1152 rows a CTA, four warps); in two, the T tiles (of 16
+           rows a warp; counted too high here, with those that stand for beginnings) are dealt evenly to 148 CTAs, so T / 148 + 1.
 Everything is multiplied by sum p |v|; then one rounding to bf16.
 """
 import numpy as np
@@ -35,6 +37,7 @@ def bounds(q, K, V, tables, lengths):
     B, Hq, d = q.shape
     pages, page, Hkv, _ = K.shape
     G, cap = Hq // Hkv, tables.shape[1] * page
+    dealt = max(18, B * -(-Hkv // 8) * -(-G // 8) * (cap // 16 + 5) // 148 + 2)
     out, sums = ora.attend(q, K, V, tables, lengths)
     tol, err, factor = np.full(out.shape, np.nan), np.zeros(sums.shape), np.zeros((B, Hq))
     for b in range(B):
@@ -59,7 +62,7 @@ def bounds(q, K, V, tables, lengths):
                 rel = 2 * (cuts.max() + 4 * E * np.abs(s[seen]).max()) + 16 * 2.0 ** -22 + (len(rows) / 8 + 200) * E
                 p = np.where(seen, np.exp(s - s[seen].max()), 0.0)
                 p /= p.sum()
-                factor[b, g] = rel + 2.0 ** -16 + (len(rows) // 16 + 1) * (34 * 2.0 ** -23 + E) + 200 * E
+                factor[b, g] = rel + 2.0 ** -16 + min(len(rows) // 16 + 1, dealt) * (34 * 2.0 ** -23 + E) + 200 * E
                 with np.errstate(invalid="ignore"):
                     tol[b, g] = U * np.abs(out[b, g]) + (1 + U) * factor[b, g] * (p @ np.abs(v))
                 err[b, h, rows] += (rel + G * E) * p
