@@ -3,13 +3,14 @@
 //
 // What bounds it is the cache: every row is read once, 4 d bytes for 4 G d operations (G query heads of a KV head), so nothing else must be what
 // the memory waits for. A warp works on one KV head, 16 rows a step, with a ring of steps of its own in shared memory that asynchronous
-// copies fill (24 KB a warp, two thirds of it in flight: 128 KB an SM) - no warp waits for another. The eight warps of a CTA take neighbouring
+// copies fill (24 KB a warp; with 128 dims three steps, two of them in flight, 128 KB an SM, with 64 six and five, 160 KB) - no warp waits for another. The eight warps of a CTA take neighbouring
 // heads of the same rows, which lie side by side in the cache, where there are as many; else several warps a head take rows in turn. The products run
 // on the tensor cores with the rows, then the dims, as 16 rows of a product and the heads of a group as its eight columns: S^T = K Q^T and O^T += V^T P^T,
 // so that half the products are not empty up to eight heads, a head's statistics and values lie in the same lanes, and V^T comes out of shared memory as it
 // is needed. P is split into two bf16 terms, so that its rounding (2^-16) is not seen beside that of the output. A head's reference moves only when a
 // logit lies 2^8 above it, which a vote finds without looking for the maximum. 64 sequences of 4160 rows, 8 heads of 128 dims: 166 us, the memory's own
-// time (what a step takes is what an SM gets out of the L2, 62 GB/s, or the memory: half the instructions did not change it).
+// time. In a long cache an SM takes 46 GB/s of rows, its share of the memory; of pages that repeat, so that they come out of the L2, 90 GB/s (with 64 dims 40
+// and 62), and the copies by themselves bring 150 to 180 on every SM at once: with 128 dims neither the L2 nor the steps are what is waited for.
 //
 // The rows of all units (a sequence's heads that a CTA takes together) are cut into tiles and dealt evenly to the CTAs in one line, so that lengths
 // need not be alike; a CTA walks the units in its share and leaves (max, sum, O) records for those that it shares with others, which a second launch
@@ -960,12 +961,13 @@ AttendPlan attend_plan(int B, int Hq, int Hkv, int d, int cap, bool sums, bool w
         if (p.tile == 1 << s) p.tile_shift = s;
     const long long tiles = static_cast<long long>(B) * p.blocks * p.groups * ((cap + p.tile - 1) / p.tile);
     p.max_ctas = static_cast<int>(tiles < kAttMaxCtas ? tiles : kAttMaxCtas);
-    // Short caches: as many CTAs a head as are resident beside each other, up to 1024 rows each (sequences need not be alike), or, where even shares of
-    // all SMs would not be many rows less, kSmallRows. us in one launch and
-    // in two, 128 dims: one sequence of 8 heads, 100 / 2000 / 4352 / 6000 / 9000 rows 4.7 and 6.8 / 6.2 and 9.2 / 9.0 and 11.8 / 10.4 and 13.2 / 14.0 and 16.0;
+    // Short caches: as many CTAs a head as are resident beside each other (7 clusters of 16, 15 of 8, 33 of 4, 74 of 2 on 148 SMs), up to 1024 rows each
+    // (sequences need not be alike), or, where even shares of all SMs would not be many rows less, kSmallRows. us in one launch and in two, 128 dims: one sequence of 8 heads, 100 / 2000 / 4352 / 6000 / 9000 rows 4.7 and 6.8 / 6.2 and 9.2 / 9.0 and 11.8 / 10.4 and 13.2 / 14.0 and 16.0;
     // 16 of them, 300 / 1000 rows 6.2 and 10.1 / 15.5 and 17.7, of unlike lengths 5.9 and 9.4 / 12.8 and 14.4; 8 of 4 heads, 7 query heads each, 4352 rows 17.3 and 18.7,
     // unlike 15.1 and 15.7, with sums 19.9 and 19.9, unlike 17.3 and 16.3; 4 of them, sums, 4352 rows (1088 a CTA, 64 CTAs) 15.2 and 14.3;
-    // one of 2 heads, 64 dims, 4352 / 9000 rows 6.2 and 7.3 / 7.7 and 8.2.
+    // one of 2 heads, 64 dims, 4352 / 9000 rows 6.2 and 7.3 / 7.7 and 8.2. With sums, between 1024 and kSmallRows: 18 of 8 heads, 1080 rows 19.6 and 21.8, unlike
+    // 15.8 and 16.5; 4 of 8 heads, 4340 rows 19.3 and 20.3, unlike 16.2 and 15.8; 8 of 4 heads, 64 dims, 15.0 and 16.0, unlike alike; 4 query heads each,
+    // 19.2 and 18.9, unlike 16.3 and 15.6.
     // Clusters of 16 take 0.5 us longer to launch: 3 sequences of 2 heads, 12 query heads each, 300 / 4000 rows 7.5 / 9.9 us with 16, 6.8 / 15.6 without.
     // More heads than SMs, a CTA of four warps each: 24 sequences of 8 heads, 100 / 300 / 600 / 1000 rows 5.3 and 9.4 / 8.6 and 12.3 / 14.6 and 16.7 / 20.6 and
     // 22.6. More than are resident: a CTA of the long form takes a sequence's heads, up to eight, together, so it depends on them. One launch against two: 64

@@ -38,7 +38,9 @@ __device__ __forceinline__ uint4 load_once(const void* p) {
 }
 
 // Launched as a programmatic dependent: everything that the kernel ahead (and those before it) wrote is there after this; only then may
-// the kernel behind be set up, which may therefore read what this kernel's predecessors wrote before its own wait.
+// the kernel behind be set up. A kernel that is always launched behind one that begins so may therefore read what that one's predecessors wrote
+// before its own wait: attend_join_kernel does (lengths), behind attend_kernel. No other may: attend_join_kernel itself and the prefill's kernels
+// let the kernel behind be set up before they have waited.
 __device__ __forceinline__ void begin_dependent() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
