@@ -13,8 +13,8 @@ from tests.test_gpu_decode_bounds import run
 pytestmark = pytest.mark.gpu
 
 
-# A thread of 512 has ceil(C / 512) keys of C chunks: up to 4, 6, 8, 10, 12 and 24 of them in registers, the first and the last C of each
-CHUNKS = [1025, 2048, 2049, 3072, 3073, 4096, 4097, 5120, 5121, 6144, 6145, 9000, 12288, 12289]
+# A thread of 512 has ceil(C / 512) keys of C chunks: up to 4, 6, 8, 10, 12 and 24 of them in registers, near the first and the last C of each
+CHUNKS = [1025, 2048, 2049, 3060, 3080, 4096, 4097, 5120, 5121, 6144, 6145, 9000, 12288, 12289]
 
 
 @pytest.mark.parametrize("kind", ["spread", "ties", "equal", "odd"])
