@@ -14,7 +14,7 @@ constexpr int kGatherThreadsSmall = 64;
 
 template <int VPR, int THREADS>
 __global__ void __launch_bounds__(THREADS)
-gather_kernel(const uint4* __restrict__ K, const uint4* __restrict__ V, const int32_t* __restrict__ idx,
+gather_kernel(const uint4* K, const uint4* V, const int32_t* idx,
               int L, int n_max, uint4* __restrict__ out_K, uint4* __restrict__ out_V,
               int32_t* __restrict__ idx_copy) {
     // launched as a programmatic dependent of the preceding kernel: let the next kernel's CTAs be
@@ -39,8 +39,8 @@ gather_kernel(const uint4* __restrict__ K, const uint4* __restrict__ V, const in
 // are skipped, never dereferenced.
 template <int VPR>
 __global__ void __launch_bounds__(kGatherThreads)
-gather_paged_kernel(const uint4* __restrict__ K, const uint4* __restrict__ V, const int32_t* __restrict__ idx,
-                    int L, int Hkv, int n_max, const int32_t* __restrict__ block_table, int page_size, int num_pages,
+gather_paged_kernel(const uint4* K, const uint4* V, const int32_t* idx,
+                    int L, int Hkv, int n_max, const int32_t* block_table, int page_size, int num_pages,
                     uint4* __restrict__ cache_K, uint4* __restrict__ cache_V) {
     const int h = blockIdx.y;
     const uint4* Kh = K + static_cast<size_t>(h) * L * VPR;
@@ -106,8 +106,8 @@ cudaError_t launch_gather_paged(const void* K, const void* V, const int32_t* idx
 // to fp32 and then to bf16 (nearest even), so that it equals the fp64 statement of the same
 // rotation bit for bit.
 namespace {
-__global__ void window_queries_kernel(const unsigned short* __restrict__ qkv, long long row_elems, int T, int Hq, int d,
-                                      int w, const float* __restrict__ cos_t, const float* __restrict__ sin_t,
+__global__ void window_queries_kernel(const unsigned short* qkv, long long row_elems, int T, int Hq, int d,
+                                      int w, const float* cos_t, const float* sin_t,
                                       unsigned short* __restrict__ q_obs) {
     const int half = d >> 1;
     const int total = Hq * w * half;
@@ -155,7 +155,7 @@ cudaError_t launch_window_queries(const void* qkv, long long row_elems, int T, i
 // stride and a head stride (in 16-byte vectors); the outputs are packed.
 template <int VPR>
 __global__ void __launch_bounds__(kGatherThreads)
-gather_strided_kernel(const uint4* __restrict__ K, const uint4* __restrict__ V, const int32_t* __restrict__ idx,
+gather_strided_kernel(const uint4* K, const uint4* V, const int32_t* idx,
                       int L, int n_max, long long k_tok, long long k_head, long long v_tok, long long v_head,
                       uint4* __restrict__ out_K, uint4* __restrict__ out_V, int32_t* __restrict__ idx_copy) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

@@ -12,7 +12,9 @@ namespace chunkkv {
 
 constexpr int kGatherRowsPerThread = 4;
 
-// Rows are read once: no L1 allocation, first in line for eviction from L2.
+// Rows are read once: no L1 allocation, first in line for eviction from L2. By coherent loads: the kernels that gather are on the SMs while the kernel
+// ahead of them, which may be the one that rotates the keys, still writes the rows, so the read-only path (data that nothing writes as long as a
+// kernel lives) is not theirs; nor do their pointers promise that to the compiler.
 __device__ __forceinline__ unsigned long long gather_policy() {
     unsigned long long p;
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
@@ -20,7 +22,7 @@ __device__ __forceinline__ unsigned long long gather_policy() {
 }
 __device__ __forceinline__ uint4 gather_ld(const uint4* p, unsigned long long policy) {
     uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+    asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                  : "l"(p), "l"(policy));
     return v;
@@ -44,7 +46,7 @@ struct PagedDst {
 // index_at(n): the source row of compacted position n (-1: none). k_row_vecs / v_row_vecs: 16-byte vectors between consecutive
 // source rows of a head (VPR for packed rows; more for a token-major cache).
 template <int VPR, class IndexAt>
-__device__ __forceinline__ void gather_rows_at(const uint4* __restrict__ Kh, const uint4* __restrict__ Vh,
+__device__ __forceinline__ void gather_rows_at(const uint4* Kh, const uint4* Vh,
                                                IndexAt index_at, int L, int n_max, int n0, int tid, int nthreads,
                                                uint4* __restrict__ oK, uint4* __restrict__ oV, int32_t* idx_copy,
                                                long long k_row_vecs, long long v_row_vecs, PagedDst pg) {
@@ -84,10 +86,10 @@ __device__ __forceinline__ void gather_rows_at(const uint4* __restrict__ Kh, con
     }
 }
 
-// The same with the indices in memory. FRESH_IDX: they were written earlier in the same kernel launch, so they must not be
-// read through the non-coherent path.
+// The same with the indices in memory. FRESH_IDX: they were written earlier in the same kernel launch, so they must not
+// come out of the L1.
 template <int VPR, bool FRESH_IDX>
-__device__ __forceinline__ void gather_rows(const uint4* __restrict__ Kh, const uint4* __restrict__ Vh,
+__device__ __forceinline__ void gather_rows(const uint4* Kh, const uint4* Vh,
                                             const int32_t* ih, int L, int n_max, int n0, int tid, int nthreads,
                                             uint4* __restrict__ oK, uint4* __restrict__ oV, int32_t* idx_copy,
                                             long long k_row_vecs = VPR, long long v_row_vecs = VPR) {

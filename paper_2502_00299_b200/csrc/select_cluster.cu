@@ -39,7 +39,7 @@ struct ClusterSel {
 // kCsThreads = 512 (every thread may use 128 registers: no spills) or 1024 (twice the keys per cluster)
 template <int kCsThreads>
 __global__ void __cluster_dims__(kCsCtas, 1, 1) __launch_bounds__(kCsThreads, 1)
-select_cluster_kernel(const float* __restrict__ scores, int L, int w, int c, int C, int k, int n_max,
+select_cluster_kernel(const float* scores, int L, int w, int c, int C, int k, int n_max,
                       int32_t* __restrict__ out_idx, int tok_cap) {
     constexpr unsigned kFull = 0xffffffffu;
     __shared__ ClusterSel cs;
