@@ -5,7 +5,7 @@
 // These kernels are on the SMs while the kernel ahead, which may be one of them, still writes what they read: queries, lengths, sums, rows, and, from a
 // program's own kernels, tables, positions and angles. All of that is therefore read with coherent loads (plain ones, asynchronous copies,
 // load_once), which stay behind the wait. The read-only path (the intrinsic and the .nc loads) is for data that nothing writes as long as a kernel
-// lives: the compiler may move such a load to the front of the wait, and no wait makes it see what was written meanwhile.
+// lives: the compiler may move such a load in front of the wait, and no wait makes it see what was written meanwhile.
 #pragma once
 #include "decode.h"
 
