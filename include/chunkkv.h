@@ -375,6 +375,72 @@ CHUNKKV_API int chunkkv_evict_paged(float* weights, const int32_t* block_tables,
                                     int32_t* out_idx, void* stream);
 
 /*
+ * Beyond single tokens: the rotary embedding in its other forms, a turn of many tokens, and batches that share a prefix. Conventions,
+ * limits and the meaning of block_tables, lengths and pages are those of the calls above; besides
+ *   starts [n + 1] int32       ascending, in [0, T]: tokens starts[i] .. starts[i + 1] - 1 belong to sequence (or group) i, which may have none.
+ *                              What belongs to none (tokens in front of starts[0] and from starts[n] on) is neither read nor written.
+ *
+ * chunkkv_rope_tables: cos_t / sin_t [n_pos, rot / 2] f32 of positions first, first + 1, ...: scale * cos(p w_i), scale * sin(p w_i), pair i
+ *   turning by w_i = base^(-2 i / rot) a position, |first| <= 2^31. scaling:
+ *     CHUNKKV_ROPE_PLAIN   as it is
+ *     CHUNKKV_ROPE_LINEAR  w_i / factor
+ *     CHUNKKV_ROPE_DIMS    with D(n) = rot ln(original / (2 pi n)) / (2 ln base), a = max(floor(D(high)), 0), b = min(ceil(D(low)), rot - 1) and
+ *                          s = min(max((i - a) / max(b - a, 0.001), 0), 1): s w_i / factor + (1 - s) w_i (pairs that turn more than `high` times
+ *                          over the `original` positions stay, those that turn less than `low` times are stretched)
+ *     CHUNKKV_ROPE_WAVES   with s = min(max((original w_i / (2 pi) - low) / (high - low), 0), 1): s w_i + (1 - s) w_i / factor
+ *   Angles are good to 2^-31 of a turn at any position, values to 2^-22 of scale. base > 1, factor > 0, original > 0, 0 < low < high.
+ *
+ * chunkkv_rotate_rows: chunkkv_rotate_qk for heads of which the first rot dims turn (a multiple of 16, at most d; tables [n_pos, rot / 2]), the
+ *   others only taking part in the norm, with pair i of a head's dims (i, i + rot / 2) or, interleaved = 1, (2 i, 2 i + 1).
+ *
+ * chunkkv_append_rows_paged: the same for a turn's tokens, T of them in B sequences: queries to out_q [T, Hq, d], keys and values
+ *   (qkv [T, row_elems], row_elems >= (Hq + 2 Hkv) d) into the cache, token i of the n of sequence b as row lengths[b, h] - n + i of
+ *   head h: `lengths` counts them already. Rows below 0 or beyond the table are dropped.
+ *
+ * chunkkv_attend_rows_paged: attention of a turn's tokens, q [T, Hq, d] bf16 (rotated): out [T, Hq, d] = softmax(q K^T / sqrt(d)) V over the
+ *   first lengths[b, h] rows of its sequence and KV head, or, causal = 1, token i of n over the first lengths[b, h] - (n - 1 - i): each sees the
+ *   rows before the turn and the turn's up to its own. Not causal, it is cross attention to an encoder's states kept in the cache. As in
+ *   chunkkv_attend_paged a head with nothing to see, or no logit above -inf, gets zeros, other infinite or not-a-number logits go the way of the formula, values may be as
+ *   large as 2^88, and an infinite one in a row that is seen makes its dim of the output infinite or not a number; rows that a token does not see
+ *   do not touch it, whatever they hold. Weights are rounded to bf16 once, before they meet the values (2^-8 of each), sums are taken in 32 bits,
+ *   in a fixed order: same result every time. scratch: chunkkv_attend_rows_scratch_bytes(...) bytes, as in chunkkv_attend_paged (0: invalid sizes).
+ *
+ * chunkkv_attend_shared_paged: attention of one new token a sequence, q [B, Hq, d], sequences starts[p] .. starts[p + 1] - 1 sharing prefix p (P
+ *   of them; P = 0: none, and the prefixes' pointers may be NULL), a sequence outside of all of them having none: over the first prefix_lengths[p, h] rows of prefix_tables
+ *   [P, max_prefix_pages] and the first lengths[b, h] rows of block_tables [B, max_pages] together. Both are pages of the same cache. A
+ *   prefix is read once for up to 256 query heads (sequences times Hq / Hkv). Otherwise as chunkkv_attend_rows_paged, with
+ *   chunkkv_attend_shared_scratch_bytes(...) bytes of scratch.
+ *
+ * Beyond the limits above, T and B (B and P) times Hq < 2^30, and blocks of 256 query heads of a KV head, (T / floor(256 / (Hq / Hkv)) + B)
+ * Hkv of them, times tiles of 128 rows of a table below 2^31. chunkkv_device_status also reports a wait that the last two calls abandoned.
+ */
+#define CHUNKKV_ROPE_PLAIN  0
+#define CHUNKKV_ROPE_LINEAR 1
+#define CHUNKKV_ROPE_DIMS   2
+#define CHUNKKV_ROPE_WAVES  3
+CHUNKKV_API int chunkkv_rope_tables(int n_pos, long long first, int rot, double base, int scaling, double factor, double original, double low,
+                                    double high, double scale, float* cos_t, float* sin_t, void* stream);
+CHUNKKV_API int chunkkv_rotate_rows(const void* qkv, long long row_elems, int T, int Hq, int Hkv, int d, int rot, int interleaved,
+                                    const void* q_gain, const void* k_gain, float eps, const float* cos_t, const float* sin_t, int n_pos,
+                                    const int32_t* positions, long long q_token_stride, long long q_head_stride,
+                                    long long k_token_stride, long long k_head_stride, void* out_q, void* out_k, void* stream);
+CHUNKKV_API int chunkkv_append_rows_paged(const void* qkv, long long row_elems, int T, const int32_t* starts, int B, int Hq, int Hkv, int d,
+                                          int rot, int interleaved, const void* q_gain, const void* k_gain, float eps, const float* cos_t,
+                                          const float* sin_t, int n_pos, const int32_t* positions, const int32_t* block_tables,
+                                          int max_pages, const int32_t* lengths, int page_size, int num_pages, void* cache_K,
+                                          void* cache_V, void* out_q, void* stream);
+CHUNKKV_API size_t chunkkv_attend_rows_scratch_bytes(int T, int B, int Hq, int Hkv, int d);
+CHUNKKV_API int chunkkv_attend_rows_paged(const void* q, int T, const int32_t* starts, const int32_t* block_tables, int max_pages,
+                                          const int32_t* lengths, int page_size, int num_pages, const void* cache_K, const void* cache_V,
+                                          int B, int Hq, int Hkv, int d, int causal, void* out, void* scratch, size_t scratch_bytes,
+                                          void* stream);
+CHUNKKV_API size_t chunkkv_attend_shared_scratch_bytes(int B, int P, int Hq, int Hkv, int d);
+CHUNKKV_API int chunkkv_attend_shared_paged(const void* q, const int32_t* starts, int P, const int32_t* prefix_tables, int max_prefix_pages,
+                                            const int32_t* prefix_lengths, const int32_t* block_tables, int max_pages, const int32_t* lengths,
+                                            int page_size, int num_pages, const void* cache_K, const void* cache_V, int B, int Hq, int Hkv,
+                                            int d, void* out, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
  * Index similarity between two layers (the paper's section on layer-wise index reuse reports the
  * Jaccard similarity of the preserved indices of adjacent layers; Algorithm 2 shares indices
  * because it is high). Per KV head h: out_ratio[h] = |A n B| / |A u B| (1 when both are empty),

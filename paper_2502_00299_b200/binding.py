@@ -103,6 +103,22 @@ def _load() -> ctypes.CDLL:
     L.chunkkv_attend_paged.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp] + [i32] * 4 + [vp, vp, vp, sz, vp]
     L.chunkkv_evict_paged.restype = i32
     L.chunkkv_evict_paged.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp] + [i32] * 6 + [vp, vp]
+    i64, f64 = ctypes.c_longlong, ctypes.c_double
+    L.chunkkv_rope_tables.restype = i32
+    L.chunkkv_rope_tables.argtypes = [i32, i64, i32, f64, i32, f64, f64, f64, f64, f64, vp, vp, vp]
+    L.chunkkv_rotate_rows.restype = i32
+    L.chunkkv_rotate_rows.argtypes = [vp, i64] + [i32] * 6 + [vp, vp, ctypes.c_float, vp, vp, i32, vp] + [i64] * 4 + [vp, vp, vp]
+    L.chunkkv_append_rows_paged.restype = i32
+    L.chunkkv_append_rows_paged.argtypes = ([vp, i64, i32, vp] + [i32] * 6 + [vp, vp, ctypes.c_float, vp, vp, i32, vp, vp, i32, vp, i32, i32]
+                                            + [vp] * 4)
+    L.chunkkv_attend_rows_scratch_bytes.restype = sz
+    L.chunkkv_attend_rows_scratch_bytes.argtypes = [i32] * 5
+    L.chunkkv_attend_rows_paged.restype = i32
+    L.chunkkv_attend_rows_paged.argtypes = [vp, i32, vp, vp, i32, vp, i32, i32, vp, vp] + [i32] * 5 + [vp, vp, sz, vp]
+    L.chunkkv_attend_shared_scratch_bytes.restype = sz
+    L.chunkkv_attend_shared_scratch_bytes.argtypes = [i32] * 5
+    L.chunkkv_attend_shared_paged.restype = i32
+    L.chunkkv_attend_shared_paged.argtypes = [vp, vp, i32, vp, i32, vp, vp, i32, vp, i32, i32, vp, vp] + [i32] * 4 + [vp, vp, sz, vp]
     L.chunkkv_jaccard.restype = i32
     L.chunkkv_jaccard.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp]
     L.chunkkv_score_noalloc.restype = i32
@@ -657,6 +673,182 @@ def evict_paged(weights: torch.Tensor, block_tables: torch.Tensor, lengths: torc
         _check(lib.chunkkv_evict_paged(weights.data_ptr(), block_tables.data_ptr(), max_pages, lengths.data_ptr(), page_size, pages, cache_K.data_ptr(),
                                        cache_V.data_ptr(), B, Hkv, d, w, c, budget, out_idx.data_ptr(), _stream(stream)), "chunkkv_evict_paged")
     return out_idx
+
+
+_SCALINGS = {"none": 0, "linear": 1, "dims": 2, "waves": 3}
+
+
+def rope_tables(n_pos: int, rot: int, base: float, scaling: str = "none", factor: float = 1.0, original: float = 0.0, low: float = 0.0,
+                high: float = 0.0, scale: float = 1.0, first: int = 0, out_cos: Optional[torch.Tensor] = None,
+                out_sin: Optional[torch.Tensor] = None, device: Optional[torch.device] = None,
+                stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """cos and sin [n_pos, rot / 2] f32 of positions first, first + 1, ..., times ``scale``; pair i turns by base^(-2 i / rot) a position. scaling:
+    "none"; "linear", by ``factor``; "dims" and "waves", by parts (see chunkkv.h): pairs that turn more than ``high`` times over the
+    ``original`` positions stay, those that turn less than ``low`` times are stretched by ``factor``."""
+    if scaling not in _SCALINGS:
+        raise ValueError(f"scaling must be one of {', '.join(_SCALINGS)}")
+    if out_cos is None and out_sin is None and device is None:
+        r = _native.rope_tables(n_pos, first, rot, base, _SCALINGS[scaling], factor, original, low, high, scale, stream)
+        if r is not None:
+            return _done(r, "chunkkv_rope_tables")
+    given = next((t for t in (out_cos, out_sin) if t is not None), None)
+    for t, name in ((out_cos, "out_cos"), (out_sin, "out_sin")):
+        if t is not None:
+            _sized(t, torch.float32, n_pos * (rot // 2), name)
+    dev = torch.device(device) if device is not None else given.device if given is not None else torch.device("cuda", torch.cuda.current_device())
+    if dev.type != "cuda":
+        raise ValueError("device must be a CUDA device")
+    if dev.index is None:
+        dev = torch.device("cuda", torch.cuda.current_device())
+    for t, name in ((out_cos, "out_cos"), (out_sin, "out_sin")):
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} must be on {dev}")
+    with _on(dev, stream):
+        if out_cos is None:
+            out_cos = torch.empty((max(n_pos, 0), max(rot, 0) // 2), dtype=torch.float32, device=dev)
+        if out_sin is None:
+            out_sin = torch.empty((max(n_pos, 0), max(rot, 0) // 2), dtype=torch.float32, device=dev)
+        _check(lib.chunkkv_rope_tables(n_pos, first, rot, base, _SCALINGS[scaling], factor, original, low, high, scale, out_cos.data_ptr(),
+                                       out_sin.data_ptr(), _stream(stream)), "chunkkv_rope_tables")
+    return out_cos, out_sin
+
+
+def _turning(cos: torch.Tensor, sin: torch.Tensor) -> Tuple[int, int]:
+    """Rows of the angle tables [n_pos, rot / 2] f32, and rot."""
+    rot = 2 * cos.shape[1] if _dev(cos, torch.float32, "cos").dim() == 2 else 0
+    return _angles(cos, sin, rot), rot
+
+
+def _starts(starts: torch.Tensor, n: int) -> None:
+    if tuple(_dev(starts, torch.int32, "starts").shape) != (n + 1,):
+        raise ValueError(f"starts must be [{n + 1}]")
+
+
+def rotate_rows(qkv: torch.Tensor, Hq: int, Hkv: int, d: int, cos: torch.Tensor, sin: torch.Tensor, positions: torch.Tensor,
+                interleaved: bool = False, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None,
+                stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """rotate_qk for heads of which the first ``rot`` dims turn, by tables cos / sin [n_pos, rot / 2] f32, as two halves or, interleaved, as
+    neighbouring pairs. The norm (where gains [d] are given) takes all dims."""
+    r = _native.rotate_rows(qkv, Hq, Hkv, d, cos, sin, positions, interleaved, q_gain, k_gain, eps, out_q, out_k, stream)
+    if r is not None:
+        return _done(r, "chunkkv_rotate_rows")
+    T, row_elems = _fused(qkv, Hq + Hkv, d, positions, q_gain, k_gain)
+    n_pos, rot = _turning(cos, sin)
+    for t, H, name in ((out_q, Hq, "out_q"), (out_k, Hkv, "out_k")):
+        if t is not None and not (t.is_cuda and t.dtype == torch.bfloat16 and tuple(t.shape) == (T, H, d) and t.stride(2) == 1):
+            raise ValueError(f"{name}: a CUDA bf16 [{T}, {H}, {d}] view with a contiguous last dimension is required")
+    _together(qkv, cos=cos, sin=sin, positions=positions, q_gain=q_gain, k_gain=k_gain, out_q=out_q, out_k=out_k)
+    with _on(qkv.device, stream):
+        if out_q is None:
+            out_q = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=qkv.device)
+        if out_k is None:
+            out_k = torch.empty((T, Hkv, d), dtype=torch.bfloat16, device=qkv.device)
+        # (the strides of a single token or head are free)
+        st = [d if n <= 1 else s for t in (out_q, out_k) for s, n in zip(t.stride()[:2], t.shape)]
+        _check(lib.chunkkv_rotate_rows(qkv.data_ptr(), row_elems, T, Hq, Hkv, d, rot, int(bool(interleaved)), _ptr(q_gain), _ptr(k_gain), eps,
+                                       cos.data_ptr(), sin.data_ptr(), n_pos, positions.data_ptr(), *st, out_q.data_ptr(), out_k.data_ptr(),
+                                       _stream(stream)), "chunkkv_rotate_rows")
+    return out_q, out_k
+
+
+def append_rows_paged(qkv: torch.Tensor, Hq: int, starts: torch.Tensor, cos: torch.Tensor, sin: torch.Tensor, positions: torch.Tensor,
+                      block_tables: torch.Tensor, lengths: torch.Tensor, cache_K: torch.Tensor, cache_V: torch.Tensor,
+                      interleaved: bool = False, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
+                      eps: float = 1e-6, out_q: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """A turn's tokens, starts[b] to starts[b + 1] - 1 (starts [B + 1] int32) of each of B sequences: their queries [T, Hq, d], rotated as by
+    rotate_rows, and their keys and values as the last of the lengths [B, Hkv] int32 rows (the tokens counted) of every head of a
+    paged cache. Tokens outside of all sequences are left out (their rows of a new out are not set)."""
+    r = _native.append_rows_paged(qkv, Hq, starts, cos, sin, positions, block_tables, lengths, cache_K, cache_V, interleaved, q_gain, k_gain, eps,
+                                  out_q, stream)
+    if r is not None:
+        return _done(r, "chunkkv_append_rows_paged")
+    B = _dev(lengths, torch.int32, "lengths").shape[0]
+    pages, page_size, Hkv, d, max_pages = _cache(block_tables, lengths, cache_K, cache_V, B)
+    T, row_elems = _fused(qkv, Hq + 2 * Hkv, d, positions, q_gain, k_gain)
+    _starts(starts, B)
+    n_pos, rot = _turning(cos, sin)
+    if out_q is not None:
+        _sized(out_q, torch.bfloat16, T * Hq * d, "out_q")
+    _together(qkv, starts=starts, cos=cos, sin=sin, positions=positions, block_tables=block_tables, lengths=lengths, cache_K=cache_K,
+              cache_V=cache_V, q_gain=q_gain, k_gain=k_gain, out_q=out_q)
+    with _on(qkv.device, stream):
+        if out_q is None:
+            out_q = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=qkv.device)
+        _check(lib.chunkkv_append_rows_paged(qkv.data_ptr(), row_elems, T, starts.data_ptr(), B, Hq, Hkv, d, rot, int(bool(interleaved)), _ptr(q_gain),
+                                             _ptr(k_gain), eps, cos.data_ptr(), sin.data_ptr(), n_pos, positions.data_ptr(), block_tables.data_ptr(),
+                                             max_pages, lengths.data_ptr(), page_size, pages, cache_K.data_ptr(), cache_V.data_ptr(), out_q.data_ptr(),
+                                             _stream(stream)), "chunkkv_append_rows_paged")
+    return out_q
+
+
+def attend_rows_paged(q: torch.Tensor, starts: torch.Tensor, block_tables: torch.Tensor, lengths: torch.Tensor, cache_K: torch.Tensor,
+                      cache_V: torch.Tensor, causal: bool = True, out: Optional[torch.Tensor] = None,
+                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Attention [T, Hq, d] of a turn's tokens (q [T, Hq, d] bf16), starts[b] to starts[b + 1] - 1 of each of B sequences, over the first
+    lengths [B, Hkv] rows of every head of a paged cache. causal: the tokens are the last of those rows, and each sees no row behind its own;
+    else (an encoder's states, say) all see all. Rows of a new out that belong to no sequence are not set."""
+    r = _native.attend_rows_paged(q, starts, block_tables, lengths, cache_K, cache_V, causal, out, stream)
+    if r is not None:
+        return _done(r, "chunkkv_attend_rows_paged")
+    if _dev(q, torch.bfloat16, "q").dim() != 3:
+        raise ValueError("q must be [T, Hq, d]")
+    T, Hq = q.shape[0], q.shape[1]
+    B = _dev(lengths, torch.int32, "lengths").shape[0]
+    pages, page_size, Hkv, d, max_pages = _cache(block_tables, lengths, cache_K, cache_V, B)
+    if q.shape[2] != d:
+        raise ValueError(f"q must be [T, Hq, {d}]")
+    _starts(starts, B)
+    if out is not None:
+        _sized(out, torch.bfloat16, T * Hq * d, "out")
+    _together(q, starts=starts, block_tables=block_tables, lengths=lengths, cache_K=cache_K, cache_V=cache_V, out=out)
+    with _on(q.device, stream):
+        if out is None:
+            out = torch.empty((T, Hq, d), dtype=torch.bfloat16, device=q.device)
+        # scratch of this call: the allocator hands it out again only behind it on its stream
+        need = int(lib.chunkkv_attend_rows_scratch_bytes(T, B, Hq, Hkv, d))
+        scratch = torch.empty(need, dtype=torch.uint8, device=q.device) if need > 0 else None
+        _check(lib.chunkkv_attend_rows_paged(q.data_ptr(), T, starts.data_ptr(), block_tables.data_ptr(), max_pages, lengths.data_ptr(), page_size, pages,
+                                             cache_K.data_ptr(), cache_V.data_ptr(), B, Hq, Hkv, d, int(bool(causal)), out.data_ptr(), _ptr(scratch), need,
+                                             _stream(stream)), "chunkkv_attend_rows_paged")
+    return out
+
+
+def attend_shared_paged(q: torch.Tensor, starts: torch.Tensor, prefix_tables: torch.Tensor, prefix_lengths: torch.Tensor,
+                        block_tables: torch.Tensor, lengths: torch.Tensor, cache_K: torch.Tensor, cache_V: torch.Tensor,
+                        out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Attention [B, Hq, d] of one token a sequence (q [B, Hq, d] bf16), sequences starts[p] to starts[p + 1] - 1 (starts [P + 1] int32) sharing
+    prefix p: over the first prefix_lengths [P, Hkv] rows of its pages prefix_tables [P, pages] and the sequence's own first lengths [B, Hkv] rows, pages
+    block_tables [B, pages] of the same cache. A prefix is read once for its sequences."""
+    r = _native.attend_shared_paged(q, starts, prefix_tables, prefix_lengths, block_tables, lengths, cache_K, cache_V, out, stream)
+    if r is not None:
+        return _done(r, "chunkkv_attend_shared_paged")
+    if _dev(q, torch.bfloat16, "q").dim() != 3:
+        raise ValueError("q must be [B, Hq, d]")
+    B, Hq = q.shape[0], q.shape[1]
+    pages, page_size, Hkv, d, max_pages = _cache(block_tables, lengths, cache_K, cache_V, B)
+    if q.shape[2] != d:
+        raise ValueError(f"q must be [B, Hq, {d}]")
+    P = _dev(prefix_lengths, torch.int32, "prefix_lengths").shape[0]
+    if tuple(prefix_lengths.shape) != (P, Hkv):
+        raise ValueError(f"prefix_lengths must be [groups, {Hkv}]")
+    if _dev(prefix_tables, torch.int32, "prefix_tables").dim() != 2 or prefix_tables.shape[0] != P:
+        raise ValueError(f"prefix_tables must be [{P}, pages of a prefix]")
+    _starts(starts, P)
+    if out is not None:
+        _sized(out, torch.bfloat16, B * Hq * d, "out")
+    _together(q, starts=starts, prefix_tables=prefix_tables, prefix_lengths=prefix_lengths, block_tables=block_tables, lengths=lengths,
+              cache_K=cache_K, cache_V=cache_V, out=out)
+    with _on(q.device, stream):
+        if out is None:
+            out = torch.empty((B, Hq, d), dtype=torch.bfloat16, device=q.device)
+        need = int(lib.chunkkv_attend_shared_scratch_bytes(B, P, Hq, Hkv, d))
+        scratch = torch.empty(need, dtype=torch.uint8, device=q.device) if need > 0 else None
+        _check(lib.chunkkv_attend_shared_paged(q.data_ptr(), starts.data_ptr(), P, prefix_tables.data_ptr(), prefix_tables.shape[1],
+                                               prefix_lengths.data_ptr(), block_tables.data_ptr(), max_pages, lengths.data_ptr(), page_size, pages,
+                                               cache_K.data_ptr(), cache_V.data_ptr(), B, Hq, Hkv, d, out.data_ptr(), _ptr(scratch), need,
+                                               _stream(stream)), "chunkkv_attend_shared_paged")
+    return out
 
 
 def jaccard(idx_a: torch.Tensor, idx_b: torch.Tensor, stream: Optional[torch.cuda.Stream] = None,

@@ -4,6 +4,7 @@
 #include "../../include/chunkkv.h"
 #include "decode.h"
 #include "internal.h"
+#include "rows.h"
 
 #include <math.h>
 #include <mutex>
@@ -30,6 +31,7 @@ struct ProfileRec {
 struct DeviceCtx {
     bool init = false;
     int num_sms = 0;
+    bool rows_called = false;        // attend_rows_paged or attend_shared_paged, whose kernels have a status word in the library's image
     int wide_clusters = -1;          // whether attend_paged can have clusters of 16; -1: not asked yet
     int smem_optin = 0;
     void* ws = nullptr;        // scratch handed over with chunkkv_set_workspace (header + payload)
@@ -515,7 +517,12 @@ int chunkkv_device_status(void* stream) {
     if (st != CHUNKKV_OK) return st;
     cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(e);
-    if (ctx->ws == nullptr) return CHUNKKV_OK;
+    bool gave_up = false;
+    if (ctx->rows_called) {
+        e = attend_rows_status(&gave_up);
+        if (e != cudaSuccess) return cuda_fail(e);
+    }
+    if (ctx->ws == nullptr) return gave_up ? CHUNKKV_EDEVICE : CHUNKKV_OK;
     int flag = 0;
     e = cudaMemcpy(&flag, ctx->ws, sizeof(int), cudaMemcpyDeviceToHost);
     if (e != cudaSuccess) return cuda_fail(e);
@@ -525,7 +532,7 @@ int chunkkv_device_status(void* stream) {
         if (ctx->slot >= 0) cudaMemset(exchange_tags(exchange_slot(ctx->slots, ctx->slot)) + 1, 0, sizeof(uint32_t));
         return CHUNKKV_EDEVICE;
     }
-    return CHUNKKV_OK;
+    return gave_up ? CHUNKKV_EDEVICE : CHUNKKV_OK;
 }
 
 // Not part of the API: for the tests of the end of the tags (resident.cuh), which 2^32 - 1 launches on a set of words take otherwise. The
@@ -913,6 +920,220 @@ int chunkkv_evict_paged(float* weights, const int32_t* block_tables, int max_pag
     if (!plan.fits) return CHUNKKV_ETOOLARGE;
     const cudaError_t e = launch_evict(a, plan, B, d, ctx->num_sms, static_cast<cudaStream_t>(stream));
     return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
+}
+
+// ---- Tables of the rotary embedding, its other layouts, and turns of many tokens: rotated, appended, attended to; batches that share a prefix.
+int chunkkv_rope_tables(int n_pos, long long first, int rot, double base, int scaling, double factor, double original, double low, double high,
+                        double scale, float* cos_t, float* sin_t, void* stream) {
+    if (n_pos < 0 || rot < 16 || rot > kMaxRot || rot % 16 != 0 || !(base > 1.0) || !isfinite(base) || !isfinite(scale)) return CHUNKKV_EINVAL_SHAPE;
+    const long long far = 1LL << 31;
+    if (first < -far || first > far) return CHUNKKV_EINVAL_SHAPE;
+    if (scaling < CHUNKKV_ROPE_PLAIN || scaling > CHUNKKV_ROPE_WAVES) return CHUNKKV_EINVAL_SHAPE;
+    if (scaling != CHUNKKV_ROPE_PLAIN && (!(factor > 0.0) || !isfinite(factor))) return CHUNKKV_EINVAL_SHAPE;
+    if (scaling >= CHUNKKV_ROPE_DIMS && (!(original > 0.0) || !isfinite(original) || !(low > 0.0) || !(high > low) || !isfinite(high))) return CHUNKKV_EINVAL_SHAPE;
+    if (n_pos == 0) return CHUNKKV_OK;
+    if (cos_t == nullptr || sin_t == nullptr) return CHUNKKV_EINVAL_NULL;
+    if (!aligned16(cos_t) || !aligned16(sin_t)) return CHUNKKV_EINVAL_ALIGN;
+    TableArgs a = {};
+    a.n_pos = n_pos;
+    a.rot = rot;
+    a.first = static_cast<unsigned long long>(first);
+    a.scale = static_cast<float>(scale);
+    a.cos_t = cos_t;
+    a.sin_t = sin_t;
+    const long double pi = 3.14159265358979323846264338327950288L, b = base;
+    // by dims: the place of the dim that turns n times over `original` positions
+    auto dim_of = [&](double turns) { return static_cast<double>(rot) * log(original / (2.0 * static_cast<double>(pi) * turns)) / (2.0 * log(base)); };
+    const double from = scaling == CHUNKKV_ROPE_DIMS ? fmax(floor(dim_of(high)), 0.0) : 0.0;
+    const double to = scaling == CHUNKKV_ROPE_DIMS ? fmin(ceil(dim_of(low)), rot - 1.0) : 0.0;
+    for (int i = 0; i < rot / 2; ++i) {
+        long double w = powl(b, -2.0L * i / rot);
+        if (scaling == CHUNKKV_ROPE_LINEAR) {
+            w /= factor;
+        } else if (scaling == CHUNKKV_ROPE_DIMS) {
+            const double stretch = fmin(fmax((i - from) / fmax(to - from, 1e-3), 0.0), 1.0);
+            w = w / factor * stretch + w * (1.0L - stretch);
+        } else if (scaling == CHUNKKV_ROPE_WAVES) {
+            const long double turns = original * w / (2.0L * pi);
+            const long double keep = fminl(fmaxl((turns - low) / (static_cast<long double>(high) - low), 0.0L), 1.0L);
+            w = w / factor * (1.0L - keep) + w * keep;
+        }
+        long double turn = w / (2.0L * pi);
+        turn -= floorl(turn);                                          // (positions are whole: whole turns do not matter)
+        a.turn[i] = static_cast<unsigned long long>(ldexpl(turn, 64));
+    }
+    std::lock_guard<std::mutex> lk(g_mu);
+    DeviceCtx* ctx;
+    const int st = get_ctx(&ctx);
+    if (st != CHUNKKV_OK) return st;
+    const cudaError_t e = launch_tables(a, ctx->num_sms, static_cast<cudaStream_t>(stream));
+    return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
+}
+
+static int check_rot(int rot, int d, int interleaved) {
+    return rot < 16 || rot > d || rot % 16 != 0 || (interleaved != 0 && interleaved != 1) ? CHUNKKV_EINVAL_SHAPE : CHUNKKV_OK;
+}
+
+int chunkkv_rotate_rows(const void* qkv, long long row_elems, int T, int Hq, int Hkv, int d, int rot, int interleaved, const void* q_gain,
+                        const void* k_gain, float eps, const float* cos_t, const float* sin_t, int n_pos, const int32_t* positions,
+                        long long q_token_stride, long long q_head_stride, long long k_token_stride, long long k_head_stride, void* out_q,
+                        void* out_k, void* stream) {
+    int st = check_decode_heads(T, Hq, Hkv, d);
+    if (st == CHUNKKV_OK) st = check_rot(rot, d, interleaved);
+    if (st != CHUNKKV_OK) return st;
+    if (row_elems < static_cast<long long>(Hq + Hkv) * d || n_pos < 1 || !(eps >= 0.f) || isinf(eps)) return CHUNKKV_EINVAL_SHAPE;
+    for (long long s : {q_token_stride, q_head_stride, k_token_stride, k_head_stride})
+        if (s < d || (s & 7) != 0) return CHUNKKV_EINVAL_SHAPE;
+    if (T == 0) return CHUNKKV_OK;
+    if (qkv == nullptr || cos_t == nullptr || sin_t == nullptr || positions == nullptr || out_q == nullptr || out_k == nullptr) return CHUNKKV_EINVAL_NULL;
+    if ((row_elems & 7) != 0 || !aligned16(qkv) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned16(cos_t) || !aligned16(sin_t) ||
+        !aligned4(positions) || !aligned16(out_q) || !aligned16(out_k))
+        return CHUNKKV_EINVAL_ALIGN;
+    std::lock_guard<std::mutex> lk(g_mu);
+    DeviceCtx* ctx;
+    st = get_ctx(&ctx);
+    if (st != CHUNKKV_OK) return st;
+    RotateRowsArgs a = {};
+    a.r.qkv = static_cast<const __nv_bfloat16*>(qkv);
+    a.r.row_elems = row_elems; a.r.T = T; a.r.Hq = Hq; a.r.Hkv = Hkv;
+    a.r.gain_q = static_cast<const __nv_bfloat16*>(q_gain);
+    a.r.gain_k = static_cast<const __nv_bfloat16*>(k_gain);
+    a.r.eps = eps; a.r.cos_t = cos_t; a.r.sin_t = sin_t; a.r.n_pos = n_pos; a.r.positions = positions;
+    a.r.out_q = static_cast<__nv_bfloat16*>(out_q);
+    a.r.out_k = static_cast<__nv_bfloat16*>(out_k);
+    a.r.q_token = q_token_stride; a.r.q_head = q_head_stride; a.r.k_token = k_token_stride; a.r.k_head = k_head_stride;
+    a.rot = rot;
+    const cudaError_t e = launch_rotate_rows(a, d, interleaved != 0, ctx->num_sms, static_cast<cudaStream_t>(stream));
+    return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
+}
+
+int chunkkv_append_rows_paged(const void* qkv, long long row_elems, int T, const int32_t* starts, int B, int Hq, int Hkv, int d, int rot,
+                              int interleaved, const void* q_gain, const void* k_gain, float eps, const float* cos_t, const float* sin_t,
+                              int n_pos, const int32_t* positions, const int32_t* block_tables, int max_pages, const int32_t* lengths,
+                              int page_size, int num_pages, void* cache_K, void* cache_V, void* out_q, void* stream) {
+    int st = check_decode_heads(T, Hq, Hkv, d);
+    if (st == CHUNKKV_OK) st = check_decode_heads(B, Hq, Hkv, d);
+    if (st == CHUNKKV_OK) st = check_decode_cache(max_pages, page_size, num_pages);
+    if (st == CHUNKKV_OK) st = check_rot(rot, d, interleaved);
+    if (st != CHUNKKV_OK) return st;
+    if (row_elems < static_cast<long long>(Hq + 2 * Hkv) * d || n_pos < 1 || !(eps >= 0.f) || isinf(eps)) return CHUNKKV_EINVAL_SHAPE;
+    if (B == 0 || T == 0) return CHUNKKV_OK;
+    if (qkv == nullptr || starts == nullptr || cos_t == nullptr || sin_t == nullptr || positions == nullptr || block_tables == nullptr ||
+        lengths == nullptr || cache_K == nullptr || cache_V == nullptr || out_q == nullptr)
+        return CHUNKKV_EINVAL_NULL;
+    if ((row_elems & 7) != 0 || !aligned16(qkv) || !aligned4(starts) || !aligned16(q_gain) || !aligned16(k_gain) || !aligned16(cos_t) ||
+        !aligned16(sin_t) || !aligned4(positions) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) ||
+        !aligned16(out_q))
+        return CHUNKKV_EINVAL_ALIGN;
+    std::lock_guard<std::mutex> lk(g_mu);
+    DeviceCtx* ctx;
+    st = get_ctx(&ctx);
+    if (st != CHUNKKV_OK) return st;
+    RotateRowsArgs a = {};
+    a.r.qkv = static_cast<const __nv_bfloat16*>(qkv);
+    a.r.row_elems = row_elems; a.r.T = T; a.r.Hq = Hq; a.r.Hkv = Hkv;
+    a.r.gain_q = static_cast<const __nv_bfloat16*>(q_gain);
+    a.r.gain_k = static_cast<const __nv_bfloat16*>(k_gain);
+    a.r.eps = eps; a.r.cos_t = cos_t; a.r.sin_t = sin_t; a.r.n_pos = n_pos; a.r.positions = positions;
+    a.r.out_q = static_cast<__nv_bfloat16*>(out_q);
+    a.r.q_token = static_cast<long long>(Hq) * d; a.r.q_head = d;
+    a.r.cache_K = static_cast<__nv_bfloat16*>(cache_K);
+    a.r.cache_V = static_cast<__nv_bfloat16*>(cache_V);
+    a.r.lengths = lengths;
+    a.r.cache = paged_cache(block_tables, max_pages, page_size, num_pages);
+    a.rot = rot; a.starts = starts; a.B = B;
+    const cudaError_t e = launch_rotate_rows(a, d, interleaved != 0, ctx->num_sms, static_cast<cudaStream_t>(stream));
+    return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
+}
+
+// What both calls take: T tokens in n sets, and, of those that share prefixes, their own rows. Units and tiles of 128 rows, one more for every beginning, are
+// counted in 32 bits.
+static int check_rows(int T, int n, int Hq, int Hkv, int d, bool shared, int most_pages, int page_size, int num_pages, AttendRowsPlan* plan) {
+    int st = check_decode_heads(T, Hq, Hkv, d);
+    if (st == CHUNKKV_OK) st = check_decode_heads(n, Hq, Hkv, d);
+    if (st == CHUNKKV_OK) st = check_decode_cache(most_pages, page_size, num_pages);
+    if (st != CHUNKKV_OK) return st;
+    *plan = attend_rows_plan(T, n, Hq, Hkv, d, shared);
+    return plan->units * (static_cast<long long>(most_pages) * page_size / 128 + 3) >= (1LL << 31) ? CHUNKKV_EINVAL_SHAPE : CHUNKKV_OK;
+}
+
+size_t chunkkv_attend_rows_scratch_bytes(int T, int B, int Hq, int Hkv, int d) {
+    AttendRowsPlan plan;
+    if (T < 1 || B < 1 || check_rows(T, B, Hq, Hkv, d, false, 1, 1, 1, &plan) != CHUNKKV_OK) return 0;
+    return plan.bytes;
+}
+size_t chunkkv_attend_shared_scratch_bytes(int B, int P, int Hq, int Hkv, int d) {
+    AttendRowsPlan plan;
+    if (B < 1 || P < 0 || check_rows(B, P, Hq, Hkv, d, true, 1, 1, 1, &plan) != CHUNKKV_OK) return 0;
+    return plan.bytes;
+}
+
+static int attend_rows_call(const AttendRowsArgs& args, const AttendRowsPlan& plan, int d, void* scratch, size_t scratch_bytes, void* stream) {
+    if (scratch == nullptr || scratch_bytes < plan.bytes) return CHUNKKV_ENOWORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return CHUNKKV_EINVAL_ALIGN;
+    std::lock_guard<std::mutex> lk(g_mu);
+    DeviceCtx* ctx;
+    const int st = get_ctx(&ctx);
+    if (st != CHUNKKV_OK) return st;
+    ctx->rows_called = true;
+    AttendRowsArgs a = args;
+    a.G = a.Hq / a.Hkv;
+    a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(d)));
+    const cudaError_t e = launch_attend_rows(a, plan, d, static_cast<char*>(scratch), ctx->num_sms, static_cast<cudaStream_t>(stream));
+    return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
+}
+
+int chunkkv_attend_rows_paged(const void* q, int T, const int32_t* starts, const int32_t* block_tables, int max_pages, const int32_t* lengths,
+                              int page_size, int num_pages, const void* cache_K, const void* cache_V, int B, int Hq, int Hkv, int d, int causal,
+                              void* out, void* scratch, size_t scratch_bytes, void* stream) {
+    AttendRowsPlan plan;
+    const int st = check_rows(T, B, Hq, Hkv, d, false, max_pages, page_size, num_pages, &plan);
+    if (st != CHUNKKV_OK) return st;
+    if (causal != 0 && causal != 1) return CHUNKKV_EINVAL_SHAPE;
+    if (T == 0 || B == 0) return CHUNKKV_OK;
+    if (q == nullptr || starts == nullptr || block_tables == nullptr || lengths == nullptr || cache_K == nullptr || cache_V == nullptr || out == nullptr)
+        return CHUNKKV_EINVAL_NULL;
+    if (!aligned16(q) || !aligned4(starts) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) || !aligned16(out))
+        return CHUNKKV_EINVAL_ALIGN;
+    AttendRowsArgs a = {};
+    a.q = static_cast<const __nv_bfloat16*>(q);
+    a.K = static_cast<const __nv_bfloat16*>(cache_K);
+    a.V = static_cast<const __nv_bfloat16*>(cache_V);
+    a.out = static_cast<__nv_bfloat16*>(out);
+    a.cache = paged_cache(block_tables, max_pages, page_size, num_pages);
+    a.sets[0] = {block_tables, lengths, starts, B, max_pages, max_pages * page_size, 0};
+    a.T = T; a.Hq = Hq; a.Hkv = Hkv;
+    a.causal = causal != 0;
+    return attend_rows_call(a, plan, d, scratch, scratch_bytes, stream);
+}
+
+int chunkkv_attend_shared_paged(const void* q, const int32_t* starts, int P, const int32_t* prefix_tables, int max_prefix_pages,
+                                const int32_t* prefix_lengths, const int32_t* block_tables, int max_pages, const int32_t* lengths, int page_size,
+                                int num_pages, const void* cache_K, const void* cache_V, int B, int Hq, int Hkv, int d, void* out, void* scratch,
+                                size_t scratch_bytes, void* stream) {
+    AttendRowsPlan plan;
+    if (max_pages < 1 || (P != 0 && max_prefix_pages < 1)) return CHUNKKV_EINVAL_SHAPE;
+    const int most = P != 0 && max_prefix_pages > max_pages ? max_prefix_pages : max_pages;
+    const int st = check_rows(B, P, Hq, Hkv, d, true, most, page_size, num_pages, &plan);
+    if (st != CHUNKKV_OK) return st;
+    if (B == 0) return CHUNKKV_OK;
+    if (q == nullptr || block_tables == nullptr || lengths == nullptr || cache_K == nullptr || cache_V == nullptr || out == nullptr ||
+        (P > 0 && (starts == nullptr || prefix_tables == nullptr || prefix_lengths == nullptr)))
+        return CHUNKKV_EINVAL_NULL;
+    if (!aligned16(q) || !aligned4(starts) || !aligned4(prefix_tables) || !aligned4(prefix_lengths) || !aligned4(block_tables) || !aligned4(lengths) ||
+        !aligned16(cache_K) || !aligned16(cache_V) || !aligned16(out))
+        return CHUNKKV_EINVAL_ALIGN;
+    AttendRowsArgs a = {};
+    a.q = static_cast<const __nv_bfloat16*>(q);
+    a.K = static_cast<const __nv_bfloat16*>(cache_K);
+    a.V = static_cast<const __nv_bfloat16*>(cache_V);
+    a.out = static_cast<__nv_bfloat16*>(out);
+    a.cache = paged_cache(block_tables, max_pages, page_size, num_pages);
+    a.sets[0] = {prefix_tables, prefix_lengths, starts, P, max_prefix_pages, P > 0 ? max_prefix_pages * page_size : 0, 0};
+    a.sets[1] = {block_tables, lengths, nullptr, B, max_pages, max_pages * page_size, 0};
+    a.T = B; a.Hq = Hq; a.Hkv = Hkv;
+    a.shared = true;
+    return attend_rows_call(a, plan, d, scratch, scratch_bytes, stream);
 }
 
 int chunkkv_compress_layer(const void* q_obs, const void* K, const void* V, int L, int Hq, int Hkv,

@@ -1,0 +1,937 @@
+// Attention of many query rows of a KV head over a paged cache: the tokens of a turn (each sequence's own rows, causal or all of them), or one
+// token of each sequence of a group that shares a long prefix, whose rows are then read once for all of them.
+//
+//   out = softmax(q K^T / sqrt(d)) V over the rows that a token sees; with a prefix, over its rows and the sequence's own together
+//
+// A unit of work is a block of up to 256 query rows - tokens times the heads of a KV head's group, so that grouped heads share what is read - of one set
+// (a sequence, a prefix) and KV head, over the set's rows in tiles of 128. A CTA has 12 warps:
+//   0-3, 4-7   a row of 128 query rows a thread each: logits out of tensor memory, maximum, exponentials, sums, P back into tensor memory as bf16
+//   8, 9       tiles of queries, keys and values into shared memory by asynchronous copies, 64 rows a warp, in the layout that the products read
+//   10         the products (tcgen05, 128 x 128 x 16): S = Q K^T and O += P V, two blocks of 128 rows in turn, so that one's exponentials run beside
+//              the other's products
+//   11         hands out the CTA's pieces of units
+// One pass over the data: a row's reference moves only when a logit lies more than 2^8 above it, and then its O is scaled in tensor memory. P is rounded
+// to bf16 once (2^-8 of a weight, independent from row to row, beside the output's own rounding of 2^-8), its sum is taken before that, in 32 bits, as O is.
+//
+// The tiles of all units stand in one line that is dealt evenly to the CTAs, one an SM, so that few rows over a long cache and many over a short one, of
+// any lengths, fill all of them. A unit that several CTAs share leaves (reference, sum, O) records in scratch of the call's own, which a second launch
+// joins in the order of the CTAs: same result every time. With a prefix, every row has two units, and all of them are joined there.
+#include "decode.cuh"
+#include "ptx.cuh"
+#include "rows.h"
+
+namespace chunkkv {
+
+namespace {
+
+__device__ int g_gave_up;                             // a kernel abandoned a bounded wait
+
+constexpr int kTile = 128;                            // rows of a tile of queries, keys or values
+constexpr int kBlock = 256;                           // query rows of a unit
+constexpr int kRowsThreads = 384;
+constexpr int kLoaders = 2;                           // warps that load
+constexpr int kLoaderRows = kTile / kLoaders;
+constexpr int kPieces = 4;                            // pieces handed out ahead
+constexpr int kMasks = 8;                             // tiles whose masks are kept
+constexpr int kBegin = 1;                             // tiles that the beginning of a unit counts as
+constexpr float kSlack = 8.f;
+constexpr int kPanelBytes = kTile * 128;              // 64 dims of 128 rows
+
+// ------------------------------------------------------------------------------------------------ units
+struct Unit {
+    int kind, set, h;        // whose rows
+    int t0, tokens, g0, heads;   // query rows: tokens t0 .., heads g0 .. of the group
+    int limit, step;         // rows that the first token sees (below 0: none), and how many more each further one does
+    int keys;                // rows that the last token sees
+    __device__ __forceinline__ int rows() const { return tokens * heads; }
+    __device__ __forceinline__ int tiles() const { return (keys + kTile - 1) / kTile; }
+    __device__ __forceinline__ int span() const { return tokens > 0 ? tiles() + kBegin : 0; }
+};
+
+// The first block of a set with starts: sets before it take at most this many.
+__device__ __forceinline__ int base_of(const AttendRowsArgs& a, const RowSets& s, int i) { return s.starts[i] / a.tokens + i; }
+// The set whose blocks hold block x.
+__device__ __forceinline__ int set_of(const AttendRowsArgs& a, const RowSets& s, int x) {
+    int lo = 0, hi = s.n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (base_of(a, s, mid) <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+__device__ __forceinline__ Unit unit_of(const AttendRowsArgs& a, int u) {
+    Unit r;
+    const int first = a.sets[0].slots * a.Hkv;
+    r.kind = u >= first;
+    const RowSets& s = a.sets[r.kind];
+    if (r.kind) u -= first;
+    r.h = u / s.slots;
+    const int slot = u - r.h * s.slots, x = slot / a.head_blocks;
+    r.g0 = (slot - x * a.head_blocks) * a.heads;
+    r.heads = min(a.heads, a.G - r.g0);
+    int n, begin;                                      // tokens of the set, the block's first
+    if (r.kind) {
+        r.set = x;
+        r.t0 = x;
+        n = 1;
+        begin = 0;
+    } else {
+        r.set = set_of(a, s, x);
+        // (starts that are not ascending make no address out of range: the tokens lie in [0, T))
+        const int t = min(max(s.starts[r.set], 0), a.T);
+        n = min(max(s.starts[r.set + 1], t), a.T) - t;
+        begin = (x - base_of(a, s, r.set)) * a.tokens;
+        r.t0 = t + begin;
+    }
+    r.tokens = begin >= 0 ? max(min(a.tokens, n - begin), 0) : 0;
+    r.step = a.causal && r.kind == 0 ? 1 : 0;
+    const int len = min(max(s.lengths[static_cast<size_t>(r.set) * a.Hkv + r.h], 0), s.cap);
+    r.limit = r.step ? len - (n - 1 - begin) : len;
+    r.keys = max(r.limit + r.step * (r.tokens - 1), 0);
+    return r;
+}
+
+// The line dealt to n CTAs: the first `more` of them have one more.
+struct Share {
+    int n, per, more;
+    __device__ __forceinline__ Share(int total, int ctas) {
+        n = min(total, ctas);
+        per = n > 0 ? total / n : 0;
+        more = total - per * n;
+    }
+    __device__ __forceinline__ int begin(int cta) const { return cta * per + min(cta, more); }
+    __device__ __forceinline__ int owner(int x) const {
+        const int wide = more * (per + 1);
+        return x < wide ? x / (per + 1) : more + (x - wide) / per;
+    }
+};
+
+// ------------------------------------------------------------------------------------------------ shared memory
+enum Leave { kOut, kWhole, kPart };
+struct Piece {
+    int tiles, tile0;        // tiles of this piece, the first; -1: no more pieces
+    int kind, set, h, t0, g0, heads, rows;
+    int limit, step, keys;
+    int stage;               // 0, 1: at most 128 rows, on that half of the CTA; 2: both halves
+    int leave, slot;
+    int found;               // a value that is not finite stood in a row that not all of the block's tokens see
+};
+template <int D>
+struct RowsSmem {
+    static constexpr int kTileBytes = kTile * D * 2;
+    static constexpr int kSlots = D == 128 ? 5 : 10;  // tiles of keys or values in flight
+    static constexpr int kAhead = D == 128 ? 4 : 7;   // of which so many may be on their way
+    alignas(1024) unsigned char q[2][kTileBytes];
+    alignas(1024) unsigned char kv[kSlots][kTileBytes];
+    Piece piece[kPieces];
+    int first_bad[kPieces][D];                        // of each dim, the first such row
+    uint32_t mask[kMasks][4];                         // rows of a tile of keys that are there
+    unsigned long long kv_full[kSlots], kv_empty[kSlots];
+    unsigned long long q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_empty[2];
+    unsigned long long piece_full[kPieces], piece_empty[kPieces], mask_full[kMasks], drained;
+    int warp_sum[kRowsThreads / 32], first_unit, first_at;
+    int abort;
+    uint32_t tmem;
+};
+static_assert(kRowsThreads == 32 * (8 + kLoaders + 2));
+static_assert(sizeof(RowsSmem<128>) <= 227 * 1024 && sizeof(RowsSmem<64>) <= 227 * 1024, "shared memory of an SM");
+
+// What a role needs to walk the pieces.
+template <int D>
+struct Pieces {
+    RowsSmem<D>& sm;
+    int at = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ explicit Pieces(RowsSmem<D>& s) : sm(s) {}
+    __device__ __forceinline__ void next() {
+        if (++at == kPieces) { at = 0; phase ^= 1u; }
+    }
+    __device__ __forceinline__ bool wait() { return mbar_wait_warp(smem_u32(&sm.piece_full[at]), phase, &sm.abort); }
+};
+
+// P (bf16, in tensor memory) times a tile of values.
+__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Values as they lie, rows of 64 dims: the second operand with its columns (dims) side by side. 8-row groups are 1024 bytes apart, panels of 64 dims
+// kPanelBytes.
+__device__ __forceinline__ uint64_t umma_desc_values(uint32_t at) {
+    uint64_t d = umma_desc_sw128(at) & ~(0x3FFFull << 16);
+    return d | static_cast<uint64_t>(kPanelBytes >> 4) << 16;
+}
+constexpr uint32_t kColumnsSideBySide = 1u << 16;     // in an instruction's descriptor: of the second operand
+
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]),
+        "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+        "r"(r[31]), "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_begin_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Until all but the last `n` groups have landed.
+__device__ __forceinline__ void copies_wait(int n) {
+    switch (n) {
+        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+        case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+        case 5: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 6;" ::: "memory"); break;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ the loading warps
+template <int D>
+struct Loader {
+    using Smem = RowsSmem<D>;
+    static constexpr int kPer = D / 8;                // 16-byte pieces of a row
+    static constexpr int kOnce = 32 / kPer;           // rows that one copy instruction of a warp takes
+    const AttendRowsArgs& a;
+    Smem& sm;
+    const int lane, warp;                             // of those that load
+    int pending = 0;
+    uint32_t jobs[Smem::kAhead];                      // oldest first: slot | type << 4 (0, 1: queries of a half, 2: keys, 3: values) | piece << 8 | last << 10 |
+                                                      // scan << 11 | tile from the first that is looked through << 12
+    __device__ __forceinline__ Loader(const AttendRowsArgs& args, Smem& s, int w) : a(args), sm(s), lane(threadIdx.x & 31), warp(w) {}
+
+    // This warp's rows of a tile, lane l's (l and 32 + l of them) `row` rows behind `base` (-1: zeros).
+    __device__ __forceinline__ void copy(unsigned char* tile, const __nv_bfloat16* base, uint32_t row_bytes, const int (&row)[kLoaderRows / 32]) const {
+        const int p = lane % kPer;
+        const uint32_t to = smem_u32(tile) + (p / 8) * kPanelBytes;
+        const char* from = reinterpret_cast<const char*>(base) + 16 * p;
+#pragma unroll
+        for (int i = 0; i < kLoaderRows / kOnce; ++i) {
+            const int in = i * kOnce + lane / kPer, r = __shfl_sync(0xffffffffu, row[i * kOnce / 32], in % 32), at = warp * kLoaderRows + in;
+            copy_async(to + at * 128 + (((p % 8) ^ (at % 8)) << 4), from + static_cast<uint64_t>(static_cast<uint32_t>(max(r, 0))) * row_bytes, r >= 0);
+        }
+    }
+    // This lane's part of a tile of values that some of the block's tokens must not see: what is not finite there would reach them as 0 * inf. It becomes
+    // zero, and each dim's first such row is kept: who sees that row gets no number there.
+    __device__ void look_through(uint32_t job) {
+        const int p = lane % kPer, piece = job >> 8 & 3;
+        unsigned char* tile = sm.kv[job & 15] + (p / 8) * kPanelBytes;
+        for (int i = 0; i < kLoaderRows / kOnce; ++i) {
+            const int at = warp * kLoaderRows + i * kOnce + lane / kPer;
+            uint4* v = reinterpret_cast<uint4*>(tile + at * 128 + (((p % 8) ^ (at % 8)) << 4));
+            uint4 x = *v;
+            uint32_t w[4] = {x.x, x.y, x.z, x.w};
+            bool bad = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if ((w[e / 2] >> (16 * (e & 1)) & 0x7f80u) == 0x7f80u) {
+                    bad = true;
+                    w[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+                    atomicMin(&sm.first_bad[piece][8 * p + e], static_cast<int>(job >> 12) * kTile + at);
+                }
+            if (bad) {
+                *v = make_uint4(w[0], w[1], w[2], w[3]);
+                *reinterpret_cast<volatile int*>(&sm.piece[piece].found) = 1;
+            }
+        }
+    }
+    // The oldest job under way has landed: say so.
+    __device__ __forceinline__ void land() {
+        copies_wait(pending - 1);
+        const uint32_t job = jobs[0];
+        if (job >> 11 & 1) look_through(job);
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+            const uint32_t type = job >> 4 & 15;
+            mbar_arrive(type < 2 ? smem_u32(&sm.q_full[type]) : smem_u32(&sm.kv_full[job & 15]));
+            if (job >> 10 & 1) mbar_arrive(smem_u32(&sm.piece_empty[job >> 8 & 3]));
+        }
+#pragma unroll
+        for (int i = 0; i + 1 < Smem::kAhead; ++i) jobs[i] = jobs[i + 1];
+        --pending;
+    }
+    __device__ __forceinline__ void queue(uint32_t job) {
+        copies_begin_group();
+#pragma unroll
+        for (int i = 0; i < Smem::kAhead; ++i)
+            if (i == pending) jobs[i] = job;
+        ++pending;
+    }
+    // Waits for a buffer. Who frees it may wait for what is under way here, so that is seen through first.
+    __device__ __forceinline__ bool room(uint32_t bar, uint32_t parity) {
+        if (pending == Smem::kAhead) land();
+        while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
+            if (pending == 0) return mbar_wait_warp(bar, parity, &sm.abort);
+            land();
+        }
+        return true;
+    }
+    __device__ void run() {
+        Pieces<D> pc(sm);
+        int slot = 0, n_tile = 0;
+        uint32_t kv_phase = 1, q_phase = 3;                              // (the first wait for an empty buffer passes)
+        for (;; pc.next()) {
+            while (pending > 0 && !__all_sync(0xffffffffu, mbar_try_wait(smem_u32(&sm.piece_full[pc.at]), pc.phase))) land();
+            if (!pc.wait()) return;
+            const Piece& x = sm.piece[pc.at];
+            const int tiles = x.tiles;
+            if (tiles < 0) break;
+            if (tiles == 0) {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sm.piece_empty[pc.at]));
+                continue;
+            }
+            const RowSets& s = a.sets[x.kind];
+            const int32_t* table = s.tables + static_cast<size_t>(x.set) * s.max_pages;
+            const int keys = x.keys, tile0 = x.tile0, h = x.h;
+            int next[kLoaderRows / 32];
+            auto look_up = [&](int tile) {
+#pragma unroll
+                for (int i = 0; i < kLoaderRows / 32; ++i) {
+                    const int r = tile * kTile + warp * kLoaderRows + 32 * i + lane;
+                    next[i] = r < keys ? paged_row(a.cache, table, r) : -1;
+                }
+            };
+            look_up(tile0);
+            // tiles from here on hold rows that the block's first token does not see
+            const int from = x.step ? max(x.limit, 0) / kTile : 1 << 30;
+            for (int half = x.stage == 2 ? 0 : x.stage; half <= (x.stage == 2 ? 1 : x.stage); ++half) {
+                if (!room(smem_u32(&sm.q_empty[half]), q_phase >> half & 1u)) return;
+                q_phase ^= 1u << half;
+                int row[kLoaderRows / 32];                             // of the queries, from the block's first on
+#pragma unroll
+                for (int i = 0; i < kLoaderRows / 32; ++i) {
+                    const int r = (x.stage == 2 ? half * kTile : 0) + warp * kLoaderRows + 32 * i + lane, tok = r / x.heads, g = r - tok * x.heads;
+                    row[i] = r < x.rows ? tok * a.Hq + g : -1;
+                }
+                copy(sm.q[half], a.q + (static_cast<size_t>(x.t0) * a.Hq + static_cast<size_t>(h) * a.G + x.g0) * D, D * 2, row);
+                queue(static_cast<uint32_t>(half) << 4 | static_cast<uint32_t>(pc.at) << 8);
+            }
+            const __nv_bfloat16 *Kh = a.K + static_cast<size_t>(h) * D, *Vh = a.V + static_cast<size_t>(h) * D;
+            const uint32_t row_bytes = static_cast<uint32_t>(a.Hkv) * (D * 2);
+            for (int t = 0; t < tiles; ++t, ++n_tile) {
+                int row[kLoaderRows / 32];
+                uint32_t there[kLoaderRows / 32];
+#pragma unroll
+                for (int i = 0; i < kLoaderRows / 32; ++i) {
+                    row[i] = next[i];
+                    there[i] = __ballot_sync(0xffffffffu, row[i] >= 0);
+                }
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    if (!room(smem_u32(&sm.kv_empty[slot]), kv_phase)) return;
+                    if (v == 0) {
+                        // (the mask's last reader is done: its tile lies further back than there are buffers of values)
+                        if (lane == 0) {
+#pragma unroll
+                            for (int i = 0; i < kLoaderRows / 32; ++i) sm.mask[n_tile % kMasks][warp * (kLoaderRows / 32) + i] = there[i];
+                            mbar_arrive(smem_u32(&sm.mask_full[n_tile % kMasks]));
+                        }
+                        if (t + 1 < tiles) look_up(tile0 + t + 1);
+                    }
+                    copy(sm.kv[slot], v ? Vh : Kh, row_bytes, row);
+                    const bool scan = v == 1 && tile0 + t >= from;
+                    queue(static_cast<uint32_t>(slot) | static_cast<uint32_t>(2 + v) << 4 | static_cast<uint32_t>(pc.at) << 8 |
+                          (v == 1 && t + 1 == tiles ? 1u << 10 : 0u) | (scan ? 1u << 11 | static_cast<uint32_t>(tile0 + t - from) << 12 : 0u));
+                    if (++slot == Smem::kSlots) { slot = 0; kv_phase ^= 1u; }
+                }
+            }
+        }
+        while (pending > 0) land();
+    }
+};
+
+// ------------------------------------------------------------------------------------------------ the products
+template <int D>
+__device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
+    using Smem = RowsSmem<D>;
+    constexpr uint32_t kS = umma_idesc_bf16(kTile, kTile), kO = umma_idesc_bf16(kTile, D) | kColumnsSideBySide;
+    int at = 0, slot = 0;
+    uint32_t piece_phase = 0, kv_phase = 0, q_phase = 0, p_phase = 0, o_phase = 3;     // (a bit a half; nothing has to be read out of O first)
+    volatile int* abort = &sm.abort;
+    const uint64_t q_desc0 = umma_desc_sw128(smem_u32(sm.q[0])), kv_desc0 = umma_desc_sw128(smem_u32(sm.kv[0])), v_desc0 = umma_desc_values(smem_u32(sm.kv[0]));
+    auto wait_kv = [&](int s, uint32_t phase) { return mbar_wait(smem_u32(&sm.kv_full[s]), phase, abort); };
+    auto advance = [&] {
+        if (++slot == Smem::kSlots) { slot = 0; kv_phase ^= 1u; }
+    };
+    auto logits = [&](int half, int s) {
+        const uint64_t k = kv_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4), q = q_desc0 + static_cast<uint64_t>(half) * (Smem::kTileBytes >> 4);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            const uint64_t off = (i / 4) * (kPanelBytes >> 4) + (i % 4) * 2;
+            umma_bf16(tmem + half * kTile, q + off, k + off, kS, i > 0);
+        }
+        umma_commit(smem_u32(&sm.s_full[half]));
+    };
+    auto values = [&](int half, int s, bool more) {
+        const uint64_t v = v_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4);
+#pragma unroll
+        for (int i = 0; i < kTile / 16; ++i)
+            umma_bf16_ts(tmem + 2 * kTile + half * D, tmem + half * kTile + i * 8, v + i * (2048 >> 4), kO, more || i > 0);
+    };
+    for (;;) {
+        if (!mbar_wait(smem_u32(&sm.piece_full[at]), piece_phase, abort)) return;
+        const int tiles = sm.piece[at].tiles, stage = sm.piece[at].stage;
+        mbar_arrive(smem_u32(&sm.piece_empty[at]));
+        if (++at == kPieces) { at = 0; piece_phase ^= 1u; }
+        if (tiles < 0) return;
+        if (tiles == 0) continue;
+        const int h0 = stage == 2 ? 0 : stage, h1 = stage == 2 ? 2 : stage + 1;
+        for (int h = h0; h < h1; ++h) {
+            if (!mbar_wait(smem_u32(&sm.q_full[h]), q_phase >> h & 1u, abort)) return;
+            q_phase ^= 1u << h;
+        }
+        if (!wait_kv(slot, kv_phase)) return;
+        tc_fence_after();
+        for (int h = h0; h < h1; ++h) {
+            logits(h, slot);
+            if (tiles == 1) umma_commit(smem_u32(&sm.q_empty[h]));
+        }
+        umma_commit(smem_u32(&sm.kv_empty[slot]));
+        advance();
+        for (int t = 0; t < tiles; ++t) {
+            const int v_slot = slot;
+            if (!wait_kv(slot, kv_phase)) return;
+            advance();
+            const int k_slot = slot;
+            const uint32_t k_phase = kv_phase;
+            const bool last = t + 1 == tiles;
+            if (!last) advance();
+            for (int h = h0; h < h1; ++h) {
+                if (t == 0) {
+                    if (!mbar_wait(smem_u32(&sm.o_empty[h]), o_phase >> h & 1u, abort)) return;
+                    o_phase ^= 1u << h;
+                }
+                if (!mbar_wait(smem_u32(&sm.p_full[h]), p_phase >> h & 1u, abort)) return;
+                p_phase ^= 1u << h;
+                tc_fence_after();
+                values(h, v_slot, t > 0);
+                if (last) {
+                    umma_commit(smem_u32(&sm.o_full[h]));
+                } else {
+                    if (h == h0) {
+                        if (!wait_kv(k_slot, k_phase)) return;
+                        tc_fence_after();
+                    }
+                    logits(h, k_slot);
+                    if (t + 2 == tiles) umma_commit(smem_u32(&sm.q_empty[h]));
+                }
+            }
+            umma_commit(smem_u32(&sm.kv_empty[v_slot]));
+            if (!last) umma_commit(smem_u32(&sm.kv_empty[k_slot]));
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ the softmax, a row a thread
+template <int D>
+__device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t tmem, int half) {
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5 & 3;
+    const uint32_t mine = static_cast<uint32_t>(w * 32) << 16;         // this warp's lanes of tensor memory
+    const uint32_t S = tmem + half * kTile + mine, O = tmem + 2 * kTile + half * D + mine;
+    Pieces<D> pc(sm);
+    int n_tile = 0;
+    uint32_t s_phase = 0, o_phase = 0;
+    for (;; pc.next()) {
+        if (!pc.wait()) return;
+        const Piece& x = sm.piece[pc.at];
+        const int tiles = x.tiles;
+        if (tiles < 0) return;
+        if (x.stage != 2 && x.stage != half) {
+            n_tile += tiles;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm.piece_empty[pc.at]));
+            continue;
+        }
+        const int row0 = (x.stage == 2 ? half * kTile : 0) + w * 32, row = row0 + lane;
+        const bool any = row0 < x.rows;                                // (of this warp)
+        const int tok = row / x.heads, limit = x.limit + x.step * tok;
+        const int least = x.limit + x.step * (row0 / x.heads);         // what the warp's first row sees: the least of its rows
+        const int tile0 = x.tile0;
+        float ref = -INFINITY, sum = 0.f;
+        for (int t = 0; t < tiles; ++t, ++n_tile) {
+            if (!mbar_wait_warp(smem_u32(&sm.s_full[half]), s_phase, &sm.abort)) return;
+            s_phase ^= 1u;
+            tc_fence_after();
+            if (any) {
+                float s[kTile];
+#pragma unroll
+                for (int i = 0; i < kTile / 32; ++i) tmem_ld_x32(S + 32 * i, s + 32 * i);
+                if (!mbar_wait_warp(smem_u32(&sm.mask_full[n_tile % kMasks]), n_tile / kMasks & 1, &sm.abort)) return;
+                uint4 m = *reinterpret_cast<const uint4*>(sm.mask[n_tile % kMasks]);
+                tmem_ld_wait();
+                const int see = limit - (tile0 + t) * kTile;
+                if ((m.x & m.y & m.z & m.w) != 0xffffffffu || least < (tile0 + t + 1) * kTile) {
+                    uint32_t b[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int left = see - 32 * i;                 // rows of this word that are seen
+                        b[i] &= left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
+                    }
+#pragma unroll
+                    for (int i = 0; i < kTile; ++i) s[i] = b[i / 32] >> (i & 31) & 1u ? s[i] : -INFINITY;
+                }
+                float top[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top[i] = fmaxf(s[i], s[i + 4]);
+#pragma unroll
+                for (int i = 8; i < kTile; i += 8)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top[e] = fmax3(top[e], s[i + e], s[i + 4 + e]);
+                const float z = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+                if (__any_sync(0xffffffffu, z > ref + kSlack)) {
+                    const float now = fmaxf(ref, z), f = ex2_below(ref, now);
+                    ref = now;
+                    sum *= f;
+                    if (t > 0) {
+                        // (S is there, so the products issued before it, O's latest among them, are done, and the next wait for P)
+#pragma unroll 1
+                        for (int i = 0; i < D; i += 32) {
+                            float o[32];
+                            tmem_ld_x32(O + i, o);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] *= f;
+                            tmem_st_x32(O + i, reinterpret_cast<const uint32_t*>(o));
+                        }
+                    }
+                }
+                const float minus = ref == -INFINITY ? 0.f : -ref;
+                const unsigned long long scale2 = pack2(a.scale_log2, a.scale_log2), minus2 = pack2(minus, minus);
+                unsigned long long acc[2] = {0ull, 0ull};
+#pragma unroll
+                for (int i = 0; i < kTile / 64; ++i) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        float u, v;
+                        unpack2(fma2(pack2(s[64 * i + 2 * e], s[64 * i + 2 * e + 1]), scale2, minus2), u, v);
+                        u = ex2_approx(u);
+                        v = ex2_approx(v);
+                        acc[e & 1] = add2(acc[e & 1], pack2(u, v));
+                        p[e] = pack_bf16(u, v);
+                    }
+                    tmem_st_x32(S + 32 * i, p);
+                }
+                float u, v;
+                unpack2(add2(acc[0], acc[1]), u, v);
+                sum += u + v;
+                tmem_st_wait();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[half]));
+        }
+        if (tiles > 0) {
+            if (!mbar_wait_warp(smem_u32(&sm.o_full[half]), o_phase, &sm.abort)) return;
+            o_phase ^= 1u;
+            tc_fence_after();
+        }
+        if (any) {
+            const bool there = row < x.rows;
+            const int g = row - tok * x.heads;
+            const int token = x.t0 + tok, q = x.h * a.G + x.g0 + g;
+            const int slot = x.slot, leave = x.leave;
+            const bool found = *reinterpret_cast<const volatile int*>(&x.found) != 0;
+            const int bad_from = x.step ? max(x.limit, 0) / kTile * kTile : 0;
+            // rows of all units of a kind, and this one among them
+            const size_t all = static_cast<size_t>(a.T) * a.Hq, whole = static_cast<size_t>(x.h) * a.T * a.G + static_cast<size_t>(token) * a.G + x.g0 + g;
+            if (there && leave == kPart) a.part_ml[static_cast<size_t>(slot) * a.record_rows + row] = make_float2(ref, sum);
+            if (there && leave == kWhole) a.whole_ml[x.kind * all + whole] = make_float2(ref, sum);
+            const float inv = 1.f / sum;
+#pragma unroll 1
+            for (int i = 0; i < D; i += 32) {
+                float o[32];
+                if (tiles > 0) {
+                    tmem_ld_x32(O + i, o);
+                    tmem_ld_wait();
+                }
+                if (found) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const int first = *reinterpret_cast<const volatile int*>(&sm.first_bad[pc.at][i + e]);
+                        if (first < limit - bad_from) o[e] = __int_as_float(0x7fffffff);
+                    }
+                }
+                if (leave == kOut) {
+                    if (there) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) p[e] = sum == 0.f ? 0u : pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);      // (nothing seen: zeros)
+                        uint4* to = reinterpret_cast<uint4*>(a.out + (static_cast<size_t>(token) * a.Hq + q) * D + i);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) to[e] = make_uint4(p[4 * e], p[4 * e + 1], p[4 * e + 2], p[4 * e + 3]);
+                    }
+                } else if (there && tiles > 0) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float4 v = make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        if (leave == kPart) a.part_o[(static_cast<size_t>(slot) * (D / 4) + i / 4 + e) * a.record_rows + row] = v;
+                        else a.whole_o[(static_cast<size_t>(x.kind) * (D / 4) + i / 4 + e) * all + whole] = v;
+                    }
+                }
+            }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            if (tiles > 0) mbar_arrive(smem_u32(&sm.o_empty[half]));
+            mbar_arrive(smem_u32(&sm.piece_empty[pc.at]));
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ pieces
+// The length of the line, and the unit with this CTA's first tile. All threads.
+template <int D>
+__device__ int deal(const AttendRowsArgs& a, RowsSmem<D>& sm, int cta, int ctas) {
+    const int per = (a.units + kRowsThreads - 1) / kRowsThreads;
+    const int u0 = min(static_cast<int>(threadIdx.x) * per, a.units), u1 = min(u0 + per, a.units);
+    int mine = 0;
+    for (int u = u0; u < u1; ++u) mine += unit_of(a, u).span();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int inc = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, inc, off);
+        if (lane >= off) inc += v;
+    }
+    if (lane == 31) sm.warp_sum[warp] = inc;
+    __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < kRowsThreads / 32; ++i) {
+        if (i < warp) inc += sm.warp_sum[i];
+        total += sm.warp_sum[i];
+    }
+    const int begin = Share(total, ctas).begin(cta);
+    int at = inc - mine;
+    if (at <= begin && begin < inc) {                                  // one thread, if any
+        int u = u0;
+        for (; u + 1 < u1; ++u) {
+            const int n = unit_of(a, u).span();
+            if (begin < at + n) break;
+            at += n;
+        }
+        sm.first_unit = u;
+        sm.first_at = at;
+    }
+    return total;
+}
+
+template <int D>
+__device__ void hand_out(const AttendRowsArgs& a, RowsSmem<D>& sm, int total, int cta, int ctas) {
+    const int lane = threadIdx.x & 31;
+    const Share share(total, ctas);
+    const int begin = share.begin(min(cta, share.n)), end = cta < share.n ? share.begin(cta + 1) : begin;
+    int at = 0, narrow = 0;
+    uint32_t phase = 1;                                                // (the first round's entries are free)
+    auto publish = [&](bool fill, const Piece& x) {
+        if (!mbar_wait_warp(smem_u32(&sm.piece_empty[at]), phase, &sm.abort)) return false;
+        for (int i = lane; i < D; i += 32) sm.first_bad[at][i] = 0x7fffffff;
+        if (fill) sm.piece[at] = x;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.piece_full[at]));
+        if (++at == kPieces) { at = 0; phase ^= 1u; }
+        return true;
+    };
+    if (!a.shared && lane == 0) a.begun[2 * cta + 1] = make_int4(0, 0, 0, -1);
+    __syncwarp();
+    if (begin < end) {
+        int u = sm.first_unit, pos = sm.first_at;
+        for (; u < a.units && pos < end; u += 32) {
+            Unit x = {};
+            int n = 0;
+            if (u + lane < a.units) {
+                x = unit_of(a, u + lane);
+                n = x.span();
+            }
+            int inc = n;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, inc, off);
+                if (lane >= off) inc += v;
+            }
+            const int start = pos + inc - n;
+            const int p0 = max(begin - start, 0), p1 = min(end - start, n);
+            uint32_t todo = __ballot_sync(0xffffffffu, n > 0 && p0 < p1);
+            Piece y;
+            y.tile0 = max(p0 - kBegin, 0);
+            y.tiles = max(p1 - kBegin, 0) - y.tile0;
+            y.kind = x.kind; y.set = x.set; y.h = x.h; y.t0 = x.t0; y.g0 = x.g0; y.heads = x.heads; y.rows = x.rows();
+            y.limit = x.limit; y.step = x.step; y.keys = x.keys;
+            y.found = 0;
+            const bool begins = p0 == 0, ends = p1 == n;
+            y.leave = !(begins && ends) ? kPart : a.shared ? kWhole : kOut;
+            y.slot = 2 * cta + (begins ? 1 : 0);
+            const bool thin = y.rows <= kTile;
+            if (p0 < p1 && begins) {
+                const int last = share.owner(start + n - 1);
+                if (a.shared) {
+                    a.owners[u + lane] = make_int2(cta, last);
+                } else if (!ends) {
+                    a.begun[2 * cta] = make_int4(x.t0, x.h * a.G + x.g0, x.heads, y.rows);
+                    a.begun[2 * cta + 1] = make_int4(0, 0, 0, last);
+                }
+            }
+            while (todo != 0) {
+                const int i = __ffs(todo) - 1;
+                todo &= todo - 1;
+                const bool one = __shfl_sync(0xffffffffu, thin, i);
+                y.stage = one ? narrow : 2;
+                if (one) narrow ^= 1;
+                if (!publish(lane == i, y)) return;
+            }
+            pos += __shfl_sync(0xffffffffu, inc, 31);
+        }
+    }
+    Piece none = {};
+    none.tiles = -1;
+    publish(lane == 0, none);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __grid_constant__ AttendRowsArgs a) {
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    RowsSmem<D>& sm = *reinterpret_cast<RowsSmem<D>*>(smem_raw);
+    const int tid = threadIdx.x, warp = tid >> 5;
+    if (warp == 0) tmem_alloc(smem_u32(&sm.tmem), 512);
+    if (tid == 32) {
+        for (int i = 0; i < RowsSmem<D>::kSlots; ++i) {
+            mbar_init(smem_u32(&sm.kv_full[i]), kLoaders);
+            mbar_init(smem_u32(&sm.kv_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sm.q_full[i]), kLoaders);
+            mbar_init(smem_u32(&sm.q_empty[i]), 1);
+            mbar_init(smem_u32(&sm.s_full[i]), 1);
+            mbar_init(smem_u32(&sm.p_full[i]), 4);
+            mbar_init(smem_u32(&sm.o_full[i]), 1);
+            mbar_init(smem_u32(&sm.o_empty[i]), 4);
+        }
+        for (int i = 0; i < kPieces; ++i) {
+            mbar_init(smem_u32(&sm.piece_full[i]), 1);
+            mbar_init(smem_u32(&sm.piece_empty[i]), 8 + kLoaders + 1);   // warps of rows, those that load, and the products'
+        }
+        for (int i = 0; i < kMasks; ++i) mbar_init(smem_u32(&sm.mask_full[i]), kLoaders);
+        mbar_init(smem_u32(&sm.drained), 1);
+        sm.abort = 0;
+        fence_mbar_init();
+    }
+    begin_dependent();
+    const int total = deal(a, sm, blockIdx.x, gridDim.x);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sm.tmem;
+    // 384 threads of 168 registers: 256 * 208 + 128 * 88
+    if (warp < 8) {
+        setmaxnreg_inc<208>();
+        softmax_rows<D>(a, sm, tmem, warp >> 2);
+    } else {
+        setmaxnreg_dec<88>();
+        if (warp < 8 + kLoaders) {
+            Loader<D>(a, sm, warp - 8).run();
+            copies_wait(0);
+        } else if (warp == 8 + kLoaders) {
+            if ((tid & 31) == 0) {
+                issue_products<D>(sm, tmem);
+                umma_commit(smem_u32(&sm.drained));                    // (nothing is under way in tensor memory when it is given back)
+                int none = 0;
+                mbar_wait(smem_u32(&sm.drained), 0, &none);
+            }
+            __syncwarp();
+        } else {
+            hand_out(a, sm, total, blockIdx.x, gridDim.x);
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) {
+        tmem_relinquish();
+        tmem_dealloc(tmem, 512);
+    }
+    if (tid == 0 && sm.abort) atomicExch(&g_gave_up, 1);
+}
+
+// ------------------------------------------------------------------------------------------------ joining
+// 32 rows a CTA, a lane each; the warps take the dims in fours in turn.
+constexpr int kJoinWarps = 8;
+
+template <int D>
+struct Joined {
+    static constexpr int kN = D / 4 / kJoinWarps;
+    float ref = -INFINITY, sum = 0.f;
+    float4 v[kN];
+    __device__ __forceinline__ Joined() {
+#pragma unroll
+        for (int i = 0; i < kN; ++i) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    // A record's (reference, sum) and its values, `stride` apart from four dims to the next. (One that saw nothing has no values.)
+    __device__ __forceinline__ void add(float2 ml, const float4* o, size_t stride) {
+        if (ml.x == -INFINITY && ml.y == 0.f) return;
+        float4 x[kN];
+#pragma unroll
+        for (int i = 0; i < kN; ++i) x[i] = o[(threadIdx.x / 32 + i * kJoinWarps) * stride];
+        const float now = fmaxf(ref, ml.x), f = ex2_below(ref, now), g = ex2_below(ml.x, now);
+        ref = now;
+        sum = sum * f + ml.y * g;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            v[i].x = v[i].x * f + x[i].x * g; v[i].y = v[i].y * f + x[i].y * g;
+            v[i].z = v[i].z * f + x[i].z * g; v[i].w = v[i].w * f + x[i].w * g;
+        }
+    }
+    __device__ __forceinline__ void write(__nv_bfloat16* out) const {
+        const float r = 1.f / sum;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const float4 x = v[i];
+            const uint2 w = sum == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(x.x * r, x.y * r), pack_bf16(x.z * r, x.w * r));
+            *reinterpret_cast<uint2*>(out + 4 * (threadIdx.x / 32 + i * kJoinWarps)) = w;
+        }
+    }
+};
+
+template <int D>
+__device__ __forceinline__ void add_parts(const AttendRowsArgs& a, Joined<D>& j, int first, int last, int row) {
+#pragma unroll 2
+    for (int c = first; c <= last; ++c) {
+        const size_t slot = 2 * c + (c == first ? 1 : 0);
+        j.add(a.part_ml[slot * a.record_rows + row], a.part_o + slot * (D / 4) * a.record_rows + row, a.record_rows);
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(32 * kJoinWarps) rows_join_kernel(const __grid_constant__ AttendRowsArgs a) {
+    begin_dependent();
+    const int chunks = a.record_rows / 32, cta = blockIdx.x / chunks, row = (blockIdx.x - cta * chunks) * 32 + (threadIdx.x & 31);
+    const int last = a.begun[2 * cta + 1].w;
+    if (last < 0) return;
+    const int4 u = a.begun[2 * cta];                                   // first token, first head, heads, rows
+    if (row >= u.w) return;
+    Joined<D> j;
+    add_parts(a, j, cta, last, row);
+    const int tok = row / u.z, g = row - tok * u.z;
+    j.write(a.out + (static_cast<size_t>(u.x + tok) * a.Hq + u.y + g) * D);
+}
+
+template <int D>
+__global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __grid_constant__ AttendRowsArgs a) {
+    begin_dependent();
+    const int rows = a.T * a.G, chunks = (rows + 31) / 32, h = blockIdx.x / chunks, i = (blockIdx.x - h * chunks) * 32 + (threadIdx.x & 31);
+    if (i >= rows) return;
+    const int b = i / a.G, g = i - b * a.G, hb = g / a.heads;
+    const size_t all = static_cast<size_t>(a.Hkv) * rows, mine = static_cast<size_t>(h) * rows + i;
+    Joined<D> j;
+    auto add_unit = [&](int u, int kind, int row) {
+        const int2 by = a.owners[u];
+        if (by.x < 0 || by.y < by.x || by.y >= kRowsCtas) return;       // (groups that are not ascending: no address out of range)
+        if (by.x == by.y) j.add(a.whole_ml[kind * all + mine], a.whole_o + kind * all * (D / 4) + mine, all);
+        else add_parts(a, j, by.x, by.y, row);
+    };
+    const RowSets &p = a.sets[0], &own = a.sets[1];
+    int group = 0;
+    {
+        int lo = 0, hi = p.n;                                          // how many groups end at or before this sequence
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (p.starts[mid + 1] <= b) lo = mid + 1; else hi = mid;
+        }
+        group = lo;
+    }
+    if (group < p.n && p.starts[group] <= b && p.starts[group] >= 0) {
+        const int k = b - p.starts[group], blk = k / a.tokens;
+        add_unit(h * p.slots + (base_of(a, p, group) + blk) * a.head_blocks + hb, 0, (k - blk * a.tokens) * min(a.heads, a.G - hb * a.heads) + g - hb * a.heads);
+    }
+    add_unit(p.slots * a.Hkv + h * own.slots + b * a.head_blocks + hb, 1, g - hb * a.heads);
+    j.write(a.out + (static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * a.G + g) * D);
+}
+
+size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
+
+template <int D>
+cudaError_t launch(const AttendRowsArgs& a, int num_sms, cudaStream_t stream) {
+    constexpr int smem = sizeof(RowsSmem<D>);
+    cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    const int ctas = num_sms < kRowsCtas ? num_sms : kRowsCtas;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.stream = stream;
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(kRowsThreads);
+    cfg.dynamicSmemBytes = smem;
+    e = cudaLaunchKernelEx(&cfg, attend_rows_kernel<D>, a);
+    if (e != cudaSuccess) return e;
+    cfg.blockDim = dim3(32 * kJoinWarps);
+    cfg.dynamicSmemBytes = 0;
+    if (a.shared) {
+        cfg.gridDim = dim3(static_cast<unsigned>((a.T * a.G + 31) / 32 * a.Hkv));
+        return cudaLaunchKernelEx(&cfg, shared_join_kernel<D>, a);
+    }
+    cfg.gridDim = dim3(static_cast<unsigned>(ctas * (a.record_rows / 32)));
+    return cudaLaunchKernelEx(&cfg, rows_join_kernel<D>, a);
+}
+
+}  // namespace
+
+AttendRowsPlan attend_rows_plan(int T, int n, int Hq, int Hkv, int d, bool shared) {
+    AttendRowsPlan p = {};
+    const int G = Hq / Hkv;
+    p.head_blocks = (G + kBlock - 1) / kBlock;
+    p.heads = (G + p.head_blocks - 1) / p.head_blocks;
+    p.tokens = p.head_blocks > 1 ? 1 : kBlock / G;
+    p.slots0 = n > 0 ? (static_cast<long long>(T) / p.tokens + n) * p.head_blocks : 0;
+    p.slots1 = shared ? static_cast<long long>(T) * p.head_blocks : 0;
+    p.units = (p.slots0 + p.slots1) * Hkv;
+    const long long most = static_cast<long long>(T < p.tokens ? T : p.tokens) * p.heads;
+    p.record_rows = static_cast<int>((most + 31) / 32 * 32);
+    const size_t rows = static_cast<size_t>(2) * kRowsCtas * p.record_rows, all = shared ? static_cast<size_t>(2) * T * Hq : 0;
+    p.off_o = up256(rows * sizeof(float2));
+    p.off_begun = up256(p.off_o + rows * d * sizeof(float));
+    p.off_owners = up256(p.off_begun + 2 * kRowsCtas * sizeof(int4));
+    p.off_whole_ml = up256(p.off_owners + (shared ? static_cast<size_t>(p.units) * sizeof(int2) : 0));
+    p.off_whole_o = up256(p.off_whole_ml + all * sizeof(float2));
+    p.bytes = up256(p.off_whole_o + all * d * sizeof(float));
+    return p;
+}
+
+cudaError_t launch_attend_rows(const AttendRowsArgs& args, const AttendRowsPlan& plan, int d, char* scratch, int num_sms, cudaStream_t stream) {
+    AttendRowsArgs a = args;
+    a.heads = plan.heads; a.head_blocks = plan.head_blocks; a.tokens = plan.tokens;
+    a.units = static_cast<int>(plan.units);
+    a.record_rows = plan.record_rows;
+    a.sets[0].slots = static_cast<int>(plan.slots0);
+    a.sets[1].slots = static_cast<int>(plan.slots1);
+    a.part_ml = reinterpret_cast<float2*>(scratch);
+    a.part_o = reinterpret_cast<float4*>(scratch + plan.off_o);
+    a.begun = reinterpret_cast<int4*>(scratch + plan.off_begun);
+    a.owners = reinterpret_cast<int2*>(scratch + plan.off_owners);
+    a.whole_ml = reinterpret_cast<float2*>(scratch + plan.off_whole_ml);
+    a.whole_o = reinterpret_cast<float4*>(scratch + plan.off_whole_o);
+    return d == 128 ? launch<128>(a, num_sms, stream) : launch<64>(a, num_sms, stream);
+}
+
+cudaError_t attend_rows_status(bool* gave_up) {
+    int flag = 0;
+    cudaError_t e = cudaMemcpyFromSymbol(&flag, g_gave_up, sizeof(int));
+    *gave_up = flag != 0;
+    if (e != cudaSuccess || flag == 0) return e;
+    flag = 0;
+    return cudaMemcpyToSymbol(g_gave_up, &flag, sizeof(int));
+}
+
+}  // namespace chunkkv

@@ -421,7 +421,7 @@ struct Cache {
         return static_cast<float*>(t.data_ptr());
     }
 };
-// The angles, positions, gains and eps of a fused activation of `heads` heads of d.
+// The angles, positions, gains and eps of a fused activation of `heads` heads of d, of which the first `rot` dims turn.
 struct Angles {
     int T, n_pos;
     long long row;
@@ -429,9 +429,9 @@ struct Angles {
     const void *x, *gq, *gk;
     const float *co, *si;
     const int32_t* pos;
-    Angles(PyObject* qkv, PyObject* cos, PyObject* sin, PyObject* positions, PyObject* q_gain, PyObject* k_gain, PyObject* eps_, long long heads, int d) {
+    Angles(PyObject* qkv, PyObject* cos, PyObject* sin, PyObject* positions, PyObject* q_gain, PyObject* k_gain, PyObject* eps_, long long heads, int d, int rot) {
         const at::Tensor &t = Cache::here(checked(qkv, at::kBFloat16)), &c = Cache::here(checked(cos, at::kFloat)), &s = Cache::here(checked(sin, at::kFloat));
-        if (t.dim() != 2 || t.size(1) < heads * d || c.dim() != 2 || c.size(1) != d / 2 || s.sizes() != c.sizes() || !PyFloat_CheckExact(eps_)) throw Decline{};
+        if (t.dim() != 2 || t.size(1) < heads * d || c.dim() != 2 || c.size(1) != rot / 2 || s.sizes() != c.sizes() || !PyFloat_CheckExact(eps_)) throw Decline{};
         T = narrow(t.size(0)); row = t.size(1); n_pos = narrow(c.size(0));
         eps = static_cast<float>(PyFloat_AS_DOUBLE(eps_));
         x = t.data_ptr();
@@ -453,7 +453,7 @@ PyObject* rotate_qk(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 13, [&]() -> PyObject* {
         const int Hq = integer(a[1]), Hkv = integer(a[2]), d = integer(a[3]);
         if (Hq < 1 || Hkv < 1 || d < 1 || a[10] != Py_None || a[11] != Py_None) throw Decline{};
-        const Angles x(a[0], a[4], a[5], a[6], a[7], a[8], a[9], static_cast<long long>(Hq) + Hkv, d);
+        const Angles x(a[0], a[4], a[5], a[6], a[7], a[8], a[9], static_cast<long long>(Hq) + Hkv, d, d);
         void* s = current_stream(a[12]);
         const at::Tensor& like = tensor(a[0]);
         Ref oq, ok;
@@ -474,7 +474,7 @@ PyObject* append_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int Hq = integer(a[1]);
         if (Hq < 1) throw Decline{};
         const Cache c(a[5], a[6], a[7], a[8]);
-        const Angles x(a[0], a[2], a[3], a[4], a[9], a[10], a[11], static_cast<long long>(Hq) + 2LL * c.Hkv, c.d);
+        const Angles x(a[0], a[2], a[3], a[4], a[9], a[10], a[11], static_cast<long long>(Hq) + 2LL * c.Hkv, c.d, c.d);
         if (x.T != c.B) throw Decline{};
         void* s = current_stream(a[13]);
         if (a[12] != Py_None) Cache::here(checked(a[12], at::kBFloat16));
@@ -538,11 +538,150 @@ PyObject* evict_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+double number(PyObject* o) {
+    if (!PyFloat_CheckExact(o)) throw Decline{};
+    return PyFloat_AS_DOUBLE(o);
+}
+int truth(PyObject* o) {
+    if (o != Py_True && o != Py_False) throw Decline{};
+    return o == Py_True;
+}
+// Scratch of a call: freed behind it on its stream, to which the allocator's blocks belong. (0 bytes: the call refuses its sizes.)
+at::Tensor scratch_of(const at::Tensor& like, size_t need) {
+    return at::empty({static_cast<long long>(need)}, at::TensorOptions().dtype(at::kByte).device(like.device()));
+}
+// Dims that turn, by the angles' tables [n_pos, rot / 2].
+int rot_of(PyObject* cos) {
+    const at::Tensor& c = checked(cos, at::kFloat);
+    if (c.dim() != 2) throw Decline{};
+    return narrow(2 * c.size(1));
+}
+const int32_t* starts_of(PyObject* o, long long n) {
+    const at::Tensor& t = Cache::here(checked(o, at::kInt));
+    if (t.dim() != 1 || t.size(0) != n + 1) throw Decline{};
+    return static_cast<const int32_t*>(t.data_ptr());
+}
+
+// rope_tables(n_pos, first, rot, base, scaling, factor, original, low, high, scale, stream) -> (cos, sin)
+PyObject* rope_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 11, [&]() -> PyObject* {
+        const int n_pos = integer(a[0]), first = integer(a[1]), rot = integer(a[2]), scaling = integer(a[4]);
+        const double base = number(a[3]), factor = number(a[5]), original = number(a[6]), low = number(a[7]), high = number(a[8]), scale = number(a[9]);
+        if (n_pos < 0 || rot < 0) throw Decline{};
+        void* s = current_stream(a[10]);
+        auto table = [&] {
+            return at::empty({n_pos, rot / 2}, at::TensorOptions().dtype(at::kFloat).device(at::Device(at::kCUDA, c10::cuda::current_device())));
+        };
+        Ref oc, os;
+        float* pc = static_cast<float*>(oc.set(Py_None, at::kFloat, 0, table));
+        float* ps = static_cast<float*>(os.set(Py_None, at::kFloat, 0, table));
+        const int st = unlocked([&] { return chunkkv_rope_tables(n_pos, first, rot, base, scaling, factor, original, low, high, scale, pc, ps, s); });
+        if (st != 0) return PyLong_FromLong(st);
+        return PyTuple_Pack(2, oc.p, os.p);
+    });
+}
+
+// rotate_rows(qkv, Hq, Hkv, d, cos, sin, positions, interleaved, q_gain, k_gain, eps, out_q, out_k, stream) -> (q, k); outputs given go the general way
+PyObject* rotate_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 14, [&]() -> PyObject* {
+        const int Hq = integer(a[1]), Hkv = integer(a[2]), d = integer(a[3]), pairs = truth(a[7]), rot = rot_of(a[4]);
+        if (Hq < 1 || Hkv < 1 || d < 1 || a[11] != Py_None || a[12] != Py_None) throw Decline{};
+        const Angles x(a[0], a[4], a[5], a[6], a[8], a[9], a[10], static_cast<long long>(Hq) + Hkv, d, rot);
+        void* s = current_stream(a[13]);
+        const at::Tensor& like = tensor(a[0]);
+        Ref oq, ok;
+        void* pq = oq.set(Py_None, at::kBFloat16, 0, [&] { return rows(like, x.T, Hq, d); });
+        void* pk = ok.set(Py_None, at::kBFloat16, 0, [&] { return rows(like, x.T, Hkv, d); });
+        const int st = unlocked([&] {
+            return chunkkv_rotate_rows(x.x, x.row, x.T, Hq, Hkv, d, rot, pairs, x.gq, x.gk, x.eps, x.co, x.si, x.n_pos, x.pos,
+                                       static_cast<long long>(Hq) * d, d, static_cast<long long>(Hkv) * d, d, pq, pk, s);
+        });
+        if (st != 0) return PyLong_FromLong(st);
+        return PyTuple_Pack(2, oq.p, ok.p);
+    });
+}
+
+// append_rows_paged(qkv, Hq, starts, cos, sin, positions, block_tables, lengths, cache_K, cache_V, interleaved, q_gain, k_gain, eps, out_q, stream) -> q
+PyObject* append_rows_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 16, [&]() -> PyObject* {
+        const int Hq = integer(a[1]), pairs = truth(a[10]), rot = rot_of(a[3]);
+        if (Hq < 1) throw Decline{};
+        const Cache c(a[6], a[7], a[8], a[9]);
+        const int32_t* starts = starts_of(a[2], c.B);
+        const Angles x(a[0], a[3], a[4], a[5], a[11], a[12], a[13], static_cast<long long>(Hq) + 2LL * c.Hkv, c.d, rot);
+        void* s = current_stream(a[15]);
+        if (a[14] != Py_None) Cache::here(checked(a[14], at::kBFloat16));
+        Ref oq;
+        void* pq = oq.set(a[14], at::kBFloat16, static_cast<long long>(x.T) * Hq * c.d, [&] { return rows(tensor(a[0]), x.T, Hq, c.d); });
+        const int st = unlocked([&] {
+            return chunkkv_append_rows_paged(x.x, x.row, x.T, starts, c.B, Hq, c.Hkv, c.d, rot, pairs, x.gq, x.gk, x.eps, x.co, x.si, x.n_pos, x.pos,
+                                             c.tables, c.max_pages, c.lengths, c.page_size, c.pages, c.K, c.V, pq, s);
+        });
+        if (st != 0) return PyLong_FromLong(st);
+        Py_INCREF(oq.p);
+        return oq.p;
+    });
+}
+
+// attend_rows_paged(q, starts, block_tables, lengths, cache_K, cache_V, causal, out, stream) -> out
+PyObject* attend_rows_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 9, [&]() -> PyObject* {
+        const Cache c(a[2], a[3], a[4], a[5]);
+        const at::Tensor& q = Cache::here(checked(a[0], at::kBFloat16));
+        if (q.dim() != 3 || q.size(2) != c.d) throw Decline{};
+        const int T = narrow(q.size(0)), Hq = narrow(q.size(1)), causal = truth(a[6]);
+        const int32_t* starts = starts_of(a[1], c.B);
+        void* s = current_stream(a[8]);
+        if (a[7] != Py_None) Cache::here(checked(a[7], at::kBFloat16));
+        Ref o;
+        void* po = o.set(a[7], at::kBFloat16, static_cast<long long>(T) * Hq * c.d, [&] { return rows(q, T, Hq, c.d); });
+        const size_t need = chunkkv_attend_rows_scratch_bytes(T, c.B, Hq, c.Hkv, c.d);
+        const at::Tensor scratch = scratch_of(q, need);
+        const void* pq = q.data_ptr();
+        void* ps = scratch.data_ptr();
+        const int st = unlocked([&] {
+            return chunkkv_attend_rows_paged(pq, T, starts, c.tables, c.max_pages, c.lengths, c.page_size, c.pages, c.K, c.V, c.B, Hq, c.Hkv, c.d, causal,
+                                             po, ps, need, s);
+        });
+        if (st != 0) return PyLong_FromLong(st);
+        Py_INCREF(o.p);
+        return o.p;
+    });
+}
+
+// attend_shared_paged(q, starts, prefix_tables, prefix_lengths, block_tables, lengths, cache_K, cache_V, out, stream) -> out
+PyObject* attend_shared_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&]() -> PyObject* {
+        const Cache c(a[4], a[5], a[6], a[7]), p(a[2], a[3], a[6], a[7]);
+        const at::Tensor& q = Cache::here(checked(a[0], at::kBFloat16));
+        if (q.dim() != 3 || q.size(0) != c.B || q.size(2) != c.d) throw Decline{};
+        const int Hq = narrow(q.size(1));
+        const int32_t* starts = starts_of(a[1], p.B);
+        void* s = current_stream(a[9]);
+        if (a[8] != Py_None) Cache::here(checked(a[8], at::kBFloat16));
+        Ref o;
+        void* po = o.set(a[8], at::kBFloat16, static_cast<long long>(c.B) * Hq * c.d, [&] { return rows(q, c.B, Hq, c.d); });
+        const size_t need = chunkkv_attend_shared_scratch_bytes(c.B, p.B, Hq, c.Hkv, c.d);
+        const at::Tensor scratch = scratch_of(q, need);
+        const void* pq = q.data_ptr();
+        void* ps = scratch.data_ptr();
+        const int st = unlocked([&] {
+            return chunkkv_attend_shared_paged(pq, starts, p.B, p.tables, p.max_pages, p.lengths, c.tables, c.max_pages, c.lengths, c.page_size, c.pages,
+                                               c.K, c.V, c.B, Hq, c.Hkv, c.d, po, ps, need, s);
+        });
+        if (st != 0) return PyLong_FromLong(st);
+        Py_INCREF(o.p);
+        return o.p;
+    });
+}
+
 PyMethodDef kMethods[] = {
 #define CKV_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
     CKV_METHOD(scratch), CKV_METHOD(layer), CKV_METHOD(layer_strided), CKV_METHOD(layer_alg1), CKV_METHOD(layer_paged),
     CKV_METHOD(window_queries), CKV_METHOD(score), CKV_METHOD(model),
-    CKV_METHOD(rotate_qk), CKV_METHOD(append_paged), CKV_METHOD(attend_paged), CKV_METHOD(evict_paged), {nullptr, nullptr, 0, nullptr}};
+    CKV_METHOD(rotate_qk), CKV_METHOD(append_paged), CKV_METHOD(attend_paged), CKV_METHOD(evict_paged),
+    CKV_METHOD(rope_tables), CKV_METHOD(rotate_rows), CKV_METHOD(append_rows_paged), CKV_METHOD(attend_rows_paged), CKV_METHOD(attend_shared_paged),
+    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "Per-call part of the binding (see binding.py).", -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

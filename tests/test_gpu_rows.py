@@ -1,0 +1,281 @@
+"""Rotary tables and layouts, turns of many tokens and shared prefixes, against oracle/rows_oracle.py in 64 bits. Tolerances: tests/rows_bounds.py."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2502_00299_b200 as ck
+from oracle import rows_oracle as ora
+from tests import rows_bounds
+from tests.decode_bounds import wide
+from tests.helpers import Guarded, bits_of, rand_bits, to_dev
+
+pytestmark = pytest.mark.gpu
+U, E = 2.0 ** -8, 2.0 ** -24
+
+
+def i32(x):
+    return torch.tensor(np.ascontiguousarray(x).astype(np.int32), device="cuda")
+
+
+def values(t):
+    return wide(bits_of(t))
+
+
+@pytest.fixture(autouse=True)
+def no_abandoned_wait():
+    yield
+    assert ck.device_status() == 0
+
+
+# ------------------------------------------------------------------------------------------------ tables
+# A pair's angle is good to 2^-31 of a turn, 3e-9; the 32-bit fraction of an eighth of a turn, its product with 2 pi and two series of at most five products and
+# sums round by 2^-24 each: 2^-22 of the scale bounds them.
+@pytest.mark.parametrize("n,rot,first", [(1, 16, 0), (7, 128, 0), (1000, 48, 12345), (3, 96, -5), (4097, 32, 1 << 20), (300, 64, (1 << 31) - 10)])
+@pytest.mark.parametrize("kind,factor,low,high", [("none", 1.0, 0.0, 0.0), ("linear", 3.0, 0.0, 0.0), ("dims", 8.0, 1.0, 32.0), ("waves", 4.0, 1.0, 4.0)])
+def test_tables(n, rot, first, kind, factor, low, high):
+    want = ora.tables(n, rot, 10000.0, kind, factor, 4096.0, low, high, 1.25, first)
+    got = ck.rope_tables(n, rot, 10000.0, kind, factor, 4096.0, low, high, 1.25, first)
+    # (the reference's own angles are products in 64 bits: 2^-53 of up to 2^31 rad)
+    for g, w in zip(got, want):
+        assert g.shape == (n, rot // 2) and np.abs(g.cpu().numpy() - w).max() <= 1.25 * (2.0 ** -22 + 2.0 ** -52 * abs(first))
+
+
+def test_tables_into_given_outputs():
+    c, s = Guarded((33, 8), torch.float32), Guarded((33, 8), torch.float32)
+    r = ck.rope_tables(33, 16, 500000.0, out_cos=c.t, out_sin=s.t)
+    assert r[0] is c.t and r[1] is s.t
+    c.check(); s.check()
+    w = ora.tables(33, 16, 500000.0)
+    assert np.abs(c.t.cpu().numpy() - w[0]).max() <= 2.0 ** -22 and np.abs(s.t.cpu().numpy() - w[1]).max() <= 2.0 ** -22
+    assert ck.rope_tables(0, 16, 10.0)[0].shape == (0, 8)
+
+
+# ------------------------------------------------------------------------------------------------ rotations
+def angles(rng, n_pos, rot):
+    a = rng.uniform(-3, 3, (n_pos, rot // 2))
+    return np.cos(a).astype(np.float32), np.sin(a).astype(np.float32)
+
+
+def rotated(x, gain, eps, cos, sin, inter):
+    """(values, tolerance): products and sums in 32 bits - the norm's sum of at most 128 squares, its root, two products, then two products and a
+    sum, 2^-24 each, 100 of them - and one rounding."""
+    y = ora.rotate(x, gain, eps, cos, sin, inter)
+    size = ora.rotate(np.abs(x), None if gain is None else np.abs(gain), eps, np.abs(cos), -np.abs(sin), inter)
+    size = np.maximum(size, ora.rotate(np.abs(x), None if gain is None else np.abs(gain), eps, np.abs(cos), np.abs(sin), inter))
+    return y, U * np.abs(y) + (1 + U) * 100 * E * np.abs(size)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("T,Hq,Hkv,d,rot,norm", [(1, 1, 1, 64, 16, False), (5, 8, 2, 64, 32, True), (37, 7, 1, 128, 128, True), (130, 12, 4, 128, 48, False),
+                                                (2000, 32, 8, 128, 64, True), (3, 6, 3, 64, 64, False), (9, 5, 5, 128, 112, True)])
+def test_rotate(T, Hq, Hkv, d, rot, norm, inter):
+    rng = np.random.default_rng(T + rot)
+    row = (Hq + 2 * Hkv) * d + 8
+    x = rand_bits(rng, (T, row))
+    gq, gk = (rand_bits(rng, d), rand_bits(rng, d)) if norm else (None, None)
+    cos, sin = angles(rng, 50, rot)
+    pos = rng.integers(0, 50, T)
+    pos[T // 2] = -1 if T > 2 else pos[T // 2]
+    q, k = ck.rotate_rows(to_dev(x), Hq, Hkv, d, torch.tensor(cos).cuda(), torch.tensor(sin).cuda(), i32(pos), inter,
+                          to_dev(gq) if norm else None, to_dev(gk) if norm else None, 1e-5)
+    heads = wide(x[:, :(Hq + Hkv) * d]).reshape(T, Hq + Hkv, d)
+    at = np.maximum(pos, 0)
+    for got, part, gain in ((q, heads[:, :Hq], gq), (k, heads[:, Hq:], gk)):
+        want, tol = rotated(part, wide(gain) if norm else None, 1e-5, cos[at].astype(np.float64)[:, None], sin[at].astype(np.float64)[:, None], inter)
+        want[pos < 0] = 0.0
+        assert (np.abs(values(got) - want) <= tol).all()
+    if not norm:
+        assert np.array_equal(bits_of(q)[pos >= 0][..., rot:], x[:, :Hq * d].reshape(T, Hq, d)[pos >= 0][..., rot:])
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_rotate_in_place_and_head_major(inter):
+    T, Hq, Hkv, d, rot = 19, 6, 2, 128, 64
+    rng = np.random.default_rng(8)
+    x = rand_bits(rng, (T, (Hq + 2 * Hkv) * d))
+    cos, sin = (torch.tensor(t).cuda() for t in angles(rng, 40, rot))
+    pos = i32(rng.integers(0, 40, T))
+    qkv = to_dev(x)
+    q, k = ck.rotate_rows(qkv, Hq, Hkv, d, cos, sin, pos, inter)
+    K = torch.zeros(Hkv, T, d, dtype=torch.bfloat16, device="cuda")
+    view = qkv.view(T, Hq + 2 * Hkv, d)
+    ck.rotate_rows(qkv, Hq, Hkv, d, cos, sin, pos, inter, out_q=view[:, :Hq], out_k=K.permute(1, 0, 2))
+    assert torch.equal(view[:, :Hq], q) and torch.equal(K.permute(1, 0, 2), k)
+    assert np.array_equal(bits_of(qkv)[:, Hq * d:], x[:, Hq * d:])
+
+
+def test_whole_heads_in_halves_are_rotate_qk():
+    T, Hq, Hkv, d = 300, 8, 2, 128
+    rng = np.random.default_rng(9)
+    x, g = to_dev(rand_bits(rng, (T, (Hq + 2 * Hkv) * d))), to_dev(rand_bits(rng, d))
+    cos, sin = (torch.tensor(t).cuda() for t in angles(rng, 40, d))
+    pos = i32(rng.integers(0, 40, T))
+    for a, b in zip(ck.rotate_rows(x, Hq, Hkv, d, cos, sin, pos, False, g, g), ck.rotate_qk(x, Hq, Hkv, d, cos, sin, pos, g, g)):
+        assert torch.equal(a, b)
+
+
+def test_dims_that_stay_and_rows_that_turn_may_be_infinite():
+    x = np.full((2, 3 * 64), 0x3F80, dtype=np.uint16)
+    x[0, 40], x[0, 64 + 3] = 0x7F80, 0x7FC0
+    one, none = torch.ones(4, 8, device="cuda"), torch.zeros(4, 8, device="cuda")
+    for inter in (False, True):
+        q, k = ck.rotate_rows(to_dev(x), 1, 1, 64, one, none, i32([0, 1]), inter)
+        q, k = values(q), values(k)
+        assert q[0, 0, 40] == np.inf and np.isfinite(np.delete(q[0, 0], 40)).all() and np.isnan(k[0, 0, 3])
+        assert np.isnan(k[0, 0]).sum() == 2 and (q[1] == 1).all() and (k[1] == 1).all()         # (it and the one that it turns with)
+
+
+# ------------------------------------------------------------------------------------------------ appended rows
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("d,rot,B,norm,page", [(64, 32, 1, False, 16), (128, 128, 3, True, 5), (128, 48, 40, False, 16), (64, 64, 1100, True, 3)])
+def test_append(d, rot, B, norm, page, inter):
+    Hq, Hkv, per = 6, 2, 6
+    rng = np.random.default_rng(B)
+    n = rng.integers(0, 9, B) if B > 1 else np.array([13])
+    if B > 2:
+        n[1] = 0
+    starts = 2 + np.r_[0, np.cumsum(n)]                                      # (tokens in front of all sequences and behind them)
+    T = int(starts[-1]) + 3
+    pages = B * per + 3
+    K0, V0 = rand_bits(rng, (pages, page, Hkv, d)), rand_bits(rng, (pages, page, Hkv, d))
+    table = rng.permutation(pages)[:B * per].reshape(B, per).astype(np.int32)
+    lengths = np.clip(n[:, None] + rng.integers(-3, per * page - 9, (B, Hkv)), 0, None)      # some have fewer rows than new tokens
+    if B > 1:
+        table[0, 0], lengths[B - 1, 1] = -1, per * page + 2                  # a page that is not there; rows beyond the table
+    x = rand_bits(rng, (T, (Hq + 2 * Hkv) * d))
+    g = rand_bits(rng, d) if norm else None
+    cos, sin = angles(rng, 50, rot)
+    pos = rng.integers(0, 50, T)
+    K, V, oq = Guarded(K0.shape, torch.bfloat16), Guarded(V0.shape, torch.bfloat16), Guarded((T, Hq, d), torch.bfloat16)
+    K.t.copy_(to_dev(K0)); V.t.copy_(to_dev(V0)); oq.t.fill_(7.0)
+    gain = to_dev(g) if norm else None
+    r = ck.append_rows_paged(to_dev(x), Hq, i32(starts), torch.tensor(cos).cuda(), torch.tensor(sin).cuda(), i32(pos), i32(table), i32(lengths), K.t, V.t,
+                             inter, gain, gain, 1e-5, oq.t)
+    assert r is oq.t
+    K.check("K"); V.check("V"); oq.check("q")
+    heads = wide(x).reshape(T, Hq + 2 * Hkv, d)
+    c, s = cos[pos].astype(np.float64)[:, None], sin[pos].astype(np.float64)[:, None]
+    q, q_tol = rotated(heads[:, :Hq], wide(g) if norm else None, 1e-5, c, s, inter)
+    k, k_tol = rotated(heads[:, Hq:Hq + Hkv], wide(g) if norm else None, 1e-5, c, s, inter)
+    got_q, got_K, got_V = values(oq.t), bits_of(K.t), bits_of(V.t)
+    at = ora.append_places(starts, T, table, lengths, page, pages)
+    same = np.ones(K0.shape[:3], dtype=bool)
+    for t in range(T):
+        if at[t] is None:
+            assert (got_q[t] == 7.0).all()
+            continue
+        assert (np.abs(got_q[t] - q[t]) <= q_tol[t]).all()
+        for h in range(Hkv):
+            if at[t][h] is not None:
+                p, slot = at[t][h]
+                same[p, slot, h] = False
+                assert (np.abs(wide(got_K[p, slot, h]) - k[t, h]) <= k_tol[t, h]).all()
+                assert np.array_equal(got_V[p, slot, h], x[t].reshape(-1, d)[Hq + Hkv + h])
+    assert np.array_equal(got_K[same], K0[same]) and np.array_equal(got_V[same], V0[same])
+
+
+def test_one_token_each_is_append_paged():
+    B, Hq, Hkv, d, page, per = 9, 8, 2, 128, 16, 3
+    rng = np.random.default_rng(11)
+    x = to_dev(rand_bits(rng, (B, (Hq + 2 * Hkv) * d)))
+    cos, sin = (torch.tensor(t).cuda() for t in angles(rng, 40, d))
+    pos, table, lengths = i32(rng.integers(0, 40, B)), i32(rng.permutation(B * per).reshape(B, per)), i32(rng.integers(0, 49, (B, Hkv)))
+    caches = [[torch.zeros(B * per, page, Hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2)]
+    a = ck.append_paged(x, Hq, cos, sin, pos, table, lengths, *caches[0])
+    b = ck.append_rows_paged(x, Hq, i32(np.arange(B + 1)), cos, sin, pos, table, lengths, *caches[1])
+    assert torch.equal(a, b) and torch.equal(caches[0][0], caches[1][0]) and torch.equal(caches[0][1], caches[1][1])
+
+
+# ------------------------------------------------------------------------------------------------ attention of turns
+def paged(rng, B, Hkv, d, page, per, spare=3, counting=False):
+    pages = B * per + spare
+    if counting:                                                             # keys of zeros, values of small whole numbers
+        from workloads import f32_to_bf16_bits
+        K = np.zeros((pages, page, Hkv, d), dtype=np.uint16)
+        V = f32_to_bf16_bits(rng.integers(-8, 9, K.shape).astype(np.float32))
+    else:
+        K, V = rand_bits(rng, (pages, page, Hkv, d)), rand_bits(rng, (pages, page, Hkv, d))
+    return K, V, rng.permutation(pages)[:B * per].reshape(B, per).astype(np.int32)
+
+
+def attend(q, starts, K, V, table, lengths, causal):
+    out = Guarded(q.shape, torch.bfloat16)
+    out.t.fill_(7.0)
+    args = to_dev(q), i32(starts), i32(table), i32(lengths), to_dev(K), to_dev(V), causal
+    r = ck.attend_rows_paged(*args, out.t)
+    assert r is out.t
+    out.check("out")
+    assert torch.equal(bits(ck.attend_rows_paged(*args, out=torch.full_like(out.t, 7.0))), bits(out.t))      # same result every time
+    return values(out.t)
+
+
+def bits(t):
+    return t.view(torch.int16)
+
+
+COUNT = [   # Hq, Hkv, d, page, tokens, rows before them (a list: of each head)
+    (1, 1, 64, 16, [1], [0]),
+    (1, 1, 128, 16, [1], [1]),
+    (4, 1, 128, 16, [1, 1], [127, 128]),
+    (8, 2, 64, 8, [3, 0, 5], [0, 7, 300]),
+    (8, 2, 128, 100, [130, 1, 77], [5, 1000, 129]),
+    (7, 1, 128, 5, [64, 40], [33, 500]),
+    (12, 4, 64, 64, [300], [1200]),
+    (6, 6, 64, 16, [257, 255, 256], [0, 1, 640]),
+    (40, 2, 128, 1, [9, 30], [200, 11]),
+    (300, 1, 64, 16, [3, 2], [200, 50]),                                     # more query heads than a block holds
+    (16, 2, 128, 32, [1] * 40, list(range(0, 800, 20))),
+    (4, 2, 128, 16, [700], [2500]),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("Hq,Hkv,d,page,n,before", COUNT)
+def test_every_row_counts_once(Hq, Hkv, d, page, n, before, causal):
+    """Logits of 0: means of what is seen."""
+    rng = np.random.default_rng(sum(n) + d)
+    B = len(n)
+    starts = 1 + np.r_[0, np.cumsum(n)]
+    T = int(starts[-1]) + 2
+    lengths = np.array([[max(0, n[b] + before[b] - 3 * (h % 2)) for h in range(Hkv)] for b in range(B)])
+    per = -(-int(lengths.max()) // page) + 1
+    K, V, table = paged(rng, B, Hkv, d, page, per, counting=True)
+    q = rand_bits(rng, (T, Hq, d))
+    out = attend(q, starts, K, V, table, lengths, causal)
+    ref = np.full(q.shape, 7.0)
+    G, v = Hq // Hkv, wide(V)
+    for b in range(B):
+        for h in range(Hkv):
+            L = lengths[b, h]
+            rows = v[table[b, np.arange(L) // page], np.arange(L) % page, h]
+            sums = np.concatenate([np.zeros((1, d)), np.cumsum(rows, 0)])
+            for i in range(n[b]):
+                m = max(L - (n[b] - 1 - i), 0) if causal else L
+                ref[starts[b] + i, h * G:(h + 1) * G] = sums[m] / max(m, 1)
+    rows_bounds.count_rows(out, ref)
+
+
+RANDOM = [
+    (1, 1, 64, 16, [1], [0]),
+    (8, 2, 128, 16, [5, 1, 9], [300, 0, 77]),
+    (7, 1, 64, 100, [64, 3], [260, 900]),
+    (8, 8, 128, 16, [130], [400]),
+    (32, 4, 128, 64, [33, 0, 17], [1000, 5, 2000]),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("scale", [1.0, 6.0])
+@pytest.mark.parametrize("Hq,Hkv,d,page,n,before", RANDOM)
+def test_attention_of_a_turn(Hq, Hkv, d, page, n, before, scale, causal):
+    rng = np.random.default_rng(sum(n) + d + Hq)
+    B = len(n)
+    starts = np.r_[0, np.cumsum(n)]
+    lengths = np.array([[max(0, n[b] + before[b] - 3 * (h % 2)) for h in range(Hkv)] for b in range(B)])
+    per = -(-int(lengths.max()) // page)
+    K, V, table = paged(rng, B, Hkv, d, page, per)
+    if page == 16:                                                           # rows in no page
+        table[0, per // 2] = -1
+    q = rand_bits(rng, (int(starts[-1]), Hq, d), scale)
+    out = attend(q, starts, K, V, table, lengths, causal)
+    rows_bounds.check_attend(out, wide(q), starts, wide(K), wide(V), table, lengths, causal)
