@@ -279,3 +279,142 @@ def test_attention_of_a_turn(Hq, Hkv, d, page, n, before, scale, causal):
     q = rand_bits(rng, (int(starts[-1]), Hq, d), scale)
     out = attend(q, starts, K, V, table, lengths, causal)
     rows_bounds.check_attend(out, wide(q), starts, wide(K), wide(V), table, lengths, causal)
+
+
+def put(K, table, b, row, h, dims, what):
+    page = K.shape[1]
+    K[table[b, row // page], row % page, h, dims] = what
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_that_are_not_seen_do_not_matter(d):
+    """Infinities, not-a-number and the largest numbers behind lengths, in nobody's pages, and in the turn's own rows behind a token."""
+    Hq, Hkv, page, B, n = 8, 2, 16, 3, [150, 5, 40]
+    rng = np.random.default_rng(21)
+    starts = np.r_[0, np.cumsum(n)]
+    lengths = np.array([[400, 391], [5, 3], [300, 260]])
+    per = 26
+    K, V, table = paged(rng, B, Hkv, d, page, per)
+    table[2, 3] = -1
+    used = np.zeros(K.shape[:3], dtype=bool)
+    for b in range(B):
+        for h in range(Hkv):
+            j = np.arange(lengths[b, h])
+            p = table[b, j // page]
+            used[p[p >= 0], (j % page)[p >= 0], h] = True
+    bad = np.array([0x7FC0, 0x7F80, 0xFF80, 0x7F7F, 0xFF7F], dtype=np.uint16)
+    for x in (K, V):
+        x[~used] = rng.choice(bad, (int((~used).sum()), d))
+    q = rand_bits(rng, (int(starts[-1]), Hq, d))
+    for causal in (False, True):
+        out = attend(q, starts, K, V, table, lengths, causal)
+        rows_bounds.check_attend(out, wide(q), starts, wide(K), wide(V), table, lengths, causal)
+    # values of the turn that later tokens only see: those dims are no numbers from there on, and nothing else changes
+    bad_rows = [(0, 300, 0, [1, d - 1], 0x7F80), (0, 393, 0, [5], 0x7FC0), (0, 250, 1, [0, 33], 0xFF80), (1, 4, 0, [7], 0x7FC0), (2, 259, 1, [2], 0x7F80)]
+    clean = attend(q, starts, K, V, table, lengths, True)
+    for b, row, h, dims, what in bad_rows:
+        put(V, table, b, row, h, dims, what)
+    out = attend(q, starts, K, V, table, lengths, True)
+    want = np.zeros(out.shape, dtype=bool)
+    for b, row, h, dims, _ in bad_rows:
+        for i in range(n[b]):
+            if row < lengths[b, h] - (n[b] - 1 - i):
+                want[starts[b] + i, h * 4:(h + 1) * 4, dims] = True
+    assert want.any() and np.array_equal(~np.isfinite(out), want) and np.array_equal(out[~want], clean[~want])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_that_are_not_finite(d):
+    """-inf in some rows and in whole tiles, in every row, one of +inf, one that is no number, logits of +-1e4, and ordinary ones beside them."""
+    page, Hkv, G, rows = 16, 6, 3, 500
+    rng = np.random.default_rng(22)
+    K, V, table = paged(rng, 1, Hkv, d, page, 32)
+    q = rand_bits(rng, (20, Hkv * G, d))
+    q[..., 0] = 0x3F80                                                       # 1.0
+    j = np.arange(rows)
+    p, s = table[0, j // page], j % page
+    some = (j % 3 != 0) | ((j >= 128) & (j < 300))
+    K[p[some], s[some], 0, 0] = 0xFF80
+    K[p, s, 1, 0] = 0xFF80
+    K[p[50], s[50], 2, 0] = 0x7F80
+    K[p, s, 3] = 0
+    K[p, s, 3, 0] = np.where(j == 333, 0x47C3, 0xC7C3)                       # +-99840
+    K[p[70], s[70], 4, 3] = 0x7FC0
+    lengths = np.full((1, Hkv), rows)
+    out = attend(q, [0, 20], K, V, table, lengths, False)
+    with np.errstate(all="ignore"):
+        ref = ora.attend_rows(wide(q), [0, 20], wide(K), wide(V), table, lengths, False)
+    assert np.array_equal(np.isnan(ref), np.isnan(out)) and not out[:, G:2 * G].any()
+    for h in (0, 3, 5):
+        k, v, at = ora.rows_of(wide(K), wide(V), table[0], rows, h)
+        keep = np.isfinite(k).all(1)
+        for g in range(h * G, (h + 1) * G):
+            rows_bounds.check_rows(out[:, g], wide(q)[:, g], k[keep], v[keep], np.ones((20, int(keep.sum())), dtype=bool), (h, g))
+
+
+def test_large_values_are_added_up_before_they_are_divided():
+    rng = np.random.default_rng(23)
+    K, V, table = paged(rng, 1, 1, 128, 16, 40)
+    V[...] = 0x6B80                                                          # 2^88
+    out = attend(rand_bits(rng, (9, 4, 128)), [0, 9], K, V, table, np.array([[600]]), True)
+    assert (np.abs(out / 2.0 ** 88 - 1) <= 2 * U).all()
+
+
+# ------------------------------------------------------------------------------------------------ shared prefixes
+def shared(q, starts, K, V, pt, pl, table, lengths):
+    out = Guarded(q.shape, torch.bfloat16)
+    out.t.fill_(7.0)
+    args = to_dev(q), i32(starts), i32(pt), i32(pl), i32(table), i32(lengths), to_dev(K), to_dev(V)
+    assert ck.attend_shared_paged(*args, out.t) is out.t
+    out.check("out")
+    assert torch.equal(bits(ck.attend_shared_paged(*args)), bits(out.t))     # same result every time
+    return values(out.t)
+
+
+SHARED = [  # Hq, Hkv, d, page, sequences of each group, prefix rows, own rows (most), sequences of no group in front and behind
+    (1, 1, 64, 16, [1], [0], 0, 0, 0),
+    (4, 1, 128, 16, [1], [1], 1, 0, 0),
+    (8, 2, 128, 8, [3, 0, 5], [300, 7, 128], 40, 2, 1),
+    (7, 1, 64, 100, [40], [1000], 200, 0, 0),
+    (32, 8, 128, 16, [64], [700], 30, 0, 0),
+    (28, 4, 64, 5, [30, 7, 50], [257, 1500, 0], 129, 0, 3),
+    (300, 1, 128, 16, [2, 1], [400, 100], 60, 1, 0),                         # more query heads than a block holds
+    (6, 6, 64, 64, [300], [900], 3, 0, 0),
+    (16, 2, 64, 16, [], [], 90, 5, 0),                                       # no prefix at all
+]
+
+
+@pytest.mark.parametrize("counting", [True, False])
+@pytest.mark.parametrize("Hq,Hkv,d,page,sizes,prefix,own,front,back", SHARED)
+def test_shared_prefixes(Hq, Hkv, d, page, sizes, prefix, own, front, back, counting):
+    rng = np.random.default_rng(Hq + d + own)
+    B, P = front + sum(sizes) + back, len(sizes)
+    starts = front + np.r_[0, np.cumsum(sizes)].astype(int)
+    lengths = rng.integers(0, own + 1, (B, Hkv))
+    lengths[rng.random((B, Hkv)) < 0.2] = 0
+    pl = np.array([[max(0, x - 3 * (h % 2)) for h in range(Hkv)] for x in prefix]).reshape(P, Hkv)
+    per, per_pre = max(1, -(-own // page)), max(1, -(-max(prefix, default=0) // page))
+    K, V, all_ = paged(rng, 1, Hkv, d, page, B * per + P * per_pre, counting=counting)
+    table, pt = all_[0, :B * per].reshape(B, per), all_[0, B * per:].reshape(P, per_pre)
+    q = rand_bits(rng, (B, Hq, d), 2.0)
+    if page == 8:                                                            # pages that are not there
+        pt[0, 2], table[3, 0] = -1, len(K)
+    out = shared(q, starts, K, V, pt, pl, table, lengths)
+    if not counting:
+        rows_bounds.check_shared(out, wide(q), starts, wide(K), wide(V), pt, pl, table, lengths)
+        return
+    rows_bounds.count_rows(out, ora.attend_shared(np.zeros(q.shape), starts, np.zeros(K.shape), wide(V), pt, pl, table, lengths))
+
+
+def test_a_prefix_of_infinite_logits_leaves_the_own_rows():
+    rng = np.random.default_rng(31)
+    K, V, all_ = paged(rng, 1, 1, 64, 16, 30)
+    pt, table = all_[:, :20], all_[0, 20:30].reshape(2, 5)
+    q = rand_bits(rng, (2, 4, 64))
+    q[..., 0] = 0x3F80
+    for p in pt[0]:
+        K[p, :, 0, 0] = 0xFF80
+    out = shared(q, [0, 2], K, V, pt, np.array([[320]]), table, np.array([[70], [0]]))
+    assert not out[1].any()
+    k, v, _ = ora.rows_of(wide(K), wide(V), table[0], 70, 0)
+    rows_bounds.check_rows(out[0], wide(q)[0], k, v, np.ones((4, 70), dtype=bool))
