@@ -1068,18 +1068,44 @@ size_t chunkkv_attend_shared_scratch_bytes(int B, int P, int Hq, int Hkv, int d)
     return plan.bytes;
 }
 
-static int attend_rows_call(const AttendRowsArgs& args, const AttendRowsPlan& plan, int d, void* scratch, size_t scratch_bytes, void* stream) {
+// A tensor of bf16, its last dim `elems` long, in boxes of 64 elements of it in the 128-byte swizzle of the tensor cores' operands.
+static int encode_boxes(CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims, const cuuint32_t* box) {
+    cuuint64_t strides[2] = {dims[0] * 2, 0};
+    if (rank > 2) strides[1] = strides[0] * dims[1];
+    const cuuint32_t step[3] = {1, 1, 1};
+    const CUresult r = g_encode(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return CHUNKKV_OK;
+    g_last_cuda_error = 100000 + static_cast<int>(r);
+    return CHUNKKV_ECUDA;
+}
+
+static int attend_rows_call(const AttendRowsArgs& args, const AttendRowsPlan& plan, const void* q, const void* K, const void* V, int d, void* scratch,
+                            size_t scratch_bytes, void* stream) {
     if (scratch == nullptr || scratch_bytes < plan.bytes) return CHUNKKV_ENOWORKSPACE;
     if ((reinterpret_cast<uintptr_t>(scratch) & 255u) != 0) return CHUNKKV_EINVAL_ALIGN;
     std::lock_guard<std::mutex> lk(g_mu);
     DeviceCtx* ctx;
-    const int st = get_ctx(&ctx);
+    int st = get_ctx(&ctx);
+    AttendRowsArgs a = args;
+    a.box = 1;                                                         // the largest power of two, up to a tile, that divides a page
+    while (a.box < 128 && a.cache.page_size % (2 * a.box) == 0) a.box *= 2;
+    if (a.box < 8) a.box = 0;
+    CUtensorMap maps[4];
+    const cuuint64_t q_dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(a.Hq), static_cast<cuuint64_t>(a.T)};
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(a.Hkv) * d, static_cast<cuuint64_t>(a.cache.num_pages) * a.cache.page_size};
+    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(a.box > 0 ? a.box : 1)};
+    const cuuint32_t q_box[3] = {64, static_cast<cuuint32_t>(plan.heads), static_cast<cuuint32_t>(plan.tokens)};
+    const cuuint32_t thin_box[3] = {64, static_cast<cuuint32_t>(plan.heads), static_cast<cuuint32_t>(plan.thin_tokens > 0 ? plan.thin_tokens : 1)};
+    if (st == CHUNKKV_OK) st = encode_boxes(&maps[0], q, 3, q_dims, q_box);
+    if (st == CHUNKKV_OK) st = encode_boxes(&maps[1], q, 3, q_dims, thin_box);
+    if (st == CHUNKKV_OK) st = encode_boxes(&maps[2], K, 2, dims, box);
+    if (st == CHUNKKV_OK) st = encode_boxes(&maps[3], V, 2, dims, box);
     if (st != CHUNKKV_OK) return st;
     ctx->rows_called = true;
-    AttendRowsArgs a = args;
     a.G = a.Hq / a.Hkv;
     a.scale_log2 = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(d)));
-    const cudaError_t e = launch_attend_rows(a, plan, d, static_cast<char*>(scratch), ctx->num_sms, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_attend_rows(a, plan, maps, d, static_cast<char*>(scratch), ctx->num_sms, static_cast<cudaStream_t>(stream));
     return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
 }
 
@@ -1096,15 +1122,12 @@ int chunkkv_attend_rows_paged(const void* q, int T, const int32_t* starts, const
     if (!aligned16(q) || !aligned4(starts) || !aligned4(block_tables) || !aligned4(lengths) || !aligned16(cache_K) || !aligned16(cache_V) || !aligned16(out))
         return CHUNKKV_EINVAL_ALIGN;
     AttendRowsArgs a = {};
-    a.q = static_cast<const __nv_bfloat16*>(q);
-    a.K = static_cast<const __nv_bfloat16*>(cache_K);
-    a.V = static_cast<const __nv_bfloat16*>(cache_V);
     a.out = static_cast<__nv_bfloat16*>(out);
     a.cache = paged_cache(block_tables, max_pages, page_size, num_pages);
     a.sets[0] = {block_tables, lengths, starts, B, max_pages, max_pages * page_size, 0};
     a.T = T; a.Hq = Hq; a.Hkv = Hkv;
     a.causal = causal != 0;
-    return attend_rows_call(a, plan, d, scratch, scratch_bytes, stream);
+    return attend_rows_call(a, plan, q, cache_K, cache_V, d, scratch, scratch_bytes, stream);
 }
 
 int chunkkv_attend_shared_paged(const void* q, const int32_t* starts, int P, const int32_t* prefix_tables, int max_prefix_pages,
@@ -1124,16 +1147,13 @@ int chunkkv_attend_shared_paged(const void* q, const int32_t* starts, int P, con
         !aligned16(cache_K) || !aligned16(cache_V) || !aligned16(out))
         return CHUNKKV_EINVAL_ALIGN;
     AttendRowsArgs a = {};
-    a.q = static_cast<const __nv_bfloat16*>(q);
-    a.K = static_cast<const __nv_bfloat16*>(cache_K);
-    a.V = static_cast<const __nv_bfloat16*>(cache_V);
     a.out = static_cast<__nv_bfloat16*>(out);
     a.cache = paged_cache(block_tables, max_pages, page_size, num_pages);
     a.sets[0] = {prefix_tables, prefix_lengths, starts, P, max_prefix_pages, P > 0 ? max_prefix_pages * page_size : 0, 0};
     a.sets[1] = {block_tables, lengths, nullptr, B, max_pages, max_pages * page_size, 0};
     a.T = B; a.Hq = Hq; a.Hkv = Hkv;
     a.shared = true;
-    return attend_rows_call(a, plan, d, scratch, scratch_bytes, stream);
+    return attend_rows_call(a, plan, q, cache_K, cache_V, d, scratch, scratch_bytes, stream);
 }
 
 int chunkkv_compress_layer(const void* q_obs, const void* K, const void* V, int L, int Hq, int Hkv,

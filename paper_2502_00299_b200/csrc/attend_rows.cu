@@ -6,10 +6,13 @@
 // A unit of work is a block of up to 256 query rows - tokens times the heads of a KV head's group, so that grouped heads share what is read - of one set
 // (a sequence, a prefix) and KV head, over the set's rows in tiles of 128. A CTA has 12 warps:
 //   0-3, 4-7   a row of 128 query rows a thread each: logits out of tensor memory, maximum, exponentials, sums, P back into tensor memory as bf16
-//   8, 9       tiles of queries, keys and values into shared memory by asynchronous copies, 64 rows a warp, in the layout that the products read
-//   10         the products (tcgen05, 128 x 128 x 16): S = Q K^T and O += P V, two blocks of 128 rows in turn, so that one's exponentials run beside
+//   8          hands out the CTA's pieces of units and brings queries and keys into shared memory, by TMA, as the products read them
+//   9          the products (tcgen05, 128 x 128 x 16): S = Q K^T and O += P V, two blocks of 128 rows in turn, so that one's exponentials run beside
 //              the other's products
-//   11         hands out the CTA's pieces of units
+//   10         brings the values
+//   11         looks through values that some of a block's tokens must not see
+// A copy takes an elected thread 23 clocks to issue, and 0.25 us a tile besides; two warps, for keys and values, bring a tile of both in 1100 clocks from pages
+// of 16 rows and in 2100 four rows at a time, beside the 2048 of its exponentials and products.
 // One pass over the data: a row's reference moves only when a logit lies more than 2^8 above it, and then its O is scaled in tensor memory. P is rounded
 // to bf16 once (2^-8 of a weight, independent from row to row, beside the output's own rounding of 2^-8), its sum is taken before that, in 32 bits, as O is.
 //
@@ -20,6 +23,8 @@
 #include "ptx.cuh"
 #include "rows.h"
 
+#include <cuda.h>
+
 namespace chunkkv {
 
 namespace {
@@ -29,8 +34,6 @@ __device__ int g_gave_up;                             // a kernel abandoned a bo
 constexpr int kTile = 128;                            // rows of a tile of queries, keys or values
 constexpr int kBlock = 256;                           // query rows of a unit
 constexpr int kRowsThreads = 384;
-constexpr int kLoaders = 2;                           // warps that load
-constexpr int kLoaderRows = kTile / kLoaders;
 constexpr int kPieces = 4;                            // pieces handed out ahead
 constexpr int kMasks = 8;                             // tiles whose masks are kept
 constexpr int kBegin = 1;                             // tiles that the beginning of a unit counts as
@@ -120,20 +123,19 @@ template <int D>
 struct RowsSmem {
     static constexpr int kTileBytes = kTile * D * 2;
     static constexpr int kSlots = D == 128 ? 5 : 10;  // tiles of keys or values in flight
-    static constexpr int kAhead = D == 128 ? 4 : 7;   // of which so many may be on their way
-    alignas(1024) unsigned char q[2][kTileBytes];
-    alignas(1024) unsigned char kv[kSlots][kTileBytes];
+    alignas(1024) unsigned char q[D / 64][kBlock][128];   // panels of 64 dims; 128 rows a half of the CTA
+    alignas(1024) unsigned char kv[kSlots][kTileBytes];   // panels of 64 dims
     Piece piece[kPieces];
-    int first_bad[kPieces][D];                        // of each dim, the first such row
+    uint32_t first_bad[kPieces][D / 2];               // of each dim, the first such row (16 bits of it: two dims a word), from the first tile with any
+    int4 box[2][kTile / 4];                           // where rows of a tile of keys, or of values, are in the cache
     uint32_t mask[kMasks][4];                         // rows of a tile of keys that are there
     unsigned long long kv_full[kSlots], kv_empty[kSlots];
     unsigned long long q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_empty[2];
-    unsigned long long piece_full[kPieces], piece_empty[kPieces], mask_full[kMasks], drained;
+    unsigned long long piece_full[kPieces], piece_empty[kPieces], mask_full[kMasks], scan, scanned, drained;
     int warp_sum[kRowsThreads / 32], first_unit, first_at;
     int abort;
     uint32_t tmem;
 };
-static_assert(kRowsThreads == 32 * (8 + kLoaders + 2));
 static_assert(sizeof(RowsSmem<128>) <= 227 * 1024 && sizeof(RowsSmem<64>) <= 227 * 1024, "shared memory of an SM");
 
 // What a role needs to walk the pieces.
@@ -175,199 +177,263 @@ __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
         "r"(r[31]), "r"(taddr)
         : "memory");
 }
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, bool there) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_begin_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// Until all but the last `n` groups have landed.
-__device__ __forceinline__ void copies_wait(int n) {
-    switch (n) {
-        case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
-        case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
-        case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
-        case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
-        case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
-        case 5: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
-        default: asm volatile("cp.async.wait_group 6;" ::: "memory"); break;
-    }
+// Four rows of 64 dims, zeros for rows behind the last, one after the other in shared memory.
+__device__ __forceinline__ void gather_rows(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, const int (&row)[4]) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3]), "r"(bar)
+        : "memory");
 }
 
-// ------------------------------------------------------------------------------------------------ the loading warps
-template <int D>
-struct Loader {
-    using Smem = RowsSmem<D>;
-    static constexpr int kPer = D / 8;                // 16-byte pieces of a row
-    static constexpr int kOnce = 32 / kPer;           // rows that one copy instruction of a warp takes
-    const AttendRowsArgs& a;
-    Smem& sm;
-    const int lane, warp;                             // of those that load
-    int pending = 0;
-    uint32_t jobs[Smem::kAhead];                      // oldest first: slot | type << 4 (0, 1: queries of a half, 2: keys, 3: values) | piece << 8 | last << 10 |
-                                                      // scan << 11 | tile from the first that is looked through << 12
-    __device__ __forceinline__ Loader(const AttendRowsArgs& args, Smem& s, int w) : a(args), sm(s), lane(threadIdx.x & 31), warp(w) {}
+// A box of rows of 64 dims.
+__device__ __forceinline__ void copy_rows(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int row) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(row), "r"(bar)
+                 : "memory");
+}
 
-    // This warp's rows of a tile, lane l's (l and 32 + l of them) `row` rows behind `base` (-1: zeros).
-    __device__ __forceinline__ void copy(unsigned char* tile, const __nv_bfloat16* base, uint32_t row_bytes, const int (&row)[kLoaderRows / 32]) const {
-        const int p = lane % kPer;
-        const uint32_t to = smem_u32(tile) + (p / 8) * kPanelBytes;
-        const char* from = reinterpret_cast<const char*>(base) + 16 * p;
-#pragma unroll
-        for (int i = 0; i < kLoaderRows / kOnce; ++i) {
-            const int in = i * kOnce + lane / kPer, r = __shfl_sync(0xffffffffu, row[i * kOnce / 32], in % 32), at = warp * kLoaderRows + in;
-            copy_async(to + at * 128 + (((p % 8) ^ (at % 8)) << 4), from + static_cast<uint64_t>(static_cast<uint32_t>(max(r, 0))) * row_bytes, r >= 0);
+// ------------------------------------------------------------------------------------------------ loading
+// q: [T, Hq, d] in boxes of a block's heads and tokens, q_thin: of at most 128 rows. k, v: rows of the cache, [pages * page_size, Hkv d], in boxes of
+// a.box rows of 64 dims, or (pages that are no multiple of eight rows) of one row, which are fetched in fours.
+struct RowMaps {
+    CUtensorMap q, q_thin, k, v;
+};
+// The first tile that holds rows which the block's first token does not see, or that nobody does.
+__device__ __forceinline__ int scan_from(const Piece& x) { return (x.step ? max(x.limit, 0) : x.keys) / kTile; }
+
+// Where the rows of tile `tile` are: lane l has box l of them (a.box rows each), or its four rows; -1: not there.
+struct Places {
+    int4 at;
+    __device__ __forceinline__ void find(const AttendRowsArgs& a, const int32_t* table, int tile, int keys) {
+        const int lane = threadIdx.x & 31, rows = a.box > 0 ? a.box : 4, r = tile * kTile + lane * rows;
+        at = make_int4(-1, -1, -1, -1);
+        if (lane * rows >= kTile || r >= keys) return;
+        if (a.box > 0) {
+            at.x = paged_row(a.cache, table, r);
+        } else {
+            at.x = paged_row(a.cache, table, r);
+            if (r + 1 < keys) at.y = paged_row(a.cache, table, r + 1);
+            if (r + 2 < keys) at.z = paged_row(a.cache, table, r + 2);
+            if (r + 3 < keys) at.w = paged_row(a.cache, table, r + 3);
         }
-    }
-    // This lane's part of a tile of values that some of the block's tokens must not see: what is not finite there would reach them as 0 * inf. It becomes
-    // zero, and each dim's first such row is kept: who sees that row gets no number there.
-    __device__ void look_through(uint32_t job) {
-        const int p = lane % kPer, piece = job >> 8 & 3;
-        unsigned char* tile = sm.kv[job & 15] + (p / 8) * kPanelBytes;
-        for (int i = 0; i < kLoaderRows / kOnce; ++i) {
-            const int at = warp * kLoaderRows + i * kOnce + lane / kPer;
-            uint4* v = reinterpret_cast<uint4*>(tile + at * 128 + (((p % 8) ^ (at % 8)) << 4));
-            uint4 x = *v;
-            uint32_t w[4] = {x.x, x.y, x.z, x.w};
-            bool bad = false;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if ((w[e / 2] >> (16 * (e & 1)) & 0x7f80u) == 0x7f80u) {
-                    bad = true;
-                    w[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
-                    atomicMin(&sm.first_bad[piece][8 * p + e], static_cast<int>(job >> 12) * kTile + at);
-                }
-            if (bad) {
-                *v = make_uint4(w[0], w[1], w[2], w[3]);
-                *reinterpret_cast<volatile int*>(&sm.piece[piece].found) = 1;
-            }
-        }
-    }
-    // The oldest job under way has landed: say so.
-    __device__ __forceinline__ void land() {
-        copies_wait(pending - 1);
-        const uint32_t job = jobs[0];
-        if (job >> 11 & 1) look_through(job);
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) {
-            const uint32_t type = job >> 4 & 15;
-            mbar_arrive(type < 2 ? smem_u32(&sm.q_full[type]) : smem_u32(&sm.kv_full[job & 15]));
-            if (job >> 10 & 1) mbar_arrive(smem_u32(&sm.piece_empty[job >> 8 & 3]));
-        }
-#pragma unroll
-        for (int i = 0; i + 1 < Smem::kAhead; ++i) jobs[i] = jobs[i + 1];
-        --pending;
-    }
-    __device__ __forceinline__ void queue(uint32_t job) {
-        copies_begin_group();
-#pragma unroll
-        for (int i = 0; i < Smem::kAhead; ++i)
-            if (i == pending) jobs[i] = job;
-        ++pending;
-    }
-    // Waits for a buffer. Who frees it may wait for what is under way here, so that is seen through first.
-    __device__ __forceinline__ bool room(uint32_t bar, uint32_t parity) {
-        if (pending == Smem::kAhead) land();
-        while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) {
-            if (pending == 0) return mbar_wait_warp(bar, parity, &sm.abort);
-            land();
-        }
-        return true;
-    }
-    __device__ void run() {
-        Pieces<D> pc(sm);
-        int slot = 0, n_tile = 0;
-        uint32_t kv_phase = 1, q_phase = 3;                              // (the first wait for an empty buffer passes)
-        for (;; pc.next()) {
-            while (pending > 0 && !__all_sync(0xffffffffu, mbar_try_wait(smem_u32(&sm.piece_full[pc.at]), pc.phase))) land();
-            if (!pc.wait()) return;
-            const Piece& x = sm.piece[pc.at];
-            const int tiles = x.tiles;
-            if (tiles < 0) break;
-            if (tiles == 0) {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sm.piece_empty[pc.at]));
-                continue;
-            }
-            const RowSets& s = a.sets[x.kind];
-            const int32_t* table = s.tables + static_cast<size_t>(x.set) * s.max_pages;
-            const int keys = x.keys, tile0 = x.tile0, h = x.h;
-            int next[kLoaderRows / 32];
-            auto look_up = [&](int tile) {
-#pragma unroll
-                for (int i = 0; i < kLoaderRows / 32; ++i) {
-                    const int r = tile * kTile + warp * kLoaderRows + 32 * i + lane;
-                    next[i] = r < keys ? paged_row(a.cache, table, r) : -1;
-                }
-            };
-            look_up(tile0);
-            // tiles from here on hold rows that the block's first token does not see
-            const int from = x.step ? max(x.limit, 0) / kTile : 1 << 30;
-            for (int half = x.stage == 2 ? 0 : x.stage; half <= (x.stage == 2 ? 1 : x.stage); ++half) {
-                if (!room(smem_u32(&sm.q_empty[half]), q_phase >> half & 1u)) return;
-                q_phase ^= 1u << half;
-                int row[kLoaderRows / 32];                             // of the queries, from the block's first on
-#pragma unroll
-                for (int i = 0; i < kLoaderRows / 32; ++i) {
-                    const int r = (x.stage == 2 ? half * kTile : 0) + warp * kLoaderRows + 32 * i + lane, tok = r / x.heads, g = r - tok * x.heads;
-                    row[i] = r < x.rows ? tok * a.Hq + g : -1;
-                }
-                copy(sm.q[half], a.q + (static_cast<size_t>(x.t0) * a.Hq + static_cast<size_t>(h) * a.G + x.g0) * D, D * 2, row);
-                queue(static_cast<uint32_t>(half) << 4 | static_cast<uint32_t>(pc.at) << 8);
-            }
-            const __nv_bfloat16 *Kh = a.K + static_cast<size_t>(h) * D, *Vh = a.V + static_cast<size_t>(h) * D;
-            const uint32_t row_bytes = static_cast<uint32_t>(a.Hkv) * (D * 2);
-            for (int t = 0; t < tiles; ++t, ++n_tile) {
-                int row[kLoaderRows / 32];
-                uint32_t there[kLoaderRows / 32];
-#pragma unroll
-                for (int i = 0; i < kLoaderRows / 32; ++i) {
-                    row[i] = next[i];
-                    there[i] = __ballot_sync(0xffffffffu, row[i] >= 0);
-                }
-#pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                    if (!room(smem_u32(&sm.kv_empty[slot]), kv_phase)) return;
-                    if (v == 0) {
-                        // (the mask's last reader is done: its tile lies further back than there are buffers of values)
-                        if (lane == 0) {
-#pragma unroll
-                            for (int i = 0; i < kLoaderRows / 32; ++i) sm.mask[n_tile % kMasks][warp * (kLoaderRows / 32) + i] = there[i];
-                            mbar_arrive(smem_u32(&sm.mask_full[n_tile % kMasks]));
-                        }
-                        if (t + 1 < tiles) look_up(tile0 + t + 1);
-                    }
-                    copy(sm.kv[slot], v ? Vh : Kh, row_bytes, row);
-                    const bool scan = v == 1 && tile0 + t >= from;
-                    queue(static_cast<uint32_t>(slot) | static_cast<uint32_t>(2 + v) << 4 | static_cast<uint32_t>(pc.at) << 8 |
-                          (v == 1 && t + 1 == tiles ? 1u << 10 : 0u) | (scan ? 1u << 11 | static_cast<uint32_t>(tile0 + t - from) << 12 : 0u));
-                    if (++slot == Smem::kSlots) { slot = 0; kv_phase ^= 1u; }
-                }
-            }
-        }
-        while (pending > 0) land();
     }
 };
 
+// A tile of the head whose dims begin at x. Boxes that are not there are zeros (values) or, skipped, whatever was there (keys: their logits are not looked
+// at). The whole warp.
+template <int D>
+__device__ __forceinline__ void load_tile(const AttendRowsArgs& a, RowsSmem<D>& sm, int slot, const CUtensorMap* map, int x, const int4& at, bool values) {
+    const int lane = threadIdx.x & 31, rows = a.box > 0 ? a.box : 4, boxes = kTile / rows;
+    const int nowhere = a.cache.num_pages * a.cache.page_size;         // behind the last row: zeros
+    const bool any = at.x >= 0 || at.y >= 0 || at.z >= 0 || at.w >= 0;
+    const uint32_t take = __ballot_sync(0xffffffffu, lane < boxes && (values || any));
+    int4* box = sm.box[values];
+    box[lane] = make_int4(at.x < 0 ? nowhere : at.x, at.y < 0 ? nowhere : at.y, at.z < 0 ? nowhere : at.z, at.w < 0 ? nowhere : at.w);
+    __syncwarp();
+    const uint32_t bar = smem_u32(&sm.kv_full[slot]), to = smem_u32(sm.kv[slot]);
+    if (elect_one()) {
+        mbar_arrive_expect_tx(bar, __popc(take) * rows * (D * 2));
+        if (a.box > 0) {
+#pragma unroll 4
+            for (int i = 0; i < boxes; ++i) {
+                if (take >> i & 1u) {
+#pragma unroll
+                    for (int p = 0; p < D / 64; ++p) copy_rows(to + p * kPanelBytes + i * rows * 128, map, bar, x + 64 * p, box[i].x);
+                }
+            }
+        } else {
+#pragma unroll 4
+            for (int i = 0; i < boxes; ++i) {
+                const int row[4] = {box[i].x, box[i].y, box[i].z, box[i].w};
+                if (take >> i & 1u) {
+#pragma unroll
+                    for (int p = 0; p < D / 64; ++p) gather_rows(to + p * kPanelBytes + i * 512, map, bar, x + 64 * p, row);
+                }
+            }
+        }
+    }
+    __syncwarp();
+}
+// Given up: what is under way lands before the CTA ends. n tiles of keys and values were asked for, this warp's are those of `parity`.
+template <int D>
+__device__ void let_land(RowsSmem<D>& sm, int n, int parity) {
+    int none = 0;
+    for (int i = max(n - RowsSmem<D>::kSlots, 0); i < n; ++i)
+        if ((i & 1) == parity) mbar_wait_warp(smem_u32(&sm.kv_full[i % RowsSmem<D>::kSlots]), i / RowsSmem<D>::kSlots & 1, &none);
+}
+
+// What the loading of keys, or of values, keeps from piece to piece.
+template <int D>
+struct KeyLoader {
+    int n_kv = 0, n_tile = 0;                                          // tiles of keys and values, and of keys, so far
+    uint32_t q_phase = 3, q_used = 0;                                  // (the first wait for an empty buffer passes)
+    __device__ bool load(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<D>& sm, const Piece& x) {
+        const int lane = threadIdx.x & 31;
+        const RowSets& s = a.sets[x.kind];
+        const int32_t* table = s.tables + static_cast<size_t>(x.set) * s.max_pages;
+        Places next;
+        next.find(a, table, x.tile0, x.keys);
+        const bool wide = x.stage == 2;
+        for (int half = wide ? 0 : x.stage; half <= (wide ? 1 : x.stage); ++half) {
+            if (!mbar_wait_warp(smem_u32(&sm.q_empty[half]), q_phase >> half & 1u, &sm.abort)) return false;
+            q_phase ^= 1u << half;
+            q_used |= 1u << half;
+        }
+        if (elect_one()) {
+            // (both halves of a wide block come as one box a panel, on the first half's barrier; the second's is only arrived at)
+            const int half = wide ? 0 : x.stage, rows = wide ? a.tokens * a.heads : a.thin_tokens * a.heads;
+            const uint32_t bar = smem_u32(&sm.q_full[half]);
+            mbar_arrive_expect_tx(bar, rows * (D * 2));
+#pragma unroll
+            for (int p = 0; p < D / 64; ++p) tma_load_3d(smem_u32(sm.q[p][half * kTile]), wide ? &maps.q : &maps.q_thin, bar, 64 * p, x.h * a.G + x.g0, x.t0);
+            if (wide) mbar_arrive(smem_u32(&sm.q_full[1]));
+        }
+        __syncwarp();
+        const int rows = a.box > 0 ? a.box : 4;
+        for (int t = 0; t < x.tiles; ++t, ++n_tile, n_kv += 2) {
+            const Places now = next;
+            const int slot = n_kv % RowsSmem<D>::kSlots, base = (x.tile0 + t) * kTile;
+            if (!mbar_wait_warp(smem_u32(&sm.kv_empty[slot]), (n_kv / RowsSmem<D>::kSlots & 1) ^ 1, &sm.abort)) return false;
+            load_tile<D>(a, sm, slot, &maps.k, x.h * D, now.at, false);
+            // which rows are there: lane l says it of rows 4 l to 4 l + 3. (The mask's last reader is done: its tile lies further back than there are buffers.)
+            uint32_t word;
+            if (a.box > 0) {
+                const uint32_t got = __ballot_sync(0xffffffffu, now.at.x >= 0);
+                word = got >> (4 * lane / rows) & 1u ? 15u : 0u;
+            } else {
+                word = (now.at.x >= 0 ? 1u : 0u) | (now.at.y >= 0 ? 2u : 0u) | (now.at.z >= 0 ? 4u : 0u) | (now.at.w >= 0 ? 8u : 0u);
+            }
+            const int left = x.keys - base - 4 * lane;
+            word = (left >= 4 ? word : left <= 0 ? 0u : word & ((1u << left) - 1u)) << (4 * (lane & 7));
+#pragma unroll
+            for (int off = 1; off < 8; off <<= 1) word |= __shfl_xor_sync(0xffffffffu, word, off);
+            if ((lane & 7) == 0) sm.mask[n_tile % kMasks][lane >> 3] = word;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm.mask_full[n_tile % kMasks]));
+            if (t + 1 < x.tiles) next.find(a, table, x.tile0 + t + 1, x.keys);
+        }
+        return true;
+    }
+    __device__ void give_up(RowsSmem<D>& sm) {
+        let_land(sm, n_kv, 0);
+        int none = 0;
+        for (int half = 0; half < 2; ++half)
+            if (q_used >> half & 1u) mbar_wait_warp(smem_u32(&sm.q_full[half]), q_phase >> half & 1u, &none);
+    }
+};
+
+template <int D>
+__device__ void load_values(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<D>& sm) {
+    const int lane = threadIdx.x & 31;
+    Pieces<D> pc(sm);
+    int n_kv = 1;
+    for (;; pc.next()) {
+        if (!pc.wait()) break;
+        const int tiles = sm.piece[pc.at].tiles, tile0 = sm.piece[pc.at].tile0, keys = sm.piece[pc.at].keys, x = sm.piece[pc.at].h * D;
+        const RowSets& s = a.sets[sm.piece[pc.at].kind];
+        const int32_t* table = s.tables + static_cast<size_t>(sm.piece[pc.at].set) * s.max_pages;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.piece_empty[pc.at]));
+        if (tiles < 0) return;
+        Places next;
+        if (tiles > 0) next.find(a, table, tile0, keys);
+        bool fine = true;
+        for (int t = 0; t < tiles; ++t, n_kv += 2) {
+            const Places now = next;
+            const int slot = n_kv % RowsSmem<D>::kSlots;
+            fine = mbar_wait_warp(smem_u32(&sm.kv_empty[slot]), (n_kv / RowsSmem<D>::kSlots & 1) ^ 1, &sm.abort);
+            if (!fine) break;
+            load_tile<D>(a, sm, slot, &maps.v, x, now.at, true);
+            if (t + 1 < tiles) next.find(a, table, tile0 + t + 1, keys);
+        }
+        if (!fine) break;
+    }
+    let_land(sm, n_kv, 1);
+}
+
+// A tile of values of which some of the block's tokens, or all, must not see every row: what is not finite there would reach them as 0 * inf. From the
+// first such row on it becomes zero, and each dim's first one is kept: who sees that row gets no number there. A warp.
+__device__ void lower(uint32_t* word, int upper, uint32_t to) {
+    uint32_t was = *reinterpret_cast<volatile uint32_t*>(word);
+    while ((was >> (16 * upper) & 0xffffu) > to) {
+        const uint32_t now = upper ? (was & 0xffffu) | to << 16 : (was & 0xffff0000u) | to, got = atomicCAS(word, was, now);
+        if (got == was) break;
+        was = got;
+    }
+}
+template <int D>
+__device__ void scan_values(RowsSmem<D>& sm) {
+    const int lane = threadIdx.x & 31;
+    Pieces<D> pc(sm);
+    int n_kv = 0;
+    uint32_t phase = 0;
+    for (;; pc.next()) {
+        if (!pc.wait()) return;
+        Piece& x = sm.piece[pc.at];
+        const int tiles = x.tiles, tile0 = x.tile0, from = scan_from(x), first = x.step ? max(x.limit, 0) : x.keys;
+        if (tiles < 0) return;
+        for (int t = max(from - tile0, 0); t < tiles; ++t) {
+            const int slot = (n_kv + 2 * t + 1) % RowsSmem<D>::kSlots;
+            if (!mbar_wait_warp(smem_u32(&sm.scan), phase, &sm.abort)) return;
+            phase ^= 1u;
+            bool changed = false;
+            const int row0 = max(first - (tile0 + t) * kTile, 0);
+#pragma unroll 1
+            for (int p = 0; p < D / 64; ++p) {
+#pragma unroll 4
+                for (int row = row0 + (lane >> 3); row < kTile; row += 4) {
+                    uint4* at = reinterpret_cast<uint4*>(sm.kv[slot] + p * kPanelBytes + row * 128) + (lane & 7);
+                    const uint4 v = *at;
+                    uint32_t w[4] = {v.x, v.y, v.z, v.w}, bad = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t y = ~w[e] & 0x7f807f80u;        // a half of zeros: all bits of its exponent are set
+                        bad |= (y - 0x00010001u) & ~y & 0x80008000u;
+                    }
+                    if (bad != 0) {
+                        const int dim = 8 * ((lane & 7) ^ (row & 7)) + 64 * p;
+                        for (int e = 0; e < 8; ++e)
+                            if ((w[e / 2] >> (16 * (e & 1)) & 0x7f80u) == 0x7f80u) {
+                                w[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+                                lower(&sm.first_bad[pc.at][(dim + e) / 2], e & 1, (tile0 + t - from) * kTile + row);
+                            }
+                        *at = make_uint4(w[0], w[1], w[2], w[3]);
+                        changed = true;
+                    }
+                }
+            }
+            if (changed) *reinterpret_cast<volatile int*>(&x.found) = 1;
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm.scanned));
+        }
+        n_kv += 2 * tiles;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm.piece_empty[pc.at]));
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ the products
+// A whole warp, one elected thread of which issues: what the products take is then the same for all lanes, and known to be. (With the loop in one lane's
+// branch every operand goes through a lane's registers, in competition with the exponentials for the issue slots: 2400 clocks a tile more.)
 template <int D>
 __device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
     using Smem = RowsSmem<D>;
     constexpr uint32_t kS = umma_idesc_bf16(kTile, kTile), kO = umma_idesc_bf16(kTile, D) | kColumnsSideBySide;
-    int at = 0, slot = 0;
-    uint32_t piece_phase = 0, kv_phase = 0, q_phase = 0, p_phase = 0, o_phase = 3;     // (a bit a half; nothing has to be read out of O first)
+    Pieces<D> pc(sm);
+    int slot = 0;
+    uint32_t kv_phase = 0, q_phase = 0, p_phase = 0, scan_phase = 0, o_phase = 3;      // (a bit a half; nothing has to be read out of O first)
     volatile int* abort = &sm.abort;
-    const uint64_t q_desc0 = umma_desc_sw128(smem_u32(sm.q[0])), kv_desc0 = umma_desc_sw128(smem_u32(sm.kv[0])), v_desc0 = umma_desc_values(smem_u32(sm.kv[0]));
-    auto wait_kv = [&](int s, uint32_t phase) { return mbar_wait(smem_u32(&sm.kv_full[s]), phase, abort); };
+    const uint64_t q_desc0 = umma_desc_sw128(smem_u32(sm.q[0][0])), kv_desc0 = umma_desc_sw128(smem_u32(sm.kv[0])), v_desc0 = umma_desc_values(smem_u32(sm.kv[0]));
+    auto wait = [&](unsigned long long& bar, uint32_t phase) { return mbar_wait_warp(smem_u32(&bar), phase, abort); };
     auto advance = [&] {
         if (++slot == Smem::kSlots) { slot = 0; kv_phase ^= 1u; }
     };
     auto logits = [&](int half, int s) {
-        const uint64_t k = kv_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4), q = q_desc0 + static_cast<uint64_t>(half) * (Smem::kTileBytes >> 4);
+        const uint64_t k = kv_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4), q = q_desc0 + static_cast<uint64_t>(half) * (kPanelBytes >> 4);
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-            const uint64_t off = (i / 4) * (kPanelBytes >> 4) + (i % 4) * 2;
-            umma_bf16(tmem + half * kTile, q + off, k + off, kS, i > 0);
-        }
+        for (int i = 0; i < D / 16; ++i)
+            umma_bf16(tmem + half * kTile, q + (i / 4) * (2 * kPanelBytes >> 4) + (i % 4) * 2, k + (i / 4) * (kPanelBytes >> 4) + (i % 4) * 2, kS, i > 0);
         umma_commit(smem_u32(&sm.s_full[half]));
     };
     auto values = [&](int half, int s, bool more) {
@@ -376,29 +442,34 @@ __device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
         for (int i = 0; i < kTile / 16; ++i)
             umma_bf16_ts(tmem + 2 * kTile + half * D, tmem + half * kTile + i * 8, v + i * (2048 >> 4), kO, more || i > 0);
     };
-    for (;;) {
-        if (!mbar_wait(smem_u32(&sm.piece_full[at]), piece_phase, abort)) return;
-        const int tiles = sm.piece[at].tiles, stage = sm.piece[at].stage;
-        mbar_arrive(smem_u32(&sm.piece_empty[at]));
-        if (++at == kPieces) { at = 0; piece_phase ^= 1u; }
+    for (;; pc.next()) {
+        if (!pc.wait()) return;
+        const int tiles = sm.piece[pc.at].tiles, stage = sm.piece[pc.at].stage, scan = scan_from(sm.piece[pc.at]) - sm.piece[pc.at].tile0;
+        __syncwarp();
+        if (elect_one()) mbar_arrive(smem_u32(&sm.piece_empty[pc.at]));
         if (tiles < 0) return;
         if (tiles == 0) continue;
         const int h0 = stage == 2 ? 0 : stage, h1 = stage == 2 ? 2 : stage + 1;
         for (int h = h0; h < h1; ++h) {
-            if (!mbar_wait(smem_u32(&sm.q_full[h]), q_phase >> h & 1u, abort)) return;
+            if (!wait(sm.q_full[h], q_phase >> h & 1u)) return;
             q_phase ^= 1u << h;
         }
-        if (!wait_kv(slot, kv_phase)) return;
+        if (!wait(sm.kv_full[slot], kv_phase)) return;
         tc_fence_after();
-        for (int h = h0; h < h1; ++h) {
-            logits(h, slot);
-            if (tiles == 1) umma_commit(smem_u32(&sm.q_empty[h]));
+        if (elect_one()) {
+            for (int h = h0; h < h1; ++h) {
+                logits(h, slot);
+                if (tiles == 1) umma_commit(smem_u32(&sm.q_empty[h]));
+            }
+            umma_commit(smem_u32(&sm.kv_empty[slot]));
         }
-        umma_commit(smem_u32(&sm.kv_empty[slot]));
+        __syncwarp();
         advance();
         for (int t = 0; t < tiles; ++t) {
             const int v_slot = slot;
-            if (!wait_kv(slot, kv_phase)) return;
+            if (!wait(sm.kv_full[slot], kv_phase)) return;
+            if (t >= scan && elect_one()) mbar_arrive(smem_u32(&sm.scan));     // (while the exponentials of this tile are taken)
+            __syncwarp();
             advance();
             const int k_slot = slot;
             const uint32_t k_phase = kv_phase;
@@ -406,26 +477,32 @@ __device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
             if (!last) advance();
             for (int h = h0; h < h1; ++h) {
                 if (t == 0) {
-                    if (!mbar_wait(smem_u32(&sm.o_empty[h]), o_phase >> h & 1u, abort)) return;
+                    if (!wait(sm.o_empty[h], o_phase >> h & 1u)) return;
                     o_phase ^= 1u << h;
                 }
-                if (!mbar_wait(smem_u32(&sm.p_full[h]), p_phase >> h & 1u, abort)) return;
+                if (!wait(sm.p_full[h], p_phase >> h & 1u)) return;
                 p_phase ^= 1u << h;
-                tc_fence_after();
-                values(h, v_slot, t > 0);
-                if (last) {
-                    umma_commit(smem_u32(&sm.o_full[h]));
-                } else {
-                    if (h == h0) {
-                        if (!wait_kv(k_slot, k_phase)) return;
-                        tc_fence_after();
-                    }
-                    logits(h, k_slot);
-                    if (t + 2 == tiles) umma_commit(smem_u32(&sm.q_empty[h]));
+                if (t >= scan && h == h0) {
+                    if (!wait(sm.scanned, scan_phase)) return;
+                    scan_phase ^= 1u;
                 }
+                if (!last && h == h0 && !wait(sm.kv_full[k_slot], k_phase)) return;
+                tc_fence_after();
+                if (elect_one()) {
+                    values(h, v_slot, t > 0);
+                    if (last) {
+                        umma_commit(smem_u32(&sm.o_full[h]));
+                    } else {
+                        logits(h, k_slot);
+                        if (t + 2 == tiles) umma_commit(smem_u32(&sm.q_empty[h]));
+                    }
+                    if (h + 1 == h1) {
+                        umma_commit(smem_u32(&sm.kv_empty[v_slot]));
+                        if (!last) umma_commit(smem_u32(&sm.kv_empty[k_slot]));
+                    }
+                }
+                __syncwarp();
             }
-            umma_commit(smem_u32(&sm.kv_empty[v_slot]));
-            if (!last) umma_commit(smem_u32(&sm.kv_empty[k_slot]));
         }
     }
 }
@@ -540,7 +617,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
             const int token = x.t0 + tok, q = x.h * a.G + x.g0 + g;
             const int slot = x.slot, leave = x.leave;
             const bool found = *reinterpret_cast<const volatile int*>(&x.found) != 0;
-            const int bad_from = x.step ? max(x.limit, 0) / kTile * kTile : 0;
+            const int bad_from = scan_from(x) * kTile;
             // rows of all units of a kind, and this one among them
             const size_t all = static_cast<size_t>(a.T) * a.Hq, whole = static_cast<size_t>(x.h) * a.T * a.G + static_cast<size_t>(token) * a.G + x.g0 + g;
             if (there && leave == kPart) a.part_ml[static_cast<size_t>(slot) * a.record_rows + row] = make_float2(ref, sum);
@@ -556,7 +633,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
                 if (found) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const int first = *reinterpret_cast<const volatile int*>(&sm.first_bad[pc.at][i + e]);
+                        const int first = *reinterpret_cast<const volatile uint32_t*>(&sm.first_bad[pc.at][(i + e) / 2]) >> (16 * (e & 1)) & 0xffff;
                         if (first < limit - bad_from) o[e] = __int_as_float(0x7fffffff);
                     }
                 }
@@ -588,7 +665,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
     }
 }
 
-// ------------------------------------------------------------------------------------------------ pieces
+// ------------------------------------------------------------------------------------------------ pieces, and their queries and keys
 // The length of the line, and the unit with this CTA's first tile. All threads.
 template <int D>
 __device__ int deal(const AttendRowsArgs& a, RowsSmem<D>& sm, int cta, int ctas) {
@@ -627,20 +704,22 @@ __device__ int deal(const AttendRowsArgs& a, RowsSmem<D>& sm, int cta, int ctas)
 }
 
 template <int D>
-__device__ void hand_out(const AttendRowsArgs& a, RowsSmem<D>& sm, int total, int cta, int ctas) {
+__device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<D>& sm, int total, int cta, int ctas) {
     const int lane = threadIdx.x & 31;
+    KeyLoader<D> keys;
     const Share share(total, ctas);
     const int begin = share.begin(min(cta, share.n)), end = cta < share.n ? share.begin(cta + 1) : begin;
     int at = 0, narrow = 0;
     uint32_t phase = 1;                                                // (the first round's entries are free)
     auto publish = [&](bool fill, const Piece& x) {
         if (!mbar_wait_warp(smem_u32(&sm.piece_empty[at]), phase, &sm.abort)) return false;
-        for (int i = lane; i < D; i += 32) sm.first_bad[at][i] = 0x7fffffff;
+        for (int i = lane; i < D / 2; i += 32) sm.first_bad[at][i] = 0xffffffffu;
         if (fill) sm.piece[at] = x;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sm.piece_full[at]));
+        const Piece& y = sm.piece[at];
         if (++at == kPieces) { at = 0; phase ^= 1u; }
-        return true;
+        return y.tiles <= 0 || keys.load(a, maps, sm, y);
     };
     if (!a.shared && lane == 0) a.begun[2 * cta + 1] = make_int4(0, 0, 0, -1);
     __syncwarp();
@@ -671,7 +750,7 @@ __device__ void hand_out(const AttendRowsArgs& a, RowsSmem<D>& sm, int total, in
             const bool begins = p0 == 0, ends = p1 == n;
             y.leave = !(begins && ends) ? kPart : a.shared ? kWhole : kOut;
             y.slot = 2 * cta + (begins ? 1 : 0);
-            const bool thin = y.rows <= kTile;
+            const bool thin = x.tokens <= a.thin_tokens;
             if (p0 < p1 && begins) {
                 const int last = share.owner(start + n - 1);
                 if (a.shared) {
@@ -687,29 +766,32 @@ __device__ void hand_out(const AttendRowsArgs& a, RowsSmem<D>& sm, int total, in
                 const bool one = __shfl_sync(0xffffffffu, thin, i);
                 y.stage = one ? narrow : 2;
                 if (one) narrow ^= 1;
-                if (!publish(lane == i, y)) return;
+                if (!publish(lane == i, y)) {
+                    keys.give_up(sm);
+                    return;
+                }
             }
             pos += __shfl_sync(0xffffffffu, inc, 31);
         }
     }
     Piece none = {};
     none.tiles = -1;
-    publish(lane == 0, none);
+    if (!publish(lane == 0, none)) keys.give_up(sm);
 }
 
 template <int D>
-__global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __grid_constant__ AttendRowsArgs a) {
+__global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __grid_constant__ RowMaps maps, const __grid_constant__ AttendRowsArgs a) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     RowsSmem<D>& sm = *reinterpret_cast<RowsSmem<D>*>(smem_raw);
     const int tid = threadIdx.x, warp = tid >> 5;
     if (warp == 0) tmem_alloc(smem_u32(&sm.tmem), 512);
     if (tid == 32) {
         for (int i = 0; i < RowsSmem<D>::kSlots; ++i) {
-            mbar_init(smem_u32(&sm.kv_full[i]), kLoaders);
+            mbar_init(smem_u32(&sm.kv_full[i]), 1);
             mbar_init(smem_u32(&sm.kv_empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&sm.q_full[i]), kLoaders);
+            mbar_init(smem_u32(&sm.q_full[i]), 1);
             mbar_init(smem_u32(&sm.q_empty[i]), 1);
             mbar_init(smem_u32(&sm.s_full[i]), 1);
             mbar_init(smem_u32(&sm.p_full[i]), 4);
@@ -718,9 +800,11 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
         }
         for (int i = 0; i < kPieces; ++i) {
             mbar_init(smem_u32(&sm.piece_full[i]), 1);
-            mbar_init(smem_u32(&sm.piece_empty[i]), 8 + kLoaders + 1);   // warps of rows, those that load, and the products'
+            mbar_init(smem_u32(&sm.piece_empty[i]), 11);               // warps of rows, and those that load, multiply and look through
         }
-        for (int i = 0; i < kMasks; ++i) mbar_init(smem_u32(&sm.mask_full[i]), kLoaders);
+        for (int i = 0; i < kMasks; ++i) mbar_init(smem_u32(&sm.mask_full[i]), 1);
+        mbar_init(smem_u32(&sm.scan), 1);
+        mbar_init(smem_u32(&sm.scanned), 1);
         mbar_init(smem_u32(&sm.drained), 1);
         sm.abort = 0;
         fence_mbar_init();
@@ -737,19 +821,20 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
         softmax_rows<D>(a, sm, tmem, warp >> 2);
     } else {
         setmaxnreg_dec<88>();
-        if (warp < 8 + kLoaders) {
-            Loader<D>(a, sm, warp - 8).run();
-            copies_wait(0);
-        } else if (warp == 8 + kLoaders) {
-            if ((tid & 31) == 0) {
-                issue_products<D>(sm, tmem);
+        if (warp == 8) {
+            hand_out(a, maps, sm, total, blockIdx.x, gridDim.x);
+        } else if (warp == 9) {
+            issue_products<D>(sm, tmem);
+            if (elect_one()) {
                 umma_commit(smem_u32(&sm.drained));                    // (nothing is under way in tensor memory when it is given back)
                 int none = 0;
                 mbar_wait(smem_u32(&sm.drained), 0, &none);
             }
             __syncwarp();
+        } else if (warp == 10) {
+            load_values<D>(a, maps, sm);
         } else {
-            hand_out(a, sm, total, blockIdx.x, gridDim.x);
+            scan_values<D>(sm);
         }
     }
     tc_fence_before();
@@ -859,7 +944,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __gr
 size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
 
 template <int D>
-cudaError_t launch(const AttendRowsArgs& a, int num_sms, cudaStream_t stream) {
+cudaError_t launch(const AttendRowsArgs& a, const CUtensorMap* maps, int num_sms, cudaStream_t stream) {
     constexpr int smem = sizeof(RowsSmem<D>);
     cudaError_t e = cudaFuncSetAttribute(attend_rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
@@ -874,7 +959,7 @@ cudaError_t launch(const AttendRowsArgs& a, int num_sms, cudaStream_t stream) {
     cfg.gridDim = dim3(ctas);
     cfg.blockDim = dim3(kRowsThreads);
     cfg.dynamicSmemBytes = smem;
-    e = cudaLaunchKernelEx(&cfg, attend_rows_kernel<D>, a);
+    e = cudaLaunchKernelEx(&cfg, attend_rows_kernel<D>, RowMaps{maps[0], maps[1], maps[2], maps[3]}, a);
     if (e != cudaSuccess) return e;
     cfg.blockDim = dim3(32 * kJoinWarps);
     cfg.dynamicSmemBytes = 0;
@@ -894,6 +979,7 @@ AttendRowsPlan attend_rows_plan(int T, int n, int Hq, int Hkv, int d, bool share
     p.head_blocks = (G + kBlock - 1) / kBlock;
     p.heads = (G + p.head_blocks - 1) / p.head_blocks;
     p.tokens = p.head_blocks > 1 ? 1 : kBlock / G;
+    p.thin_tokens = kTile / p.heads;
     p.slots0 = n > 0 ? (static_cast<long long>(T) / p.tokens + n) * p.head_blocks : 0;
     p.slots1 = shared ? static_cast<long long>(T) * p.head_blocks : 0;
     p.units = (p.slots0 + p.slots1) * Hkv;
@@ -909,9 +995,9 @@ AttendRowsPlan attend_rows_plan(int T, int n, int Hq, int Hkv, int d, bool share
     return p;
 }
 
-cudaError_t launch_attend_rows(const AttendRowsArgs& args, const AttendRowsPlan& plan, int d, char* scratch, int num_sms, cudaStream_t stream) {
+cudaError_t launch_attend_rows(const AttendRowsArgs& args, const AttendRowsPlan& plan, const CUtensorMap* maps, int d, char* scratch, int num_sms, cudaStream_t stream) {
     AttendRowsArgs a = args;
-    a.heads = plan.heads; a.head_blocks = plan.head_blocks; a.tokens = plan.tokens;
+    a.heads = plan.heads; a.head_blocks = plan.head_blocks; a.tokens = plan.tokens; a.thin_tokens = plan.thin_tokens;
     a.units = static_cast<int>(plan.units);
     a.record_rows = plan.record_rows;
     a.sets[0].slots = static_cast<int>(plan.slots0);
@@ -922,7 +1008,7 @@ cudaError_t launch_attend_rows(const AttendRowsArgs& args, const AttendRowsPlan&
     a.owners = reinterpret_cast<int2*>(scratch + plan.off_owners);
     a.whole_ml = reinterpret_cast<float2*>(scratch + plan.off_whole_ml);
     a.whole_o = reinterpret_cast<float4*>(scratch + plan.off_whole_o);
-    return d == 128 ? launch<128>(a, num_sms, stream) : launch<64>(a, num_sms, stream);
+    return d == 128 ? launch<128>(a, maps, num_sms, stream) : launch<64>(a, maps, num_sms, stream);
 }
 
 cudaError_t attend_rows_status(bool* gave_up) {

@@ -2,6 +2,8 @@
 #pragma once
 #include "decode.h"
 
+#include <cuda.h>
+
 namespace chunkkv {
 
 // Tables of the rotary embedding (rotate_rows.cu): row p, pair i turns by (first + p) * turn[i] / 2^64 of a full turn.
@@ -34,7 +36,6 @@ struct RowSets {
     int slots;                                // blocks of tokens and heads of a KV head, some of them empty
 };
 struct AttendRowsArgs {
-    const __nv_bfloat16 *q, *K, *V;
     __nv_bfloat16* out;
     RowSets sets[2];                          // shared prefixes: the prefixes, then the sequences' own rows; else the sequences, and nothing
     PagedCache cache;                         // page_size, num_pages, magic, shift (tables and cap: of the sets)
@@ -42,6 +43,8 @@ struct AttendRowsArgs {
     bool causal, shared;
     float scale_log2;                         // log2(e) / sqrt(d)
     int heads, head_blocks, tokens;           // a block: this many heads of a group (head_blocks such blocks) and tokens
+    int thin_tokens;                          // tokens of a block that takes at most 128 rows
+    int box;                                  // rows of the cache that are fetched together; 0: single ones, in fours
     int units, record_rows;
     float2* part_ml;                          // [2 CTAs][record_rows] of units that several CTAs share: (reference, sum)
     float4* part_o;                           // [2 CTAs][d / 4][record_rows]
@@ -52,12 +55,15 @@ struct AttendRowsArgs {
 };
 struct AttendRowsPlan {
     long long slots0, slots1, units;
-    int heads, head_blocks, tokens, record_rows;
+    int heads, head_blocks, tokens, thin_tokens, record_rows;
     size_t off_o, off_begun, off_owners, off_whole_ml, off_whole_o, bytes;
 };
 // T tokens in n sets; shared: T sequences in n groups.
 AttendRowsPlan attend_rows_plan(int T, int n, int Hq, int Hkv, int d, bool shared);
-cudaError_t launch_attend_rows(const AttendRowsArgs& args, const AttendRowsPlan& plan, int d, char* scratch, int num_sms, cudaStream_t stream);
+// maps: of the queries [T, Hq, d], boxes of 64 dims, plan.heads heads and plan.tokens, or plan.thin_tokens, tokens; of the cache's rows, keys and values
+// [num_pages * page_size, Hkv d], boxes of 64 dims and args.box rows, or one.
+cudaError_t launch_attend_rows(const AttendRowsArgs& args, const AttendRowsPlan& plan, const CUtensorMap* maps, int d, char* scratch, int num_sms,
+                               cudaStream_t stream);
 // Whether a kernel of the current device gave up on a bounded wait since the last call.
 cudaError_t attend_rows_status(bool* gave_up);
 
