@@ -130,7 +130,7 @@ struct RowsSmem {
     int4 box[2][kTile / 4];                           // where rows of a tile of keys, or of values, are in the cache
     uint32_t mask[kMasks][4];                         // rows of a tile of keys that are there
     unsigned long long kv_full[kSlots], kv_empty[kSlots];
-    unsigned long long q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], o_empty[2];
+    unsigned long long q_full[2], q_empty[2], s_full[2], p_half[2], p_full[2], o_full[2], o_empty[2];
     unsigned long long piece_full[kPieces], piece_empty[kPieces], mask_full[kMasks], scan, scanned, drained;
     int warp_sum[kRowsThreads / 32], first_unit, first_at;
     int abort;
@@ -167,6 +167,12 @@ __device__ __forceinline__ uint64_t umma_desc_values(uint32_t at) {
 }
 constexpr uint32_t kColumnsSideBySide = 1u << 16;     // in an instruction's descriptor: of the second operand
 
+__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]),
+                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+                 "r"(r[15]), "r"(taddr)
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
@@ -436,11 +442,11 @@ __device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
             umma_bf16(tmem + half * kTile, q + (i / 4) * (2 * kPanelBytes >> 4) + (i % 4) * 2, k + (i / 4) * (kPanelBytes >> 4) + (i % 4) * 2, kS, i > 0);
         umma_commit(smem_u32(&sm.s_full[half]));
     };
-    auto values = [&](int half, int s, bool more) {
-        const uint64_t v = v_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4);
+    auto values = [&](int half, int s, int part, bool more) {          // by the weights of the tile's first or second 64 rows
+        const uint64_t v = v_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4) + part * (64 * 128 >> 4);
 #pragma unroll
-        for (int i = 0; i < kTile / 16; ++i)
-            umma_bf16_ts(tmem + 2 * kTile + half * D, tmem + half * kTile + i * 8, v + i * (2048 >> 4), kO, more || i > 0);
+        for (int i = 0; i < kTile / 32; ++i)
+            umma_bf16_ts(tmem + 2 * kTile + half * D, tmem + half * kTile + part * 32 + i * 8, v + i * (2048 >> 4), kO, more || i > 0);
     };
     for (;; pc.next()) {
         if (!pc.wait()) return;
@@ -480,16 +486,20 @@ __device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
                     if (!wait(sm.o_empty[h], o_phase >> h & 1u)) return;
                     o_phase ^= 1u << h;
                 }
-                if (!wait(sm.p_full[h], p_phase >> h & 1u)) return;
-                p_phase ^= 1u << h;
                 if (t >= scan && h == h0) {
                     if (!wait(sm.scanned, scan_phase)) return;
                     scan_phase ^= 1u;
                 }
+                if (!wait(sm.p_half[h], p_phase >> h & 1u)) return;
+                tc_fence_after();
+                if (elect_one()) values(h, v_slot, 0, t > 0);
+                __syncwarp();
+                if (!wait(sm.p_full[h], p_phase >> h & 1u)) return;
+                p_phase ^= 1u << h;
                 if (!last && h == h0 && !wait(sm.kv_full[k_slot], k_phase)) return;
                 tc_fence_after();
                 if (elect_one()) {
-                    values(h, v_slot, t > 0);
+                    values(h, v_slot, 1, true);
                     if (last) {
                         umma_commit(smem_u32(&sm.o_full[h]));
                     } else {
@@ -508,6 +518,79 @@ __device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
 }
 
 // ------------------------------------------------------------------------------------------------ the softmax, a row a thread
+// The row's logits pass twice, 32 at a time, the next ones on their way out of tensor memory while these are worked on: for their maximum, and for the
+// weights. (All 128 in registers take fewer instructions and are slower: what is run once a tile, 20 KB of it, has to be fetched anew every time.) PART:
+// a bit of `seen` says whether a logit counts.
+template <bool PART>
+__device__ __forceinline__ float masked(float s, uint32_t seen, int i) { return !PART || (seen >> i & 1u) ? s : -INFINITY; }
+template <bool PART>
+__device__ __forceinline__ float max_of(const float (&s)[32], uint32_t seen, float top) {
+    float x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = fmaxf(masked<PART>(s[i], seen, i), masked<PART>(s[i + 4], seen, i + 4));
+#pragma unroll
+    for (int i = 8; i < 32; i += 8)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = fmax3(x[e], masked<PART>(s[i + e], seen, i + e), masked<PART>(s[i + 4 + e], seen, i + 4 + e));
+    return fmax3(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]), top);
+}
+template <bool PART>
+__device__ __forceinline__ float row_max(uint32_t S, const uint32_t (&seen)[4]) {
+    float a[32], b[32], top = -INFINITY;
+    tmem_ld_x32(S, a);
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) {
+        tmem_ld_wait();
+        tmem_ld_x32(S + 64 * i + 32, b);
+        top = max_of<PART>(a, i == 0 ? seen[0] : seen[2], top);
+        tmem_ld_wait();
+        if (i == 0) tmem_ld_x32(S + 64, a);
+        top = max_of<PART>(b, i == 0 ? seen[1] : seen[3], top);
+    }
+    return top;
+}
+// 2^(s scale + minus) of 32 logits, as bf16, and added up.
+template <bool PART>
+__device__ __forceinline__ void weights_of(const float (&s)[32], uint32_t seen, uint32_t (&p)[16], unsigned long long scale2, unsigned long long minus2,
+                                           unsigned long long (&acc)[2]) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        unsigned long long x = fma2(pack2(masked<PART>(s[2 * e], seen, 2 * e), masked<PART>(s[2 * e + 1], seen, 2 * e + 1)), scale2, minus2);
+        float u, v;
+        unpack2(x, u, v);
+        u = ex2_approx(u);
+        v = ex2_approx(v);
+        x = pack2(u, v);
+        acc[e & 1] = add2(acc[e & 1], x);
+        p[e] = pack_bf16(u, v);
+    }
+}
+// A row's weights into the place of its logits; half(0), half(1) when those of the first and the second 64 are there. Their sum.
+template <bool PART, class Half>
+__device__ __forceinline__ float row_weights(uint32_t S, const uint32_t (&seen)[4], float scale, float minus, Half half) {
+    const unsigned long long scale2 = pack2(scale, scale), minus2 = pack2(minus, minus);
+    unsigned long long acc[2] = {0ull, 0ull};
+    float a[32], b[32];
+    uint32_t p[16];
+    tmem_ld_x32(S, a);
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) {
+        tmem_ld_wait();
+        tmem_ld_x32(S + 64 * i + 32, b);
+        weights_of<PART>(a, i == 0 ? seen[0] : seen[2], p, scale2, minus2, acc);
+        tmem_ld_wait();
+        if (i == 0) tmem_ld_x32(S + 64, a);
+        tmem_st_x16(S + 32 * i, p);                                    // (behind the loads of the logits that stood there)
+        weights_of<PART>(b, i == 0 ? seen[1] : seen[3], p, scale2, minus2, acc);
+        tmem_st_x16(S + 32 * i + 16, p);
+        tmem_st_wait();
+        half(i);
+    }
+    float u, v;
+    unpack2(add2(acc[0], acc[1]), u, v);
+    return u + v;
+}
+
 template <int D>
 __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t tmem, int half) {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5 & 3;
@@ -534,35 +617,26 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
         const int tile0 = x.tile0;
         float ref = -INFINITY, sum = 0.f;
         for (int t = 0; t < tiles; ++t, ++n_tile) {
+            uint4 m = make_uint4(0u, 0u, 0u, 0u);
+            if (any) {
+                if (!mbar_wait_warp(smem_u32(&sm.mask_full[n_tile % kMasks]), n_tile / kMasks & 1, &sm.abort)) return;
+                m = *reinterpret_cast<const uint4*>(sm.mask[n_tile % kMasks]);
+            }
             if (!mbar_wait_warp(smem_u32(&sm.s_full[half]), s_phase, &sm.abort)) return;
             s_phase ^= 1u;
             tc_fence_after();
             if (any) {
-                float s[kTile];
-#pragma unroll
-                for (int i = 0; i < kTile / 32; ++i) tmem_ld_x32(S + 32 * i, s + 32 * i);
-                if (!mbar_wait_warp(smem_u32(&sm.mask_full[n_tile % kMasks]), n_tile / kMasks & 1, &sm.abort)) return;
-                uint4 m = *reinterpret_cast<const uint4*>(sm.mask[n_tile % kMasks]);
-                tmem_ld_wait();
                 const int see = limit - (tile0 + t) * kTile;
-                if ((m.x & m.y & m.z & m.w) != 0xffffffffu || least < (tile0 + t + 1) * kTile) {
-                    uint32_t b[4] = {m.x, m.y, m.z, m.w};
+                const bool part = (m.x & m.y & m.z & m.w) != 0xffffffffu || least < (tile0 + t + 1) * kTile;
+                uint32_t seen[4] = {m.x, m.y, m.z, m.w};
+                if (part) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int left = see - 32 * i;                 // rows of this word that are seen
-                        b[i] &= left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
+                        seen[i] &= left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
                     }
-#pragma unroll
-                    for (int i = 0; i < kTile; ++i) s[i] = b[i / 32] >> (i & 31) & 1u ? s[i] : -INFINITY;
                 }
-                float top[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top[i] = fmaxf(s[i], s[i + 4]);
-#pragma unroll
-                for (int i = 8; i < kTile; i += 8)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) top[e] = fmax3(top[e], s[i + e], s[i + 4 + e]);
-                const float z = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+                const float z = (part ? row_max<true>(S, seen) : row_max<false>(S, seen)) * a.scale_log2;
                 if (__any_sync(0xffffffffu, z > ref + kSlack)) {
                     const float now = fmaxf(ref, z), f = ex2_below(ref, now);
                     ref = now;
@@ -581,30 +655,21 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
                     }
                 }
                 const float minus = ref == -INFINITY ? 0.f : -ref;
-                const unsigned long long scale2 = pack2(a.scale_log2, a.scale_log2), minus2 = pack2(minus, minus);
-                unsigned long long acc[2] = {0ull, 0ull};
-#pragma unroll
-                for (int i = 0; i < kTile / 64; ++i) {
-                    uint32_t p[32];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        float u, v;
-                        unpack2(fma2(pack2(s[64 * i + 2 * e], s[64 * i + 2 * e + 1]), scale2, minus2), u, v);
-                        u = ex2_approx(u);
-                        v = ex2_approx(v);
-                        acc[e & 1] = add2(acc[e & 1], pack2(u, v));
-                        p[e] = pack_bf16(u, v);
-                    }
-                    tmem_st_x32(S + 32 * i, p);
+                // the first half's products begin while the second's weights are taken
+                auto ready = [&](int i) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(i == 0 ? &sm.p_half[half] : &sm.p_full[half]));
+                };
+                sum += part ? row_weights<true>(S, seen, a.scale_log2, minus, ready) : row_weights<false>(S, seen, a.scale_log2, minus, ready);
+            } else {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&sm.p_half[half]));
+                    mbar_arrive(smem_u32(&sm.p_full[half]));
                 }
-                float u, v;
-                unpack2(add2(acc[0], acc[1]), u, v);
-                sum += u + v;
-                tmem_st_wait();
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[half]));
         }
         if (tiles > 0) {
             if (!mbar_wait_warp(smem_u32(&sm.o_full[half]), o_phase, &sm.abort)) return;
@@ -794,6 +859,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
             mbar_init(smem_u32(&sm.q_full[i]), 1);
             mbar_init(smem_u32(&sm.q_empty[i]), 1);
             mbar_init(smem_u32(&sm.s_full[i]), 1);
+            mbar_init(smem_u32(&sm.p_half[i]), 4);
             mbar_init(smem_u32(&sm.p_full[i]), 4);
             mbar_init(smem_u32(&sm.o_full[i]), 1);
             mbar_init(smem_u32(&sm.o_empty[i]), 4);
@@ -815,12 +881,12 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sm.tmem;
-    // 384 threads of 168 registers: 256 * 208 + 128 * 88
+    // 384 threads of 168 registers, at least 256 * 184 + 128 * 128
     if (warp < 8) {
-        setmaxnreg_inc<208>();
+        setmaxnreg_inc<184>();
         softmax_rows<D>(a, sm, tmem, warp >> 2);
     } else {
-        setmaxnreg_dec<88>();
+        setmaxnreg_dec<128>();
         if (warp == 8) {
             hand_out(a, maps, sm, total, blockIdx.x, gridDim.x);
         } else if (warp == 9) {
