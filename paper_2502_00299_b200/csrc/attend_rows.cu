@@ -5,10 +5,11 @@
 //
 // A unit of work is a block of up to 256 query rows - tokens times the heads of a KV head's group, so that grouped heads share what is read - of one set
 // (a sequence, a prefix) and KV head, over the set's rows in tiles of 128. A CTA has 12 warps:
-//   0-3, 4-7   a row of 128 query rows a thread each: logits out of tensor memory, maximum, exponentials, sums, P back into tensor memory as bf16
+//   0-3, 4-7   a query row a thread, 128 each: 64 logits out of tensor memory, their maximum, exponentials and sum, and as bf16 back into tensor memory
 //   8          hands out the CTA's pieces of units and brings queries and keys into shared memory, by TMA, as the products read them
-//   9          the products (tcgen05, 128 x 128 x 16): S = Q K^T and O += P V, two blocks of 128 rows in turn, so that one's exponentials run beside
-//              the other's products
+//   9          the products (tcgen05, M = 128): S = Q K^T of 64 keys and O += P V. Each half has two such S, so that the next one's logits are there when the
+//              exponentials of one are taken, and neither waits for the other: with one S of 128 keys the rows wait for two products and the products for
+//              the rows, in turn (4096 tokens over 8192 rows: 440 us)
 //   10         brings the values
 //   11         looks through values that some of a block's tokens must not see
 // A copy takes an elected thread 23 clocks to issue, and 0.25 us a tile besides; two warps, for keys and values, bring a tile of both in 1100 clocks from pages
@@ -34,6 +35,8 @@ __device__ int g_gave_up;                             // a kernel abandoned a bo
 constexpr int kTile = 128;                            // rows of a tile of queries, keys or values
 constexpr int kBlock = 256;                           // query rows of a unit
 constexpr int kRowsThreads = 384;
+constexpr int kRowWarps = 8;                          // those with query rows
+constexpr int kSub = 64;                              // keys of one S
 constexpr int kPieces = 4;                            // pieces handed out ahead
 constexpr int kMasks = 8;                             // tiles whose masks are kept
 constexpr int kBegin = 1;                             // tiles that the beginning of a unit counts as
@@ -112,7 +115,7 @@ struct Share {
 // ------------------------------------------------------------------------------------------------ shared memory
 enum Leave { kOut, kWhole, kPart };
 struct Piece {
-    int tiles, tile0;        // tiles of this piece, the first; -1: no more pieces
+    int tiles, tile0, subs;  // tiles of this piece (-1: no more pieces), the first, and how many 64 keys they hold
     int kind, set, h, t0, g0, heads, rows;
     int limit, step, keys;
     int stage;               // 0, 1: at most 128 rows, on that half of the CTA; 2: both halves
@@ -126,11 +129,9 @@ struct RowsSmem {
     alignas(1024) unsigned char q[D / 64][kBlock][128];   // panels of 64 dims; 128 rows a half of the CTA
     alignas(1024) unsigned char kv[kSlots][kTileBytes];   // panels of 64 dims
     Piece piece[kPieces];
-    uint32_t first_bad[kPieces][D / 2];               // of each dim, the first such row (16 bits of it: two dims a word), from the first tile with any
-    int4 box[2][kTile / 4];                           // where rows of a tile of keys, or of values, are in the cache
     uint32_t mask[kMasks][4];                         // rows of a tile of keys that are there
     unsigned long long kv_full[kSlots], kv_empty[kSlots];
-    unsigned long long q_full[2], q_empty[2], s_full[2], p_half[2], p_full[2], o_full[2], o_empty[2];
+    unsigned long long q_full[2], q_empty[2], s_full[2][2], p_full[2][2], o_empty[2];
     unsigned long long piece_full[kPieces], piece_empty[kPieces], mask_full[kMasks], scan, scanned, drained;
     int warp_sum[kRowsThreads / 32], first_unit, first_at;
     int abort;
@@ -167,13 +168,8 @@ __device__ __forceinline__ uint64_t umma_desc_values(uint32_t at) {
 }
 constexpr uint32_t kColumnsSideBySide = 1u << 16;     // in an instruction's descriptor: of the second operand
 
-__device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[16]) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]),
-                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
-                 "r"(r[15]), "r"(taddr)
-                 : "memory");
-}
-__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const float (&v)[32]) {
+    const uint32_t* r = reinterpret_cast<const uint32_t*>(v);
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
         "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
@@ -233,28 +229,27 @@ __device__ __forceinline__ void load_tile(const AttendRowsArgs& a, RowsSmem<D>& 
     const int nowhere = a.cache.num_pages * a.cache.page_size;         // behind the last row: zeros
     const bool any = at.x >= 0 || at.y >= 0 || at.z >= 0 || at.w >= 0;
     const uint32_t take = __ballot_sync(0xffffffffu, lane < boxes && (values || any));
-    int4* box = sm.box[values];
-    box[lane] = make_int4(at.x < 0 ? nowhere : at.x, at.y < 0 ? nowhere : at.y, at.z < 0 ? nowhere : at.z, at.w < 0 ? nowhere : at.w);
-    __syncwarp();
+    const int4 row = make_int4(at.x < 0 ? nowhere : at.x, at.y < 0 ? nowhere : at.y, at.z < 0 ? nowhere : at.z, at.w < 0 ? nowhere : at.w);
     const uint32_t bar = smem_u32(&sm.kv_full[slot]), to = smem_u32(sm.kv[slot]);
-    if (elect_one()) {
-        mbar_arrive_expect_tx(bar, __popc(take) * rows * (D * 2));
-        if (a.box > 0) {
+    const bool leader = elect_one();
+    if (leader) mbar_arrive_expect_tx(bar, __popc(take) * rows * (D * 2));
+    if (a.box > 0) {
 #pragma unroll 4
-            for (int i = 0; i < boxes; ++i) {
-                if (take >> i & 1u) {
+        for (int i = 0; i < boxes; ++i) {
+            const int r = __shfl_sync(0xffffffffu, row.x, i);
+            if (leader && (take >> i & 1u)) {
 #pragma unroll
-                    for (int p = 0; p < D / 64; ++p) copy_rows(to + p * kPanelBytes + i * rows * 128, map, bar, x + 64 * p, box[i].x);
-                }
+                for (int p = 0; p < D / 64; ++p) copy_rows(to + p * kPanelBytes + i * rows * 128, map, bar, x + 64 * p, r);
             }
-        } else {
+        }
+    } else {
 #pragma unroll 4
-            for (int i = 0; i < boxes; ++i) {
-                const int row[4] = {box[i].x, box[i].y, box[i].z, box[i].w};
-                if (take >> i & 1u) {
+        for (int i = 0; i < boxes; ++i) {
+            const int r[4] = {__shfl_sync(0xffffffffu, row.x, i), __shfl_sync(0xffffffffu, row.y, i), __shfl_sync(0xffffffffu, row.z, i),
+                              __shfl_sync(0xffffffffu, row.w, i)};
+            if (leader && (take >> i & 1u)) {
 #pragma unroll
-                    for (int p = 0; p < D / 64; ++p) gather_rows(to + p * kPanelBytes + i * 512, map, bar, x + 64 * p, row);
-                }
+                for (int p = 0; p < D / 64; ++p) gather_rows(to + p * kPanelBytes + i * 512, map, bar, x + 64 * p, r);
             }
         }
     }
@@ -359,16 +354,40 @@ __device__ void load_values(const AttendRowsArgs& a, const RowMaps& maps, RowsSm
 
 // A tile of values of which some of the block's tokens, or all, must not see every row: what is not finite there would reach them as 0 * inf. From the
 // first such row on it becomes zero, and each dim's first one is kept: who sees that row gets no number there. A warp.
-__device__ void lower(uint32_t* word, int upper, uint32_t to) {
-    uint32_t was = *reinterpret_cast<volatile uint32_t*>(word);
-    while ((was >> (16 * upper) & 0xffffu) > to) {
-        const uint32_t now = upper ? (was & 0xffffu) | to << 16 : (was & 0xffff0000u) | to, got = atomicCAS(word, was, now);
-        if (got == was) break;
-        was = got;
+template <int D, class Each>
+__device__ __forceinline__ void each_value(unsigned char* tile, int row0, Each each) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int p = 0; p < D / 64; ++p) {
+#pragma unroll 4
+        for (int row = row0 + (lane >> 3); row < kTile; row += 4)
+            each(reinterpret_cast<uint4*>(tile + p * kPanelBytes + row * 128) + (lane & 7), row, 8 * ((lane & 7) ^ (row & 7)) + 64 * p);
     }
 }
 template <int D>
-__device__ void scan_values(RowsSmem<D>& sm) {
+__device__ __noinline__ void take_out(unsigned char* tile, int row0, int* first_bad, bool first, int row_of) {
+    if (first) {
+        for (int i = threadIdx.x & 31; i < D; i += 32) first_bad[i] = 0x7fffffff;
+        __threadfence_block();
+        __syncwarp();
+    }
+    each_value<D>(tile, row0, [&](uint4* at, int row, int dim) {
+        const uint4 v = *at;
+        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        bool bad = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if ((w[e / 2] >> (16 * (e & 1)) & 0x7f80u) == 0x7f80u) {
+                w[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+                atomicMin(&first_bad[dim + e], row_of + row);
+                bad = true;
+            }
+        if (bad) *at = make_uint4(w[0], w[1], w[2], w[3]);
+    });
+    __threadfence();
+}
+template <int D>
+__device__ void scan_values(const AttendRowsArgs& a, RowsSmem<D>& sm) {
     const int lane = threadIdx.x & 31;
     Pieces<D> pc(sm);
     int n_kv = 0;
@@ -378,37 +397,27 @@ __device__ void scan_values(RowsSmem<D>& sm) {
         Piece& x = sm.piece[pc.at];
         const int tiles = x.tiles, tile0 = x.tile0, from = scan_from(x), first = x.step ? max(x.limit, 0) : x.keys;
         if (tiles < 0) return;
+        bool found = false;
         for (int t = max(from - tile0, 0); t < tiles; ++t) {
-            const int slot = (n_kv + 2 * t + 1) % RowsSmem<D>::kSlots;
+            unsigned char* tile = sm.kv[(n_kv + 2 * t + 1) % RowsSmem<D>::kSlots];
             if (!mbar_wait_warp(smem_u32(&sm.scan), phase, &sm.abort)) return;
             phase ^= 1u;
-            bool changed = false;
             const int row0 = max(first - (tile0 + t) * kTile, 0);
-#pragma unroll 1
-            for (int p = 0; p < D / 64; ++p) {
-#pragma unroll 4
-                for (int row = row0 + (lane >> 3); row < kTile; row += 4) {
-                    uint4* at = reinterpret_cast<uint4*>(sm.kv[slot] + p * kPanelBytes + row * 128) + (lane & 7);
-                    const uint4 v = *at;
-                    uint32_t w[4] = {v.x, v.y, v.z, v.w}, bad = 0;
+            uint32_t bad = 0;
+            each_value<D>(tile, row0, [&](uint4* at, int, int) {
+                const uint4 v = *at;
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t y = ~w[e] & 0x7f807f80u;        // a half of zeros: all bits of its exponent are set
-                        bad |= (y - 0x00010001u) & ~y & 0x80008000u;
-                    }
-                    if (bad != 0) {
-                        const int dim = 8 * ((lane & 7) ^ (row & 7)) + 64 * p;
-                        for (int e = 0; e < 8; ++e)
-                            if ((w[e / 2] >> (16 * (e & 1)) & 0x7f80u) == 0x7f80u) {
-                                w[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
-                                lower(&sm.first_bad[pc.at][(dim + e) / 2], e & 1, (tile0 + t - from) * kTile + row);
-                            }
-                        *at = make_uint4(w[0], w[1], w[2], w[3]);
-                        changed = true;
-                    }
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t y = ~w[e] & 0x7f807f80u;            // a half of zeros: all bits of its exponent are set
+                    bad |= (y - 0x00010001u) & ~y & 0x80008000u;
                 }
+            });
+            if (__any_sync(0xffffffffu, bad != 0)) {
+                take_out<D>(tile, row0, a.first_bad + (static_cast<size_t>(blockIdx.x) * kPieces + pc.at) * D, !found, (tile0 + t - from) * kTile);
+                found = true;
+                *reinterpret_cast<volatile int*>(&x.found) = 1;
             }
-            if (changed) *reinterpret_cast<volatile int*>(&x.found) = 1;
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sm.scanned));
@@ -425,7 +434,7 @@ __device__ void scan_values(RowsSmem<D>& sm) {
 template <int D>
 __device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
     using Smem = RowsSmem<D>;
-    constexpr uint32_t kS = umma_idesc_bf16(kTile, kTile), kO = umma_idesc_bf16(kTile, D) | kColumnsSideBySide;
+    constexpr uint32_t kS = umma_idesc_bf16(kTile, kSub), kO = umma_idesc_bf16(kTile, D) | kColumnsSideBySide;
     Pieces<D> pc(sm);
     int slot = 0;
     uint32_t kv_phase = 0, q_phase = 0, p_phase = 0, scan_phase = 0, o_phase = 3;      // (a bit a half; nothing has to be read out of O first)
@@ -435,22 +444,23 @@ __device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
     auto advance = [&] {
         if (++slot == Smem::kSlots) { slot = 0; kv_phase ^= 1u; }
     };
-    auto logits = [&](int half, int s) {
-        const uint64_t k = kv_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4), q = q_desc0 + static_cast<uint64_t>(half) * (kPanelBytes >> 4);
+    // S[sub] of a half, by the first or second 64 keys of the tile in slot s
+    auto logits = [&](int half, int s, int sub) {
+        const uint64_t k = kv_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4) + sub * (kSub * 128 >> 4), q = q_desc0 + static_cast<uint64_t>(half) * (kPanelBytes >> 4);
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
-            umma_bf16(tmem + half * kTile, q + (i / 4) * (2 * kPanelBytes >> 4) + (i % 4) * 2, k + (i / 4) * (kPanelBytes >> 4) + (i % 4) * 2, kS, i > 0);
-        umma_commit(smem_u32(&sm.s_full[half]));
+            umma_bf16(tmem + half * kTile + sub * kSub, q + (i / 4) * (2 * kPanelBytes >> 4) + (i % 4) * 2, k + (i / 4) * (kPanelBytes >> 4) + (i % 4) * 2, kS, i > 0);
     };
-    auto values = [&](int half, int s, int part, bool more) {          // by the weights of the tile's first or second 64 rows
-        const uint64_t v = v_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4) + part * (64 * 128 >> 4);
+    auto values = [&](int half, int s, int sub, bool more) {
+        const uint64_t v = v_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4) + sub * (kSub * 128 >> 4);
 #pragma unroll
-        for (int i = 0; i < kTile / 32; ++i)
-            umma_bf16_ts(tmem + 2 * kTile + half * D, tmem + half * kTile + part * 32 + i * 8, v + i * (2048 >> 4), kO, more || i > 0);
+        for (int i = 0; i < kSub / 16; ++i)
+            umma_bf16_ts(tmem + 2 * kTile + half * D, tmem + half * kTile + sub * kSub + i * 8, v + i * (2048 >> 4), kO, more || i > 0);
     };
     for (;; pc.next()) {
         if (!pc.wait()) return;
-        const int tiles = sm.piece[pc.at].tiles, stage = sm.piece[pc.at].stage, scan = scan_from(sm.piece[pc.at]) - sm.piece[pc.at].tile0;
+        const int tiles = sm.piece[pc.at].tiles, subs = sm.piece[pc.at].subs, stage = sm.piece[pc.at].stage;
+        const int scan = scan_from(sm.piece[pc.at]) - sm.piece[pc.at].tile0;
         __syncwarp();
         if (elect_one()) mbar_arrive(smem_u32(&sm.piece_empty[pc.at]));
         if (tiles < 0) return;
@@ -463,53 +473,57 @@ __device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
         if (!wait(sm.kv_full[slot], kv_phase)) return;
         tc_fence_after();
         if (elect_one()) {
-            for (int h = h0; h < h1; ++h) {
-                logits(h, slot);
-                if (tiles == 1) umma_commit(smem_u32(&sm.q_empty[h]));
-            }
+            for (int sub = 0; sub < 2 && sub < subs; ++sub)
+                for (int h = h0; h < h1; ++h) {
+                    logits(h, slot, sub);
+                    umma_commit(smem_u32(&sm.s_full[h][sub]));
+                }
             umma_commit(smem_u32(&sm.kv_empty[slot]));
+            if (subs <= 2)
+                for (int h = h0; h < h1; ++h) umma_commit(smem_u32(&sm.q_empty[h]));
         }
         __syncwarp();
         advance();
-        for (int t = 0; t < tiles; ++t) {
-            const int v_slot = slot;
-            if (!wait(sm.kv_full[slot], kv_phase)) return;
-            if (t >= scan && elect_one()) mbar_arrive(smem_u32(&sm.scan));     // (while the exponentials of this tile are taken)
-            __syncwarp();
-            advance();
-            const int k_slot = slot;
-            const uint32_t k_phase = kv_phase;
-            const bool last = t + 1 == tiles;
-            if (!last) advance();
-            for (int h = h0; h < h1; ++h) {
-                if (t == 0) {
-                    if (!wait(sm.o_empty[h], o_phase >> h & 1u)) return;
-                    o_phase ^= 1u << h;
+        int v_slot = 0, k_slot = 0;
+        for (int u = 0; u < subs; ++u) {
+            const int sub = u & 1, t = u >> 1;
+            const bool more = u + 2 < subs;                            // there is a next S for this one's place
+            uint32_t k_phase = 0;
+            if (sub == 0) {
+                if (!wait(sm.kv_full[slot], kv_phase)) return;
+                if (t >= scan) {
+                    if (elect_one()) mbar_arrive(smem_u32(&sm.scan));  // (while the exponentials of this tile are taken)
+                    __syncwarp();
                 }
-                if (t >= scan && h == h0) {
+                v_slot = slot;
+                advance();
+                if (more) {
+                    k_slot = slot;
+                    k_phase = kv_phase;
+                    advance();
+                }
+                if (t >= scan) {
                     if (!wait(sm.scanned, scan_phase)) return;
                     scan_phase ^= 1u;
                 }
-                if (!wait(sm.p_half[h], p_phase >> h & 1u)) return;
-                tc_fence_after();
-                if (elect_one()) values(h, v_slot, 0, t > 0);
-                __syncwarp();
-                if (!wait(sm.p_full[h], p_phase >> h & 1u)) return;
-                p_phase ^= 1u << h;
-                if (!last && h == h0 && !wait(sm.kv_full[k_slot], k_phase)) return;
+                if (more && !wait(sm.kv_full[k_slot], k_phase)) return;
+            }
+            for (int h = h0; h < h1; ++h) {
+                if (u == 0) {
+                    if (!wait(sm.o_empty[h], o_phase >> h & 1u)) return;
+                    o_phase ^= 1u << h;
+                }
+                if (!wait(sm.p_full[h][sub], p_phase >> (2 * h + sub) & 1u)) return;
+                p_phase ^= 1u << (2 * h + sub);
                 tc_fence_after();
                 if (elect_one()) {
-                    values(h, v_slot, 1, true);
-                    if (last) {
-                        umma_commit(smem_u32(&sm.o_full[h]));
-                    } else {
-                        logits(h, k_slot);
-                        if (t + 2 == tiles) umma_commit(smem_u32(&sm.q_empty[h]));
-                    }
-                    if (h + 1 == h1) {
-                        umma_commit(smem_u32(&sm.kv_empty[v_slot]));
-                        if (!last) umma_commit(smem_u32(&sm.kv_empty[k_slot]));
-                    }
+                    values(h, v_slot, sub, u > 0);
+                    if (more) logits(h, k_slot, sub);
+                    // (also where no S comes any more: it says that these values have been added)
+                    umma_commit(smem_u32(&sm.s_full[h][sub]));
+                    if (u + 3 == subs) umma_commit(smem_u32(&sm.q_empty[h]));
+                    if (h + 1 == h1 && (sub == 1 || u + 1 == subs)) umma_commit(smem_u32(&sm.kv_empty[v_slot]));
+                    if (h + 1 == h1 && more && (sub == 1 || u + 3 == subs)) umma_commit(smem_u32(&sm.kv_empty[k_slot]));
                 }
                 __syncwarp();
             }
@@ -518,91 +532,36 @@ __device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
 }
 
 // ------------------------------------------------------------------------------------------------ the softmax, a row a thread
-// The row's logits pass twice, 32 at a time, the next ones on their way out of tensor memory while these are worked on: for their maximum, and for the
-// weights. (All 128 in registers take fewer instructions and are slower: what is run once a tile, 20 KB of it, has to be fetched anew every time.) PART:
-// a bit of `seen` says whether a logit counts.
+// PART: a bit of `seen` says whether a logit counts.
 template <bool PART>
-__device__ __forceinline__ float masked(float s, uint32_t seen, int i) { return !PART || (seen >> i & 1u) ? s : -INFINITY; }
-template <bool PART>
-__device__ __forceinline__ float max_of(const float (&s)[32], uint32_t seen, float top) {
+__device__ __forceinline__ float row_max(float (&s)[kSub], const uint32_t (&seen)[2]) {
+    if constexpr (PART) {
+#pragma unroll
+        for (int i = 0; i < kSub; ++i) s[i] = seen[i / 32] >> (i & 31) & 1u ? s[i] : -INFINITY;
+    }
     float x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = fmaxf(masked<PART>(s[i], seen, i), masked<PART>(s[i + 4], seen, i + 4));
+    for (int i = 0; i < 4; ++i) x[i] = fmaxf(s[i], s[i + 4]);
 #pragma unroll
-    for (int i = 8; i < 32; i += 8)
+    for (int i = 8; i < kSub; i += 8)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = fmax3(x[e], masked<PART>(s[i + e], seen, i + e), masked<PART>(s[i + 4 + e], seen, i + 4 + e));
-    return fmax3(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]), top);
-}
-template <bool PART>
-__device__ __forceinline__ float row_max(uint32_t S, const uint32_t (&seen)[4]) {
-    float a[32], b[32], top = -INFINITY;
-    tmem_ld_x32(S, a);
-#pragma unroll 1
-    for (int i = 0; i < 2; ++i) {
-        tmem_ld_wait();
-        tmem_ld_x32(S + 64 * i + 32, b);
-        top = max_of<PART>(a, i == 0 ? seen[0] : seen[2], top);
-        tmem_ld_wait();
-        if (i == 0) tmem_ld_x32(S + 64, a);
-        top = max_of<PART>(b, i == 0 ? seen[1] : seen[3], top);
-    }
-    return top;
-}
-// 2^(s scale + minus) of 32 logits, as bf16, and added up.
-template <bool PART>
-__device__ __forceinline__ void weights_of(const float (&s)[32], uint32_t seen, uint32_t (&p)[16], unsigned long long scale2, unsigned long long minus2,
-                                           unsigned long long (&acc)[2]) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        unsigned long long x = fma2(pack2(masked<PART>(s[2 * e], seen, 2 * e), masked<PART>(s[2 * e + 1], seen, 2 * e + 1)), scale2, minus2);
-        float u, v;
-        unpack2(x, u, v);
-        u = ex2_approx(u);
-        v = ex2_approx(v);
-        x = pack2(u, v);
-        acc[e & 1] = add2(acc[e & 1], x);
-        p[e] = pack_bf16(u, v);
-    }
-}
-// A row's weights into the place of its logits; half(0), half(1) when those of the first and the second 64 are there. Their sum.
-template <bool PART, class Half>
-__device__ __forceinline__ float row_weights(uint32_t S, const uint32_t (&seen)[4], float scale, float minus, Half half) {
-    const unsigned long long scale2 = pack2(scale, scale), minus2 = pack2(minus, minus);
-    unsigned long long acc[2] = {0ull, 0ull};
-    float a[32], b[32];
-    uint32_t p[16];
-    tmem_ld_x32(S, a);
-#pragma unroll 1
-    for (int i = 0; i < 2; ++i) {
-        tmem_ld_wait();
-        tmem_ld_x32(S + 64 * i + 32, b);
-        weights_of<PART>(a, i == 0 ? seen[0] : seen[2], p, scale2, minus2, acc);
-        tmem_ld_wait();
-        if (i == 0) tmem_ld_x32(S + 64, a);
-        tmem_st_x16(S + 32 * i, p);                                    // (behind the loads of the logits that stood there)
-        weights_of<PART>(b, i == 0 ? seen[1] : seen[3], p, scale2, minus2, acc);
-        tmem_st_x16(S + 32 * i + 16, p);
-        tmem_st_wait();
-        half(i);
-    }
-    float u, v;
-    unpack2(add2(acc[0], acc[1]), u, v);
-    return u + v;
+        for (int e = 0; e < 4; ++e) x[e] = fmax3(x[e], s[i + e], s[i + 4 + e]);
+    return fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
 }
 
 template <int D>
 __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t tmem, int half) {
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5 & 3;
     const uint32_t mine = static_cast<uint32_t>(w * 32) << 16;         // this warp's lanes of tensor memory
-    const uint32_t S = tmem + half * kTile + mine, O = tmem + 2 * kTile + half * D + mine;
+    const uint32_t O = tmem + 2 * kTile + half * D + mine;
     Pieces<D> pc(sm);
     int n_tile = 0;
-    uint32_t s_phase = 0, o_phase = 0;
+    uint32_t s_phase = 0;                                              // (a bit for each S)
+    auto wait = [&](int sub) { return mbar_wait_warp(smem_u32(&sm.s_full[half][sub]), s_phase >> sub & 1u, &sm.abort); };
     for (;; pc.next()) {
         if (!pc.wait()) return;
         const Piece& x = sm.piece[pc.at];
-        const int tiles = x.tiles;
+        const int tiles = x.tiles, subs = x.subs;
         if (tiles < 0) return;
         if (x.stage != 2 && x.stage != half) {
             n_tile += tiles;
@@ -614,35 +573,43 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
         const bool any = row0 < x.rows;                                // (of this warp)
         const int tok = row / x.heads, limit = x.limit + x.step * tok;
         const int least = x.limit + x.step * (row0 / x.heads);         // what the warp's first row sees: the least of its rows
-        const int tile0 = x.tile0;
+        const int first = x.tile0 * kTile;
         float ref = -INFINITY, sum = 0.f;
-        for (int t = 0; t < tiles; ++t, ++n_tile) {
-            uint4 m = make_uint4(0u, 0u, 0u, 0u);
+        for (int u = 0; u < subs; ++u) {
+            const int sub = u & 1, n = (n_tile + (u >> 1)) % kMasks;
+            uint2 m = make_uint2(0u, 0u);
             if (any) {
-                if (!mbar_wait_warp(smem_u32(&sm.mask_full[n_tile % kMasks]), n_tile / kMasks & 1, &sm.abort)) return;
-                m = *reinterpret_cast<const uint4*>(sm.mask[n_tile % kMasks]);
+                if (!mbar_wait_warp(smem_u32(&sm.mask_full[n]), (n_tile + (u >> 1)) / kMasks & 1, &sm.abort)) return;
+                m = *reinterpret_cast<const uint2*>(&sm.mask[n][2 * sub]);
             }
-            if (!mbar_wait_warp(smem_u32(&sm.s_full[half]), s_phase, &sm.abort)) return;
-            s_phase ^= 1u;
+            if (!wait(sub)) return;
+            s_phase ^= 1u << sub;
             tc_fence_after();
             if (any) {
-                const int see = limit - (tile0 + t) * kTile;
-                const bool part = (m.x & m.y & m.z & m.w) != 0xffffffffu || least < (tile0 + t + 1) * kTile;
-                uint32_t seen[4] = {m.x, m.y, m.z, m.w};
+                const uint32_t S = tmem + half * kTile + sub * kSub + mine;
+                float s[kSub];
+                tmem_ld_x32(S, s);
+                tmem_ld_x32(S + 32, s + 32);
+                const int base = first + u * kSub;
+                uint32_t seen[2] = {m.x, m.y};
+                const bool part = (m.x & m.y) != 0xffffffffu || least < base + kSub;
                 if (part) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int left = see - 32 * i;                 // rows of this word that are seen
+                    for (int i = 0; i < 2; ++i) {
+                        const int left = limit - base - 32 * i;        // rows of this word that are seen
                         seen[i] &= left >= 32 ? 0xffffffffu : left <= 0 ? 0u : (1u << left) - 1u;
                     }
                 }
-                const float z = (part ? row_max<true>(S, seen) : row_max<false>(S, seen)) * a.scale_log2;
+                tmem_ld_wait();
+                const float z = (part ? row_max<true>(s, seen) : row_max<false>(s, seen)) * a.scale_log2;
                 if (__any_sync(0xffffffffu, z > ref + kSlack)) {
                     const float now = fmaxf(ref, z), f = ex2_below(ref, now);
                     ref = now;
                     sum *= f;
-                    if (t > 0) {
-                        // (S is there, so the products issued before it, O's latest among them, are done, and the next wait for P)
+                    if (u > 0) {
+                        // (the other S is said to be there behind the last products that O took; the next wait for this P)
+                        if (!wait(sub ^ 1)) return;
+                        tc_fence_after();
 #pragma unroll 1
                         for (int i = 0; i < D; i += 32) {
                             float o[32];
@@ -650,38 +617,48 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
                             tmem_ld_wait();
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] *= f;
-                            tmem_st_x32(O + i, reinterpret_cast<const uint32_t*>(o));
+                            tmem_st_x32(O + i, o);
                         }
                     }
                 }
+                // weights 2^(s scale - reference), their sum, and as bf16 into the place of the logits
                 const float minus = ref == -INFINITY ? 0.f : -ref;
-                // the first half's products begin while the second's weights are taken
-                auto ready = [&](int i) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(i == 0 ? &sm.p_half[half] : &sm.p_full[half]));
-                };
-                sum += part ? row_weights<true>(S, seen, a.scale_log2, minus, ready) : row_weights<false>(S, seen, a.scale_log2, minus, ready);
-            } else {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(smem_u32(&sm.p_half[half]));
-                    mbar_arrive(smem_u32(&sm.p_full[half]));
+                const unsigned long long scale2 = pack2(a.scale_log2, a.scale_log2), minus2 = pack2(minus, minus);
+                unsigned long long acc[2] = {0ull, 0ull};
+                float p[kSub / 2];                                     // (pairs of bf16)
+#pragma unroll
+                for (int e = 0; e < kSub / 2; ++e) {
+                    float v0, v1;
+                    unpack2(fma2(pack2(s[2 * e], s[2 * e + 1]), scale2, minus2), v0, v1);
+                    v0 = ex2_approx(v0);
+                    v1 = ex2_approx(v1);
+                    acc[e & 1] = add2(acc[e & 1], pack2(v0, v1));
+                    p[e] = __uint_as_float(pack_bf16(v0, v1));
                 }
+                tmem_st_x32(S, p);
+                float v0, v1;
+                unpack2(add2(acc[0], acc[1]), v0, v1);
+                sum += v0 + v1;
+                tmem_st_wait();
             }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[half][sub]));
         }
-        if (tiles > 0) {
-            if (!mbar_wait_warp(smem_u32(&sm.o_full[half]), o_phase, &sm.abort)) return;
-            o_phase ^= 1u;
-            tc_fence_after();
+        n_tile += tiles;
+        // the last products of either S have been added
+        for (int sub = 0; sub < 2 && sub < subs; ++sub) {
+            if (!wait(sub)) return;
+            s_phase ^= 1u << sub;
         }
+        tc_fence_after();
         if (any) {
             const bool there = row < x.rows;
             const int g = row - tok * x.heads;
             const int token = x.t0 + tok, q = x.h * a.G + x.g0 + g;
             const int slot = x.slot, leave = x.leave;
             const bool found = *reinterpret_cast<const volatile int*>(&x.found) != 0;
+            const int* first_bad = a.first_bad + (static_cast<size_t>(blockIdx.x) * kPieces + pc.at) * D;
             const int bad_from = scan_from(x) * kTile;
             // rows of all units of a kind, and this one among them
             const size_t all = static_cast<size_t>(a.T) * a.Hq, whole = static_cast<size_t>(x.h) * a.T * a.G + static_cast<size_t>(token) * a.G + x.g0 + g;
@@ -697,10 +674,8 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
                 }
                 if (found) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const int first = *reinterpret_cast<const volatile uint32_t*>(&sm.first_bad[pc.at][(i + e) / 2]) >> (16 * (e & 1)) & 0xffff;
-                        if (first < limit - bad_from) o[e] = __int_as_float(0x7fffffff);
-                    }
+                    for (int e = 0; e < 32; ++e)
+                        if (*const_cast<const volatile int*>(first_bad + i + e) < limit - bad_from) o[e] = __int_as_float(0x7fffffff);
                 }
                 if (leave == kOut) {
                     if (there) {
@@ -778,7 +753,6 @@ __device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<
     uint32_t phase = 1;                                                // (the first round's entries are free)
     auto publish = [&](bool fill, const Piece& x) {
         if (!mbar_wait_warp(smem_u32(&sm.piece_empty[at]), phase, &sm.abort)) return false;
-        for (int i = lane; i < D / 2; i += 32) sm.first_bad[at][i] = 0xffffffffu;
         if (fill) sm.piece[at] = x;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sm.piece_full[at]));
@@ -809,6 +783,7 @@ __device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<
             Piece y;
             y.tile0 = max(p0 - kBegin, 0);
             y.tiles = max(p1 - kBegin, 0) - y.tile0;
+            y.subs = y.tiles > 0 ? (min(x.keys - y.tile0 * kTile, y.tiles * kTile) + kSub - 1) / kSub : 0;
             y.kind = x.kind; y.set = x.set; y.h = x.h; y.t0 = x.t0; y.g0 = x.g0; y.heads = x.heads; y.rows = x.rows();
             y.limit = x.limit; y.step = x.step; y.keys = x.keys;
             y.found = 0;
@@ -858,15 +833,15 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sm.q_full[i]), 1);
             mbar_init(smem_u32(&sm.q_empty[i]), 1);
-            mbar_init(smem_u32(&sm.s_full[i]), 1);
-            mbar_init(smem_u32(&sm.p_half[i]), 4);
-            mbar_init(smem_u32(&sm.p_full[i]), 4);
-            mbar_init(smem_u32(&sm.o_full[i]), 1);
+            for (int j = 0; j < 2; ++j) {
+                mbar_init(smem_u32(&sm.s_full[i][j]), 1);
+                mbar_init(smem_u32(&sm.p_full[i][j]), 4);
+            }
             mbar_init(smem_u32(&sm.o_empty[i]), 4);
         }
         for (int i = 0; i < kPieces; ++i) {
             mbar_init(smem_u32(&sm.piece_full[i]), 1);
-            mbar_init(smem_u32(&sm.piece_empty[i]), 11);               // warps of rows, and those that load, multiply and look through
+            mbar_init(smem_u32(&sm.piece_empty[i]), kRowWarps + 3);    // and those that load values, multiply and look through
         }
         for (int i = 0; i < kMasks; ++i) mbar_init(smem_u32(&sm.mask_full[i]), 1);
         mbar_init(smem_u32(&sm.scan), 1);
@@ -882,14 +857,14 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
     tc_fence_after();
     const uint32_t tmem = sm.tmem;
     // 384 threads of 168 registers, at least 256 * 184 + 128 * 128
-    if (warp < 8) {
+    if (warp < kRowWarps) {
         setmaxnreg_inc<184>();
         softmax_rows<D>(a, sm, tmem, warp >> 2);
     } else {
         setmaxnreg_dec<128>();
-        if (warp == 8) {
+        if (warp == kRowWarps) {
             hand_out(a, maps, sm, total, blockIdx.x, gridDim.x);
-        } else if (warp == 9) {
+        } else if (warp == kRowWarps + 1) {
             issue_products<D>(sm, tmem);
             if (elect_one()) {
                 umma_commit(smem_u32(&sm.drained));                    // (nothing is under way in tensor memory when it is given back)
@@ -897,10 +872,10 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
                 mbar_wait(smem_u32(&sm.drained), 0, &none);
             }
             __syncwarp();
-        } else if (warp == 10) {
+        } else if (warp == kRowWarps + 2) {
             load_values<D>(a, maps, sm);
         } else {
-            scan_values<D>(sm);
+            scan_values<D>(a, sm);
         }
     }
     tc_fence_before();
@@ -1054,7 +1029,8 @@ AttendRowsPlan attend_rows_plan(int T, int n, int Hq, int Hkv, int d, bool share
     const size_t rows = static_cast<size_t>(2) * kRowsCtas * p.record_rows, all = shared ? static_cast<size_t>(2) * T * Hq : 0;
     p.off_o = up256(rows * sizeof(float2));
     p.off_begun = up256(p.off_o + rows * d * sizeof(float));
-    p.off_owners = up256(p.off_begun + 2 * kRowsCtas * sizeof(int4));
+    p.off_bad = up256(p.off_begun + 2 * kRowsCtas * sizeof(int4));
+    p.off_owners = up256(p.off_bad + static_cast<size_t>(kRowsCtas) * kPieces * d * sizeof(int));
     p.off_whole_ml = up256(p.off_owners + (shared ? static_cast<size_t>(p.units) * sizeof(int2) : 0));
     p.off_whole_o = up256(p.off_whole_ml + all * sizeof(float2));
     p.bytes = up256(p.off_whole_o + all * d * sizeof(float));
@@ -1071,6 +1047,7 @@ cudaError_t launch_attend_rows(const AttendRowsArgs& args, const AttendRowsPlan&
     a.part_ml = reinterpret_cast<float2*>(scratch);
     a.part_o = reinterpret_cast<float4*>(scratch + plan.off_o);
     a.begun = reinterpret_cast<int4*>(scratch + plan.off_begun);
+    a.first_bad = reinterpret_cast<int*>(scratch + plan.off_bad);
     a.owners = reinterpret_cast<int2*>(scratch + plan.off_owners);
     a.whole_ml = reinterpret_cast<float2*>(scratch + plan.off_whole_ml);
     a.whole_o = reinterpret_cast<float4*>(scratch + plan.off_whole_o);

@@ -49,6 +49,7 @@ struct AttendRowsArgs {
     float2* part_ml;                          // [2 CTAs][record_rows] of units that several CTAs share: (reference, sum)
     float4* part_o;                           // [2 CTAs][d / 4][record_rows]
     int4* begun;                              // [CTAs][2]: the unit that a CTA begins and does not end
+    int* first_bad;                           // [CTAs][pieces][d]: of a piece's dims, the first row with a value that is not finite
     int2* owners;                             // [units]: first and last CTA (shared)
     float2* whole_ml;                         // [2][Hkv][T G] of units that one CTA has (shared)
     float4* whole_o;                          // [2][d / 4][Hkv][T G]
@@ -56,7 +57,7 @@ struct AttendRowsArgs {
 struct AttendRowsPlan {
     long long slots0, slots1, units;
     int heads, head_blocks, tokens, thin_tokens, record_rows;
-    size_t off_o, off_begun, off_owners, off_whole_ml, off_whole_o, bytes;
+    size_t off_o, off_begun, off_bad, off_owners, off_whole_ml, off_whole_o, bytes;
 };
 // T tokens in n sets; shared: T sequences in n groups.
 AttendRowsPlan attend_rows_plan(int T, int n, int Hq, int Hkv, int d, bool shared);
