@@ -152,19 +152,29 @@ struct Pieces {
     __device__ __forceinline__ bool wait() { return mbar_wait_warp(smem_u32(&sm.piece_full[at]), phase, &sm.abort); }
 };
 
-// P (bf16, in tensor memory) times a tile of values.
-__device__ __forceinline__ void umma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// A value that is the same for all lanes, and known to be.
+__device__ __forceinline__ int same(int v) { return __shfl_sync(0xffffffffu, v, 0); }
+
+// Descriptors of tiles in shared memory (ptx.cuh) with their upper halves apart, which are all alike: 8-row groups 1024 bytes apart, 128-byte swizzle. The
+// lower ones are added to in 32 bits, which halves what the products' warp has to execute.
+constexpr uint32_t kDescUpper = (1024 >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_lower(uint32_t at, uint32_t panels) { return (at & 0x3FFFFu) >> 4 | (panels >> 4) << 16; }
+// D (+)= A B^T, both in shared memory.
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint32_t a_lower, uint32_t b_lower, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_lower), "r"(b_lower), "r"(idesc), "r"(accumulate), "r"(kDescUpper)
         : "memory");
 }
-// Values as they lie, rows of 64 dims: the second operand with its columns (dims) side by side. 8-row groups are 1024 bytes apart, panels of 64 dims
-// kPanelBytes.
-__device__ __forceinline__ uint64_t umma_desc_values(uint32_t at) {
-    uint64_t d = umma_desc_sw128(at) & ~(0x3FFFull << 16);
-    return d | static_cast<uint64_t>(kPanelBytes >> 4) << 16;
+// P (bf16, in tensor memory) times a tile of values, as they lie: rows of 64 dims, the second operand with its columns (dims) side by side, panels of 64 dims
+// kPanelBytes apart.
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lower, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d_tmem), "r"(a_tmem), "r"(b_lower), "r"(idesc), "r"(accumulate), "r"(kDescUpper)
+        : "memory");
 }
 constexpr uint32_t kColumnsSideBySide = 1u << 16;     // in an instruction's descriptor: of the second operand
 
@@ -429,116 +439,135 @@ __device__ void scan_values(const AttendRowsArgs& a, RowsSmem<D>& sm) {
 }
 
 // ------------------------------------------------------------------------------------------------ the products
-// A whole warp, one elected thread of which issues: what the products take is then the same for all lanes, and known to be. (With the loop in one lane's
-// branch every operand goes through a lane's registers, in competition with the exponentials for the issue slots: 2400 clocks a tile more.)
+// A whole warp, one elected thread of which issues: what the products take is then the same for all lanes, and known to be. Little code, in one line for
+// both halves: what other warps of its quarter of the SM have pushed out of the instruction cache is fetched anew, 100 to 400 clocks in which the tensor
+// cores run dry. Waits that mostly lie behind it are tested together.
 template <int D>
-__device__ void issue_products(RowsSmem<D>& sm, uint32_t tmem) {
+struct Products {
     using Smem = RowsSmem<D>;
-    constexpr uint32_t kS = umma_idesc_bf16(kTile, kSub), kO = umma_idesc_bf16(kTile, D) | kColumnsSideBySide;
-    Pieces<D> pc(sm);
+    static constexpr uint32_t kS = umma_idesc_bf16(kTile, kSub), kO = umma_idesc_bf16(kTile, D) | kColumnsSideBySide;
+    Smem& sm;
+    const uint32_t tmem, q_desc, k_desc, v_desc;
     int slot = 0;
-    uint32_t kv_phase = 0, q_phase = 0, p_phase = 0, scan_phase = 0, o_phase = 3;      // (a bit a half; nothing has to be read out of O first)
-    volatile int* abort = &sm.abort;
-    const uint64_t q_desc0 = umma_desc_sw128(smem_u32(sm.q[0][0])), kv_desc0 = umma_desc_sw128(smem_u32(sm.kv[0])), v_desc0 = umma_desc_values(smem_u32(sm.kv[0]));
-    auto wait = [&](unsigned long long& bar, uint32_t phase) { return mbar_wait_warp(smem_u32(&bar), phase, abort); };
-    auto advance = [&] {
+    uint32_t kv_phase = 0, q_phase = 0, p_phase = 0, scan_phase = 0, o_phase = 3;      // (a bit a half, or 2 * half + S; nothing has to be read out of O first)
+    __device__ __forceinline__ Products(Smem& s, uint32_t t)
+        : sm(s), tmem(t), q_desc(desc_lower(smem_u32(s.q[0][0]), 16)), k_desc(desc_lower(smem_u32(s.kv[0]), 16)), v_desc(desc_lower(smem_u32(s.kv[0]), kPanelBytes)) {}
+    __device__ __forceinline__ bool wait(unsigned long long& bar, uint32_t phase) { return mbar_wait_warp(smem_u32(&bar), phase, &sm.abort); }
+    __device__ __forceinline__ void advance() {
         if (++slot == Smem::kSlots) { slot = 0; kv_phase ^= 1u; }
-    };
+    }
     // S[sub] of a half, by the first or second 64 keys of the tile in slot s
-    auto logits = [&](int half, int s, int sub) {
-        const uint64_t k = kv_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4) + sub * (kSub * 128 >> 4), q = q_desc0 + static_cast<uint64_t>(half) * (kPanelBytes >> 4);
+    __device__ __forceinline__ void logits(int half, int s, int sub) {
+        const uint32_t k = k_desc + s * (Smem::kTileBytes >> 4) + sub * (kSub * 128 >> 4), q = q_desc + half * (kPanelBytes >> 4), to = tmem + half * kTile + sub * kSub;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i)
-            umma_bf16(tmem + half * kTile + sub * kSub, q + (i / 4) * (2 * kPanelBytes >> 4) + (i % 4) * 2, k + (i / 4) * (kPanelBytes >> 4) + (i % 4) * 2, kS, i > 0);
-    };
-    auto values = [&](int half, int s, int sub, bool more) {
-        const uint64_t v = v_desc0 + static_cast<uint64_t>(s) * (Smem::kTileBytes >> 4) + sub * (kSub * 128 >> 4);
+        for (int i = 0; i < D / 16; ++i) umma_ss(to, q + (i / 4) * (2 * kPanelBytes >> 4) + (i % 4) * 2, k + (i / 4) * (kPanelBytes >> 4) + (i % 4) * 2, kS, i > 0);
+    }
+    __device__ __forceinline__ void values(int half, int s, int sub, bool more) {
+        const uint32_t v = v_desc + s * (Smem::kTileBytes >> 4) + sub * (kSub * 128 >> 4), p = tmem + half * kTile + sub * kSub, to = tmem + 2 * kTile + half * D;
 #pragma unroll
-        for (int i = 0; i < kSub / 16; ++i)
-            umma_bf16_ts(tmem + 2 * kTile + half * D, tmem + half * kTile + sub * kSub + i * 8, v + i * (2048 >> 4), kO, more || i > 0);
-    };
-    for (;; pc.next()) {
-        if (!pc.wait()) return;
-        const int tiles = sm.piece[pc.at].tiles, subs = sm.piece[pc.at].subs, stage = sm.piece[pc.at].stage;
-        const int scan = scan_from(sm.piece[pc.at]) - sm.piece[pc.at].tile0;
-        __syncwarp();
-        if (elect_one()) mbar_arrive(smem_u32(&sm.piece_empty[pc.at]));
-        if (tiles < 0) return;
-        if (tiles == 0) continue;
-        const int h0 = stage == 2 ? 0 : stage, h1 = stage == 2 ? 2 : stage + 1;
-        for (int h = h0; h < h1; ++h) {
-            if (!wait(sm.q_full[h], q_phase >> h & 1u)) return;
-            q_phase ^= 1u << h;
-        }
-        if (!wait(sm.kv_full[slot], kv_phase)) return;
+        for (int i = 0; i < kSub / 16; ++i) umma_ts(to, p + i * 8, v + i * (2048 >> 4), kO, more || i > 0);
+    }
+    // P of a half times values, and the next logits in its place. u: the 64 keys' number, of `subs`.
+    __device__ __forceinline__ void block(int half, int u, int subs, int v_slot, int k_slot, bool last_half) {
+        const int sub = u & 1;
+        const bool more = u + 2 < subs;                                // there is a next S for this one's place
         tc_fence_after();
         if (elect_one()) {
+            values(half, v_slot, sub, u > 0);
+            if (more) logits(half, k_slot, sub);
+            // (also where no S comes any more: it says that these values have been added)
+            umma_commit(smem_u32(&sm.s_full[half][sub]));
+            if (last_half && (sub == 1 || u + 1 == subs)) umma_commit(smem_u32(&sm.kv_empty[v_slot]));
+            if (last_half && more && (sub == 1 || u + 3 == subs)) umma_commit(smem_u32(&sm.kv_empty[k_slot]));
+            if (u + 3 == subs) umma_commit(smem_u32(&sm.q_empty[half]));
+        }
+        __syncwarp();
+    }
+    // WIDE: both halves; else `only`.
+    template <bool WIDE>
+    __device__ __forceinline__ bool piece(int subs, int scan, int only) {
+        const int h0 = WIDE ? 0 : only;
+        if (!wait(sm.q_full[h0], q_phase >> h0 & 1u)) return false;
+        q_phase ^= 1u << h0;
+        if (WIDE) {
+            if (!wait(sm.q_full[1], q_phase >> 1 & 1u)) return false;
+            q_phase ^= 2u;
+        }
+        if (!wait(sm.kv_full[slot], kv_phase)) return false;
+        tc_fence_after();
+        if (elect_one()) {
+#pragma unroll 1
             for (int sub = 0; sub < 2 && sub < subs; ++sub)
-                for (int h = h0; h < h1; ++h) {
+                for (int h = h0; h < (WIDE ? 2 : h0 + 1); ++h) {
                     logits(h, slot, sub);
                     umma_commit(smem_u32(&sm.s_full[h][sub]));
                 }
             umma_commit(smem_u32(&sm.kv_empty[slot]));
             if (subs <= 2)
-                for (int h = h0; h < h1; ++h) umma_commit(smem_u32(&sm.q_empty[h]));
+                for (int h = h0; h < (WIDE ? 2 : h0 + 1); ++h) umma_commit(smem_u32(&sm.q_empty[h]));
         }
         __syncwarp();
         advance();
+        if (!wait(sm.o_empty[h0], o_phase >> h0 & 1u)) return false;
+        o_phase ^= 1u << h0;
+        if (WIDE) {
+            if (!wait(sm.o_empty[1], o_phase >> 1 & 1u)) return false;
+            o_phase ^= 2u;
+        }
         int v_slot = 0, k_slot = 0;
+        uint32_t v_phase = 0, k_phase = 0;
+#pragma unroll 1
         for (int u = 0; u < subs; ++u) {
-            const int sub = u & 1, t = u >> 1;
-            const bool more = u + 2 < subs;                            // there is a next S for this one's place
-            uint32_t k_phase = 0;
-            if (sub == 0) {
-                if (!wait(sm.kv_full[slot], kv_phase)) return;
-                if (t >= scan) {
-                    if (elect_one()) mbar_arrive(smem_u32(&sm.scan));  // (while the exponentials of this tile are taken)
-                    __syncwarp();
-                }
-                v_slot = slot;
+            if ((u & 1) == 0) {
+                v_slot = k_slot = slot;                                // (no next tile: the values' once more, which is as well)
+                v_phase = k_phase = kv_phase;
                 advance();
-                if (more) {
+                if (u + 2 < subs) {
                     k_slot = slot;
                     k_phase = kv_phase;
                     advance();
                 }
-                if (t >= scan) {
-                    if (!wait(sm.scanned, scan_phase)) return;
+                if (__builtin_expect(u >= 2 * scan, 0)) {
+                    if (!wait(sm.kv_full[v_slot], v_phase)) return false;
+                    if (elect_one()) mbar_arrive(smem_u32(&sm.scan));  // (while the exponentials of this tile are taken)
+                    __syncwarp();
+                    if (!wait(sm.scanned, scan_phase)) return false;
                     scan_phase ^= 1u;
                 }
-                if (more && !wait(sm.kv_full[k_slot], k_phase)) return;
             }
-            for (int h = h0; h < h1; ++h) {
-                if (u == 0) {
-                    if (!wait(sm.o_empty[h], o_phase >> h & 1u)) return;
-                    o_phase ^= 1u << h;
-                }
-                if (!wait(sm.p_full[h][sub], p_phase >> (2 * h + sub) & 1u)) return;
-                p_phase ^= 1u << (2 * h + sub);
-                tc_fence_after();
-                if (elect_one()) {
-                    values(h, v_slot, sub, u > 0);
-                    if (more) logits(h, k_slot, sub);
-                    // (also where no S comes any more: it says that these values have been added)
-                    umma_commit(smem_u32(&sm.s_full[h][sub]));
-                    if (u + 3 == subs) umma_commit(smem_u32(&sm.q_empty[h]));
-                    if (h + 1 == h1 && (sub == 1 || u + 1 == subs)) umma_commit(smem_u32(&sm.kv_empty[v_slot]));
-                    if (h + 1 == h1 && more && (sub == 1 || u + 3 == subs)) umma_commit(smem_u32(&sm.kv_empty[k_slot]));
-                }
-                __syncwarp();
+            const int bit = 2 * h0 + (u & 1);
+            const bool v_in = mbar_try_wait(smem_u32(&sm.kv_full[v_slot]), v_phase), k_in = mbar_try_wait(smem_u32(&sm.kv_full[k_slot]), k_phase);
+            const bool p_in = mbar_try_wait(smem_u32(&sm.p_full[h0][u & 1]), p_phase >> bit & 1u);
+            if (__builtin_expect(!__all_sync(0xffffffffu, v_in && k_in && p_in), 0) &&
+                !(wait(sm.kv_full[v_slot], v_phase) && wait(sm.kv_full[k_slot], k_phase) && wait(sm.p_full[h0][u & 1], p_phase >> bit & 1u)))
+                return false;
+            p_phase ^= 1u << bit;
+            block(h0, u, subs, v_slot, k_slot, !WIDE);
+            if (WIDE) {
+                if (!wait(sm.p_full[1][u & 1], p_phase >> (2 + (u & 1)) & 1u)) return false;
+                p_phase ^= 4u << (u & 1);
+                block(1, u, subs, v_slot, k_slot, true);
             }
         }
+        return true;
     }
-}
+    __device__ __forceinline__ void run() {
+        Pieces<D> pc(sm);
+        for (;; pc.next()) {
+            if (!pc.wait()) return;
+            const int tiles = same(sm.piece[pc.at].tiles), subs = same(sm.piece[pc.at].subs), stage = same(sm.piece[pc.at].stage);
+            const int scan = same(scan_from(sm.piece[pc.at]) - sm.piece[pc.at].tile0);
+            __syncwarp();
+            if (elect_one()) mbar_arrive(smem_u32(&sm.piece_empty[pc.at]));
+            if (tiles < 0) return;
+            if (tiles == 0) continue;
+            if (!(stage == 2 ? piece<true>(subs, scan, 0) : piece<false>(subs, scan, stage))) return;
+        }
+    }
+};
 
 // ------------------------------------------------------------------------------------------------ the softmax, a row a thread
-// PART: a bit of `seen` says whether a logit counts.
-template <bool PART>
-__device__ __forceinline__ float row_max(float (&s)[kSub], const uint32_t (&seen)[2]) {
-    if constexpr (PART) {
-#pragma unroll
-        for (int i = 0; i < kSub; ++i) s[i] = seen[i / 32] >> (i & 31) & 1u ? s[i] : -INFINITY;
-    }
+__device__ __forceinline__ float row_max(const float (&s)[kSub]) {
     float x[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = fmaxf(s[i], s[i + 4]);
@@ -577,15 +606,13 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
         float ref = -INFINITY, sum = 0.f;
         for (int u = 0; u < subs; ++u) {
             const int sub = u & 1, n = (n_tile + (u >> 1)) % kMasks;
-            uint2 m = make_uint2(0u, 0u);
-            if (any) {
-                if (!mbar_wait_warp(smem_u32(&sm.mask_full[n]), (n_tile + (u >> 1)) / kMasks & 1, &sm.abort)) return;
-                m = *reinterpret_cast<const uint2*>(&sm.mask[n][2 * sub]);
-            }
-            if (!wait(sub)) return;
+            const uint32_t n_phase = (n_tile + (u >> 1)) / kMasks & 1;
+            const bool m_in = mbar_try_wait(smem_u32(&sm.mask_full[n]), n_phase), s_in = mbar_try_wait(smem_u32(&sm.s_full[half][sub]), s_phase >> sub & 1u);
+            if (__builtin_expect(!__all_sync(0xffffffffu, m_in && s_in), 0) && !(mbar_wait_warp(smem_u32(&sm.mask_full[n]), n_phase, &sm.abort) && wait(sub))) return;
+            const uint2 m = *reinterpret_cast<const uint2*>(&sm.mask[n][2 * sub]);
             s_phase ^= 1u << sub;
             tc_fence_after();
-            if (any) {
+            if (__builtin_expect(any, 1)) {
                 const uint32_t S = tmem + half * kTile + sub * kSub + mine;
                 float s[kSub];
                 tmem_ld_x32(S, s);
@@ -593,7 +620,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
                 const int base = first + u * kSub;
                 uint32_t seen[2] = {m.x, m.y};
                 const bool part = (m.x & m.y) != 0xffffffffu || least < base + kSub;
-                if (part) {
+                if (__builtin_expect(part, 0)) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int left = limit - base - 32 * i;        // rows of this word that are seen
@@ -601,8 +628,12 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
                     }
                 }
                 tmem_ld_wait();
-                const float z = (part ? row_max<true>(s, seen) : row_max<false>(s, seen)) * a.scale_log2;
-                if (__any_sync(0xffffffffu, z > ref + kSlack)) {
+                if (__builtin_expect(part, 0)) {
+#pragma unroll
+                    for (int i = 0; i < kSub; ++i) s[i] = seen[i / 32] >> (i & 31) & 1u ? s[i] : -INFINITY;
+                }
+                const float z = row_max(s) * a.scale_log2;
+                if (__builtin_expect(__any_sync(0xffffffffu, z > ref + kSlack), 0)) {
                     const float now = fmaxf(ref, z), f = ex2_below(ref, now);
                     ref = now;
                     sum *= f;
@@ -865,7 +896,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
         if (warp == kRowWarps) {
             hand_out(a, maps, sm, total, blockIdx.x, gridDim.x);
         } else if (warp == kRowWarps + 1) {
-            issue_products<D>(sm, tmem);
+            Products<D>(sm, same(tmem)).run();
             if (elect_one()) {
                 umma_commit(smem_u32(&sm.drained));                    // (nothing is under way in tensor memory when it is given back)
                 int none = 0;
