@@ -39,7 +39,7 @@ constexpr int kRowWarps = 8;                          // those with query rows
 constexpr int kSub = 64;                              // keys of one S
 constexpr int kPieces = 4;                            // pieces handed out ahead
 constexpr int kMasks = 8;                             // tiles whose masks are kept
-constexpr int kBegin = 1;                             // tiles that the beginning of a unit counts as
+constexpr int kBegin = 2;                             // tiles that the beginning of a unit counts as
 constexpr float kSlack = 8.f;
 constexpr int kPanelBytes = kTile * 128;              // 64 dims of 128 rows
 
@@ -452,7 +452,7 @@ struct Products {
     uint32_t kv_phase = 0, q_phase = 0, p_phase = 0, scan_phase = 0, o_phase = 3;      // (a bit a half, or 2 * half + S; nothing has to be read out of O first)
     __device__ __forceinline__ Products(Smem& s, uint32_t t)
         : sm(s), tmem(t), q_desc(desc_lower(smem_u32(s.q[0][0]), 16)), k_desc(desc_lower(smem_u32(s.kv[0]), 16)), v_desc(desc_lower(smem_u32(s.kv[0]), kPanelBytes)) {}
-    __device__ __forceinline__ bool wait(unsigned long long& bar, uint32_t phase) { return mbar_wait_warp(smem_u32(&bar), phase, &sm.abort); }
+    __device__ __forceinline__ bool wait(unsigned long long& bar, uint32_t phase) const { return mbar_wait_warp(smem_u32(&bar), phase, &sm.abort); }
     __device__ __forceinline__ void advance() {
         if (++slot == Smem::kSlots) { slot = 0; kv_phase ^= 1u; }
     }
@@ -468,18 +468,23 @@ struct Products {
         for (int i = 0; i < kSub / 16; ++i) umma_ts(to, p + i * 8, v + i * (2048 >> 4), kO, more || i > 0);
     }
     // P of a half times values, and the next logits in its place. u: the 64 keys' number, of `subs`.
-    __device__ __forceinline__ void block(int half, int u, int subs, int v_slot, int k_slot, bool last_half) {
+    template <bool WIDE>
+    __device__ __forceinline__ void block(int h0, int u, int subs, int v_slot, int k_slot) {
         const int sub = u & 1;
         const bool more = u + 2 < subs;                                // there is a next S for this one's place
         tc_fence_after();
         if (elect_one()) {
-            values(half, v_slot, sub, u > 0);
-            if (more) logits(half, k_slot, sub);
-            // (also where no S comes any more: it says that these values have been added)
-            umma_commit(smem_u32(&sm.s_full[half][sub]));
-            if (last_half && (sub == 1 || u + 1 == subs)) umma_commit(smem_u32(&sm.kv_empty[v_slot]));
-            if (last_half && more && (sub == 1 || u + 3 == subs)) umma_commit(smem_u32(&sm.kv_empty[k_slot]));
-            if (u + 3 == subs) umma_commit(smem_u32(&sm.q_empty[half]));
+#pragma unroll
+            for (int i = 0; i < (WIDE ? 2 : 1); ++i) {
+                const int half = WIDE ? i : h0;
+                values(half, v_slot, sub, u > 0);
+                if (more) logits(half, k_slot, sub);
+                // (also where no S comes any more: it says that these values have been added)
+                umma_commit(smem_u32(&sm.s_full[half][sub]));
+                if (u + 3 == subs) umma_commit(smem_u32(&sm.q_empty[half]));
+            }
+            if (sub == 1 || u + 1 == subs) umma_commit(smem_u32(&sm.kv_empty[v_slot]));
+            if (more && (sub == 1 || u + 3 == subs)) umma_commit(smem_u32(&sm.kv_empty[k_slot]));
         }
         __syncwarp();
     }
@@ -538,16 +543,13 @@ struct Products {
             const int bit = 2 * h0 + (u & 1);
             const bool v_in = mbar_try_wait(smem_u32(&sm.kv_full[v_slot]), v_phase), k_in = mbar_try_wait(smem_u32(&sm.kv_full[k_slot]), k_phase);
             const bool p_in = mbar_try_wait(smem_u32(&sm.p_full[h0][u & 1]), p_phase >> bit & 1u);
-            if (__builtin_expect(!__all_sync(0xffffffffu, v_in && k_in && p_in), 0) &&
-                !(wait(sm.kv_full[v_slot], v_phase) && wait(sm.kv_full[k_slot], k_phase) && wait(sm.p_full[h0][u & 1], p_phase >> bit & 1u)))
+            const bool p1_in = !WIDE || mbar_try_wait(smem_u32(&sm.p_full[1][u & 1]), p_phase >> (2 + (u & 1)) & 1u);
+            if (__builtin_expect(!__all_sync(0xffffffffu, v_in && k_in && p_in && p1_in), 0) &&
+                !(wait(sm.kv_full[v_slot], v_phase) && wait(sm.kv_full[k_slot], k_phase) && wait(sm.p_full[h0][u & 1], p_phase >> bit & 1u) &&
+                  (!WIDE || wait(sm.p_full[1][u & 1], p_phase >> (2 + (u & 1)) & 1u))))
                 return false;
-            p_phase ^= 1u << bit;
-            block(h0, u, subs, v_slot, k_slot, !WIDE);
-            if (WIDE) {
-                if (!wait(sm.p_full[1][u & 1], p_phase >> (2 + (u & 1)) & 1u)) return false;
-                p_phase ^= 4u << (u & 1);
-                block(1, u, subs, v_slot, k_slot, true);
-            }
+            p_phase ^= (WIDE ? 5u : 1u << (2 * h0)) << (u & 1);
+            block<WIDE>(h0, u, subs, v_slot, k_slot);
         }
         return true;
     }
@@ -920,97 +922,119 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
 }
 
 // ------------------------------------------------------------------------------------------------ joining
-// 32 rows a CTA, a lane each; the warps take the dims in fours in turn.
-constexpr int kJoinWarps = 8;
-
+// A CTA takes as many rows as leave four dims a thread, neighbouring rows in neighbouring lanes, as the records have them. The (reference, sum) of all records of a
+// row are read side by side by a warp, which leaves a factor for each; then every thread adds up its dims, with as many loads under way as there are records.
+constexpr int kJoinThreads = 256;
 template <int D>
-struct Joined {
-    static constexpr int kN = D / 4 / kJoinWarps;
-    float ref = -INFINITY, sum = 0.f;
-    float4 v[kN];
-    __device__ __forceinline__ Joined() {
-#pragma unroll
-        for (int i = 0; i < kN; ++i) v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    // A record's (reference, sum) and its values, `stride` apart from four dims to the next. (One that saw nothing has no values.)
-    __device__ __forceinline__ void add(float2 ml, const float4* o, size_t stride) {
-        if (ml.x == -INFINITY && ml.y == 0.f) return;
-        float4 x[kN];
-#pragma unroll
-        for (int i = 0; i < kN; ++i) x[i] = o[(threadIdx.x / 32 + i * kJoinWarps) * stride];
-        const float now = fmaxf(ref, ml.x), f = ex2_below(ref, now), g = ex2_below(ml.x, now);
-        ref = now;
-        sum = sum * f + ml.y * g;
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            v[i].x = v[i].x * f + x[i].x * g; v[i].y = v[i].y * f + x[i].y * g;
-            v[i].z = v[i].z * f + x[i].z * g; v[i].w = v[i].w * f + x[i].w * g;
-        }
-    }
-    __device__ __forceinline__ void write(__nv_bfloat16* out) const {
-        const float r = 1.f / sum;
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const float4 x = v[i];
-            const uint2 w = sum == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(x.x * r, x.y * r), pack_bf16(x.z * r, x.w * r));
-            *reinterpret_cast<uint2*>(out + 4 * (threadIdx.x / 32 + i * kJoinWarps)) = w;
-        }
-    }
+struct JoinSmem {
+    static constexpr int kRows = kJoinThreads * 4 / D;
+    int4 from[2][kRows];                               // first and last CTA (last < first: none), row of their records; 1: one CTA's that has the whole unit
+    float factor[2][kRows][kRowsCtas];                 // below 0: a record that saw nothing, and has no values
+    float sum[kRows];
 };
 
-template <int D>
-__device__ __forceinline__ void add_parts(const AttendRowsArgs& a, Joined<D>& j, int first, int last, int row) {
-#pragma unroll 2
-    for (int c = first; c <= last; ++c) {
-        const size_t slot = 2 * c + (c == first ? 1 : 0);
-        j.add(a.part_ml[slot * a.record_rows + row], a.part_o + slot * (D / 4) * a.record_rows + row, a.record_rows);
+template <int D, bool SHARED>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendRowsArgs a) {
+    using Smem = JoinSmem<D>;
+    constexpr int kRows = Smem::kRows, kSources = SHARED ? 2 : 1;
+    __shared__ Smem sm;
+    begin_dependent();
+    const int tid = threadIdx.x, lane = tid & 31, rows = a.T * a.G;
+    const int chunks = SHARED ? (rows + kRows - 1) / kRows : (a.record_rows + kRows - 1) / kRows;
+    const int group = blockIdx.x / chunks, row0 = (blockIdx.x - group * chunks) * kRows;       // a KV head, or the CTA that began a unit
+    int4 unit = make_int4(0, 0, 1, rows);              // first token, first head, heads, rows
+    int last = 0;
+    if constexpr (!SHARED) {
+        last = a.begun[2 * group + 1].w;
+        unit = a.begun[2 * group];
+        if (last < 0 || row0 >= unit.w) return;        // (the whole CTA)
     }
-}
-
-template <int D>
-__global__ void __launch_bounds__(32 * kJoinWarps) rows_join_kernel(const __grid_constant__ AttendRowsArgs a) {
-    begin_dependent();
-    const int chunks = a.record_rows / 32, cta = blockIdx.x / chunks, row = (blockIdx.x - cta * chunks) * 32 + (threadIdx.x & 31);
-    const int last = a.begun[2 * cta + 1].w;
-    if (last < 0) return;
-    const int4 u = a.begun[2 * cta];                                   // first token, first head, heads, rows
-    if (row >= u.w) return;
-    Joined<D> j;
-    add_parts(a, j, cta, last, row);
-    const int tok = row / u.z, g = row - tok * u.z;
-    j.write(a.out + (static_cast<size_t>(u.x + tok) * a.Hq + u.y + g) * D);
-}
-
-template <int D>
-__global__ void __launch_bounds__(32 * kJoinWarps) shared_join_kernel(const __grid_constant__ AttendRowsArgs a) {
-    begin_dependent();
-    const int rows = a.T * a.G, chunks = (rows + 31) / 32, h = blockIdx.x / chunks, i = (blockIdx.x - h * chunks) * 32 + (threadIdx.x & 31);
-    if (i >= rows) return;
-    const int b = i / a.G, g = i - b * a.G, hb = g / a.heads;
-    const size_t all = static_cast<size_t>(a.Hkv) * rows, mine = static_cast<size_t>(h) * rows + i;
-    Joined<D> j;
-    auto add_unit = [&](int u, int kind, int row) {
-        const int2 by = a.owners[u];
-        if (by.x < 0 || by.y < by.x || by.y >= kRowsCtas) return;       // (groups that are not ascending: no address out of range)
-        if (by.x == by.y) j.add(a.whole_ml[kind * all + mine], a.whole_o + kind * all * (D / 4) + mine, all);
-        else add_parts(a, j, by.x, by.y, row);
-    };
-    const RowSets &p = a.sets[0], &own = a.sets[1];
-    int group = 0;
-    {
-        int lo = 0, hi = p.n;                                          // how many groups end at or before this sequence
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (p.starts[mid + 1] <= b) lo = mid + 1; else hi = mid;
+    if (tid < kRows) {
+        const int i = row0 + tid;
+        int4 x[2] = {make_int4(0, -1, 0, 0), make_int4(0, -1, 0, 0)};
+        if (i < unit.w) {
+            if constexpr (SHARED) {
+                const int b = i / a.G, g = i - b * a.G, hb = g / a.heads;
+                auto put = [&](int kind, int u, int row) {
+                    const int2 by = a.owners[u];
+                    if (by.x >= 0 && by.y >= by.x && by.y < kRowsCtas) x[kind] = make_int4(by.x, by.y, row, by.x == by.y);     // (groups that are not ascending: no address out of range)
+                };
+                const RowSets &p = a.sets[0], &own = a.sets[1];
+                int lo = 0, hi = p.n;                  // how many groups end at or before this sequence
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (p.starts[mid + 1] <= b) lo = mid + 1; else hi = mid;
+                }
+                if (lo < p.n && p.starts[lo] <= b && p.starts[lo] >= 0) {
+                    const int k = b - p.starts[lo], blk = k / a.tokens;
+                    put(0, group * p.slots + (base_of(a, p, lo) + blk) * a.head_blocks + hb, (k - blk * a.tokens) * min(a.heads, a.G - hb * a.heads) + g - hb * a.heads);
+                }
+                put(1, p.slots * a.Hkv + group * own.slots + b * a.head_blocks + hb, g - hb * a.heads);
+            } else {
+                x[0] = make_int4(group, last, i, 0);
+            }
         }
-        group = lo;
+        sm.from[0][tid] = x[0];
+        sm.from[1][tid] = x[1];
     }
-    if (group < p.n && p.starts[group] <= b && p.starts[group] >= 0) {
-        const int k = b - p.starts[group], blk = k / a.tokens;
-        add_unit(h * p.slots + (base_of(a, p, group) + blk) * a.head_blocks + hb, 0, (k - blk * a.tokens) * min(a.heads, a.G - hb * a.heads) + g - hb * a.heads);
+    __syncthreads();
+    const size_t all = static_cast<size_t>(a.T) * a.Hq, head0 = static_cast<size_t>(group) * rows;      // (of the shared form's whole records)
+    for (int r = tid >> 5; r < kRows; r += kJoinThreads / 32) {
+        constexpr int kOwn = (kRowsCtas + 31) / 32;
+        float2 ml[kSources][kOwn];
+        float top = -INFINITY;
+#pragma unroll
+        for (int s = 0; s < kSources; ++s) {
+            const int4 x = sm.from[s][r];
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                const int c = x.x + lane + 32 * i;
+                ml[s][i] = make_float2(-INFINITY, 0.f);
+                if (c <= x.y) ml[s][i] = x.w ? a.whole_ml[s * all + head0 + row0 + r] : a.part_ml[static_cast<size_t>(2 * c + (c == x.x ? 1 : 0)) * a.record_rows + x.z];
+                top = fmaxf(top, ml[s][i].x);
+            }
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        float sum = 0.f;
+#pragma unroll
+        for (int s = 0; s < kSources; ++s) {
+            const int4 x = sm.from[s][r];
+#pragma unroll
+            for (int i = 0; i < kOwn; ++i) {
+                const float2 v = ml[s][i];
+                const float f = v.x == -INFINITY && v.y == 0.f ? -1.f : ex2_below(v.x, top);
+                if (x.x + lane + 32 * i <= x.y) sm.factor[s][r][lane + 32 * i] = f;
+                if (f != -1.f) sum += v.y * f;
+            }
+        }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        if (lane == 0) sm.sum[r] = sum;
     }
-    add_unit(p.slots * a.Hkv + h * own.slots + b * a.head_blocks + hb, 1, g - hb * a.heads);
-    j.write(a.out + (static_cast<size_t>(b) * a.Hq + static_cast<size_t>(h) * a.G + g) * D);
+    __syncthreads();
+    const int r = tid % kRows, c4 = tid / kRows, i = row0 + r;
+    if (i >= unit.w) return;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float f, const float4& y) {
+        if (f >= 0.f || f != f) { v.x = fmaf(y.x, f, v.x); v.y = fmaf(y.y, f, v.y); v.z = fmaf(y.z, f, v.z); v.w = fmaf(y.w, f, v.w); }
+    };
+#pragma unroll
+    for (int s = 0; s < kSources; ++s) {
+        const int4 x = sm.from[s][r];
+        if (SHARED && x.w) {
+            add(sm.factor[s][r][0], a.whole_o[(static_cast<size_t>(s) * (D / 4) + c4) * all + head0 + i]);
+            continue;
+        }
+        const float4* o = a.part_o + static_cast<size_t>(c4) * a.record_rows + x.z;
+        const size_t slot = static_cast<size_t>(D / 4) * a.record_rows;
+#pragma unroll 8
+        for (int c = x.x; c <= x.y; ++c) add(sm.factor[s][r][c - x.x], o[(2 * c + (c == x.x ? 1 : 0)) * slot]);
+    }
+    const float sum = sm.sum[r], inv = 1.f / sum;
+    const size_t row = SHARED ? static_cast<size_t>(i / a.G) * a.Hq + static_cast<size_t>(group) * a.G + i % a.G
+                              : static_cast<size_t>(unit.x + i / unit.z) * a.Hq + unit.y + i % unit.z;
+    *reinterpret_cast<uint2*>(a.out + row * D + 4 * c4) = sum == 0.f ? make_uint2(0u, 0u) : make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
 }
 
 size_t up256(size_t n) { return (n + 255) & ~static_cast<size_t>(255); }
@@ -1033,14 +1057,15 @@ cudaError_t launch(const AttendRowsArgs& a, const CUtensorMap* maps, int num_sms
     cfg.dynamicSmemBytes = smem;
     e = cudaLaunchKernelEx(&cfg, attend_rows_kernel<D>, RowMaps{maps[0], maps[1], maps[2], maps[3]}, a);
     if (e != cudaSuccess) return e;
-    cfg.blockDim = dim3(32 * kJoinWarps);
+    cfg.blockDim = dim3(kJoinThreads);
     cfg.dynamicSmemBytes = 0;
+    constexpr int rows = JoinSmem<D>::kRows;
     if (a.shared) {
-        cfg.gridDim = dim3(static_cast<unsigned>((a.T * a.G + 31) / 32 * a.Hkv));
-        return cudaLaunchKernelEx(&cfg, shared_join_kernel<D>, a);
+        cfg.gridDim = dim3(static_cast<unsigned>((a.T * a.G + rows - 1) / rows) * a.Hkv);
+        return cudaLaunchKernelEx(&cfg, join_kernel<D, true>, a);
     }
-    cfg.gridDim = dim3(static_cast<unsigned>(ctas * (a.record_rows / 32)));
-    return cudaLaunchKernelEx(&cfg, rows_join_kernel<D>, a);
+    cfg.gridDim = dim3(static_cast<unsigned>(ctas * ((a.record_rows + rows - 1) / rows)));
+    return cudaLaunchKernelEx(&cfg, join_kernel<D, false>, a);
 }
 
 }  // namespace
