@@ -418,3 +418,187 @@ def test_a_prefix_of_infinite_logits_leaves_the_own_rows():
     assert not out[1].any()
     k, v, _ = ora.rows_of(wide(K), wide(V), table[0], 70, 0)
     rows_bounds.check_rows(out[0], wide(q)[0], k, v, np.ones((4, 70), dtype=bool))
+
+
+# ------------------------------------------------------------------------------------------------ as they are used
+def turn_inputs(rng, Hq=8, Hkv=2, d=128, page=16, sizes=(40, 3, 130), before=(300, 7, 0), per=32):
+    """A batch of conversations in one cache, a turn's activations, and tables of angles."""
+    B = len(sizes)
+    starts = np.r_[0, np.cumsum(sizes)]
+    T = int(starts[-1])
+    K, V, table = paged(rng, B, Hkv, d, page, per)
+    lengths = np.array([[b + n for _ in range(Hkv)] for b, n in zip(before, sizes)])
+    x = rand_bits(rng, (T, (Hq + 2 * Hkv) * d))
+    pos = np.concatenate([b + np.arange(n) for b, n in zip(before, sizes)])
+    return starts, K, V, table, lengths, x, pos
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_a_turn_then_single_tokens_on_what_was_compressed(inter):
+    """Tables, rotated prompts, compressed into pages; a turn appended and attended to; then a token each, over a shared prefix as over one table."""
+    Hq, Hkv, d, page, L, w, c, budget = 8, 2, 128, 16, 1024, 16, 10, 256
+    rng = np.random.default_rng(41)
+    cos, sin = ck.rope_tables(2048, 64, 10000.0, "dims", 4.0, 512.0, 1.0, 32.0)
+    x = to_dev(rand_bits(rng, (L, (Hq + 2 * Hkv) * d)))
+    q, k = ck.rotate_rows(x, Hq, Hkv, d, cos, sin, i32(np.arange(L)), inter)
+    K, V = k.permute(1, 0, 2).contiguous(), x.view(L, Hq + 2 * Hkv, d)[:, Hq + Hkv:].permute(1, 0, 2).contiguous()
+    per, n = 24, 100
+    cK, cV = (torch.zeros(2 * per, page, Hkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = i32(rng.permutation(2 * per).reshape(2, per))
+    idx = ck.compress_layer_paged(q[L - w:].permute(1, 0, 2).contiguous(), K, V, Hq, w, c, budget, table[0], cK, cV)
+    kept = (idx >= 0).sum(1, dtype=torch.int32)
+    # a turn of n tokens
+    y = to_dev(rand_bits(rng, (n, (Hq + 2 * Hkv) * d)))
+    pos = i32(L + np.arange(n))
+    lengths = (kept + n)[None].contiguous()
+    starts = i32([0, n])
+    qt = ck.append_rows_paged(y, Hq, starts, cos, sin, pos, table[:1].contiguous(), lengths, cK, cV, inter)
+    out = ck.attend_rows_paged(qt, starts, table[:1].contiguous(), lengths, cK, cV)
+    args = values(qt), [0, n], values(cK), values(cV), table[:1].cpu().numpy(), lengths.cpu().numpy()
+    rows_bounds.check_attend(values(out), *args, True)
+    want, _ = ck.rotate_rows(y, Hq, Hkv, d, cos, sin, pos, inter)
+    assert torch.equal(want, qt)
+    # two sequences that share it, each with a token of its own, as rows of a second table
+    own = torch.stack([table[1, :8], table[1, 8:16]]).contiguous()
+    z = to_dev(rand_bits(rng, (2, (Hq + 2 * Hkv) * d)))
+    one = torch.ones(2, Hkv, dtype=torch.int32, device="cuda")
+    q1 = ck.append_rows_paged(z, Hq, i32([0, 1, 2]), cos, sin, i32([L + n] * 2), own, one, cK, cV, inter)
+    got = ck.attend_shared_paged(q1, i32([0, 2]), table[:1].contiguous(), lengths, own, one, cK, cV)
+    rows_bounds.check_shared(values(got), values(q1), [0, 2], values(cK), values(cV), table[:1].cpu().numpy(), lengths.cpu().numpy(), own.cpu().numpy(), np.ones((2, Hkv), int))
+
+
+def test_streams_graphs_and_calls_side_by_side():
+    """Two captured graphs and eager calls on other streams: nothing in common but the tensors given."""
+    rng = np.random.default_rng(42)
+    starts, K, V, table, lengths, x, pos = turn_inputs(rng)
+    Hq = 8
+    dK, dV, dt, dl, ds = to_dev(K), to_dev(V), i32(table), i32(lengths), i32(starts)
+    q = to_dev(rand_bits(rng, (int(starts[-1]), Hq, 128)))
+    qs = to_dev(rand_bits(rng, (3, Hq, 128)))
+    one = i32([0, 3])
+    want = ck.attend_rows_paged(q, ds, dt, dl, dK, dV)
+    want_s = ck.attend_shared_paged(qs, one, dt[:1].contiguous(), dl[:1].contiguous(), dt, dl, dK, dV)
+    graphs, outs = [], []
+    for kind in (0, 1):
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                o = ck.attend_rows_paged(q, ds, dt, dl, dK, dV) if kind == 0 else ck.attend_shared_paged(qs, one, dt[:1].contiguous(), dl[:1].contiguous(), dt, dl, dK, dV)
+        graphs.append((g, s))
+        outs.append(o)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for g, s in graphs:
+            with torch.cuda.stream(s):
+                g.replay()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        a = ck.attend_rows_paged(q, ds, dt, dl, dK, dV, stream=side)
+        b = ck.attend_shared_paged(qs, one, dt[:1].contiguous(), dl[:1].contiguous(), dt, dl, dK, dV)
+        torch.cuda.synchronize()
+        assert torch.equal(bits(outs[0]), bits(want)) and torch.equal(bits(outs[1]), bits(want_s)) and torch.equal(bits(a), bits(want)) and torch.equal(bits(b), bits(want_s))
+
+
+def test_calls_directly_behind_one_another():
+    """Appended rows, lengths and queries that the call ahead still writes, time after time, against calls one by one."""
+    rng = np.random.default_rng(43)
+    starts, K, V, table, lengths, x, pos = turn_inputs(rng)
+    cos, sin = (torch.tensor(t).cuda() for t in angles(rng, 512, 128))
+    dx, dp, dt, dl, ds = to_dev(x), i32(pos), i32(table), i32(lengths), i32(starts)
+    q0 = i32([0, 1, 2, 3])
+
+    def run(wait):
+        cK, cV = to_dev(K), to_dev(V)
+        res = []
+        for _ in range(6):
+            q = ck.append_rows_paged(dx, 8, ds, cos, sin, dp, dt, dl, cK, cV)
+            if wait:
+                torch.cuda.synchronize()
+            o = ck.attend_rows_paged(q, ds, dt, dl, cK, cV)
+            if wait:
+                torch.cuda.synchronize()
+            res += [ck.attend_shared_paged(o[:3].contiguous(), q0, dt, dl, dt, dl, cK, cV), ck.attend_paged(q[:3].contiguous(), dt, dl, cK, cV)]
+            if wait:
+                torch.cuda.synchronize()
+            dx.copy_(dx.roll(1, 0))
+        for _ in range(6):
+            dx.copy_(dx.roll(-1, 0))
+        torch.cuda.synchronize()
+        return res
+
+    for a, b in zip(run(True), run(False)):
+        assert torch.equal(bits(a), bits(b))
+
+
+def test_native_and_general_calls_agree(monkeypatch):
+    from paper_2502_00299_b200 import binding
+    rng = np.random.default_rng(44)
+    starts, K, V, table, lengths, x, pos = turn_inputs(rng)
+    cos, sin = (torch.tensor(t).cuda() for t in angles(rng, 512, 64))
+    q = to_dev(rand_bits(rng, (int(starts[-1]), 8, 128)))
+
+    def run():
+        cK, cV = to_dev(K), to_dev(V)
+        return [*ck.rope_tables(100, 64, 10000.0, "waves", 8.0, 512.0, 1.0, 4.0, first=7), *ck.rotate_rows(to_dev(x), 8, 2, 128, cos, sin, i32(pos), True),
+                ck.append_rows_paged(to_dev(x), 8, i32(starts), cos, sin, i32(pos), i32(table), i32(lengths), cK, cV), cK, cV,
+                ck.attend_rows_paged(q, i32(starts), i32(table), i32(lengths), cK, cV, False),
+                ck.attend_shared_paged(q[:3].contiguous(), i32([0, 1, 3]), i32(table[:2]), i32(lengths[:2]), i32(table), i32(lengths), cK, cV)]
+
+    native = run()
+
+    class General:
+        def __getattr__(self, name):
+            return lambda *a: None
+
+    monkeypatch.setattr(binding, "_native", General())
+    for a, b in zip(native, run()):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("page", [16, 1000])
+def test_rows_beyond_32_bits_of_a_long_cache(page):
+    """Pages at the end of a cache of more than 2^32 bytes."""
+    Hkv, d, per = 8, 128, max(1, 640 // page)
+    pages = (1 << 33) // (page * Hkv * d * 2) // 2 + 8
+    rng = np.random.default_rng(45)
+    table = (pages - 1 - np.arange(per)).reshape(1, per)
+    K = torch.zeros(pages, page, Hkv, d, dtype=torch.bfloat16, device="cuda")
+    V = torch.zeros_like(K)
+    rows = rand_bits(rng, (2, per, page, Hkv, d))
+    K[pages - per:], V[pages - per:] = to_dev(rows[0]), to_dev(rows[1])
+    n = 600
+    q = rand_bits(rng, (20, 16, d))
+    lengths = np.full((1, Hkv), n)
+    out = values(ck.attend_rows_paged(to_dev(q), i32([0, 20]), i32(table), i32(lengths), K, V))
+    local = per - 1 - np.arange(per)
+    rows_bounds.check_attend(out, wide(q), [0, 20], wide(rows[0]), wide(rows[1]), local.reshape(1, per), lengths, True)
+    got = values(ck.attend_shared_paged(to_dev(q), i32([0, 20]), i32(table), i32(lengths), i32(np.full((20, 1), -1)), i32(np.zeros((20, Hkv))), K, V))
+    rows_bounds.check_shared(got, wide(q), [0, 20], wide(rows[0]), wide(rows[1]), local.reshape(1, per), lengths, np.full((20, 1), -1), np.zeros((20, Hkv), int))
+    x = to_dev(rand_bits(rng, (1, 32 * d)))
+    one = torch.ones(4, 64, device="cuda")
+    ck.append_rows_paged(x, 16, i32([0, 1]), one, torch.zeros_like(one), i32([0]), i32(table), i32(lengths), K, V)
+    assert torch.equal(V[pages - 1 - (n - 1) // page, (n - 1) % page], x.view(32, d)[24:])
+
+
+def test_starts_that_make_no_sense_read_and_write_nothing_out_of_range():
+    """Descending, negative and too large: whatever comes out, it is written inside of out, and the call ends."""
+    rng = np.random.default_rng(46)
+    starts, K, V, table, lengths, x, pos = turn_inputs(rng)
+    T = int(starts[-1])
+    q = to_dev(rand_bits(rng, (T, 8, 128)))
+    cos, sin = (torch.tensor(t).cuda() for t in angles(rng, 512, 128))
+    for bad in ([5, 3, 100, 20], [-7, 2, T + 500, 4], [T, T, T, T], [2**31 - 1, -2**31, 0, 9]):
+        out, oq = Guarded((T, 8, 128), torch.bfloat16), Guarded((T, 8, 128), torch.bfloat16)
+        cK, cV = Guarded(K.shape, torch.bfloat16), Guarded(V.shape, torch.bfloat16)
+        cK.t.copy_(to_dev(K)); cV.t.copy_(to_dev(V))
+        ck.attend_rows_paged(q, i32(bad), i32(table), i32(lengths), cK.t, cV.t, True, out.t)
+        ck.attend_shared_paged(q[:3].contiguous(), i32(bad), i32(table), i32(lengths), i32(table), i32(lengths), cK.t, cV.t)
+        ck.append_rows_paged(to_dev(x), 8, i32(bad), cos, sin, i32(pos), i32(table), i32(lengths), cK.t, cV.t, out_q=oq.t)
+        torch.cuda.synchronize()
+        for t in (out, oq, cK, cV):
+            t.check()
