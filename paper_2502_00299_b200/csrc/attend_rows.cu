@@ -40,6 +40,7 @@ constexpr int kSub = 64;                              // keys of one S
 constexpr int kPieces = 4;                            // pieces handed out ahead
 constexpr int kMasks = 8;                             // tiles whose masks are kept
 constexpr int kBegin = 2;                             // tiles that the beginning of a unit counts as
+constexpr int kWide = 1;                              // thin tiles (of one half's rows) that one for both halves counts as
 constexpr float kSlack = 8.f;
 constexpr int kPanelBytes = kTile * 128;              // 64 dims of 128 rows
 
@@ -51,7 +52,10 @@ struct Unit {
     int keys;                // rows that the last token sees
     __device__ __forceinline__ int rows() const { return tokens * heads; }
     __device__ __forceinline__ int tiles() const { return (keys + kTile - 1) / kTile; }
-    __device__ __forceinline__ int span() const { return tokens > 0 ? tiles() + kBegin : 0; }
+    // The unit's part of the line, and how many of its tiles lie before place p of it.
+    __device__ __forceinline__ int weight(const AttendRowsArgs& a) const { return tokens > a.thin_tokens ? kWide : 1; }
+    __device__ __forceinline__ int span(const AttendRowsArgs& a) const { return tokens > 0 ? (tiles() + kBegin) * weight(a) : 0; }
+    __device__ __forceinline__ int tiles_before(const AttendRowsArgs& a, int p) const { return max(p / weight(a) - kBegin, 0); }
 };
 
 // The first block of a set with starts: sets before it take at most this many.
@@ -129,6 +133,7 @@ struct RowsSmem {
     alignas(1024) unsigned char q[D / 64][kBlock][128];   // panels of 64 dims; 128 rows a half of the CTA
     alignas(1024) unsigned char kv[kSlots][kTileBytes];   // panels of 64 dims
     Piece piece[kPieces];
+    int4 box[2][kTile / 4];                           // where rows of a tile of keys, or of values, are in the cache
     uint32_t mask[kMasks][4];                         // rows of a tile of keys that are there
     unsigned long long kv_full[kSlots], kv_empty[kSlots];
     unsigned long long q_full[2], q_empty[2], s_full[2][2], p_full[2][2], o_empty[2];
@@ -239,27 +244,29 @@ __device__ __forceinline__ void load_tile(const AttendRowsArgs& a, RowsSmem<D>& 
     const int nowhere = a.cache.num_pages * a.cache.page_size;         // behind the last row: zeros
     const bool any = at.x >= 0 || at.y >= 0 || at.z >= 0 || at.w >= 0;
     const uint32_t take = __ballot_sync(0xffffffffu, lane < boxes && (values || any));
-    const int4 row = make_int4(at.x < 0 ? nowhere : at.x, at.y < 0 ? nowhere : at.y, at.z < 0 ? nowhere : at.z, at.w < 0 ? nowhere : at.w);
+    // (one thread issues, with all that a copy takes known to be the same for the warp: 23 clocks a copy, where lanes that hand over their rows one by one take 180)
+    int4* box = sm.box[values];
+    box[lane] = make_int4(at.x < 0 ? nowhere : at.x, at.y < 0 ? nowhere : at.y, at.z < 0 ? nowhere : at.z, at.w < 0 ? nowhere : at.w);
+    __syncwarp();
     const uint32_t bar = smem_u32(&sm.kv_full[slot]), to = smem_u32(sm.kv[slot]);
-    const bool leader = elect_one();
-    if (leader) mbar_arrive_expect_tx(bar, __popc(take) * rows * (D * 2));
-    if (a.box > 0) {
+    if (elect_one()) {
+        mbar_arrive_expect_tx(bar, __popc(take) * rows * (D * 2));
+        if (a.box > 0) {
 #pragma unroll 4
-        for (int i = 0; i < boxes; ++i) {
-            const int r = __shfl_sync(0xffffffffu, row.x, i);
-            if (leader && (take >> i & 1u)) {
+            for (int i = 0; i < boxes; ++i) {
+                if (take >> i & 1u) {
 #pragma unroll
-                for (int p = 0; p < D / 64; ++p) copy_rows(to + p * kPanelBytes + i * rows * 128, map, bar, x + 64 * p, r);
+                    for (int p = 0; p < D / 64; ++p) copy_rows(to + p * kPanelBytes + i * rows * 128, map, bar, x + 64 * p, box[i].x);
+                }
             }
-        }
-    } else {
+        } else {
 #pragma unroll 4
-        for (int i = 0; i < boxes; ++i) {
-            const int r[4] = {__shfl_sync(0xffffffffu, row.x, i), __shfl_sync(0xffffffffu, row.y, i), __shfl_sync(0xffffffffu, row.z, i),
-                              __shfl_sync(0xffffffffu, row.w, i)};
-            if (leader && (take >> i & 1u)) {
+            for (int i = 0; i < boxes; ++i) {
+                const int row[4] = {box[i].x, box[i].y, box[i].z, box[i].w};
+                if (take >> i & 1u) {
 #pragma unroll
-                for (int p = 0; p < D / 64; ++p) gather_rows(to + p * kPanelBytes + i * 512, map, bar, x + 64 * p, r);
+                    for (int p = 0; p < D / 64; ++p) gather_rows(to + p * kPanelBytes + i * 512, map, bar, x + 64 * p, row);
+                }
             }
         }
     }
@@ -745,7 +752,7 @@ __device__ int deal(const AttendRowsArgs& a, RowsSmem<D>& sm, int cta, int ctas)
     const int per = (a.units + kRowsThreads - 1) / kRowsThreads;
     const int u0 = min(static_cast<int>(threadIdx.x) * per, a.units), u1 = min(u0 + per, a.units);
     int mine = 0;
-    for (int u = u0; u < u1; ++u) mine += unit_of(a, u).span();
+    for (int u = u0; u < u1; ++u) mine += unit_of(a, u).span(a);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int inc = mine;
 #pragma unroll
@@ -766,7 +773,7 @@ __device__ int deal(const AttendRowsArgs& a, RowsSmem<D>& sm, int cta, int ctas)
     if (at <= begin && begin < inc) {                                  // one thread, if any
         int u = u0;
         for (; u + 1 < u1; ++u) {
-            const int n = unit_of(a, u).span();
+            const int n = unit_of(a, u).span(a);
             if (begin < at + n) break;
             at += n;
         }
@@ -802,7 +809,7 @@ __device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<
             int n = 0;
             if (u + lane < a.units) {
                 x = unit_of(a, u + lane);
-                n = x.span();
+                n = x.span(a);
             }
             int inc = n;
 #pragma unroll
@@ -814,8 +821,8 @@ __device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<
             const int p0 = max(begin - start, 0), p1 = min(end - start, n);
             uint32_t todo = __ballot_sync(0xffffffffu, n > 0 && p0 < p1);
             Piece y;
-            y.tile0 = max(p0 - kBegin, 0);
-            y.tiles = max(p1 - kBegin, 0) - y.tile0;
+            y.tile0 = x.tiles_before(a, p0);
+            y.tiles = x.tiles_before(a, p1) - y.tile0;
             y.subs = y.tiles > 0 ? (min(x.keys - y.tile0 * kTile, y.tiles * kTile) + kSub - 1) / kSub : 0;
             y.kind = x.kind; y.set = x.set; y.h = x.h; y.t0 = x.t0; y.g0 = x.g0; y.heads = x.heads; y.rows = x.rows();
             y.limit = x.limit; y.step = x.step; y.keys = x.keys;

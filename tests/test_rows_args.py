@@ -68,7 +68,7 @@ def test_sizes_are_refused():
     for bad in (dict(row=1279), dict(st=(1024, 64, 256, 128)), dict(st=(1024, 128, 252, 128)), dict(st=(-1024, 128, 256, 128))):
         assert _rotate(**bad) == SHAPE, bad
     assert _append(row=1535) == SHAPE and _attend(causal=2) == SHAPE
-    # blocks times tiles of 128 rows: 8 heads of (T / 256 + B) blocks, 2^23 tiles
+    # blocks times tiles of 128 rows: 8 heads of (T / 256 + B) blocks, 2^22 tiles
     assert _attend(T=4, B=16, Hq=8, Hkv=8, per=1 << 29, page=1) == NOWS and _attend(T=4, B=64, Hq=8, Hkv=8, per=1 << 29, page=1) == SHAPE
     assert _shared(P_=0, pper=0, starts=None, pt=None, pl=None) == NOWS
 
