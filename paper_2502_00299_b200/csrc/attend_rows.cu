@@ -63,6 +63,7 @@ __device__ __forceinline__ int base_of(const AttendRowsArgs& a, const RowSets& s
 // The set whose blocks hold block x.
 __device__ __forceinline__ int set_of(const AttendRowsArgs& a, const RowSets& s, int x) {
     int lo = 0, hi = s.n - 1;
+#pragma unroll 1
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (base_of(a, s, mid) <= x) lo = mid; else hi = mid - 1;
@@ -144,6 +145,20 @@ struct RowsSmem {
 };
 static_assert(sizeof(RowsSmem<128>) <= 227 * 1024 && sizeof(RowsSmem<64>) <= 227 * 1024, "shared memory of an SM");
 
+// Bounded wait of a whole warp: all lanes test, some 60 clocks or more a time, until the phase is over, another warp has given up, or after 2^26 times (two
+// seconds at least). Few instructions, as it stands in many places: with ptx.cuh's polling in each of them the kernel was 161 KB of code, which no
+// instruction cache holds.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    bool ready = __all_sync(0xffffffffu, mbar_try_wait(bar, parity));
+#pragma unroll 1
+    for (uint32_t n = 0; !ready; ++n) {
+        if (n >= 1u << 26) *abort_flag = 1;
+        if (*abort_flag) return false;
+        ready = __all_sync(0xffffffffu, mbar_try_wait(bar, parity));
+    }
+    return true;
+}
+
 // What a role needs to walk the pieces.
 template <int D>
 struct Pieces {
@@ -154,7 +169,7 @@ struct Pieces {
     __device__ __forceinline__ void next() {
         if (++at == kPieces) { at = 0; phase ^= 1u; }
     }
-    __device__ __forceinline__ bool wait() { return mbar_wait_warp(smem_u32(&sm.piece_full[at]), phase, &sm.abort); }
+    __device__ __forceinline__ bool wait() { return wait_warp(smem_u32(&sm.piece_full[at]), phase, &sm.abort); }
 };
 
 // A value that is the same for all lanes, and known to be.
@@ -276,8 +291,9 @@ __device__ __forceinline__ void load_tile(const AttendRowsArgs& a, RowsSmem<D>& 
 template <int D>
 __device__ void let_land(RowsSmem<D>& sm, int n, int parity) {
     int none = 0;
+#pragma unroll 1
     for (int i = max(n - RowsSmem<D>::kSlots, 0); i < n; ++i)
-        if ((i & 1) == parity) mbar_wait_warp(smem_u32(&sm.kv_full[i % RowsSmem<D>::kSlots]), i / RowsSmem<D>::kSlots & 1, &none);
+        if ((i & 1) == parity) wait_warp(smem_u32(&sm.kv_full[i % RowsSmem<D>::kSlots]), i / RowsSmem<D>::kSlots & 1, &none);
 }
 
 // What the loading of keys, or of values, keeps from piece to piece.
@@ -292,8 +308,9 @@ struct KeyLoader {
         Places next;
         next.find(a, table, x.tile0, x.keys);
         const bool wide = x.stage == 2;
+#pragma unroll 1
         for (int half = wide ? 0 : x.stage; half <= (wide ? 1 : x.stage); ++half) {
-            if (!mbar_wait_warp(smem_u32(&sm.q_empty[half]), q_phase >> half & 1u, &sm.abort)) return false;
+            if (!wait_warp(smem_u32(&sm.q_empty[half]), q_phase >> half & 1u, &sm.abort)) return false;
             q_phase ^= 1u << half;
             q_used |= 1u << half;
         }
@@ -308,10 +325,11 @@ struct KeyLoader {
         }
         __syncwarp();
         const int rows = a.box > 0 ? a.box : 4;
+#pragma unroll 1
         for (int t = 0; t < x.tiles; ++t, ++n_tile, n_kv += 2) {
             const Places now = next;
             const int slot = n_kv % RowsSmem<D>::kSlots, base = (x.tile0 + t) * kTile;
-            if (!mbar_wait_warp(smem_u32(&sm.kv_empty[slot]), (n_kv / RowsSmem<D>::kSlots & 1) ^ 1, &sm.abort)) return false;
+            if (!wait_warp(smem_u32(&sm.kv_empty[slot]), (n_kv / RowsSmem<D>::kSlots & 1) ^ 1, &sm.abort)) return false;
             load_tile<D>(a, sm, slot, &maps.k, x.h * D, now.at, false);
             // which rows are there: lane l says it of rows 4 l to 4 l + 3. (The mask's last reader is done: its tile lies further back than there are buffers.)
             uint32_t word;
@@ -335,8 +353,9 @@ struct KeyLoader {
     __device__ void give_up(RowsSmem<D>& sm) {
         let_land(sm, n_kv, 0);
         int none = 0;
+#pragma unroll 1
         for (int half = 0; half < 2; ++half)
-            if (q_used >> half & 1u) mbar_wait_warp(smem_u32(&sm.q_full[half]), q_phase >> half & 1u, &none);
+            if (q_used >> half & 1u) wait_warp(smem_u32(&sm.q_full[half]), q_phase >> half & 1u, &none);
     }
 };
 
@@ -356,10 +375,11 @@ __device__ void load_values(const AttendRowsArgs& a, const RowMaps& maps, RowsSm
         Places next;
         if (tiles > 0) next.find(a, table, tile0, keys);
         bool fine = true;
+#pragma unroll 1
         for (int t = 0; t < tiles; ++t, n_kv += 2) {
             const Places now = next;
             const int slot = n_kv % RowsSmem<D>::kSlots;
-            fine = mbar_wait_warp(smem_u32(&sm.kv_empty[slot]), (n_kv / RowsSmem<D>::kSlots & 1) ^ 1, &sm.abort);
+            fine = wait_warp(smem_u32(&sm.kv_empty[slot]), (n_kv / RowsSmem<D>::kSlots & 1) ^ 1, &sm.abort);
             if (!fine) break;
             load_tile<D>(a, sm, slot, &maps.v, x, now.at, true);
             if (t + 1 < tiles) next.find(a, table, tile0 + t + 1, keys);
@@ -376,7 +396,7 @@ __device__ __forceinline__ void each_value(unsigned char* tile, int row0, Each e
     const int lane = threadIdx.x & 31;
 #pragma unroll 1
     for (int p = 0; p < D / 64; ++p) {
-#pragma unroll 4
+#pragma unroll 2
         for (int row = row0 + (lane >> 3); row < kTile; row += 4)
             each(reinterpret_cast<uint4*>(tile + p * kPanelBytes + row * 128) + (lane & 7), row, 8 * ((lane & 7) ^ (row & 7)) + 64 * p);
     }
@@ -417,7 +437,7 @@ __device__ void scan_values(const AttendRowsArgs& a, RowsSmem<D>& sm) {
         bool found = false;
         for (int t = max(from - tile0, 0); t < tiles; ++t) {
             unsigned char* tile = sm.kv[(n_kv + 2 * t + 1) % RowsSmem<D>::kSlots];
-            if (!mbar_wait_warp(smem_u32(&sm.scan), phase, &sm.abort)) return;
+            if (!wait_warp(smem_u32(&sm.scan), phase, &sm.abort)) return;
             phase ^= 1u;
             const int row0 = max(first - (tile0 + t) * kTile, 0);
             uint32_t bad = 0;
@@ -459,7 +479,7 @@ struct Products {
     uint32_t kv_phase = 0, q_phase = 0, p_phase = 0, scan_phase = 0, o_phase = 3;      // (a bit a half, or 2 * half + S; nothing has to be read out of O first)
     __device__ __forceinline__ Products(Smem& s, uint32_t t)
         : sm(s), tmem(t), q_desc(desc_lower(smem_u32(s.q[0][0]), 16)), k_desc(desc_lower(smem_u32(s.kv[0]), 16)), v_desc(desc_lower(smem_u32(s.kv[0]), kPanelBytes)) {}
-    __device__ __forceinline__ bool wait(unsigned long long& bar, uint32_t phase) const { return mbar_wait_warp(smem_u32(&bar), phase, &sm.abort); }
+    __device__ __forceinline__ bool wait(unsigned long long& bar, uint32_t phase) const { return wait_warp(smem_u32(&bar), phase, &sm.abort); }
     __device__ __forceinline__ void advance() {
         if (++slot == Smem::kSlots) { slot = 0; kv_phase ^= 1u; }
     }
@@ -510,6 +530,7 @@ struct Products {
         if (elect_one()) {
 #pragma unroll 1
             for (int sub = 0; sub < 2 && sub < subs; ++sub)
+#pragma unroll 1
                 for (int h = h0; h < (WIDE ? 2 : h0 + 1); ++h) {
                     logits(h, slot, sub);
                     umma_commit(smem_u32(&sm.s_full[h][sub]));
@@ -595,7 +616,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
     Pieces<D> pc(sm);
     int n_tile = 0;
     uint32_t s_phase = 0;                                              // (a bit for each S)
-    auto wait = [&](int sub) { return mbar_wait_warp(smem_u32(&sm.s_full[half][sub]), s_phase >> sub & 1u, &sm.abort); };
+    auto wait = [&](int sub) { return wait_warp(smem_u32(&sm.s_full[half][sub]), s_phase >> sub & 1u, &sm.abort); };
     for (;; pc.next()) {
         if (!pc.wait()) return;
         const Piece& x = sm.piece[pc.at];
@@ -613,11 +634,12 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
         const int least = x.limit + x.step * (row0 / x.heads);         // what the warp's first row sees: the least of its rows
         const int first = x.tile0 * kTile;
         float ref = -INFINITY, sum = 0.f;
+#pragma unroll 1
         for (int u = 0; u < subs; ++u) {
             const int sub = u & 1, n = (n_tile + (u >> 1)) % kMasks;
             const uint32_t n_phase = (n_tile + (u >> 1)) / kMasks & 1;
             const bool m_in = mbar_try_wait(smem_u32(&sm.mask_full[n]), n_phase), s_in = mbar_try_wait(smem_u32(&sm.s_full[half][sub]), s_phase >> sub & 1u);
-            if (__builtin_expect(!__all_sync(0xffffffffu, m_in && s_in), 0) && !(mbar_wait_warp(smem_u32(&sm.mask_full[n]), n_phase, &sm.abort) && wait(sub))) return;
+            if (__builtin_expect(!__all_sync(0xffffffffu, m_in && s_in), 0) && !(wait_warp(smem_u32(&sm.mask_full[n]), n_phase, &sm.abort) && wait(sub))) return;
             const uint2 m = *reinterpret_cast<const uint2*>(&sm.mask[n][2 * sub]);
             s_phase ^= 1u << sub;
             tc_fence_after();
@@ -687,6 +709,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
         }
         n_tile += tiles;
         // the last products of either S have been added
+#pragma unroll 1
         for (int sub = 0; sub < 2 && sub < subs; ++sub) {
             if (!wait(sub)) return;
             s_phase ^= 1u << sub;
@@ -751,34 +774,38 @@ template <int D>
 __device__ int deal(const AttendRowsArgs& a, RowsSmem<D>& sm, int cta, int ctas) {
     const int per = (a.units + kRowsThreads - 1) / kRowsThreads;
     const int u0 = min(static_cast<int>(threadIdx.x) * per, a.units), u1 = min(u0 + per, a.units);
-    int mine = 0;
-    for (int u = u0; u < u1; ++u) mine += unit_of(a, u).span(a);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int inc = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, inc, off);
-        if (lane >= off) inc += v;
-    }
-    if (lane == 31) sm.warp_sum[warp] = inc;
-    __syncthreads();
-    int total = 0;
-#pragma unroll
-    for (int i = 0; i < kRowsThreads / 32; ++i) {
-        if (i < warp) inc += sm.warp_sum[i];
-        total += sm.warp_sum[i];
-    }
-    const int begin = Share(total, ctas).begin(cta);
-    int at = inc - mine;
-    if (at <= begin && begin < inc) {                                  // one thread, if any
-        int u = u0;
-        for (; u + 1 < u1; ++u) {
+    int total = 0, at = 0, inc = 0, begin = -1;
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {                             // this thread's units added up; then, by one thread if any, looked through for the first
+        int place = at;
+#pragma unroll 1
+        for (int u = u0; u < u1; ++u) {
             const int n = unit_of(a, u).span(a);
-            if (begin < at + n) break;
-            at += n;
+            if (pass == 1 && place <= begin && begin < place + n) {
+                sm.first_unit = u;
+                sm.first_at = place;
+            }
+            place += n;
         }
-        sm.first_unit = u;
-        sm.first_at = at;
+        if (pass == 1) break;
+        inc = place;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, inc, off);
+            if (lane >= off) inc += v;
+        }
+        if (lane == 31) sm.warp_sum[warp] = inc;
+        __syncthreads();
+        at = inc - place;
+#pragma unroll 1
+        for (int i = 0; i < kRowsThreads / 32; ++i) {
+            if (i < warp) at += sm.warp_sum[i];
+            total += sm.warp_sum[i];
+        }
+        inc = at + place;
+        begin = Share(total, ctas).begin(cta);
+        if (!(at <= begin && begin < inc)) break;
     }
     return total;
 }
@@ -792,18 +819,18 @@ __device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<
     int at = 0, narrow = 0;
     uint32_t phase = 1;                                                // (the first round's entries are free)
     auto publish = [&](bool fill, const Piece& x) {
-        if (!mbar_wait_warp(smem_u32(&sm.piece_empty[at]), phase, &sm.abort)) return false;
+        if (!wait_warp(smem_u32(&sm.piece_empty[at]), phase, &sm.abort)) return false;
         if (fill) sm.piece[at] = x;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sm.piece_full[at]));
-        const Piece& y = sm.piece[at];
         if (++at == kPieces) { at = 0; phase ^= 1u; }
-        return y.tiles <= 0 || keys.load(a, maps, sm, y);
+        return true;
     };
     if (!a.shared && lane == 0) a.begun[2 * cta + 1] = make_int4(0, 0, 0, -1);
     __syncwarp();
     if (begin < end) {
         int u = sm.first_unit, pos = sm.first_at;
+#pragma unroll 1
         for (; u < a.units && pos < end; u += 32) {
             Unit x = {};
             int n = 0;
@@ -840,13 +867,15 @@ __device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<
                     a.begun[2 * cta + 1] = make_int4(0, 0, 0, last);
                 }
             }
+#pragma unroll 1
             while (todo != 0) {
                 const int i = __ffs(todo) - 1;
                 todo &= todo - 1;
                 const bool one = __shfl_sync(0xffffffffu, thin, i);
                 y.stage = one ? narrow : 2;
                 if (one) narrow ^= 1;
-                if (!publish(lane == i, y)) {
+                const Piece& z = sm.piece[at];
+                if (!publish(lane == i, y) || (z.tiles > 0 && !keys.load(a, maps, sm, z))) {
                     keys.give_up(sm);
                     return;
                 }
