@@ -412,7 +412,8 @@ CHUNKKV_API int chunkkv_evict_paged(float* weights, const int32_t* block_tables,
  *   chunkkv_attend_shared_scratch_bytes(...) bytes of scratch.
  *
  * Beyond the limits above, T and B (B and P) times Hq < 2^30, and blocks of 256 query heads of a KV head, (T / floor(256 / (Hq / Hkv)) + B)
- * Hkv of them (with P for B, and B more, where prefixes are shared), times tiles of 128 rows of a table below 2^30. chunkkv_device_status also reports a wait that the last two calls abandoned.
+ * Hkv of them (with P for B, and B more, where prefixes are shared), times tiles of 128 rows of a table below 2^31. chunkkv_device_status also
+ * reports a wait that one of the last two calls abandoned.
  */
 #define CHUNKKV_ROPE_PLAIN  0
 #define CHUNKKV_ROPE_LINEAR 1

@@ -1046,15 +1046,15 @@ int chunkkv_append_rows_paged(const void* qkv, long long row_elems, int T, const
     return e != cudaSuccess ? cuda_fail(e) : CHUNKKV_OK;
 }
 
-// What both calls take: T tokens in n sets, and, of those that share prefixes, their own rows. Units and tiles of 128 rows, two more for every beginning and all
-// of them twice where a unit has more than 128 query rows, are counted in 32 bits.
+// What both calls take: T tokens in n sets, and, of those that share prefixes, their own rows. Units and tiles of 128 rows, two more for every beginning, are
+// counted in 32 bits.
 static int check_rows(int T, int n, int Hq, int Hkv, int d, bool shared, int most_pages, int page_size, int num_pages, AttendRowsPlan* plan) {
     int st = check_decode_heads(T, Hq, Hkv, d);
     if (st == CHUNKKV_OK) st = check_decode_heads(n, Hq, Hkv, d);
     if (st == CHUNKKV_OK) st = check_decode_cache(most_pages, page_size, num_pages);
     if (st != CHUNKKV_OK) return st;
     *plan = attend_rows_plan(T, n, Hq, Hkv, d, shared);
-    return plan->units * (static_cast<long long>(most_pages) * page_size / 128 + 4) >= (1LL << 30) ? CHUNKKV_EINVAL_SHAPE : CHUNKKV_OK;
+    return plan->units * (static_cast<long long>(most_pages) * page_size / 128 + 4) >= (1LL << 31) ? CHUNKKV_EINVAL_SHAPE : CHUNKKV_OK;
 }
 
 size_t chunkkv_attend_rows_scratch_bytes(int T, int B, int Hq, int Hkv, int d) {

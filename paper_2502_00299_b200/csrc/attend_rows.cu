@@ -7,13 +7,16 @@
 // (a sequence, a prefix) and KV head, over the set's rows in tiles of 128. A CTA has 12 warps:
 //   0-3, 4-7   a query row a thread, 128 each: 64 logits out of tensor memory, their maximum, exponentials and sum, and as bf16 back into tensor memory
 //   8          hands out the CTA's pieces of units and brings queries and keys into shared memory, by TMA, as the products read them
-//   9          the products (tcgen05, M = 128): S = Q K^T of 64 keys and O += P V. Each half has two such S, so that the next one's logits are there when the
-//              exponentials of one are taken, and neither waits for the other: with one S of 128 keys the rows wait for two products and the products for
-//              the rows, in turn (4096 tokens over 8192 rows: 440 us)
+//   9          the products (tcgen05, M = 128): S = Q K^T of 64 keys and O += P V. Each half has two such S, so that the next logits are there when the
+//              exponentials of the last have been taken, and neither waits for the other (with one S of 128 keys, whose products take 1024 clocks instead of
+//              1240, rows and products wait in turn: 4096 tokens 425 us instead of 405, 64 sequences 111 instead of 102)
 //   10         brings the values
 //   11         looks through values that some of a block's tokens must not see
-// A copy takes an elected thread 23 clocks to issue, and 0.25 us a tile besides; two warps, for keys and values, bring a tile of both in 1100 clocks from pages
-// of 16 rows and in 2100 four rows at a time, beside the 2048 of its exponentials and products.
+// A copy takes an elected thread 23 clocks to issue, and a tile 460 besides; two warps, for keys and values, bring a tile of both in 1100 clocks from pages of
+// 16 rows, and in 2100 where rows come four at a time. A tile of 256 x 128 logits takes 2048 clocks of exponentials and 2480 of products (their operands
+// come out of shared memory at its full rate). What bounds it now, 4096 tokens of 32 heads over 8192 rows, 396 us, 1040 TFLOP/s: 3800 clocks a tile, 54 % of them
+// products. 64 keys take their rows 1000 clocks (270 for the maximum, 600 for the exponentials, the rest in barriers), the products of both halves 1900, of which 1400 to
+// issue and the rest between them, when the tensor cores mostly run dry.
 // One pass over the data: a row's reference moves only when a logit lies more than 2^8 above it, and then its O is scaled in tensor memory. P is rounded
 // to bf16 once (2^-8 of a weight, independent from row to row, beside the output's own rounding of 2^-8), its sum is taken before that, in 32 bits, as O is.
 //
@@ -39,8 +42,10 @@ constexpr int kRowWarps = 8;                          // those with query rows
 constexpr int kSub = 64;                              // keys of one S
 constexpr int kPieces = 4;                            // pieces handed out ahead
 constexpr int kMasks = 8;                             // tiles whose masks are kept
-constexpr int kBegin = 2;                             // tiles that the beginning of a unit counts as
-constexpr int kWide = 1;                              // thin tiles (of one half's rows) that one for both halves counts as
+// Tiles that the beginning of a unit counts as. us with 1, 2, 3: 8 x 5 tokens 34.7, 34.7, 35.4; 8 x 448 tokens of 64 dims 47.3, 45.0, 51.0; 64 sequences on
+// 32768 rows 90, 95, 101; 23 on three prefixes 41.8, 41.6, 40.8; 4096 tokens 399, 396, 394. A tile of a block with rows for one half counts as much as
+// one for both (as half of one: 64 sequences 116): it takes its warps as long.
+constexpr int kBegin = 2;
 constexpr float kSlack = 8.f;
 constexpr int kPanelBytes = kTile * 128;              // 64 dims of 128 rows
 
@@ -53,9 +58,8 @@ struct Unit {
     __device__ __forceinline__ int rows() const { return tokens * heads; }
     __device__ __forceinline__ int tiles() const { return (keys + kTile - 1) / kTile; }
     // The unit's part of the line, and how many of its tiles lie before place p of it.
-    __device__ __forceinline__ int weight(const AttendRowsArgs& a) const { return tokens > a.thin_tokens ? kWide : 1; }
-    __device__ __forceinline__ int span(const AttendRowsArgs& a) const { return tokens > 0 ? (tiles() + kBegin) * weight(a) : 0; }
-    __device__ __forceinline__ int tiles_before(const AttendRowsArgs& a, int p) const { return max(p / weight(a) - kBegin, 0); }
+    __device__ __forceinline__ int span() const { return tokens > 0 ? tiles() + kBegin : 0; }
+    __device__ __forceinline__ static int tiles_before(int p) { return max(p - kBegin, 0); }
 };
 
 // The first block of a set with starts: sets before it take at most this many.
@@ -781,7 +785,7 @@ __device__ int deal(const AttendRowsArgs& a, RowsSmem<D>& sm, int cta, int ctas)
         int place = at;
 #pragma unroll 1
         for (int u = u0; u < u1; ++u) {
-            const int n = unit_of(a, u).span(a);
+            const int n = unit_of(a, u).span();
             if (pass == 1 && place <= begin && begin < place + n) {
                 sm.first_unit = u;
                 sm.first_at = place;
@@ -836,7 +840,7 @@ __device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<
             int n = 0;
             if (u + lane < a.units) {
                 x = unit_of(a, u + lane);
-                n = x.span(a);
+                n = x.span();
             }
             int inc = n;
 #pragma unroll
@@ -848,8 +852,8 @@ __device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<
             const int p0 = max(begin - start, 0), p1 = min(end - start, n);
             uint32_t todo = __ballot_sync(0xffffffffu, n > 0 && p0 < p1);
             Piece y;
-            y.tile0 = x.tiles_before(a, p0);
-            y.tiles = x.tiles_before(a, p1) - y.tile0;
+            y.tile0 = x.tiles_before(p0);
+            y.tiles = x.tiles_before(p1) - y.tile0;
             y.subs = y.tiles > 0 ? (min(x.keys - y.tile0 * kTile, y.tiles * kTile) + kSub - 1) / kSub : 0;
             y.kind = x.kind; y.set = x.set; y.h = x.h; y.t0 = x.t0; y.g0 = x.g0; y.heads = x.heads; y.rows = x.rows();
             y.limit = x.limit; y.step = x.step; y.keys = x.keys;
