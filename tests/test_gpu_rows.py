@@ -223,6 +223,8 @@ COUNT = [   # Hq, Hkv, d, page, tokens, rows before them (a list: of each head)
     (12, 4, 64, 64, [300], [1200]),
     (6, 6, 64, 16, [257, 255, 256], [0, 1, 640]),
     (40, 2, 128, 1, [9, 30], [200, 11]),
+    (200, 1, 128, 16, [3, 0, 1], [300, 4, 77]),
+    (130, 1, 64, 32, [2], [129]),
     (300, 1, 64, 16, [3, 2], [200, 50]),                                     # more query heads than a block holds
     (16, 2, 128, 32, [1] * 40, list(range(0, 800, 20))),
     (4, 2, 128, 16, [700], [2500]),
@@ -378,6 +380,7 @@ SHARED = [  # Hq, Hkv, d, page, sequences of each group, prefix rows, own rows (
     (7, 1, 64, 100, [40], [1000], 200, 0, 0),
     (32, 8, 128, 16, [64], [700], 30, 0, 0),
     (28, 4, 64, 5, [30, 7, 50], [257, 1500, 0], 129, 0, 3),
+    (200, 1, 64, 16, [3], [300], 60, 1, 1),
     (300, 1, 128, 16, [2, 1], [400, 100], 60, 1, 0),                         # more query heads than a block holds
     (6, 6, 64, 64, [300], [900], 3, 0, 0),
     (16, 2, 64, 16, [], [], 90, 5, 0),                                       # no prefix at all
