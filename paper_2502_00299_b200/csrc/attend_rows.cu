@@ -14,7 +14,7 @@
 //   11         looks through values that some of a block's tokens must not see
 // A copy takes an elected thread 23 clocks to issue, and a tile 460 besides; two warps, for keys and values, bring a tile of both in 1100 clocks from pages of
 // 16 rows, and in 2100 where rows come four at a time. A tile of 256 x 128 logits takes 2048 clocks of exponentials and 2480 of products (their operands
-// come out of shared memory at its full rate). What bounds it now, 4096 tokens of 32 heads over 8192 rows, 396 us, 1040 TFLOP/s: 3800 clocks a tile, 54 % of them
+// come out of shared memory at its full rate). What bounds it now, 4096 tokens of 32 heads over 8192 rows, 390 us, 1060 TFLOP/s: 3800 clocks a tile, 54 % of them
 // products. 64 keys take their rows 1000 clocks (270 for the maximum, 600 for the exponentials, the rest in barriers), the products of both halves 1900, of which 1400 to
 // issue and the rest between them, when the tensor cores mostly run dry.
 // One pass over the data: a row's reference moves only when a logit lies more than 2^8 above it, and then its O is scaled in tensor memory. P is rounded
@@ -929,12 +929,12 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sm.tmem;
-    // 384 threads of 168 registers, at least 256 * 184 + 128 * 128
+    // 384 threads of 168 registers, of which 256 take 200 and 128 take 96
     if (warp < kRowWarps) {
-        setmaxnreg_inc<184>();
+        setmaxnreg_inc<200>();
         softmax_rows<D>(a, sm, tmem, warp >> 2);
     } else {
-        setmaxnreg_dec<128>();
+        setmaxnreg_dec<96>();
         if (warp == kRowWarps) {
             hand_out(a, maps, sm, total, blockIdx.x, gridDim.x);
         } else if (warp == kRowWarps + 1) {
