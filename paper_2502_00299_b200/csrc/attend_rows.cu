@@ -141,7 +141,16 @@ struct RowsSmem {
     int4 box[2][kTile / 4];                           // where rows of a tile of keys, or of values, are in the cache
     uint32_t mask[kMasks][4];                         // rows of a tile of keys that are there
     unsigned long long kv_full[kSlots], kv_empty[kSlots];
-    unsigned long long q_full[2], q_empty[2], s_full[2][2], p_full[2][2], o_empty[2];
+    // A wait names a phase by its parity, so no barrier may complete two phases while a warp still stands in front of a test for the first of them.
+    //   *_empty, p_full, scan, scanned   the next phase needs what the waiting warp does behind its wait, so it cannot come
+    //   q_full                           the next one needs the buffer given back, which the products' warp does behind its last test
+    //   piece_full                       the next one needs piece_empty of every warp that waits
+    //   mask_full                        the next one is eight tiles on, and keys are at most five ahead of the rows' weights
+    //   s_full                           the next one is the commit of a block that needs these weights of all four warps. In the last but one block of a piece no logits
+    //                                    come any more, but the last block's rows may wait for its values to move a reference: it commits here too
+    //   o_full                           all values of a piece have been added; the next one needs weights that the warp gives behind this wait. (Not s_full: the next
+    //                                    piece's logits, which need nothing of the rows' warps, would complete that once more, in front of a warp that comes late.)
+    unsigned long long q_full[2], q_empty[2], s_full[2][2], p_full[2][2], o_full[2], o_empty[2];
     unsigned long long piece_full[kPieces], piece_empty[kPieces], mask_full[kMasks], scan, scanned, drained;
     int warp_sum[kRowsThreads / 32], first_unit, first_at;
     int abort;
@@ -510,8 +519,9 @@ struct Products {
                 const int half = WIDE ? i : h0;
                 values(half, v_slot, sub, u > 0);
                 if (more) logits(half, k_slot, sub);
-                // (also where no S comes any more: it says that these values have been added)
-                umma_commit(smem_u32(&sm.s_full[half][sub]));
+                // (s_full also in the last but one block, where no S comes any more: it says that these values have been added)
+                if (u + 1 < subs) umma_commit(smem_u32(&sm.s_full[half][sub]));
+                else umma_commit(smem_u32(&sm.o_full[half]));
                 if (u + 3 == subs) umma_commit(smem_u32(&sm.q_empty[half]));
             }
             if (sub == 1 || u + 1 == subs) umma_commit(smem_u32(&sm.kv_empty[v_slot]));
@@ -619,7 +629,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
     const uint32_t O = tmem + 2 * kTile + half * D + mine;
     Pieces<D> pc(sm);
     int n_tile = 0;
-    uint32_t s_phase = 0;                                              // (a bit for each S)
+    uint32_t s_phase = 0, o_phase = 0;                                 // (of s_phase a bit for each S)
     auto wait = [&](int sub) { return wait_warp(smem_u32(&sm.s_full[half][sub]), s_phase >> sub & 1u, &sm.abort); };
     for (;; pc.next()) {
         if (!pc.wait()) return;
@@ -712,11 +722,10 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
             if (lane == 0) mbar_arrive(smem_u32(&sm.p_full[half][sub]));
         }
         n_tile += tiles;
-        // the last products of either S have been added
-#pragma unroll 1
-        for (int sub = 0; sub < 2 && sub < subs; ++sub) {
-            if (!wait(sub)) return;
-            s_phase ^= 1u << sub;
+        if (tiles > 0) {                                               // the last products have been added
+            if (!wait_warp(smem_u32(&sm.o_full[half]), o_phase, &sm.abort)) return;
+            o_phase ^= 1u;
+            if (subs > 1) s_phase ^= 1u << (subs & 1);                 // (those before them long since; where no reference moved, nobody has waited for it)
         }
         tc_fence_after();
         if (any) {
@@ -910,6 +919,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
                 mbar_init(smem_u32(&sm.s_full[i][j]), 1);
                 mbar_init(smem_u32(&sm.p_full[i][j]), 4);
             }
+            mbar_init(smem_u32(&sm.o_full[i]), 1);
             mbar_init(smem_u32(&sm.o_empty[i]), 4);
         }
         for (int i = 0; i < kPieces; ++i) {
