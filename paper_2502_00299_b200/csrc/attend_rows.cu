@@ -143,7 +143,7 @@ struct RowsSmem {
     unsigned long long kv_full[kSlots], kv_empty[kSlots];
     // A wait names a phase by its parity, so no barrier may complete two phases while a warp still stands in front of a test for the first of them.
     //   *_empty, p_full, scan, scanned   the next phase needs what the waiting warp does behind its wait, so it cannot come
-    //   q_full                           the next one needs the buffer given back, which the products' warp does behind its last test
+    //   kv_full, q_full                  the next one needs the buffer given back, which the products' warp does behind its last test
     //   piece_full                       the next one needs piece_empty of every warp that waits
     //   mask_full                        the next one is eight tiles on, and keys are at most five ahead of the rows' weights
     //   s_full                           the next one is the commit of a block that needs these weights of all four warps. In the last but one block of a piece no logits
@@ -583,11 +583,12 @@ struct Products {
                 }
             }
             const int bit = 2 * h0 + (u & 1);
-            const bool v_in = mbar_try_wait(smem_u32(&sm.kv_full[v_slot]), v_phase), k_in = mbar_try_wait(smem_u32(&sm.kv_full[k_slot]), k_phase);
+            // (keys only in the turn that takes them: in the other one their buffer may have been given back already)
+            const bool v_in = mbar_try_wait(smem_u32(&sm.kv_full[v_slot]), v_phase), k_in = (u & 1) != 0 || mbar_try_wait(smem_u32(&sm.kv_full[k_slot]), k_phase);
             const bool p_in = mbar_try_wait(smem_u32(&sm.p_full[h0][u & 1]), p_phase >> bit & 1u);
             const bool p1_in = !WIDE || mbar_try_wait(smem_u32(&sm.p_full[1][u & 1]), p_phase >> (2 + (u & 1)) & 1u);
             if (__builtin_expect(!__all_sync(0xffffffffu, v_in && k_in && p_in && p1_in), 0) &&
-                !(wait(sm.kv_full[v_slot], v_phase) && wait(sm.kv_full[k_slot], k_phase) && wait(sm.p_full[h0][u & 1], p_phase >> bit & 1u) &&
+                !(wait(sm.kv_full[v_slot], v_phase) && ((u & 1) != 0 || wait(sm.kv_full[k_slot], k_phase)) && wait(sm.p_full[h0][u & 1], p_phase >> bit & 1u) &&
                   (!WIDE || wait(sm.p_full[1][u & 1], p_phase >> (2 + (u & 1)) & 1u))))
                 return false;
             p_phase ^= (WIDE ? 5u : 1u << (2 * h0)) << (u & 1);

@@ -37,10 +37,11 @@ class Barrier:
 
 
 class Order:
-    """end: the last values of a piece are announced on a barrier of their own ("own") or on that of its logits ("logits")."""
+    """end: the last values of a piece are announced on a barrier of their own ("own") or on that of its logits ("logits").
+    keys: the next keys' buffer is tested in every turn of the products ("twice") or in that which takes it ("once")."""
 
-    def __init__(self, end="own"):
-        self.end = end
+    def __init__(self, end="own", keys="once"):
+        self.end, self.keys = end, keys
 
 
 class Kernel:
@@ -155,7 +156,7 @@ class Kernel:
                         yield [(self.scanned, scans)]
                         scans += 1
                 waits = [(self.kv_full[v % self.slots], v // self.slots)]
-                if u % 2 == 0:
+                if self.order.keys == "twice" or u % 2 == 0:
                     waits.append((self.kv_full[k % self.slots], k // self.slots))
                 yield waits + [(self.p_full[h][u % 2], p_n[h][u % 2]) for h in halves]
                 for h in halves:
@@ -291,6 +292,12 @@ def test_last_values_announced_where_logits_are_make_rows_late():
     assert late and all("s_full" in why for _, why in late)
 
 
+def test_keys_tested_behind_their_return_make_the_products_late():
+    """What the kernel did with an odd number of 64s of keys: the last turn but two gives the buffer back, the next one tested it again."""
+    late = found(Order(keys="twice"))
+    assert late and all("kv_full" in why for _, why in late) and all(any(subs % 2 for _, subs, _ in pieces) for pieces, _ in late)
+
+
 ORDER = {   # every wait (w), arrival (a) and commit (c) in the text, one after the other
     "block": "c s_full c o_full c q_empty c kv_empty c kv_empty",
     "piece": "w q_full w q_full w kv_full c s_full c kv_empty c q_empty w o_empty w o_empty w kv_full a scan w scanned "
@@ -319,3 +326,9 @@ def told(name):
 @pytest.mark.parametrize("name", sorted(ORDER))
 def test_the_kernel_waits_and_arrives_in_this_order(name):
     assert told(name) == ORDER[name]
+
+
+def test_the_kernel_tests_the_next_keys_in_the_turn_that_takes_them():
+    code = open(os.path.join(ROOT, "paper_2502_00299_b200", "csrc", "attend_rows.cu")).read()
+    tests = re.findall(r"(.{0,20})\b(?:mbar_try_wait\(smem_u32\(&sm\.kv_full\[k_slot\]\)|wait\(sm\.kv_full\[k_slot\])", code)
+    assert len(tests) == 2 and all(before.endswith("(u & 1) != 0 || ") for before in tests)
