@@ -548,6 +548,17 @@ CHUNKKV_API int chunkkv_test_last_tag(unsigned last_tag) {
     return e == cudaSuccess ? CHUNKKV_OK : cuda_fail(e);
 }
 
+// Not part of the API: for the tests of waits that run out, the clocks behind which attend_rows_paged's and attend_shared_paged's do (0: as ever).
+CHUNKKV_API int chunkkv_test_rows_wait_clocks(long long clocks) {
+    std::lock_guard<std::mutex> lk(g_mu);
+    DeviceCtx* ctx;
+    int st = get_ctx(&ctx);
+    if (st != CHUNKKV_OK) return st;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = attend_rows_wait_clocks(clocks);
+    return e == cudaSuccess ? CHUNKKV_OK : cuda_fail(e);
+}
+
 int chunkkv_score(const void* q_obs, const void* K, int L, int Hq, int Hkv, int d, int w, int c,
                   float* out_token_scores, float* out_chunk_scores, void* stream) {
     if (w < 1 || c < 1 || L < w) return CHUNKKV_EINVAL_SHAPE;

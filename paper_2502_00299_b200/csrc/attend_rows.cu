@@ -34,6 +34,7 @@ namespace chunkkv {
 namespace {
 
 __device__ int g_gave_up;                             // a kernel abandoned a bounded wait
+__device__ long long g_wait_clocks = kWaitLimitClocks;   // behind which it does
 
 constexpr int kTile = 128;                            // rows of a tile of queries, keys or values
 constexpr int kBlock = 256;                           // query rows of a unit
@@ -131,6 +132,10 @@ struct Piece {
     int leave, slot;
     int found;               // a value that is not finite stood in a row that not all of the block's tokens see
 };
+struct Stop {
+    long long since[kRowsThreads / 32];               // when a warp that waits began to
+    int abort;                                        // a warp has given up
+};
 template <int D>
 struct RowsSmem {
     static constexpr int kTileBytes = kTile * D * 2;
@@ -153,23 +158,37 @@ struct RowsSmem {
     unsigned long long q_full[2], q_empty[2], s_full[2][2], p_full[2][2], o_full[2], o_empty[2];
     unsigned long long piece_full[kPieces], piece_empty[kPieces], mask_full[kMasks], scan, scanned, drained;
     int warp_sum[kRowsThreads / 32], first_unit, first_at;
-    int abort;
+    Stop stop;
     uint32_t tmem;
 };
 static_assert(sizeof(RowsSmem<128>) <= 227 * 1024 && sizeof(RowsSmem<64>) <= 227 * 1024, "shared memory of an SM");
 
-// Bounded wait of a whole warp: all lanes test, some 60 clocks or more a time, until the phase is over, another warp has given up, or after 2^26 times (two
-// seconds at least). Few instructions, as it stands in many places: with ptx.cuh's polling in each of them the kernel was 161 KB of code, which no
-// instruction cache holds.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-    bool ready = __all_sync(0xffffffffu, mbar_try_wait(bar, parity));
-#pragma unroll 1
-    for (uint32_t n = 0; !ready; ++n) {
-        if (n >= 1u << 26) *abort_flag = 1;
-        if (*abort_flag) return false;
-        ready = __all_sync(0xffffffffu, mbar_try_wait(bar, parity));
+// Whether a warp that has tested n times gives up: another one has, or g_wait_clocks have passed since its 16th test. For all lanes together.
+__device__ __noinline__ bool out_of_time(uint32_t n, Stop* stop) {
+    const long long now = clock64();
+    long long* since = &stop->since[threadIdx.x >> 5];
+    if (n == 16) {
+        if ((threadIdx.x & 31) == 0) *since = now;
+        __syncwarp();
+    } else if (now - *since > g_wait_clocks) {
+        *const_cast<volatile int*>(&stop->abort) = 1;
     }
+    return __any_sync(0xffffffffu, *const_cast<volatile int*>(&stop->abort));
+}
+// Bounded wait of a whole warp: all lanes test, 60 clocks a time if the phase is over soon and 7800 if not, until it is; every 16th time they look whether to give up,
+// so two seconds and 60 us at most. Few instructions, as it stands in many places: with ptx.cuh's polling in each of them the kernel was 161 KB of code, which no
+// instruction cache holds, with out_of_time inlined 17 KB more than now (4096 tokens over 8192 rows 402 us instead of 388).
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, Stop* stop) {
+#pragma unroll 1
+    for (uint32_t n = 1; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++n)
+        if ((n & 15u) == 0 && out_of_time(n, stop)) return false;
     return true;
+}
+// Given up: what is under way lands before the CTA ends, which takes microseconds; until a time that all of a role's copies share.
+constexpr long long kLandClocks = 1LL << 26;
+__device__ __forceinline__ void wait_landing(uint32_t bar, uint32_t parity, long long until) {
+#pragma unroll 1
+    while (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)) && !__any_sync(0xffffffffu, clock64() > until)) {}
 }
 
 // What a role needs to walk the pieces.
@@ -182,7 +201,7 @@ struct Pieces {
     __device__ __forceinline__ void next() {
         if (++at == kPieces) { at = 0; phase ^= 1u; }
     }
-    __device__ __forceinline__ bool wait() { return wait_warp(smem_u32(&sm.piece_full[at]), phase, &sm.abort); }
+    __device__ __forceinline__ bool wait() { return wait_warp(smem_u32(&sm.piece_full[at]), phase, &sm.stop); }
 };
 
 // A value that is the same for all lanes, and known to be.
@@ -300,13 +319,12 @@ __device__ __forceinline__ void load_tile(const AttendRowsArgs& a, RowsSmem<D>& 
     }
     __syncwarp();
 }
-// Given up: what is under way lands before the CTA ends. n tiles of keys and values were asked for, this warp's are those of `parity`.
+// n tiles of keys and values were asked for, this warp's are those of `parity`.
 template <int D>
-__device__ void let_land(RowsSmem<D>& sm, int n, int parity) {
-    int none = 0;
+__device__ void let_land(RowsSmem<D>& sm, int n, int parity, long long until) {
 #pragma unroll 1
     for (int i = max(n - RowsSmem<D>::kSlots, 0); i < n; ++i)
-        if ((i & 1) == parity) wait_warp(smem_u32(&sm.kv_full[i % RowsSmem<D>::kSlots]), i / RowsSmem<D>::kSlots & 1, &none);
+        if ((i & 1) == parity) wait_landing(smem_u32(&sm.kv_full[i % RowsSmem<D>::kSlots]), i / RowsSmem<D>::kSlots & 1, until);
 }
 
 // What the loading of keys, or of values, keeps from piece to piece.
@@ -323,7 +341,7 @@ struct KeyLoader {
         const bool wide = x.stage == 2;
 #pragma unroll 1
         for (int half = wide ? 0 : x.stage; half <= (wide ? 1 : x.stage); ++half) {
-            if (!wait_warp(smem_u32(&sm.q_empty[half]), q_phase >> half & 1u, &sm.abort)) return false;
+            if (!wait_warp(smem_u32(&sm.q_empty[half]), q_phase >> half & 1u, &sm.stop)) return false;
             q_phase ^= 1u << half;
             q_used |= 1u << half;
         }
@@ -342,7 +360,7 @@ struct KeyLoader {
         for (int t = 0; t < x.tiles; ++t, ++n_tile, n_kv += 2) {
             const Places now = next;
             const int slot = n_kv % RowsSmem<D>::kSlots, base = (x.tile0 + t) * kTile;
-            if (!wait_warp(smem_u32(&sm.kv_empty[slot]), (n_kv / RowsSmem<D>::kSlots & 1) ^ 1, &sm.abort)) return false;
+            if (!wait_warp(smem_u32(&sm.kv_empty[slot]), (n_kv / RowsSmem<D>::kSlots & 1) ^ 1, &sm.stop)) return false;
             load_tile<D>(a, sm, slot, &maps.k, x.h * D, now.at, false);
             // which rows are there: lane l says it of rows 4 l to 4 l + 3. (The mask's last reader is done: its tile lies further back than there are buffers.)
             uint32_t word;
@@ -364,11 +382,11 @@ struct KeyLoader {
         return true;
     }
     __device__ void give_up(RowsSmem<D>& sm) {
-        let_land(sm, n_kv, 0);
-        int none = 0;
+        const long long until = clock64() + kLandClocks;
+        let_land(sm, n_kv, 0, until);
 #pragma unroll 1
         for (int half = 0; half < 2; ++half)
-            if (q_used >> half & 1u) wait_warp(smem_u32(&sm.q_full[half]), q_phase >> half & 1u, &none);
+            if (q_used >> half & 1u) wait_landing(smem_u32(&sm.q_full[half]), q_phase >> half & 1u, until);
     }
 };
 
@@ -392,14 +410,14 @@ __device__ void load_values(const AttendRowsArgs& a, const RowMaps& maps, RowsSm
         for (int t = 0; t < tiles; ++t, n_kv += 2) {
             const Places now = next;
             const int slot = n_kv % RowsSmem<D>::kSlots;
-            fine = wait_warp(smem_u32(&sm.kv_empty[slot]), (n_kv / RowsSmem<D>::kSlots & 1) ^ 1, &sm.abort);
+            fine = wait_warp(smem_u32(&sm.kv_empty[slot]), (n_kv / RowsSmem<D>::kSlots & 1) ^ 1, &sm.stop);
             if (!fine) break;
             load_tile<D>(a, sm, slot, &maps.v, x, now.at, true);
             if (t + 1 < tiles) next.find(a, table, tile0 + t + 1, keys);
         }
         if (!fine) break;
     }
-    let_land(sm, n_kv, 1);
+    let_land(sm, n_kv, 1, clock64() + kLandClocks);
 }
 
 // A tile of values of which some of the block's tokens, or all, must not see every row: what is not finite there would reach them as 0 * inf. From the
@@ -450,7 +468,7 @@ __device__ void scan_values(const AttendRowsArgs& a, RowsSmem<D>& sm) {
         bool found = false;
         for (int t = max(from - tile0, 0); t < tiles; ++t) {
             unsigned char* tile = sm.kv[(n_kv + 2 * t + 1) % RowsSmem<D>::kSlots];
-            if (!wait_warp(smem_u32(&sm.scan), phase, &sm.abort)) return;
+            if (!wait_warp(smem_u32(&sm.scan), phase, &sm.stop)) return;
             phase ^= 1u;
             const int row0 = max(first - (tile0 + t) * kTile, 0);
             uint32_t bad = 0;
@@ -492,7 +510,7 @@ struct Products {
     uint32_t kv_phase = 0, q_phase = 0, p_phase = 0, scan_phase = 0, o_phase = 3;      // (a bit a half, or 2 * half + S; nothing has to be read out of O first)
     __device__ __forceinline__ Products(Smem& s, uint32_t t)
         : sm(s), tmem(t), q_desc(desc_lower(smem_u32(s.q[0][0]), 16)), k_desc(desc_lower(smem_u32(s.kv[0]), 16)), v_desc(desc_lower(smem_u32(s.kv[0]), kPanelBytes)) {}
-    __device__ __forceinline__ bool wait(unsigned long long& bar, uint32_t phase) const { return wait_warp(smem_u32(&bar), phase, &sm.abort); }
+    __device__ __forceinline__ bool wait(unsigned long long& bar, uint32_t phase) const { return wait_warp(smem_u32(&bar), phase, &sm.stop); }
     __device__ __forceinline__ void advance() {
         if (++slot == Smem::kSlots) { slot = 0; kv_phase ^= 1u; }
     }
@@ -631,7 +649,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
     Pieces<D> pc(sm);
     int n_tile = 0;
     uint32_t s_phase = 0, o_phase = 0;                                 // (of s_phase a bit for each S)
-    auto wait = [&](int sub) { return wait_warp(smem_u32(&sm.s_full[half][sub]), s_phase >> sub & 1u, &sm.abort); };
+    auto wait = [&](int sub) { return wait_warp(smem_u32(&sm.s_full[half][sub]), s_phase >> sub & 1u, &sm.stop); };
     for (;; pc.next()) {
         if (!pc.wait()) return;
         const Piece& x = sm.piece[pc.at];
@@ -654,7 +672,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
             const int sub = u & 1, n = (n_tile + (u >> 1)) % kMasks;
             const uint32_t n_phase = (n_tile + (u >> 1)) / kMasks & 1;
             const bool m_in = mbar_try_wait(smem_u32(&sm.mask_full[n]), n_phase), s_in = mbar_try_wait(smem_u32(&sm.s_full[half][sub]), s_phase >> sub & 1u);
-            if (__builtin_expect(!__all_sync(0xffffffffu, m_in && s_in), 0) && !(wait_warp(smem_u32(&sm.mask_full[n]), n_phase, &sm.abort) && wait(sub))) return;
+            if (__builtin_expect(!__all_sync(0xffffffffu, m_in && s_in), 0) && !(wait_warp(smem_u32(&sm.mask_full[n]), n_phase, &sm.stop) && wait(sub))) return;
             const uint2 m = *reinterpret_cast<const uint2*>(&sm.mask[n][2 * sub]);
             s_phase ^= 1u << sub;
             tc_fence_after();
@@ -724,7 +742,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
         }
         n_tile += tiles;
         if (tiles > 0) {                                               // the last products have been added
-            if (!wait_warp(smem_u32(&sm.o_full[half]), o_phase, &sm.abort)) return;
+            if (!wait_warp(smem_u32(&sm.o_full[half]), o_phase, &sm.stop)) return;
             o_phase ^= 1u;
             if (subs > 1) s_phase ^= 1u << (subs & 1);                 // (those before them long since; where no reference moved, nobody has waited for it)
         }
@@ -833,7 +851,7 @@ __device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<
     int at = 0, narrow = 0;
     uint32_t phase = 1;                                                // (the first round's entries are free)
     auto publish = [&](bool fill, const Piece& x) {
-        if (!wait_warp(smem_u32(&sm.piece_empty[at]), phase, &sm.abort)) return false;
+        if (!wait_warp(smem_u32(&sm.piece_empty[at]), phase, &sm.stop)) return false;
         if (fill) sm.piece[at] = x;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sm.piece_full[at]));
@@ -931,7 +949,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
         mbar_init(smem_u32(&sm.scan), 1);
         mbar_init(smem_u32(&sm.scanned), 1);
         mbar_init(smem_u32(&sm.drained), 1);
-        sm.abort = 0;
+        sm.stop.abort = 0;
         fence_mbar_init();
     }
     begin_dependent();
@@ -969,7 +987,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
         tmem_relinquish();
         tmem_dealloc(tmem, 512);
     }
-    if (tid == 0 && sm.abort) atomicExch(&g_gave_up, 1);
+    if (tid == 0 && sm.stop.abort) atomicExch(&g_gave_up, 1);
 }
 
 // ------------------------------------------------------------------------------------------------ joining
@@ -1168,6 +1186,10 @@ cudaError_t attend_rows_status(bool* gave_up) {
     if (e != cudaSuccess || flag == 0) return e;
     flag = 0;
     return cudaMemcpyToSymbol(g_gave_up, &flag, sizeof(int));
+}
+cudaError_t attend_rows_wait_clocks(long long clocks) {
+    if (clocks <= 0) clocks = kWaitLimitClocks;
+    return cudaMemcpyToSymbol(g_wait_clocks, &clocks, sizeof(clocks));
 }
 
 }  // namespace chunkkv

@@ -67,5 +67,7 @@ cudaError_t launch_attend_rows(const AttendRowsArgs& args, const AttendRowsPlan&
                                cudaStream_t stream);
 // Whether a kernel of the current device gave up on a bounded wait since the last call.
 cudaError_t attend_rows_status(bool* gave_up);
+// For tests: the clocks behind which a wait of the current device's kernels is abandoned (0: as ever).
+cudaError_t attend_rows_wait_clocks(long long clocks);
 
 }  // namespace chunkkv
