@@ -48,6 +48,7 @@ constexpr int kMasks = 8;                             // tiles whose masks are k
 // one for both (as half of one: 64 sequences 116): it takes its warps as long.
 constexpr int kBegin = 2;
 constexpr float kSlack = 8.f;
+constexpr float kNoValues = -1.f;                     // the sum of a record of no tiles, which has no O. (One whose logits are all -inf has: its values may be infinite.)
 constexpr int kPanelBytes = kTile * 128;              // 64 dims of 128 rows
 
 // ------------------------------------------------------------------------------------------------ units
@@ -177,7 +178,7 @@ __device__ __noinline__ bool out_of_time(uint32_t n, Stop* stop) {
 }
 // Bounded wait of a whole warp: all lanes test, 60 clocks a time if the phase is over soon and 7800 if not, until it is; every 16th time they look whether to give up,
 // so two seconds and 60 us at most. Few instructions, as it stands in many places: with ptx.cuh's polling in each of them the kernel was 161 KB of code, which no
-// instruction cache holds, with out_of_time inlined 17 KB more than now (4096 tokens over 8192 rows 402 us instead of 388).
+// instruction cache holds, with out_of_time inlined 10 KB more than now (4096 tokens over 8192 rows 402 us instead of 388).
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, Stop* stop) {
 #pragma unroll 1
     for (uint32_t n = 1; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++n)
@@ -757,8 +758,9 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
             const int bad_from = scan_from(x) * kTile;
             // rows of all units of a kind, and this one among them
             const size_t all = static_cast<size_t>(a.T) * a.Hq, whole = static_cast<size_t>(x.h) * a.T * a.G + static_cast<size_t>(token) * a.G + x.g0 + g;
-            if (there && leave == kPart) a.part_ml[static_cast<size_t>(slot) * a.record_rows + row] = make_float2(ref, sum);
-            if (there && leave == kWhole) a.whole_ml[x.kind * all + whole] = make_float2(ref, sum);
+            const float2 ml = make_float2(ref, tiles > 0 ? sum : kNoValues);
+            if (there && leave == kPart) a.part_ml[static_cast<size_t>(slot) * a.record_rows + row] = ml;
+            if (there && leave == kWhole) a.whole_ml[x.kind * all + whole] = ml;
             const float inv = 1.f / sum;
 #pragma unroll 1
             for (int i = 0; i < D; i += 32) {
@@ -998,7 +1000,7 @@ template <int D>
 struct JoinSmem {
     static constexpr int kRows = kJoinThreads * 4 / D;
     int4 from[2][kRows];                               // first and last CTA (last < first: none), row of their records; 1: one CTA's that has the whole unit
-    float factor[2][kRows][kRowsCtas];                 // below 0: a record that saw nothing, and has no values
+    float factor[2][kRows][kRowsCtas];                 // below 0: a record that has no values
     float sum[kRows];
 };
 
@@ -1072,7 +1074,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
 #pragma unroll
             for (int i = 0; i < kOwn; ++i) {
                 const float2 v = ml[s][i];
-                const float f = v.x == -INFINITY && v.y == 0.f ? -1.f : ex2_below(v.x, top);
+                const float f = v.y == kNoValues ? -1.f : ex2_below(v.x, top);
                 if (x.x + lane + 32 * i <= x.y) sm.factor[s][r][lane + 32 * i] = f;
                 if (f != -1.f) sum += v.y * f;
             }
