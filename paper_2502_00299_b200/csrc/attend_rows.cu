@@ -667,6 +667,9 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
         const int tok = row / x.heads, limit = x.limit + x.step * tok;
         const int least = x.limit + x.step * (row0 / x.heads);         // what the warp's first row sees: the least of its rows
         const int first = x.tile0 * kTile;
+        // (lanes behind the last row have other tokens' queries, or what was left in shared memory: they have no say in whether references move, which would
+        // change how the others' weights are rounded)
+        const float slack = row < x.rows ? kSlack : INFINITY;
         float ref = -INFINITY, sum = 0.f;
 #pragma unroll 1
         for (int u = 0; u < subs; ++u) {
@@ -698,7 +701,7 @@ __device__ void softmax_rows(const AttendRowsArgs& a, RowsSmem<D>& sm, uint32_t 
                     for (int i = 0; i < kSub; ++i) s[i] = seen[i / 32] >> (i & 31) & 1u ? s[i] : -INFINITY;
                 }
                 const float z = row_max(s) * a.scale_log2;
-                if (__builtin_expect(__any_sync(0xffffffffu, z > ref + kSlack), 0)) {
+                if (__builtin_expect(__any_sync(0xffffffffu, z > ref + slack), 0)) {
                     const float now = fmaxf(ref, z), f = ex2_below(ref, now);
                     ref = now;
                     sum *= f;
