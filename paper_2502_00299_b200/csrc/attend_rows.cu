@@ -34,7 +34,7 @@ namespace chunkkv {
 namespace {
 
 __device__ int g_gave_up;                             // a kernel abandoned a bounded wait
-__device__ long long g_wait_clocks = kWaitLimitClocks;   // behind which it does
+__device__ long long g_wait_clocks = kWaitLimitClocks;   // behind which it does, and more for more work (Stop)
 
 constexpr int kTile = 128;                            // rows of a tile of queries, keys or values
 constexpr int kBlock = 256;                           // query rows of a unit
@@ -135,7 +135,13 @@ struct Piece {
 };
 struct Stop {
     long long since[kRowsThreads / 32];               // when a warp that waits began to
+    // A warp may have nothing to do while others work on all that the CTA has, so the limit of a wait grows with that: 2^-16 of it (30 us) for a tile, which takes 2 us,
+    // and 2^-20 for a unit, 32 of which take a few us to look through.
+    long long limit;                                  // (none until the warp that hands out pieces has set it)
     int abort;                                        // a warp has given up
+    __device__ __forceinline__ void begin(int tiles, int units) {
+        limit = g_wait_clocks + (g_wait_clocks >> 16) * tiles + (g_wait_clocks >> 20) * units;
+    }
 };
 template <int D>
 struct RowsSmem {
@@ -164,20 +170,20 @@ struct RowsSmem {
 };
 static_assert(sizeof(RowsSmem<128>) <= 227 * 1024 && sizeof(RowsSmem<64>) <= 227 * 1024, "shared memory of an SM");
 
-// Whether a warp that has tested n times gives up: another one has, or g_wait_clocks have passed since its 16th test. For all lanes together.
+// Whether a warp that has tested n times gives up: another one has, or the limit has passed since its 16th test. For all lanes together.
 __device__ __noinline__ bool out_of_time(uint32_t n, Stop* stop) {
     const long long now = clock64();
     long long* since = &stop->since[threadIdx.x >> 5];
     if (n == 16) {
         if ((threadIdx.x & 31) == 0) *since = now;
         __syncwarp();
-    } else if (now - *since > g_wait_clocks) {
+    } else if (now - *since > stop->limit) {
         *const_cast<volatile int*>(&stop->abort) = 1;
     }
     return __any_sync(0xffffffffu, *const_cast<volatile int*>(&stop->abort));
 }
 // Bounded wait of a whole warp: all lanes test, 60 clocks a time if the phase is over soon and 7800 if not, until it is; every 16th time they look whether to give up,
-// so two seconds and 60 us at most. Few instructions, as it stands in many places: with ptx.cuh's polling in each of them the kernel was 161 KB of code, which no
+// 60 us late at most. Few instructions, as it stands in many places: with ptx.cuh's polling in each of them the kernel was 161 KB of code, which no
 // instruction cache holds, with out_of_time inlined 10 KB more than now (4096 tokens over 8192 rows 402 us instead of 388).
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, Stop* stop) {
 #pragma unroll 1
@@ -852,6 +858,7 @@ __device__ void hand_out(const AttendRowsArgs& a, const RowMaps& maps, RowsSmem<
     const int lane = threadIdx.x & 31;
     KeyLoader<D> keys;
     const Share share(total, ctas);
+    if (lane == 0) sm.stop.begin(share.per + 1, a.units);
     const int begin = share.begin(min(cta, share.n)), end = cta < share.n ? share.begin(cta + 1) : begin;
     int at = 0, narrow = 0;
     uint32_t phase = 1;                                                // (the first round's entries are free)
@@ -955,6 +962,7 @@ __global__ void __launch_bounds__(kRowsThreads, 1) attend_rows_kernel(const __gr
         mbar_init(smem_u32(&sm.scanned), 1);
         mbar_init(smem_u32(&sm.drained), 1);
         sm.stop.abort = 0;
+        sm.stop.limit = 1LL << 62;
         fence_mbar_init();
     }
     begin_dependent();

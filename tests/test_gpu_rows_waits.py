@@ -63,3 +63,28 @@ def test_a_wait_that_runs_out_is_reported_once_and_the_next_call_is_right(d, sha
     for _ in range(3):
         assert torch.equal(call(), want)
     assert ck.device_status() == 0
+
+
+def test_a_wait_for_long_work_does_not_run_out():
+    """Warps that have nothing to do wait while others go through all rows of a long cache: beyond the limit's fixed part, here 2^28 clocks."""
+    d, page, pages, per, T = 64, 128, 40, 160000, 256 * 148
+    rng = np.random.default_rng(3)
+    K = torch.zeros(pages, page, 1, d, dtype=torch.bfloat16, device="cuda")
+    V = torch.tensor(rng.integers(-8, 9, K.shape), device="cuda").bfloat16()
+    q = to_dev(rand_bits(rng, (T, 1, d)))
+    table, lengths = i32(np.arange(per)[None] % pages), i32([[per * page]])  # (every page 4000 times: the mean of them once)
+    wait_clocks(1 << 28)
+    try:
+        e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        e[0].record()
+        out = ck.attend_rows_paged(q, i32([0, T]), table, lengths, K, V, False)
+        e[1].record()
+        assert ck.device_status() == 0
+    finally:
+        wait_clocks(0)
+    assert e[0].elapsed_time(e[1]) > (1 << 28) / 1.965e6                     # ms, at the fastest clock
+    # logits of 0 give weights of 1, added up 64 at a time, and sums of whole numbers below 2^24 are exact: a reciprocal, a product and a rounding are left
+    ref = V.double().mean((0, 1, 2))
+    sums = V.double().view(-1, d).cumsum(0).abs().max().item() + (ref.abs().max() * per * page).item()
+    assert sums < 2 ** 24
+    assert ((out.double() - ref).abs() <= (2.0 ** -8 + 2.0 ** -22) * ref.abs()).all()
