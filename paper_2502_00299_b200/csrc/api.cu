@@ -962,7 +962,8 @@ int chunkkv_rope_tables(int n_pos, long long first, int rot, double base, int sc
         if (scaling == CHUNKKV_ROPE_LINEAR) {
             w /= factor;
         } else if (scaling == CHUNKKV_ROPE_DIMS) {
-            const double stretch = fmin(fmax((i - from) / fmax(to - from, 1e-3), 0.0), 1.0);
+            // (in 64 bits: half a step of a double here is 2^-28 of a turn 2^32 positions on)
+            const long double stretch = fminl(fmaxl((i - from) / static_cast<long double>(fmax(to - from, 1e-3)), 0.0L), 1.0L);
             w = w / factor * stretch + w * (1.0L - stretch);
         } else if (scaling == CHUNKKV_ROPE_WAVES) {
             const long double turns = original * w / (2.0L * pi);
@@ -971,7 +972,8 @@ int chunkkv_rope_tables(int n_pos, long long first, int rot, double base, int sc
         }
         long double turn = w / (2.0L * pi);
         turn -= floorl(turn);                                          // (positions are whole: whole turns do not matter)
-        a.turn[i] = static_cast<unsigned long long>(ldexpl(turn, 64));
+        turn = roundl(ldexpl(turn, 64));
+        a.turn[i] = turn < 0x1p64L ? static_cast<unsigned long long>(turn) : 0;
     }
     std::lock_guard<std::mutex> lk(g_mu);
     DeviceCtx* ctx;
