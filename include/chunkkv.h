@@ -389,7 +389,7 @@ CHUNKKV_API int chunkkv_evict_paged(float* weights, const int32_t* block_tables,
  *                          over the `original` positions stay, those that turn less than `low` times are stretched)
  *     CHUNKKV_ROPE_WAVES   with s = min(max((original w_i / (2 pi) - low) / (high - low), 0), 1): s w_i + (1 - s) w_i / factor
  *   Angles are good to 2^-31 of a turn at any position (2^-31 / factor with a factor below 1), values to 2^-22 of scale. base > 1, factor > 0,
- *   original > 0, 0 < low < high.
+ *   original > 0, 0 < low < high; scale finite as a float.
  *
  * chunkkv_rotate_rows: chunkkv_rotate_qk for heads of which the first rot dims turn (a multiple of 16, at most d; tables [n_pos, rot / 2]), the
  *   others only taking part in the norm, with pair i of a head's dims (i, i + rot / 2) or, interleaved = 1, (2 i, 2 i + 1).

@@ -936,7 +936,7 @@ int chunkkv_evict_paged(float* weights, const int32_t* block_tables, int max_pag
 // ---- Tables of the rotary embedding, its other layouts, and turns of many tokens: rotated, appended, attended to; batches that share a prefix.
 int chunkkv_rope_tables(int n_pos, long long first, int rot, double base, int scaling, double factor, double original, double low, double high,
                         double scale, float* cos_t, float* sin_t, void* stream) {
-    if (n_pos < 0 || rot < 16 || rot > kMaxRot || rot % 16 != 0 || !(base > 1.0) || !isfinite(base) || !isfinite(scale)) return CHUNKKV_EINVAL_SHAPE;
+    if (n_pos < 0 || rot < 16 || rot > kMaxRot || rot % 16 != 0 || !(base > 1.0) || !isfinite(base) || !isfinite(static_cast<float>(scale))) return CHUNKKV_EINVAL_SHAPE;
     const long long far = 1LL << 31;
     if (first < -far || first > far) return CHUNKKV_EINVAL_SHAPE;
     if (scaling < CHUNKKV_ROPE_PLAIN || scaling > CHUNKKV_ROPE_WAVES) return CHUNKKV_EINVAL_SHAPE;
