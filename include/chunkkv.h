@@ -412,9 +412,10 @@ CHUNKKV_API int chunkkv_evict_paged(float* weights, const int32_t* block_tables,
  *   prefix is read once for up to 256 query heads (sequences times Hq / Hkv). Otherwise as chunkkv_attend_rows_paged, with
  *   chunkkv_attend_shared_scratch_bytes(...) bytes of scratch.
  *
- * Beyond the limits above, T and B (B and P) times Hq < 2^30, and blocks of 256 query heads of a KV head, (T / floor(256 / (Hq / Hkv)) + B)
- * Hkv of them (with P for B, and B more, where prefixes are shared), times tiles of 128 rows of a table below 2^31. chunkkv_device_status also
- * reports a wait that one of the last two calls abandoned.
+ * Beyond the limits above, T and B (B and P) times Hq < 2^30, and of the last two calls units * (floor(max_pages * page_size / 128) + 4) < 2^31, with
+ * the larger of both tables' pages. A unit is a block of a set's tokens and of a KV head's query heads: with G = Hq / Hkv, t = max(1, floor(256 / G)) and
+ * s = ceil(G / 256) there are up to (floor(T / t) + B) s Hkv of them, of shared prefixes (floor(B / t) + P + B) s Hkv, with P = 0 B s Hkv.
+ * chunkkv_device_status also reports a wait that one of the last two calls abandoned.
  */
 #define CHUNKKV_ROPE_PLAIN  0
 #define CHUNKKV_ROPE_LINEAR 1
