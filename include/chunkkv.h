@@ -403,8 +403,10 @@ CHUNKKV_API int chunkkv_evict_paged(float* weights, const int32_t* block_tables,
  *   rows before the turn and the turn's up to its own. Not causal, it is cross attention to an encoder's states kept in the cache. As in
  *   chunkkv_attend_paged a head with nothing to see, or no logit above -inf, gets zeros, other infinite or not-a-number logits go the way of the formula, values may be as
  *   large as 2^88, and an infinite one in a row that is seen makes its dim of the output infinite or not a number; rows that a token does not see
- *   do not touch it, whatever they hold. Weights are rounded to bf16 once, before they meet the values (2^-8 of each), sums are taken in 32 bits,
- *   in a fixed order: same result every time. scratch: chunkkv_attend_rows_scratch_bytes(...) bytes, as in chunkkv_attend_paged (0: invalid sizes).
+ *   do not touch it, whatever they hold. Weights are rounded to bf16 once, before they meet the values (2^-8 of each; chunkkv_attend_paged keeps 2^-16),
+ *   sums are taken in 32 bits, in a fixed order: same result every time. There are no `weights`: a turn adds nothing to the sums that chunkkv_evict_paged goes by, and
+ *   the rows that it appended have none either until single tokens' calls add to them. An eviction behind a turn would take the turn's own chunks first, but for the last w rows:
+ *   a program that evicts sets their sums before (to those of the chunks that it wants to keep them with). scratch: chunkkv_attend_rows_scratch_bytes(...) bytes, as in chunkkv_attend_paged (0: invalid sizes).
  *
  * chunkkv_attend_shared_paged: attention of one new token a sequence, q [B, Hq, d], sequences starts[p] .. starts[p + 1] - 1 sharing prefix p (P
  *   of them; P = 0: none, and the prefixes' pointers may be NULL), a sequence outside of all of them having none: over the first prefix_lengths[p, h] rows of prefix_tables

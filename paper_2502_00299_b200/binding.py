@@ -787,7 +787,8 @@ def attend_rows_paged(q: torch.Tensor, starts: torch.Tensor, block_tables: torch
                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """Attention [T, Hq, d] of a turn's tokens (q [T, Hq, d] bf16), starts[b] to starts[b + 1] - 1 of each of B sequences, over the first
     lengths [B, Hkv] rows of every head of a paged cache. causal: the tokens are the last of those rows, and each sees no row behind its own;
-    else (an encoder's states, say) all see all. Rows of a new out that belong to no sequence are not set."""
+    else (an encoder's states, say) all see all. Rows of a new out that belong to no sequence are not set. Nothing is added to the sums that
+    evict_paged goes by (see chunkkv.h)."""
     r = _native.attend_rows_paged(q, starts, block_tables, lengths, cache_K, cache_V, causal, out, stream)
     if r is not None:
         return _done(r, "chunkkv_attend_rows_paged")

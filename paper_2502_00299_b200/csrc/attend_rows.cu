@@ -18,7 +18,8 @@
 // products. 64 keys take their rows 1000 clocks (270 for the maximum, 600 for the exponentials, the rest in barriers), the products of both halves 1900, of which 1400 to
 // issue and the rest between them, when the tensor cores mostly run dry.
 // One pass over the data: a row's reference moves only when a logit lies more than 2^8 above it, and then its O is scaled in tensor memory. P is rounded
-// to bf16 once (2^-8 of a weight, independent from row to row, beside the output's own rounding of 2^-8), its sum is taken before that, in 32 bits, as O is.
+// to bf16 once (2^-8 of a weight, independent from row to row, beside the output's own rounding of 2^-8; a second term for the rest, as attend.cu has, would be half as
+// many products again), its sum is taken before that, in 32 bits, as O is.
 //
 // The tiles of all units stand in one line that is dealt evenly to the CTAs, one an SM, so that few rows over a long cache and many over a short one, of
 // any lengths, fill all of them. A unit that several CTAs share leaves (reference, sum, O) records in scratch of the call's own, which a second launch
