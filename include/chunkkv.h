@@ -378,7 +378,7 @@ CHUNKKV_API int chunkkv_evict_paged(float* weights, const int32_t* block_tables,
  * Beyond single tokens: the rotary embedding in its other forms, a turn of many tokens, and batches that share a prefix. Conventions,
  * limits and the meaning of block_tables, lengths and pages are those of the calls above; besides
  *   starts [n + 1] int32       ascending, in [0, T]: tokens starts[i] .. starts[i + 1] - 1 belong to sequence (or group) i, which may have none.
- *                              What belongs to none (tokens in front of starts[0] and from starts[n] on) is neither read nor written.
+ *                              What belongs to none (tokens in front of starts[0] and from starts[n] on) does not matter and is not written.
  *
  * chunkkv_rope_tables: cos_t / sin_t [n_pos, rot / 2] f32 of positions first, first + 1, ...: scale * cos(p w_i), scale * sin(p w_i), pair i
  *   turning by w_i = base^(-2 i / rot) a position, |first| <= 2^31. scaling:
